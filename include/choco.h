@@ -393,6 +393,153 @@ int choco_profile_set_stride(choco_ctx* ctx, int32_t stride);
 int choco_profile_read(choco_ctx* ctx, int32_t* steps_recorded, double* update_ms_total,
                        void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Either side of the gossip step: the token table of a language model and a local optimizer.
+ *
+ * The calls below serve all n workers at once on the arrays a run has anyway (rows of X and G),
+ * or on separate tensors.  They follow the rules at the top: asynchronous on `stream`, calls on
+ * one handle in stream order from one host thread at a time, nothing allocated after the init
+ * call, nothing enqueued on error, same inputs give the same bits.  A handle belongs to the
+ * device that was current at its init; a call with another device current returns
+ * CHOCO_ERR_INVALID_ARG.  Pointers are aligned to their elements (CHOCO_ERR_MISALIGNED).
+ * ------------------------------------------------------------------------------------------ */
+
+/* Element types of the arrays these calls take. */
+typedef enum {
+    CHOCO_F32 = 0,
+    CHOCO_BF16 = 1,
+    CHOCO_F16 = 2
+} choco_dtype;
+
+/*
+ * Token lookup and its gradient.  Worker i's table starts `table_ld` elements after worker i-1's
+ * (for a table that is a layer of X: its row pitch, with the table pointer advanced to the layer),
+ * its rows are `table_row` elements apart.  Tokens outside [0, vocab) stand for nothing (ragged
+ * batches are filled up with -1): their output is zeros and they take no part in the gradient.
+ */
+typedef struct choco_embedding choco_embedding;
+typedef struct {
+    int32_t n;          /* workers, 1 .. 65535                                                 */
+    float scale;        /* factor on every row looked up (and on its gradient), finite         */
+    int64_t vocab;      /* rows of a table, 1 .. 2^31 - 2                                      */
+    int64_t dim;        /* elements of a row, 1 .. 2^24                                        */
+    int64_t table_row;  /* elements between rows, >= dim; 0 = dim                              */
+    int64_t table_ld;   /* elements between tables, >= (vocab-1) table_row + dim; 0 = vocab table_row */
+    int64_t max_tokens; /* most tokens of one worker in a backward call; n max_tokens < 2^31   */
+    int64_t padding;    /* a token whose row is looked up as usual but gets no gradient, or -1  */
+} choco_embedding_params;
+
+/* Allocates the workspace of the backward call (nothing if max_tokens = 0: forward only). */
+int choco_embedding_init(choco_embedding** out, const choco_embedding_params* p);
+int choco_embedding_destroy(choco_embedding* emb);
+
+/*
+ * choco_embedding_forward -- out[i, t, :] = scale * table_i[tokens[i, t], :], formed in float32
+ * and rounded once to the output's type.
+ *   tokens     DEVICE, int32 (index_bits = 32) or int64 (64), `count` >= 0 per worker (no limit
+ *              but n count < 2^31), rows `tokens_ld` >= count elements apart.
+ *   out        DEVICE; element (i, t, c) at i out_ld + t out_row + c; out_row >= dim.
+ * Table, tokens and out do not overlap.
+ */
+int choco_embedding_forward(choco_embedding* emb, const void* table, int32_t table_dtype, const void* tokens,
+                            int32_t index_bits, int64_t count, int64_t tokens_ld, void* out, int32_t out_dtype,
+                            int64_t out_row, int64_t out_ld, void* stream);
+
+/*
+ * choco_embedding_backward -- the gradient of that lookup, in the layout of the table:
+ *     grad_i[r, :] = scale * sum over t with tokens[i, t] = r of dout[i, t, :]
+ * for every row r of every worker (rows that no token names become zeros); with accumulate = 1 the
+ * sum is added to what grad_i[r, :] holds instead (the gradient of an output layer that shares
+ * the table, or of earlier micro-batches), and rows that no token names are neither read nor
+ * written.  The tokens are sorted, rows summed in float32 in an order that depends on the tokens
+ * and the sizes alone, and the result is rounded once.
+ * What dout holds at tokens outside [0, vocab) is not read into any sum.
+ *   count      <= max_tokens (CHOCO_ERR_TOO_LARGE); 0 writes zeros (or nothing).
+ *   dout       DEVICE; element (i, t, c) at i dout_ld + t dout_row + c.
+ * Elements of grad between rows (table_row > dim) and between tables are not touched.
+ */
+int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t index_bits, int64_t count,
+                             int64_t tokens_ld, const void* dout, int32_t dout_dtype, int64_t dout_row,
+                             int64_t dout_ld, void* grad, int32_t grad_dtype, int32_t accumulate, void* stream);
+
+/*
+ * AdamW over many tensors at once (decoupled weight decay).  Per element, with t the number of
+ * steps the element's group has taken including this one:
+ *     g' = c g ;   m = beta1 m + (1 - beta1) g' ;   v = beta2 v + ((1 - beta2) g') g'
+ *     x  = x - ( (m / (sqrt(v) / sqrt(1 - beta2^t) + eps)) lr / (1 - beta1^t) + x (lr weight_decay) )
+ * in float32 from the operands' own types, rounded once per array.  Tensors belong to groups (the
+ * workers of a run): a group has its own gradient factor c, its own norm and its own t.
+ */
+typedef struct choco_adamw choco_adamw;
+typedef struct {
+    void* x;              /* parameters, updated in place (NULL: a list for choco_adamw_grad_norm only) */
+    const void* g;        /* gradients, read-only                                                */
+    void* copy;           /* second copy of the new parameters in another type, or NULL          */
+    int64_t numel;        /* elements, >= 0                                                      */
+    int32_t x_dtype, g_dtype, copy_dtype;
+    int32_t group;        /* in [0, groups)                                                      */
+    double weight_decay;  /* >= 0                                                                */
+    double lr_scale;      /* factor on the learning rate of this tensor, >= 0                    */
+} choco_adamw_tensor;
+typedef struct {
+    double beta1, beta2;  /* in [0, 1)                                                           */
+    double eps;           /* > 0                                                                 */
+    int32_t state_bits;   /* 32 or 8                                                             */
+    int32_t groups;       /* >= 1                                                                */
+} choco_adamw_params;
+
+/*
+ * The moments are caller-owned DEVICE arrays over all tensors, in the order of the list, every
+ * tensor starting on a multiple of 256 elements (the gaps are neither read nor written):
+ * choco_adamw_state_size elements in all.
+ *   state_bits = 32   m, v float32; m_scale, v_scale unused (NULL).
+ *   state_bits = 8    m int8, v uint8 codes, and one float32 scale per 256 elements in m_scale and
+ *                     v_scale.  With a the largest |m| of a block (at least 1e-30), its scale
+ *                     is s = a / 127^2 and an element is sgn(m) s k^2 with k the nearest to
+ *                     127 sqrt(|m| / a), so the step between neighbouring values is 2/k of the
+ *                     value.  For v the same is done with sqrt(v), k up to 255 and s = a / 255^2;
+ *                     k is at least 1 where v > 0 (an element that has seen gradients never
+ *                     divides by eps alone).  Codes and scales of zero are moments of zero: a
+ *                     fresh run starts from zeroed arrays.
+ * m and v (and the 8-bit codes) are 16-byte aligned, the scales 4-byte.
+ * The list is copied; the tensors it points to have to stay where they are.
+ */
+int choco_adamw_init(choco_adamw** out, int32_t n_tensors, const choco_adamw_tensor* tensors,
+                     const choco_adamw_params* p);
+int choco_adamw_destroy(choco_adamw* opt);
+/* *elements: length of m and v (a multiple of 256); offsets (may be NULL): n_tensors starts. */
+int choco_adamw_state_size(const choco_adamw* opt, int64_t* elements, int64_t* offsets);
+/* New gradient pointers for all tensors (HOST array).  Synchronises `stream`. */
+int choco_adamw_set_grads(choco_adamw* opt, const void* const* g, void* stream);
+
+/*
+ * choco_adamw_grad_norm -- for every group the 2-norm over the gradients of all its tensors,
+ * times `unscale` (the reciprocal of a loss scale; 1 otherwise), and the factor that clips it,
+ *     norm[k] = unscale sqrt(sum g^2) ;   factor[k] = unscale min(1, max_norm / (norm[k] + 1e-6))
+ * (max_norm = 0: no clipping, factor = unscale), summed in float64 in a fixed order.  factor[k] is
+ * NaN where the norm is infinite or NaN.  norm, factor: DEVICE float [groups].
+ */
+int choco_adamw_grad_norm(choco_adamw* opt, float max_norm, float unscale, float* norm, float* factor, void* stream);
+
+/*
+ * choco_adamw_step -- one step of all tensors.  factor: DEVICE float [groups], the gradient
+ * factors c, or NULL for 1.  A group whose factor is infinite or NaN is left as it is, parameters,
+ * moments, copy and step number, so that a step with overflowed gradients is skipped without a
+ * host synchronisation.  After it, X has changed outside the gossip step: call choco_invalidate
+ * (or run with choco_set_carry(ctx, 0)) before the next choco_gossip_step.
+ */
+int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* v_scale, double lr,
+                     const float* factor, void* stream);
+
+/* The values the moments stand for, as float32, bfloat16 or float16 arrays of choco_adamw_state_size
+ * elements (gaps are written as the zeros they hold).  Either output may be NULL. */
+int choco_adamw_read_state(choco_adamw* opt, const void* m, const void* v, const float* m_scale,
+                           const float* v_scale, void* m_out, void* v_out, int32_t out_dtype, void* stream);
+
+/* Steps taken per group (HOST int64 [groups]); get synchronises `stream`, set resumes a run. */
+int choco_adamw_get_steps(choco_adamw* opt, int64_t* steps, void* stream);
+int choco_adamw_set_steps(choco_adamw* opt, const int64_t* steps, void* stream);
+
 const char* choco_strerror(int code);
 /* cudaError_t of the last failing CUDA call on this context (0 if none). */
 int choco_last_cuda_error(const choco_ctx* ctx);

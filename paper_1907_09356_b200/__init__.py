@@ -29,7 +29,12 @@ EXPORTS = [
     "choco_layers_init", "choco_layers_destroy", "choco_layers_gossip_step", "choco_layers_sgd_step",
     "choco_layers_sgd_momentum_step", "choco_layers_message_bytes", "choco_layers_get_layer",
     "choco_layers_invalidate", "choco_layers_set_step", "choco_layers_set_nesterov", "choco_layers_set_graphs", "choco_layers_combined_steps",
+    "choco_embedding_init", "choco_embedding_destroy", "choco_embedding_forward", "choco_embedding_backward",
+    "choco_adamw_init", "choco_adamw_destroy", "choco_adamw_state_size", "choco_adamw_set_grads", "choco_adamw_grad_norm",
+    "choco_adamw_step", "choco_adamw_read_state", "choco_adamw_get_steps", "choco_adamw_set_steps",
 ]
+
+DTYPES = {"float32": 0, "bfloat16": 1, "float16": 2}   # choco_dtype
 
 
 ERR_TIMEOUT = -8
@@ -54,6 +59,22 @@ class choco_stats(ctypes.Structure):
                 ("kernel_launches", ctypes.c_uint64), ("device_timeouts", ctypes.c_uint64),
                 ("graph_replays", ctypes.c_uint64), ("rescued_rows", ctypes.c_uint64)]
 
+
+class choco_embedding_params(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("scale", ctypes.c_float), ("vocab", ctypes.c_int64), ("dim", ctypes.c_int64),
+                ("table_row", ctypes.c_int64), ("table_ld", ctypes.c_int64), ("max_tokens", ctypes.c_int64),
+                ("padding", ctypes.c_int64)]
+
+
+class choco_adamw_params(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("state_bits", ctypes.c_int32), ("groups", ctypes.c_int32)]
+
+
+# choco_adamw_tensor as a numpy record: a list of tensors is an array of these
+ADAMW_TENSOR = [("x", "<u8"), ("g", "<u8"), ("copy", "<u8"), ("numel", "<i8"), ("x_dtype", "<i4"), ("g_dtype", "<i4"),
+                ("copy_dtype", "<i4"), ("group", "<i4"), ("weight_decay", "<f8"), ("lr_scale", "<f8")]
+ADAMW_BLOCK = 256   # elements that share a scale; tensors start on multiples of it in the moments
 
 _lib = None
 
@@ -111,6 +132,20 @@ def load() -> ctypes.CDLL:
         lib.choco_layers_set_nesterov.argtypes = [vp, i32]
         lib.choco_layers_set_graphs.argtypes = [vp, i32, ctypes.POINTER(u64)]
         lib.choco_layers_combined_steps.argtypes = [vp, ctypes.POINTER(u64)]
+        lib.choco_embedding_init.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(choco_embedding_params)]
+        lib.choco_embedding_destroy.argtypes = [vp]
+        lib.choco_embedding_forward.argtypes = [vp, vp, i32, vp, i32, i64, i64, vp, i32, i64, i64, vp]
+        lib.choco_embedding_backward.argtypes = [vp, vp, i32, i64, i64, vp, i32, i64, i64, vp, i32, i32, vp]
+        f64 = ctypes.c_double
+        lib.choco_adamw_init.argtypes = [ctypes.POINTER(vp), i32, vp, ctypes.POINTER(choco_adamw_params)]
+        lib.choco_adamw_destroy.argtypes = [vp]
+        lib.choco_adamw_state_size.argtypes = [vp, ctypes.POINTER(i64), vp]
+        lib.choco_adamw_set_grads.argtypes = [vp, vp, vp]
+        lib.choco_adamw_grad_norm.argtypes = [vp, f32, f32, vp, vp, vp]
+        lib.choco_adamw_step.argtypes = [vp, vp, vp, vp, vp, f64, vp, vp]
+        lib.choco_adamw_read_state.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp]
+        lib.choco_adamw_get_steps.argtypes = [vp, vp, vp]
+        lib.choco_adamw_set_steps.argtypes = [vp, vp, vp]
         for name in EXPORTS:
             if name not in ("choco_strerror",):
                 getattr(lib, name).restype = ctypes.c_int
@@ -364,7 +399,151 @@ def choco_layers_set_nesterov(layers, enable: bool) -> None:
     _check(load().choco_layers_set_nesterov(layers, 1 if enable else 0))
 
 
+def _dtype(t) -> int:
+    """choco_dtype of a tensor (or of a torch dtype)."""
+    name = str(getattr(t, "dtype", t)).rpartition(".")[2]
+    if name not in DTYPES:
+        raise ChocoError(f"libchoco: {name} arrays are not supported (float32, bfloat16 or float16)", -1)
+    return DTYPES[name]
+
+
+def _index_bits(t) -> int:
+    name = str(t.dtype).rpartition(".")[2]
+    if name not in ("int32", "int64"):
+        raise ChocoError(f"libchoco: tokens are int32 or int64, not {name}", -1)
+    return 32 if name == "int32" else 64
+
+
+def _rows3(t, what: str, n: int, count: int, dim: int) -> tuple[int, int]:
+    """(row, worker) strides of an [n, count, dim] tensor with unit stride inside a row."""
+    if tuple(t.shape) != (n, count, dim) or (dim > 1 and count and t.stride(2) != 1):
+        raise ChocoError(f"libchoco: {what} must be [{n}, {count}, {dim}] with contiguous rows, not {tuple(t.shape)}", -1)
+    return (t.stride(1) if count > 1 else max(dim, t.stride(1))), t.stride(0)
+
+
+def choco_embedding_init(n: int, vocab: int, dim: int, max_tokens: int, table_row: int = 0, table_ld: int = 0,
+                         scale: float = 1.0, padding: int = -1):
+    """Handle for the token tables of n workers (see choco.h); max_tokens = 0 serves lookups only."""
+    p = choco_embedding_params(n, scale, vocab, dim, table_row, table_ld, max_tokens, padding)
+    h = ctypes.c_void_p()
+    _check(load().choco_embedding_init(ctypes.byref(h), ctypes.byref(p)))
+    return h
+
+
+def choco_embedding_destroy(emb) -> None:
+    _check(load().choco_embedding_destroy(emb))
+
+
+def choco_embedding_forward(emb, table, tokens, out, stream=None) -> None:
+    """out[i, t] = scale * table_i[tokens[i, t]].  `table` is a tensor that starts at worker 0's first
+    row; tokens [n, T] int32 or int64; out [n, T, dim]."""
+    n, count = tokens.shape
+    if count > 1 and tokens.stride(1) != 1:
+        raise ChocoError("libchoco: tokens must be contiguous inside a worker's row", -1)
+    row, ld = _rows3(out, "out", n, count, out.shape[2])
+    _check(load().choco_embedding_forward(emb, _ptr(table), _dtype(table), _ptr(tokens), _index_bits(tokens), count,
+                                          tokens.stride(0), _ptr(out), _dtype(out), row, ld, _stream(stream)))
+
+
+def choco_embedding_backward(emb, tokens, dout, grad, accumulate: bool = False, stream=None) -> None:
+    """grad_i[r] (+)= scale * sum of dout[i, t] over the t with tokens[i, t] = r, in the table's layout."""
+    n, count = tokens.shape
+    if count > 1 and tokens.stride(1) != 1:
+        raise ChocoError("libchoco: tokens must be contiguous inside a worker's row", -1)
+    row, ld = _rows3(dout, "dout", n, count, dout.shape[2])
+    _check(load().choco_embedding_backward(emb, _ptr(tokens), _index_bits(tokens), count, tokens.stride(0), _ptr(dout),
+                                           _dtype(dout), row, ld, _ptr(grad), _dtype(grad), 1 if accumulate else 0,
+                                           _stream(stream)))
+
+
+def choco_adamw_init(tensors, groups: int = 1, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                     state_bits: int = 32):
+    """tensors: numpy array of ADAMW_TENSOR records (see adamw_layer_tensors)."""
+    import numpy as np
+    t = np.ascontiguousarray(tensors, dtype=ADAMW_TENSOR)
+    p = choco_adamw_params(beta1, beta2, eps, state_bits, groups)
+    h = ctypes.c_void_p()
+    _check(load().choco_adamw_init(ctypes.byref(h), len(t), t.ctypes.data if len(t) else None, ctypes.byref(p)))
+    return h
+
+
+def choco_adamw_destroy(opt) -> None:
+    _check(load().choco_adamw_destroy(opt))
+
+
+def choco_adamw_state_size(opt, n_tensors: int = 0):
+    """(elements of the moments, first element of every tensor: an int64 array of n_tensors, all of the list)."""
+    import numpy as np
+    e = ctypes.c_int64()
+    off = np.zeros(n_tensors, dtype=np.int64)
+    _check(load().choco_adamw_state_size(opt, ctypes.byref(e), off.ctypes.data if n_tensors else None))
+    return e.value, off
+
+
+def choco_adamw_set_grads(opt, pointers, stream=None) -> None:
+    """New gradient addresses, one per tensor of the list."""
+    import numpy as np
+    g = np.ascontiguousarray(pointers, dtype=np.uint64)
+    _check(load().choco_adamw_set_grads(opt, g.ctypes.data, _stream(stream)))
+
+
+def choco_adamw_grad_norm(opt, max_norm: float, norm, factor, unscale: float = 1.0, stream=None) -> None:
+    _check(load().choco_adamw_grad_norm(opt, max_norm, unscale, _ptr(norm), _ptr(factor), _stream(stream)))
+
+
+def choco_adamw_step(opt, m, v, m_scale, v_scale, lr: float, factor=None, stream=None) -> None:
+    _check(load().choco_adamw_step(opt, _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), lr, _ptr(factor), _stream(stream)))
+
+
+def choco_adamw_read_state(opt, m, v, m_scale, v_scale, m_out, v_out, stream=None) -> None:
+    """The values of the moments; m_out and v_out (either may be None) have one type."""
+    out = m_out if m_out is not None else v_out
+    if m_out is not None and v_out is not None and m_out.dtype != v_out.dtype:
+        raise ChocoError("libchoco: m_out and v_out have one type", -1)
+    _check(load().choco_adamw_read_state(opt, _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), _ptr(m_out), _ptr(v_out),
+                                         0 if out is None else _dtype(out), _stream(stream)))
+
+
+def choco_adamw_get_steps(opt, groups: int, stream=None):
+    """Steps that every group has taken (int64 array)."""
+    import numpy as np
+    steps = np.zeros(groups, dtype=np.int64)
+    _check(load().choco_adamw_get_steps(opt, steps.ctypes.data, _stream(stream)))
+    return steps
+
+
+def choco_adamw_set_steps(opt, steps, stream=None) -> None:
+    import numpy as np
+    s = np.ascontiguousarray(steps, dtype=np.int64)
+    _check(load().choco_adamw_set_steps(opt, s.ctypes.data, _stream(stream)))
+
+
 # --------------------------------------------------------------------------- convenience
+
+
+def adamw_layer_tensors(X, G, layer_off, weight_decay=0.0, lr_scale=1.0, copy=None):
+    """The list of tensors (worker by worker, layer by layer, group = worker) for rows of X and G
+    [n, >= layer_off[-1]] cut at layer_off; weight_decay and lr_scale are numbers or one per layer.
+    X may be None (a list for norms only)."""
+    import numpy as np
+    off = np.asarray(layer_off, dtype=np.int64)
+    n, layers = G.shape[0], len(off) - 1
+    if layers < 1 or off[0] != 0 or np.any(np.diff(off) < 0):
+        raise ChocoError("libchoco: layer_off must start at 0 and not decrease", -1)
+    t = np.zeros((n, layers), dtype=ADAMW_TENSOR)
+    rows = np.arange(n, dtype=np.int64)[:, None]
+    for name, a in (("x", X), ("g", G), ("copy", copy)):
+        if a is None:
+            continue
+        if a.dim() != 2 or a.shape[0] != n or a.shape[1] < off[-1] or (a.shape[1] > 1 and a.stride(1) != 1):
+            raise ChocoError(f"libchoco: {name} must be [{n}, >= {int(off[-1])}] with contiguous rows", -1)
+        t[name] = (a.data_ptr() + (rows * a.stride(0) + off[None, :-1]) * a.element_size()).astype(np.uint64)
+        t[name + "_dtype"] = _dtype(a)
+    t["numel"] = np.diff(off)[None]
+    t["group"] = rows
+    t["weight_decay"] = np.broadcast_to(np.asarray(weight_decay, dtype=np.float64), (layers,))[None]
+    t["lr_scale"] = np.broadcast_to(np.asarray(lr_scale, dtype=np.float64), (layers,))[None]
+    return t.reshape(-1)
 
 
 @dataclasses.dataclass
@@ -399,6 +578,107 @@ class Choco:
         if getattr(self, "ctx", None) is not None:
             choco_destroy(self.ctx)
             self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Embedding:
+    """Owns a choco_embedding handle; see choco_embedding_init."""
+
+    def __init__(self, n: int, vocab: int, dim: int, max_tokens: int, table_row: int = 0, table_ld: int = 0,
+                 scale: float = 1.0, padding: int = -1):
+        self.n, self.vocab, self.dim = n, vocab, dim
+        self.handle = choco_embedding_init(n, vocab, dim, max_tokens, table_row, table_ld, scale, padding)
+
+    def _shape(self, tokens, rows):
+        if tokens.dim() != 2 or tokens.shape[0] != self.n or rows.dim() != 3 or rows.shape[2] != self.dim:
+            raise ChocoError(f"libchoco: tokens must be [{self.n}, T], rows [{self.n}, T, {self.dim}]", -1)
+
+    def forward(self, table, tokens, out, stream=None):
+        self._shape(tokens, out)
+        choco_embedding_forward(self.handle, table, tokens, out, stream)
+
+    def backward(self, tokens, dout, grad, accumulate: bool = False, stream=None):
+        self._shape(tokens, dout)
+        choco_embedding_backward(self.handle, tokens, dout, grad, accumulate, stream)
+
+    def close(self):
+        if getattr(self, "handle", None) is not None:
+            choco_embedding_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class AdamW:
+    """AdamW over the layers of all workers' rows: X and G are [n, ld] tensors, every worker a group.
+    Owns the handle and (unless `states` hands them over) the moments: (m, v), or with 8-bit
+    moments (m, v, m_scale, v_scale), flat arrays in the layout choco.h gives.  With X = None only
+    grad_norm can be called."""
+
+    def __init__(self, X, G, layer_off, weight_decay=0.0, lr_scale=1.0, copy=None, beta1: float = 0.9,
+                 beta2: float = 0.999, eps: float = 1e-8, state_bits: int = 32, states=None, step: int = 0):
+        tensors = adamw_layer_tensors(X, G, layer_off, weight_decay, lr_scale, copy)
+        self.groups = G.shape[0]
+        self._keep = (X, G, copy)      # the list holds their addresses
+        self.handle = choco_adamw_init(tensors, self.groups, beta1, beta2, eps, state_bits)
+        self.m = self.v = self.m_scale = self.v_scale = None
+        self.elements, self.offsets = choco_adamw_state_size(self.handle, len(tensors))
+        if X is not None:
+            if states is None:
+                import torch
+                new = lambda count, dtype: torch.zeros(count, dtype=dtype, device=X.device)  # noqa: E731
+                if state_bits == 32:
+                    states = (new(self.elements, torch.float32), new(self.elements, torch.float32))
+                else:
+                    blocks = self.elements // ADAMW_BLOCK
+                    states = (new(self.elements, torch.int8), new(self.elements, torch.uint8),
+                              new(blocks, torch.float32), new(blocks, torch.float32))
+            self._check_states(states, state_bits)
+            self.m, self.v, self.m_scale, self.v_scale = (tuple(states) + (None, None))[:4]
+        if step:
+            self.set_steps([step] * self.groups)
+
+    def _check_states(self, states, bits):
+        want = [("float32", self.elements)] * 2 if bits == 32 else [
+            ("int8", self.elements), ("uint8", self.elements), ("float32", self.elements // ADAMW_BLOCK),
+            ("float32", self.elements // ADAMW_BLOCK)]
+        got = [(str(a.dtype).rpartition(".")[2], a.numel()) for a in states]
+        if got != want or not all(a.is_contiguous() for a in states):
+            raise ChocoError(f"libchoco: the moments must be contiguous arrays of {want}, not {got}", -1)
+
+    def grad_norm(self, max_norm: float, norm, factor, unscale: float = 1.0, stream=None):
+        choco_adamw_grad_norm(self.handle, max_norm, norm, factor, unscale, stream)
+
+    def step(self, lr: float, factor=None, stream=None):
+        choco_adamw_step(self.handle, self.m, self.v, self.m_scale, self.v_scale, lr, factor, stream)
+
+    def read_state(self, m_out, v_out, stream=None):
+        for a in (m_out, v_out):
+            if a is not None and (a.numel() != self.elements or not a.is_contiguous()):
+                raise ChocoError(f"libchoco: outputs must be contiguous with {self.elements} elements", -1)
+        choco_adamw_read_state(self.handle, self.m, self.v, self.m_scale, self.v_scale, m_out, v_out, stream)
+
+    def get_steps(self, stream=None):
+        return choco_adamw_get_steps(self.handle, self.groups, stream)
+
+    def set_steps(self, steps, stream=None):
+        if len(steps) != self.groups:
+            raise ChocoError(f"libchoco: one step count for each of {self.groups} groups", -1)
+        choco_adamw_set_steps(self.handle, steps, stream)
+
+    def close(self):
+        if getattr(self, "handle", None) is not None:
+            choco_adamw_destroy(self.handle)
+            self.handle = None
 
     def __del__(self):
         try:
