@@ -422,7 +422,7 @@ typedef struct {
     int32_t n;          /* workers, 1 .. 65535                                                 */
     float scale;        /* factor on every row looked up (and on its gradient), finite         */
     int64_t vocab;      /* rows of a table, 1 .. 2^31 - 2                                      */
-    int64_t dim;        /* elements of a row, 1 .. 2^24                                        */
+    int64_t dim;        /* elements of a row, 1 .. 2^22                                        */
     int64_t table_row;  /* elements between rows, >= dim; 0 = dim                              */
     int64_t table_ld;   /* elements between tables, >= (vocab-1) table_row + dim; 0 = vocab table_row */
     int64_t max_tokens; /* most tokens of one worker in a backward call; n max_tokens < 2^31   */
