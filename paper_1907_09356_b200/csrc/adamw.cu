@@ -35,7 +35,8 @@ struct Tensor {
     int64_t state;          // first element in m and v
     float weight_decay, lr_scale;
     int32_t group;
-    int8_t x_dtype, g_dtype, copy_dtype, pad;
+    int8_t x_dtype, g_dtype, copy_dtype;
+    int8_t aligned;         // every array on a 16-byte boundary
 };
 
 // A run of elements of one tensor.  `first`: the first one of its group (exactly one per group).
@@ -62,73 +63,193 @@ __host__ __device__ inline double pow_int(double b, int64_t e)
     return r;
 }
 
+// largest of a warp's non-negative values (their order is that of their bits)
 __device__ __forceinline__ float warp_max(float v)
 {
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
+}
+
+// The nearest k to sqrt(y), y in [0, levels^2]: the number of edges (j - 1/2)^2, j = 1 .., that y
+// reaches (the edges are exact in float32, so that the code does not hang on a square root's
+// rounding).  The approximate root is off by less than 255 * 2^-21 = 1.22e-4; taken 1.3e-4 too low
+// it rounds to k or k - 1, and one comparison decides.  Returned as a float.
+__device__ __forceinline__ float nearest_root(float y)
+{
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
+    constexpr float kRound = 12582912.0f; // 1.5 * 2^23: adding it rounds to an integer
+    const float k = __fadd_rn(__fadd_rn(__fadd_rn(r, -1.3e-4f), kRound), -kRound);
+    const float edge = k + 0.5f;
+    return y >= edge * edge ? k + 1.0f : k;
+}
+// the low byte of an integer held as a float in [-128, 255]
+__device__ __forceinline__ uint32_t byte_of(float k) { return __float_as_uint(__fadd_rn(k, 12582912.0f)); }
+__device__ __forceinline__ uint32_t pack4(const float* k)
+{
+    const uint32_t lo = __byte_perm(byte_of(k[0]), byte_of(k[1]), 0x0040), hi = __byte_perm(byte_of(k[2]), byte_of(k[3]), 0x0040);
+    return __byte_perm(lo, hi, 0x5410);
+}
+// byte e of a word as a float: the byte becomes the last one of 2^23's mantissa
+__device__ __forceinline__ float ubyte(uint32_t w, int e)
+{
+    return __fadd_rn(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 | e)), -8388608.0f);
+}
+__device__ __forceinline__ float sbyte(uint32_t w, int e) // of w ^ 0x80808080
+{
+    return __fadd_rn(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 | e)), -8388736.0f);
+}
+__device__ __forceinline__ float moment_m(float k, float scale) { return (k * fabsf(k)) * scale; }
+__device__ __forceinline__ float root_v(float k, float scale) { return (k * k) * scale; }
+
+// 8 elements whose type is known at run time: 16 or 32 bytes, unpacked after all loads are under way
+struct Raw8 {
+    uint4 a, b;
+};
+__device__ __forceinline__ Raw8 load8(const void* p, int64_t i, int32_t dtype)
+{
+    Raw8 r;
+    if (dtype == CHOCO_F32) {
+        const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + i);
+        r.a = q[0];
+        r.b = q[1];
+    } else {
+        r.a = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(p) + i);
+        r.b = make_uint4(0, 0, 0, 0);
+    }
+    return r;
+}
+__device__ __forceinline__ void unpack8(const Raw8& r, int32_t dtype, float (&f)[8])
+{
+    if (dtype == CHOCO_F32) {
+        f[0] = __uint_as_float(r.a.x); f[1] = __uint_as_float(r.a.y); f[2] = __uint_as_float(r.a.z); f[3] = __uint_as_float(r.a.w);
+        f[4] = __uint_as_float(r.b.x); f[5] = __uint_as_float(r.b.y); f[6] = __uint_as_float(r.b.z); f[7] = __uint_as_float(r.b.w);
+        return;
+    }
+    const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
 #pragma unroll
-    for (int m = 16; m > 0; m >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, m));
-    return v;
-}
-
-// The nearest k to sqrt(y): the code is the number of edges (j - 1/2)^2, j = 1 .., that y reaches
-// (the edges are exact in float32).  The square root is only a first guess.
-__device__ __forceinline__ int nearest_root(float y, int levels)
-{
-    int k = (int)__fsqrt_rn(y);
-    k = min(k, levels);
-    const float up = (float)k + 0.5f;
-    if (k < levels && y >= up * up) k += 1;
-    const float dn = (float)k - 0.5f;
-    if (k > 0 && y < dn * dn) k -= 1;
-    return k;
-}
-
-template <int BITS>
-__global__ void __launch_bounds__(kStepThreads)
-step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
-            int64_t* __restrict__ skipped, void* m_arr, void* v_arr, float* m_scale, float* v_scale, StepScalars sc)
-{
-    const Chunk ch = chunks[blockIdx.x];
-    const Tensor t = tensors[ch.tensor];
-    const int lane = threadIdx.x & 31;
-    float c = 1.0f;
-    if (factor) {
-        c = factor[t.group];
-        if (!isfinite(c)) { // overflowed gradients: the group sits this step out
-            if (ch.first && threadIdx.x == 0) skipped[t.group] += 1;
-            return;
+    for (int k = 0; k < 4; ++k) {
+        if (dtype == CHOCO_BF16) {
+            f[2 * k] = __uint_as_float(w[k] << 16);
+            f[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+        } else {
+            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+            f[2 * k] = v.x;
+            f[2 * k + 1] = v.y;
         }
     }
-    const int64_t base = ch.begin + (int64_t)(threadIdx.x >> 5) * kBlock;
-    if (base >= t.numel) return;
-    const int count = (int)min((int64_t)kBlock, t.numel - base);
-    float step_size = sc.step_size, rs = sc.rsqrt_bc2;
-    const int64_t sk = skipped[t.group];
-    if (sk != 0) { // this group has taken fewer steps than the others
-        const int64_t n = sc.t - sk;
-        step_size = (float)(sc.lrd / (1.0 - pow_int(sc.beta1d, n)));
-        rs = (float)(1.0 / sqrt(1.0 - pow_int(sc.beta2d, n)));
-    }
-    step_size *= t.lr_scale;
-    const float lrwd = t.weight_decay * (sc.lr * t.lr_scale);
-    const int64_t s0 = t.state + base;
-    const int64_t sb = s0 / kBlock;
+}
+__device__ __forceinline__ void store8(void* p, int64_t i, int32_t dtype, const float* f)
+{
+    if (dtype == CHOCO_F32) store_vec<float, 8>(static_cast<float*>(p) + i, f);
+    else if (dtype == CHOCO_BF16) store_vec<__nv_bfloat16, 8>(static_cast<__nv_bfloat16*>(p) + i, f);
+    else store_vec<__half, 8>(static_cast<__half*>(p) + i, f);
+}
 
-    float m[8], v[8];
+// What a step multiplies with, for one tensor of one group.
+struct Factors {
+    float c, step_size, rsqrt_bc2, decay;
+};
+
+// One element: m, v and x in, new ones out; returns sqrt(v).
+__device__ __forceinline__ float adamw_element(const StepScalars& sc, const Factors& f, float g, float& x, float& m, float& v)
+{
+    g *= f.c;
+    m = m * sc.beta1 + g * sc.omb1;
+    v = v * sc.beta2 + (g * sc.omb2) * g;
+    const float r = __fsqrt_rn(v);
+    const float den = r * f.rsqrt_bc2 + sc.eps;
+    x = x - (__fdiv_rn(m, den) * f.step_size + x * f.decay);
+    return r;
+}
+
+struct State {
+    void *m, *v;
+    float *m_scale, *v_scale;
+};
+
+// A whole block of an aligned tensor: a lane owns 8 consecutive elements, moved in 128-bit accesses.
+template <int BITS>
+__device__ __forceinline__ void step_block(const Tensor& t, const State& st, const StepScalars& sc, const Factors& f, int64_t base)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t i = base + lane * 8, s = t.state + i, sb = (t.state + base) / kBlock;
+    const Raw8 rg = load8(t.g, i, t.g_dtype), rx = load8(t.x, i, t.x_dtype);
+    float g[8], x[8], m[8], v[8];
+    if constexpr (BITS == 32) {
+        const Raw8 rm = load8(st.m, s, CHOCO_F32), rv = load8(st.v, s, CHOCO_F32);
+        unpack8(rm, CHOCO_F32, m);
+        unpack8(rv, CHOCO_F32, v);
+    } else {
+        const uint2 km = *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(st.m) + s);
+        const uint2 kv = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(st.v) + s);
+        const float sm = st.m_scale[sb], sv = st.v_scale[sb];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            m[e] = moment_m(sbyte((e < 4 ? km.x : km.y) ^ 0x80808080u, e & 3), sm);
+            const float r = root_v(ubyte(e < 4 ? kv.x : kv.y, e & 3), sv);
+            v[e] = r * r;
+        }
+    }
+    unpack8(rg, t.g_dtype, g);
+    unpack8(rx, t.x_dtype, x);
+    float amax = 0.f, rmax = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float r = adamw_element(sc, f, g[e], x[e], m[e], v[e]);
+        if constexpr (BITS == 8) {
+            v[e] = r;
+            amax = fmaxf(amax, fabsf(m[e]));
+            rmax = fmaxf(rmax, r);
+        }
+    }
+    store8(t.x, i, t.x_dtype, x);
+    if (t.copy) store8(t.copy, i, t.copy_dtype, x);
+    if constexpr (BITS == 32) {
+        store8(st.m, s, CHOCO_F32, m);
+        store8(st.v, s, CHOCO_F32, v);
+    } else {
+        amax = fmaxf(warp_max(amax), kTiny);
+        rmax = fmaxf(warp_max(rmax), kTiny);
+        const float im = __fdiv_rn(kLevelsM, amax), iv = __fdiv_rn(kLevelsV, rmax);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            m[e] = copysignf(nearest_root(fabsf(m[e]) * im), m[e]);
+            const float k = nearest_root(v[e] * iv);
+            v[e] = v[e] > 0.f ? fmaxf(k, 1.0f) : k;
+        }
+        *reinterpret_cast<uint2*>(static_cast<int8_t*>(st.m) + s) = make_uint2(pack4(m), pack4(m + 4));
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(st.v) + s) = make_uint2(pack4(v), pack4(v + 4));
+        if (lane == 0) {
+            st.m_scale[sb] = amax * (1.0f / kLevelsM);
+            st.v_scale[sb] = rmax * (1.0f / kLevelsV);
+        }
+    }
+}
+
+// Any block: a lane owns every 32nd element, so that single elements still make whole lines; the
+// last block of a tensor and tensors that do not start on 16 bytes.
+template <int BITS>
+__device__ __forceinline__ void step_block_any(const Tensor& t, const State& st, const StepScalars& sc, const Factors& f, int64_t base,
+                                               int count)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t s0 = t.state + base, sb = s0 / kBlock;
+    float g[8], x[8], m[8], v[8];
+    float sm = 0.f, sv = 0.f;
+    if (BITS == 8) { sm = st.m_scale[sb]; sv = st.v_scale[sb]; }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int e = j * 32 + lane;
-        m[j] = 0.f;
-        v[j] = 0.f;
+        g[j] = x[j] = m[j] = v[j] = 0.f;
         if (e >= count) continue;
-        if (BITS == 32) {
-            m[j] = static_cast<const float*>(m_arr)[s0 + e];
-            v[j] = static_cast<const float*>(v_arr)[s0 + e];
+        g[j] = load_as_float(t.g, base + e, t.g_dtype);
+        x[j] = load_as_float(t.x, base + e, t.x_dtype);
+        if constexpr (BITS == 32) {
+            m[j] = static_cast<const float*>(st.m)[s0 + e];
+            v[j] = static_cast<const float*>(st.v)[s0 + e];
         } else {
-            const float km = (float)static_cast<const int8_t*>(m_arr)[s0 + e];
-            const float kv = (float)static_cast<const uint8_t*>(v_arr)[s0 + e];
-            m[j] = (km * fabsf(km)) * m_scale[sb];
-            const float r = (kv * kv) * v_scale[sb];
-            v[j] = r * r;
+            m[j] = (float)static_cast<const int8_t*>(st.m)[s0 + e];
+            v[j] = (float)static_cast<const uint8_t*>(st.v)[s0 + e];
         }
     }
     float amax = 0.f, rmax = 0.f;
@@ -136,25 +257,24 @@ step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks
     for (int j = 0; j < 8; ++j) {
         const int e = j * 32 + lane;
         if (e >= count) continue;
-        const float g = load_as_float(t.g, base + e, t.g_dtype) * c;
-        const float x = load_as_float(t.x, base + e, t.x_dtype);
-        m[j] = m[j] * sc.beta1 + g * sc.omb1;
-        v[j] = v[j] * sc.beta2 + (g * sc.omb2) * g;
-        const float r = __fsqrt_rn(v[j]);
-        const float den = r * rs + sc.eps;
-        const float nx = x - (__fdiv_rn(m[j], den) * step_size + x * lrwd);
-        store_from_float(t.x, base + e, t.x_dtype, nx);
-        if (t.copy) store_from_float(t.copy, base + e, t.copy_dtype, nx);
-        if (BITS == 32) {
-            static_cast<float*>(m_arr)[s0 + e] = m[j];
-            static_cast<float*>(v_arr)[s0 + e] = v[j];
+        if constexpr (BITS == 8) {
+            m[j] = moment_m(m[j], sm);
+            const float r = root_v(v[j], sv);
+            v[j] = r * r;
+        }
+        const float r = adamw_element(sc, f, g[j], x[j], m[j], v[j]);
+        store_from_float(t.x, base + e, t.x_dtype, x[j]);
+        if (t.copy) store_from_float(t.copy, base + e, t.copy_dtype, x[j]);
+        if constexpr (BITS == 32) {
+            static_cast<float*>(st.m)[s0 + e] = m[j];
+            static_cast<float*>(st.v)[s0 + e] = v[j];
         } else {
             v[j] = r;
             amax = fmaxf(amax, fabsf(m[j]));
             rmax = fmaxf(rmax, r);
         }
     }
-    if (BITS == 8) {
+    if constexpr (BITS == 8) {
         amax = fmaxf(warp_max(amax), kTiny);
         rmax = fmaxf(warp_max(rmax), kTiny);
         const float im = __fdiv_rn(kLevelsM, amax), iv = __fdiv_rn(kLevelsV, rmax);
@@ -162,46 +282,82 @@ step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks
         for (int j = 0; j < 8; ++j) {
             const int e = j * 32 + lane;
             if (e >= count) continue;
-            const int km = nearest_root(fabsf(m[j]) * im, 127);
-            int kv = nearest_root(v[j] * iv, 255);
-            if (kv == 0 && v[j] > 0.f) kv = 1;
-            static_cast<int8_t*>(m_arr)[s0 + e] = (int8_t)(m[j] < 0.f ? -km : km);
-            static_cast<uint8_t*>(v_arr)[s0 + e] = (uint8_t)kv;
+            const float km = copysignf(nearest_root(fabsf(m[j]) * im), m[j]);
+            float kv = nearest_root(v[j] * iv);
+            if (v[j] > 0.f) kv = fmaxf(kv, 1.0f);
+            static_cast<uint8_t*>(st.m)[s0 + e] = (uint8_t)byte_of(km);
+            static_cast<uint8_t*>(st.v)[s0 + e] = (uint8_t)byte_of(kv);
         }
         if (lane == 0) {
-            m_scale[sb] = amax * (1.0f / kLevelsM);
-            v_scale[sb] = rmax * (1.0f / kLevelsV);
+            st.m_scale[sb] = amax * (1.0f / kLevelsM);
+            st.v_scale[sb] = rmax * (1.0f / kLevelsV);
         }
     }
 }
 
-__global__ void __launch_bounds__(256) read_state_kernel(const void* m, const void* v, const float* m_scale,
-                                                         const float* v_scale, void* m_out, void* v_out, int32_t dtype,
-                                                         int32_t bits, int64_t elements)
+// One block of threads per chunk, one warp per block of elements.  The chunks are taken from the
+// last one: choco_adamw_grad_norm has read the gradients from the first one on, and what it read
+// last is what the L2 cache still holds.
+template <int BITS>
+__global__ void __launch_bounds__(kStepThreads)
+step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
+            int64_t* __restrict__ skipped, State st, StepScalars sc)
 {
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= elements) return;
-    if (m_out) {
-        float a;
-        if (bits == 32) {
-            a = static_cast<const float*>(m)[e];
-        } else {
-            const float k = (float)static_cast<const int8_t*>(m)[e];
-            a = (k * fabsf(k)) * m_scale[e / kBlock];
+    wait_for_previous_kernel();
+    allow_next_kernel();
+    const Chunk ch = chunks[gridDim.x - 1 - blockIdx.x];
+    const Tensor t = tensors[ch.tensor];
+    Factors f;
+    f.c = 1.0f;
+    if (factor) {
+        f.c = factor[t.group];
+        if (!isfinite(f.c)) { // overflowed gradients: the group sits this step out
+            if (ch.first && threadIdx.x == 0) skipped[t.group] += 1;
+            return;
         }
-        store_from_float(m_out, e, dtype, a);
     }
-    if (v_out) {
-        float a;
-        if (bits == 32) {
-            a = static_cast<const float*>(v)[e];
-        } else {
-            const float k = (float)static_cast<const uint8_t*>(v)[e];
-            const float r = (k * k) * v_scale[e / kBlock];
-            a = r * r;
+    const int64_t base = ch.begin + (int64_t)(threadIdx.x >> 5) * kBlock;
+    if (base >= t.numel) return;
+    f.step_size = sc.step_size;
+    f.rsqrt_bc2 = sc.rsqrt_bc2;
+    const int64_t sk = skipped[t.group];
+    if (sk != 0) { // this group has taken fewer steps than the others
+        const int64_t n = sc.t - sk;
+        f.step_size = (float)(sc.lrd / (1.0 - pow_int(sc.beta1d, n)));
+        f.rsqrt_bc2 = (float)(1.0 / sqrt(1.0 - pow_int(sc.beta2d, n)));
+    }
+    f.step_size *= t.lr_scale;
+    f.decay = t.weight_decay * (sc.lr * t.lr_scale);
+    if (t.aligned && base + kBlock <= t.numel) step_block<BITS>(t, st, sc, f, base);
+    else step_block_any<BITS>(t, st, sc, f, base, (int)min((int64_t)kBlock, t.numel - base));
+}
+
+// 8 elements per thread; the moments are whole blocks.
+template <int BITS>
+__global__ void __launch_bounds__(256) read_state_kernel(State st, void* m_out, void* v_out, int32_t dtype, int64_t elements)
+{
+    wait_for_previous_kernel();
+    allow_next_kernel();
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (i >= elements) return;
+    float m[8], v[8];
+    if constexpr (BITS == 32) {
+        if (m_out) unpack8(load8(st.m, i, CHOCO_F32), CHOCO_F32, m);
+        if (v_out) unpack8(load8(st.v, i, CHOCO_F32), CHOCO_F32, v);
+    } else {
+        uint2 km = make_uint2(0, 0), kv = make_uint2(0, 0);
+        float sm = 0.f, sv = 0.f;
+        if (m_out) { km = *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(st.m) + i); sm = st.m_scale[i / kBlock]; }
+        if (v_out) { kv = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(st.v) + i); sv = st.v_scale[i / kBlock]; }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            m[e] = moment_m(sbyte((e < 4 ? km.x : km.y) ^ 0x80808080u, e & 3), sm);
+            const float r = root_v(ubyte(e < 4 ? kv.x : kv.y, e & 3), sv);
+            v[e] = r * r;
         }
-        store_from_float(v_out, e, dtype, a);
     }
+    if (m_out) store8(m_out, i, dtype, m);
+    if (v_out) store8(v_out, i, dtype, v);
 }
 
 // Sum of squares of one unit (a run of one tensor's gradient), in float64: squares of float32
@@ -210,22 +366,42 @@ __global__ void __launch_bounds__(kNormThreads) norm_partial_kernel(const Tensor
                                                                     const Chunk* __restrict__ units, int64_t unit_elems,
                                                                     double* __restrict__ partial)
 {
-    __shared__ double red[kNormThreads];
+    __shared__ double red[kNormThreads / 32];
+    wait_for_previous_kernel();
+    allow_next_kernel();
     const Chunk u = units[blockIdx.x];
     const Tensor t = tensors[u.tensor];
     const int64_t end = min(u.begin + unit_elems, t.numel);
     double acc = 0.0;
-    for (int64_t e = u.begin + threadIdx.x; e < end; e += kNormThreads) {
+    int64_t done = u.begin;
+    if (t.aligned) {
+        constexpr int kAhead = 4;           // vectors of a thread in flight
+        constexpr int kSpanElems = kNormThreads * 8;
+        for (; done + kAhead * kSpanElems <= end; done += kAhead * kSpanElems) {
+            Raw8 r[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) r[k] = load8(t.g, done + k * kSpanElems + threadIdx.x * 8, t.g_dtype);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                float g[8];
+                unpack8(r[k], t.g_dtype, g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc = __fma_rn((double)g[e], (double)g[e], acc);
+            }
+        }
+    }
+    for (int64_t e = done + threadIdx.x; e < end; e += kNormThreads) {
         const double g = (double)load_as_float(t.g, e, t.g_dtype);
         acc = __fma_rn(g, g, acc);
     }
-    red[threadIdx.x] = acc;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = acc;
     __syncthreads();
-    for (int o = kNormThreads / 2; o > 0; o >>= 1) {
-        if (threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-        __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kNormThreads / 32; ++w) acc += red[w];
+        partial[blockIdx.x] = acc;
     }
-    if (threadIdx.x == 0) partial[blockIdx.x] = red[0];
 }
 
 // One block per group: the units of a group are contiguous.
@@ -233,17 +409,18 @@ __global__ void __launch_bounds__(kNormThreads) norm_finish_kernel(const double*
                                                                    const int64_t* __restrict__ unit_begin, float max_norm,
                                                                    float unscale, float* norm, float* factor)
 {
-    __shared__ double red[kNormThreads];
+    __shared__ double red[kNormThreads / 32];
+    wait_for_previous_kernel();
+    allow_next_kernel();
     double acc = 0.0;
     for (int64_t u = unit_begin[blockIdx.x] + threadIdx.x; u < unit_begin[blockIdx.x + 1]; u += kNormThreads) acc += partial[u];
-    red[threadIdx.x] = acc;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = acc;
     __syncthreads();
-    for (int o = kNormThreads / 2; o > 0; o >>= 1) {
-        if (threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-        __syncthreads();
-    }
     if (threadIdx.x == 0) {
-        const double nrm = (double)unscale * sqrt(red[0]);
+        for (int w = 1; w < kNormThreads / 32; ++w) acc += red[w];
+        const double nrm = (double)unscale * sqrt(acc);
         norm[blockIdx.x] = (float)nrm;
         double f = (double)unscale;
         if (max_norm > 0.f) {
@@ -291,7 +468,12 @@ bool upload(T** out, const T* src, size_t count)
     return count == 0 || cudaMemcpy(*out, src, sizeof(T) * count, cudaMemcpyHostToDevice) == cudaSuccess;
 }
 
-int status_of_launch() { return cudaGetLastError() == cudaSuccess ? CHOCO_OK : CHOCO_ERR_CUDA; }
+int status_of(cudaError_t e)
+{
+    if (e == cudaSuccess) return CHOCO_OK;
+    cudaGetLastError();
+    return CHOCO_ERR_CUDA;
+}
 
 void free_all(choco_adamw* o)
 {
@@ -303,6 +485,8 @@ void free_all(choco_adamw* o)
     cudaFree(o->d_partial);
     delete o;
 }
+
+bool all_aligned(const Tensor& t) { return aligned_to(t.x, 16) && aligned_to(t.g, 16) && aligned_to(t.copy, 16); }
 
 // Fills the host tables of `o`.  Throws std::bad_alloc.
 int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Chunk>& chunks, std::vector<Chunk>& units,
@@ -331,6 +515,7 @@ int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Ch
         d.lr_scale = (float)t.lr_scale;
         d.group = t.group;
         d.x_dtype = (int8_t)t.x_dtype; d.g_dtype = (int8_t)t.g_dtype; d.copy_dtype = (int8_t)t.copy_dtype;
+        d.aligned = all_aligned(d);
         o->tensors.push_back(d);
         o->offsets.push_back(at);
         at += (t.numel + kBlock - 1) / kBlock * kBlock;
@@ -419,7 +604,10 @@ int choco_adamw_set_grads(choco_adamw* opt, const void* const* g, void* stream)
     }
     cudaStream_t st = (cudaStream_t)stream;
     if (cudaStreamSynchronize(st) != cudaSuccess) return CHOCO_ERR_CUDA;
-    for (size_t i = 0; i < opt->tensors.size(); ++i) opt->tensors[i].g = g[i];
+    for (size_t i = 0; i < opt->tensors.size(); ++i) {
+        opt->tensors[i].g = g[i];
+        opt->tensors[i].aligned = all_aligned(opt->tensors[i]);
+    }
     if (cudaMemcpyAsync(opt->d_tensors, opt->tensors.data(), sizeof(Tensor) * opt->tensors.size(), cudaMemcpyHostToDevice, st) !=
             cudaSuccess ||
         cudaStreamSynchronize(st) != cudaSuccess)
@@ -434,12 +622,15 @@ int choco_adamw_grad_norm(choco_adamw* opt, float max_norm, float unscale, float
         return CHOCO_ERR_INVALID_ARG;
     if (!aligned_to(norm, 4) || !aligned_to(factor, 4)) return CHOCO_ERR_MISALIGNED;
     cudaStream_t st = (cudaStream_t)stream;
+    const dim3 threads(kNormThreads);
+    cudaError_t err = cudaSuccess;
     if (opt->nunits > 0)
-        norm_partial_kernel<<<(unsigned)opt->nunits, kNormThreads, 0, st>>>(opt->d_tensors, opt->d_units, opt->unit_elems,
-                                                                            opt->d_partial);
-    norm_finish_kernel<<<(unsigned)opt->params.groups, kNormThreads, 0, st>>>(opt->d_partial, opt->d_unit_begin, max_norm,
-                                                                             unscale, norm, factor);
-    return status_of_launch();
+        err = launch_overlapped(norm_partial_kernel, dim3((unsigned)opt->nunits), threads, 0, st, HotRange{}, opt->d_tensors, opt->d_units,
+                                opt->unit_elems, opt->d_partial);
+    if (err == cudaSuccess)
+        err = launch_overlapped(norm_finish_kernel, dim3((unsigned)opt->params.groups), threads, 0, st, HotRange{}, opt->d_partial,
+                                opt->d_unit_begin, max_norm, unscale, norm, factor);
+    return status_of(err);
 }
 
 int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* v_scale, double lr, const float* factor,
@@ -462,13 +653,10 @@ int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* 
     sc.rsqrt_bc2 = (float)(1.0 / std::sqrt(1.0 - pow_int(p.beta2, sc.t)));
     cudaStream_t st = (cudaStream_t)stream;
     if (opt->nchunks > 0) {
-        if (eight)
-            step_kernel<8><<<(unsigned)opt->nchunks, kStepThreads, 0, st>>>(opt->d_tensors, opt->d_chunks, factor, opt->d_skipped, m,
-                                                                            v, m_scale, v_scale, sc);
-        else
-            step_kernel<32><<<(unsigned)opt->nchunks, kStepThreads, 0, st>>>(opt->d_tensors, opt->d_chunks, factor, opt->d_skipped,
-                                                                             m, v, m_scale, v_scale, sc);
-        const int rc = status_of_launch();
+        const State state = {m, v, m_scale, v_scale};
+        const int rc = status_of(launch_overlapped(eight ? step_kernel<8> : step_kernel<32>, dim3((unsigned)opt->nchunks),
+                                                   dim3(kStepThreads), 0, st, HotRange{}, opt->d_tensors, opt->d_chunks, factor,
+                                                   opt->d_skipped, state, sc));
         if (rc != CHOCO_OK) return rc;
     }
     opt->t += 1;
@@ -485,9 +673,10 @@ int choco_adamw_read_state(choco_adamw* opt, const void* m, const void* v, const
         !aligned_to(m_out, 16) || !aligned_to(v_out, 16))
         return CHOCO_ERR_MISALIGNED;
     if (opt->elements == 0 || (!m_out && !v_out)) return CHOCO_OK;
-    read_state_kernel<<<(unsigned)((opt->elements + 255) / 256), 256, 0, (cudaStream_t)stream>>>(
-        m, v, m_scale, v_scale, m_out, v_out, out_dtype, opt->params.state_bits, opt->elements);
-    return status_of_launch();
+    const State state = {const_cast<void*>(m), const_cast<void*>(v), const_cast<float*>(m_scale), const_cast<float*>(v_scale)};
+    const dim3 grid((unsigned)((opt->elements / 8 + 255) / 256)), threads(256);
+    return status_of(launch_overlapped(eight ? read_state_kernel<8> : read_state_kernel<32>, grid, threads, 0, (cudaStream_t)stream,
+                                       HotRange{}, state, m_out, v_out, out_dtype, opt->elements));
 }
 
 int choco_adamw_get_steps(choco_adamw* opt, int64_t* steps, void* stream)
