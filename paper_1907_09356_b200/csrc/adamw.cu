@@ -18,12 +18,14 @@ using namespace choco;
 namespace {
 
 constexpr int kBlock = 256;                 // elements that share a scale; tensors start on multiples of it in m and v
-constexpr int kStepThreads = 256;
+constexpr int kStepThreads = 128;            // short blocks: 256 threads took 5 % more, 64 no less
 constexpr int kStepWarps = kStepThreads / 32;
 constexpr int kChunkElems = kStepWarps * kBlock;
+// blocks on an SM: 64 registers a thread with 32-bit moments, 48 with codes, where more warps pay (552 us against 579)
+constexpr int kStepBlocks32 = 8, kStepBlocks8 = 10;
 constexpr int kNormThreads = 256;
-constexpr float kLevelsM = 127.0f * 127.0f; // codes k stand for s k^2, k up to 127 (m) and 255 (sqrt v)
-constexpr float kLevelsV = 255.0f * 255.0f;
+constexpr float kCodesM = 127.0f;           // codes k stand for s k^2, k up to 127 (m) and 255 (sqrt v)
+constexpr float kCodesV = 255.0f;
 constexpr float kTiny = 1e-30f;             // smallest largest-value of a block: keeps its reciprocal finite
 constexpr double kNormEps = 1e-6;
 
@@ -48,14 +50,15 @@ struct Chunk {
 
 struct StepScalars {
     float beta1, beta2, omb1, omb2, eps;
+    float root_beta2, root_omb2; // sqrt(beta2), sqrt(1 - beta2)
     float lr;
     float step_size;        // lr / (1 - beta1^t)
     float rsqrt_bc2;        // 1 / sqrt(1 - beta2^t)
-    double beta1d, beta2d, lrd;
+    float log_beta1, log_beta2; // natural logarithms
     int64_t t;
 };
 
-__host__ __device__ inline double pow_int(double b, int64_t e)
+inline double pow_int(double b, int64_t e)
 {
     double r = 1.0;
     for (; e > 0; e >>= 1, b *= b)
@@ -69,37 +72,40 @@ __device__ __forceinline__ float warp_max(float v)
     return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
 }
 
-// The nearest k to sqrt(y), y in [0, levels^2]: the number of edges (j - 1/2)^2, j = 1 .., that y
-// reaches (the edges are exact in float32, so that the code does not hang on a square root's
-// rounding).  The approximate root is off by less than 255 * 2^-21 = 1.22e-4; taken 1.3e-4 too low
-// it rounds to k or k - 1, and one comparison decides.  Returned as a float.
-__device__ __forceinline__ float nearest_root(float y)
+__device__ __forceinline__ float root_approx(float v) // within 2^-22 of sqrt(v)
 {
     float r;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
-    constexpr float kRound = 12582912.0f; // 1.5 * 2^23: adding it rounds to an integer
-    const float k = __fadd_rn(__fadd_rn(__fadd_rn(r, -1.3e-4f), kRound), -kRound);
-    const float edge = k + 0.5f;
-    return y >= edge * edge ? k + 1.0f : k;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
 }
-// the low byte of an integer held as a float in [-128, 255]
-__device__ __forceinline__ uint32_t byte_of(float k) { return __float_as_uint(__fadd_rn(k, 12582912.0f)); }
-__device__ __forceinline__ uint32_t pack4(const float* k)
+__device__ __forceinline__ float reciprocal_approx(float v) // within 2^-22 of 1 / v
 {
-    const uint32_t lo = __byte_perm(byte_of(k[0]), byte_of(k[1]), 0x0040), hi = __byte_perm(byte_of(k[2]), byte_of(k[3]), 0x0040);
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+constexpr float kRound = 12582912.0f; // 1.5 * 2^23: adding it rounds to an integer, held in the low bits
+__device__ __forceinline__ uint32_t pack4(const float* k) // low bytes of four of those
+{
+    const uint32_t lo = __byte_perm(__float_as_uint(k[0]), __float_as_uint(k[1]), 0x0040);
+    const uint32_t hi = __byte_perm(__float_as_uint(k[2]), __float_as_uint(k[3]), 0x0040);
     return __byte_perm(lo, hi, 0x5410);
 }
-// byte e of a word as a float: the byte becomes the last one of 2^23's mantissa
-__device__ __forceinline__ float ubyte(uint32_t w, int e)
+// 2^23 plus byte e of a word
+__device__ __forceinline__ float byte_bits(uint32_t w, int e) { return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 | e)); }
+
+// Codes as byte_bits leaves them (m's with 128 added) to k |k| and k^2: times the block's scale, m and sqrt(v).
+__device__ __forceinline__ float square_m(float bits)
 {
-    return __fadd_rn(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 | e)), -8388608.0f);
+    const float k = __fadd_rn(bits, -8388736.0f);
+    return k * fabsf(k);
 }
-__device__ __forceinline__ float sbyte(uint32_t w, int e) // of w ^ 0x80808080
+__device__ __forceinline__ float square_v(float bits)
 {
-    return __fadd_rn(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 | e)), -8388736.0f);
+    const float k = __fadd_rn(bits, -8388608.0f);
+    return k * k;
 }
-__device__ __forceinline__ float moment_m(float k, float scale) { return (k * fabsf(k)) * scale; }
-__device__ __forceinline__ float root_v(float k, float scale) { return (k * k) * scale; }
 
 // 8 elements whose type is known at run time: 16 or 32 bytes, unpacked after all loads are under way
 struct Raw8 {
@@ -150,186 +156,277 @@ struct Factors {
     float c, step_size, rsqrt_bc2, decay;
 };
 
-// One element: m, v and x in, new ones out; returns sqrt(v).
-__device__ __forceinline__ float adamw_element(const StepScalars& sc, const Factors& f, float g, float& x, float& m, float& v)
-{
-    g *= f.c;
-    m = m * sc.beta1 + g * sc.omb1;
-    v = v * sc.beta2 + (g * sc.omb2) * g;
-    const float r = __fsqrt_rn(v);
-    const float den = r * f.rsqrt_bc2 + sc.eps;
-    x = x - (__fdiv_rn(m, den) * f.step_size + x * f.decay);
-    return r;
-}
-
 struct State {
     void *m, *v;
     float *m_scale, *v_scale;
 };
 
-// A whole block of an aligned tensor: a lane owns 8 consecutive elements, moved in 128-bit accesses.
-template <int BITS>
-__device__ __forceinline__ void step_block(const Tensor& t, const State& st, const StepScalars& sc, const Factors& f, int64_t base)
+// 8 elements with moments in 32 bits: IEEE operations one by one, so that the result is the
+// formula's in float32, bit for bit.
+__device__ __forceinline__ void update8(const StepScalars& sc, const Factors& f, float (&g)[8], float (&x)[8], float (&m)[8], float (&v)[8])
 {
-    const int lane = threadIdx.x & 31;
-    const int64_t i = base + lane * 8, s = t.state + i, sb = (t.state + base) / kBlock;
-    const Raw8 rg = load8(t.g, i, t.g_dtype), rx = load8(t.x, i, t.x_dtype);
-    float g[8], x[8], m[8], v[8];
-    if constexpr (BITS == 32) {
-        const Raw8 rm = load8(st.m, s, CHOCO_F32), rv = load8(st.v, s, CHOCO_F32);
-        unpack8(rm, CHOCO_F32, m);
-        unpack8(rv, CHOCO_F32, v);
-    } else {
-        const uint2 km = *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(st.m) + s);
-        const uint2 kv = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(st.v) + s);
-        const float sm = st.m_scale[sb], sv = st.v_scale[sb];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            m[e] = moment_m(sbyte((e < 4 ? km.x : km.y) ^ 0x80808080u, e & 3), sm);
-            const float r = root_v(ubyte(e < 4 ? kv.x : kv.y, e & 3), sv);
-            v[e] = r * r;
-        }
-    }
-    unpack8(rg, t.g_dtype, g);
-    unpack8(rx, t.x_dtype, x);
-    float amax = 0.f, rmax = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float r = adamw_element(sc, f, g[e], x[e], m[e], v[e]);
-        if constexpr (BITS == 8) {
-            v[e] = r;
-            amax = fmaxf(amax, fabsf(m[e]));
-            rmax = fmaxf(rmax, r);
-        }
+        g[e] *= f.c;
+        m[e] = m[e] * sc.beta1 + g[e] * sc.omb1;
+        v[e] = v[e] * sc.beta2 + (g[e] * sc.omb2) * g[e];
+        const float den = __fsqrt_rn(v[e]) * f.rsqrt_bc2 + sc.eps;
+        x[e] = x[e] - (__fdiv_rn(m[e], den) * f.step_size + x[e] * f.decay);
     }
-    store8(t.x, i, t.x_dtype, x);
-    if (t.copy) store8(t.copy, i, t.copy_dtype, x);
-    if constexpr (BITS == 32) {
-        store8(st.m, s, CHOCO_F32, m);
-        store8(st.v, s, CHOCO_F32, v);
-    } else {
-        amax = fmaxf(warp_max(amax), kTiny);
-        rmax = fmaxf(warp_max(rmax), kTiny);
-        const float im = __fdiv_rn(kLevelsM, amax), iv = __fdiv_rn(kLevelsV, rmax);
+}
+
+// A lane's 8 elements of a block with moments in 8 bits.  In: the codes as byte_bits leaves them and
+// the block's scales; out: x, the new codes as floats that hold them in their low bytes, and the new
+// scales.  Here instructions and registers, not bytes, would be the bound (with IEEE roots, quotients
+// and separate products 99 instructions an element: 828 us for 8 x 25.6 M elements whose bytes take
+// 507): products are fused, and roots and quotients are the approximate ones, whose 2^-22 is
+// nothing beside the per cent that a code rounds by.  Elements past the end of a tensor come as
+// zeros and stay zeros.
+__device__ __forceinline__ void update8_codes(const StepScalars& sc, const Factors& f, float (&g)[8], float (&x)[8], float (&m)[8],
+                                              float (&v)[8], float& sm, float& sv)
+{
+    float amax = 0.f, rmax = 0.f;
+    const float sm1 = sm * sc.beta1, sv2 = sv * sc.root_beta2, gm = f.c * sc.omb1, gv = f.c * sc.root_omb2;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            m[e] = copysignf(nearest_root(fabsf(m[e]) * im), m[e]);
-            const float k = nearest_root(v[e] * iv);
-            v[e] = v[e] > 0.f ? fmaxf(k, 1.0f) : k;
-        }
-        *reinterpret_cast<uint2*>(static_cast<int8_t*>(st.m) + s) = make_uint2(pack4(m), pack4(m + 4));
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(st.v) + s) = make_uint2(pack4(v), pack4(v + 4));
-        if (lane == 0) {
-            st.m_scale[sb] = amax * (1.0f / kLevelsM);
-            st.v_scale[sb] = rmax * (1.0f / kLevelsV);
+    for (int e = 0; e < 8; ++e) {
+        m[e] = __fmaf_rn(square_m(m[e]), sm1, g[e] * gm);
+        const float r0 = square_v(v[e]) * sv2, q = g[e] * gv;
+        v[e] = root_approx(__fmaf_rn(r0, r0, q * q));
+        const float ratio = m[e] * reciprocal_approx(__fmaf_rn(v[e], f.rsqrt_bc2, sc.eps));
+        x[e] = __fmaf_rn(-f.step_size, ratio, __fmaf_rn(-f.decay, x[e], x[e]));
+        amax = fmaxf(amax, fabsf(m[e]));
+        rmax = fmaxf(rmax, v[e]);
+    }
+    amax = fmaxf(warp_max(amax), kTiny);
+    rmax = fmaxf(warp_max(rmax), kTiny);
+    sm = amax * (1.0f / (kCodesM * kCodesM));
+    sv = rmax * (1.0f / (kCodesV * kCodesV));
+    const float to_m = kCodesM * rsqrtf(amax), to_v = kCodesV * rsqrtf(rmax);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        m[e] = __fmaf_rn(copysignf(root_approx(fabsf(m[e])), m[e]), to_m, kRound);
+        const float k = __fmaf_rn(root_approx(v[e]), to_v, kRound);
+        v[e] = v[e] > 0.f ? fmaxf(k, kRound + 1.0f) : k; // at least 1 where v > 0
+    }
+}
+
+// What a lane needs of a whole block of an aligned tensor: 8 consecutive elements, moved in 128-bit
+// accesses.
+template <int BITS, typename XT, typename GT>
+struct Loaded {
+    Raw<GT, 8> g;
+    Raw<XT, 8> x;
+    Raw<float, BITS == 32 ? 8 : 2> m, v; // in 8 bits the two words are the codes
+    float sm, sv;
+};
+
+template <int BITS, typename XT, typename GT>
+__device__ __forceinline__ void load_block(Loaded<BITS, XT, GT>& l, const Tensor& t, const State& st, int64_t base)
+{
+    const int64_t i = base + (threadIdx.x & 31) * 8, s = t.state + i;
+    load_raw(l.g, static_cast<const GT*>(t.g) + i);
+    load_raw(l.x, static_cast<const XT*>(t.x) + i);
+    if constexpr (BITS == 32) {
+        load_raw(l.m, static_cast<const float*>(st.m) + s);
+        load_raw(l.v, static_cast<const float*>(st.v) + s);
+    } else {
+        load_raw(l.m, reinterpret_cast<const float*>(static_cast<const uint8_t*>(st.m) + s));
+        load_raw(l.v, reinterpret_cast<const float*>(static_cast<const uint8_t*>(st.v) + s));
+        l.sm = st.m_scale[s / kBlock];
+        l.sv = st.v_scale[s / kBlock];
+    }
+}
+
+template <int BITS, typename XT, typename GT>
+__device__ __forceinline__ void finish_block(Loaded<BITS, XT, GT>& l, const Tensor& t, const State& st, const StepScalars& sc,
+                                             const Factors& f, int64_t base)
+{
+    const int64_t i = base + (threadIdx.x & 31) * 8, s = t.state + i;
+    float g[8], x[8], m[8], v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        g[e] = raw_get(l.g, e);
+        x[e] = raw_get(l.x, e);
+        if constexpr (BITS == 32) {
+            m[e] = raw_get(l.m, e);
+            v[e] = raw_get(l.v, e);
+        } else {
+            m[e] = byte_bits(l.m.w[e / 4] ^ 0x80808080u, e & 3);
+            v[e] = byte_bits(l.v.w[e / 4], e & 3);
         }
     }
+    if constexpr (BITS == 32) {
+        update8(sc, f, g, x, m, v);
+        store_vec<float, 8>(static_cast<float*>(st.m) + s, m);
+        store_vec<float, 8>(static_cast<float*>(st.v) + s, v);
+    } else {
+        update8_codes(sc, f, g, x, m, v, l.sm, l.sv);
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(st.m) + s) = make_uint2(pack4(m), pack4(m + 4));
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(st.v) + s) = make_uint2(pack4(v), pack4(v + 4));
+        if ((threadIdx.x & 31) == 0) {
+            st.m_scale[s / kBlock] = l.sm;
+            st.v_scale[s / kBlock] = l.sv;
+        }
+    }
+    store_vec<XT, 8>(static_cast<XT*>(t.x) + i, x);
+    if (t.copy) store8(t.copy, i, t.copy_dtype, x);
 }
 
 // Any block: a lane owns every 32nd element, so that single elements still make whole lines; the
 // last block of a tensor and tensors that do not start on 16 bytes.
 template <int BITS>
-__device__ __forceinline__ void step_block_any(const Tensor& t, const State& st, const StepScalars& sc, const Factors& f, int64_t base,
-                                               int count)
+struct LoadedAny {
+    uint32_t g[8], x[8];
+    float m[8], v[8], sm, sv;
+};
+template <int BITS>
+__device__ __forceinline__ void load_block_any(LoadedAny<BITS>& l, const Tensor& t, const State& st, int64_t base, int count)
 {
     const int lane = threadIdx.x & 31;
-    const int64_t s0 = t.state + base, sb = s0 / kBlock;
-    float g[8], x[8], m[8], v[8];
-    float sm = 0.f, sv = 0.f;
-    if (BITS == 8) { sm = st.m_scale[sb]; sv = st.v_scale[sb]; }
+    const int64_t s0 = t.state + base;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int e = j * 32 + lane;
-        g[j] = x[j] = m[j] = v[j] = 0.f;
+        l.g[j] = l.x[j] = 0;
+        l.m[j] = BITS == 32 ? 0.f : 8388736.0f; // code 0
+        l.v[j] = BITS == 32 ? 0.f : 8388608.0f;
         if (e >= count) continue;
-        g[j] = load_as_float(t.g, base + e, t.g_dtype);
-        x[j] = load_as_float(t.x, base + e, t.x_dtype);
+        l.g[j] = load_bits(t.g, base + e, t.g_dtype);
+        l.x[j] = load_bits(t.x, base + e, t.x_dtype);
         if constexpr (BITS == 32) {
-            m[j] = static_cast<const float*>(st.m)[s0 + e];
-            v[j] = static_cast<const float*>(st.v)[s0 + e];
+            l.m[j] = static_cast<const float*>(st.m)[s0 + e];
+            l.v[j] = static_cast<const float*>(st.v)[s0 + e];
         } else {
-            m[j] = (float)static_cast<const int8_t*>(st.m)[s0 + e];
-            v[j] = (float)static_cast<const uint8_t*>(st.v)[s0 + e];
-        }
-    }
-    float amax = 0.f, rmax = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int e = j * 32 + lane;
-        if (e >= count) continue;
-        if constexpr (BITS == 8) {
-            m[j] = moment_m(m[j], sm);
-            const float r = root_v(v[j], sv);
-            v[j] = r * r;
-        }
-        const float r = adamw_element(sc, f, g[j], x[j], m[j], v[j]);
-        store_from_float(t.x, base + e, t.x_dtype, x[j]);
-        if (t.copy) store_from_float(t.copy, base + e, t.copy_dtype, x[j]);
-        if constexpr (BITS == 32) {
-            static_cast<float*>(st.m)[s0 + e] = m[j];
-            static_cast<float*>(st.v)[s0 + e] = v[j];
-        } else {
-            v[j] = r;
-            amax = fmaxf(amax, fabsf(m[j]));
-            rmax = fmaxf(rmax, r);
+            l.m[j] = byte_bits(static_cast<const uint8_t*>(st.m)[s0 + e] ^ 0x80u, 0);
+            l.v[j] = byte_bits(static_cast<const uint8_t*>(st.v)[s0 + e], 0);
         }
     }
     if constexpr (BITS == 8) {
-        amax = fmaxf(warp_max(amax), kTiny);
-        rmax = fmaxf(warp_max(rmax), kTiny);
-        const float im = __fdiv_rn(kLevelsM, amax), iv = __fdiv_rn(kLevelsV, rmax);
+        l.sm = st.m_scale[s0 / kBlock];
+        l.sv = st.v_scale[s0 / kBlock];
+    }
+}
+template <int BITS>
+__device__ __forceinline__ void finish_block_any(LoadedAny<BITS>& l, const Tensor& t, const State& st, const StepScalars& sc,
+                                                 const Factors& f, int64_t base, int count)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t s0 = t.state + base;
+    float g[8], x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int e = j * 32 + lane;
-            if (e >= count) continue;
-            const float km = copysignf(nearest_root(fabsf(m[j]) * im), m[j]);
-            float kv = nearest_root(v[j] * iv);
-            if (v[j] > 0.f) kv = fmaxf(kv, 1.0f);
-            static_cast<uint8_t*>(st.m)[s0 + e] = (uint8_t)byte_of(km);
-            static_cast<uint8_t*>(st.v)[s0 + e] = (uint8_t)byte_of(kv);
-        }
+    for (int j = 0; j < 8; ++j) {
+        g[j] = bits_to_float(l.g[j], t.g_dtype);
+        x[j] = bits_to_float(l.x[j], t.x_dtype);
+    }
+    if constexpr (BITS == 32) {
+        update8(sc, f, g, x, l.m, l.v);
+    } else {
+        update8_codes(sc, f, g, x, l.m, l.v, l.sm, l.sv);
         if (lane == 0) {
-            st.m_scale[sb] = amax * (1.0f / kLevelsM);
-            st.v_scale[sb] = rmax * (1.0f / kLevelsV);
+            st.m_scale[s0 / kBlock] = l.sm;
+            st.v_scale[s0 / kBlock] = l.sv;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int e = j * 32 + lane;
+        if (e >= count) continue;
+        store_from_float(t.x, base + e, t.x_dtype, x[j]);
+        if (t.copy) store_from_float(t.copy, base + e, t.copy_dtype, x[j]);
+        if constexpr (BITS == 32) {
+            static_cast<float*>(st.m)[s0 + e] = l.m[j];
+            static_cast<float*>(st.v)[s0 + e] = l.v[j];
+        } else {
+            static_cast<uint8_t*>(st.m)[s0 + e] = (uint8_t)__float_as_uint(l.m[j]);
+            static_cast<uint8_t*>(st.v)[s0 + e] = (uint8_t)__float_as_uint(l.v[j]);
         }
     }
 }
 
-// One block of threads per chunk, one warp per block of elements.  The chunks are taken from the
-// last one: choco_adamw_grad_norm has read the gradients from the first one on, and what it read
-// last is what the L2 cache still holds.
-template <int BITS>
-__global__ void __launch_bounds__(kStepThreads)
-step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
-            int64_t* __restrict__ skipped, State st, StepScalars sc)
+// What this step multiplies with in one tensor; false: its group sits the step out.
+__device__ __forceinline__ bool factors_of(Factors& f, const Tensor& t, float c, int64_t skipped, const StepScalars& sc)
 {
-    wait_for_previous_kernel();
-    allow_next_kernel();
-    const Chunk ch = chunks[gridDim.x - 1 - blockIdx.x];
-    const Tensor t = tensors[ch.tensor];
-    Factors f;
-    f.c = 1.0f;
-    if (factor) {
-        f.c = factor[t.group];
-        if (!isfinite(f.c)) { // overflowed gradients: the group sits this step out
-            if (ch.first && threadIdx.x == 0) skipped[t.group] += 1;
-            return;
-        }
-    }
-    const int64_t base = ch.begin + (int64_t)(threadIdx.x >> 5) * kBlock;
-    if (base >= t.numel) return;
+    f.c = c;
     f.step_size = sc.step_size;
     f.rsqrt_bc2 = sc.rsqrt_bc2;
-    const int64_t sk = skipped[t.group];
-    if (sk != 0) { // this group has taken fewer steps than the others
-        const int64_t n = sc.t - sk;
-        f.step_size = (float)(sc.lrd / (1.0 - pow_int(sc.beta1d, n)));
-        f.rsqrt_bc2 = (float)(1.0 / sqrt(1.0 - pow_int(sc.beta2d, n)));
+    if (skipped != 0) { // this group has taken fewer steps than the others
+        const float n = (float)(sc.t - skipped);
+        f.step_size = __fdividef(sc.lr, -expm1f(n * sc.log_beta1));
+        f.rsqrt_bc2 = rsqrtf(-expm1f(n * sc.log_beta2));
     }
     f.step_size *= t.lr_scale;
     f.decay = t.weight_decay * (sc.lr * t.lr_scale);
-    if (t.aligned && base + kBlock <= t.numel) step_block<BITS>(t, st, sc, f, base);
-    else step_block_any<BITS>(t, st, sc, f, base, (int)min((int64_t)kBlock, t.numel - base));
+    return isfinite(c);
+}
+
+// A step is a launch of `step_rest_kernel` for the blocks that need single accesses and one of
+// `step_kernel` for each pair of types whose tensors have whole aligned blocks; most lists need one
+// or two.  (In one kernel the first would set the registers of the others; a stack frame of 160
+// bytes alone cost 40 % of their speed.)  They touch different elements and run side by side: each
+// lets the next start as soon as all that came before the step has ended, and waits for the
+// one before it only at its end.
+// Nobody but the thread that finds `first` looks at the count of a group that sits a step out.
+
+// one block of threads per chunk, one warp per block of elements
+template <int BITS>
+__global__ void __launch_bounds__(kStepThreads)
+step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
+                 int64_t* skipped, State st, StepScalars sc)
+{
+    const Chunk ch = chunks[blockIdx.x];
+    const Tensor t = tensors[ch.tensor];
+    wait_for_previous_kernel();
+    allow_next_kernel();
+    const int64_t base = ch.begin + (int64_t)(threadIdx.x >> 5) * kBlock;
+    if (base >= t.numel) return;
+    const int count = (int)min((int64_t)kBlock, t.numel - base);
+    LoadedAny<BITS> l;
+    load_block_any<BITS>(l, t, st, base, count);
+    Factors f;
+    if (factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc)) finish_block_any<BITS>(l, t, st, sc, f, base, count);
+    else if (ch.first && threadIdx.x == 0) skipped[t.group] += 1;
+}
+
+// One block of threads per chunk, one warp per block of elements.  The chunks are taken from the
+// last one: choco_adamw_grad_norm has read the gradients from the first one on, and what it read
+// last is what the L2 cache still holds.  The list does not change between calls, so it is read
+// before the previous kernel has ended; a warp's operands are asked for before the group's factor
+// is known, since every latency in this chain is time in which nothing is in flight.
+// A resident grid that walks over the chunks, with the list read ahead, was slower (16 x 28.95 M
+// float32: 2.55 ms against 2.10 ms): short blocks started in order keep what is in flight together
+// in memory.
+template <int BITS, typename XT, typename GT>
+__global__ void __launch_bounds__(kStepThreads, BITS == 8 ? kStepBlocks8 : kStepBlocks32)
+step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
+            int64_t* skipped, State st, StepScalars sc, int32_t beside)
+{
+    const Chunk ch = chunks[gridDim.x - 1 - blockIdx.x];
+    const Tensor t = tensors[ch.tensor];
+    if (!beside) wait_for_previous_kernel();
+    allow_next_kernel();
+    const int64_t base = ch.begin + (int64_t)(threadIdx.x >> 5) * kBlock;
+    if (base + kBlock <= t.numel) {
+        Loaded<BITS, XT, GT> l;
+        load_block(l, t, st, base);
+        Factors f;
+        if (factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc)) finish_block(l, t, st, sc, f, base);
+        else if (ch.first && threadIdx.x == 0) skipped[t.group] += 1;
+    }
+    if (beside) wait_for_previous_kernel();
+}
+
+using StepKernel = void (*)(const Tensor*, const Chunk*, const float*, int64_t*, State, StepScalars, int32_t);
+template <int BITS, typename XT>
+StepKernel step_kernel_of(int32_t g_dtype)
+{
+    return g_dtype == CHOCO_F32 ? step_kernel<BITS, XT, float> : g_dtype == CHOCO_BF16 ? step_kernel<BITS, XT, __nv_bfloat16>
+                                                                                       : step_kernel<BITS, XT, __half>;
+}
+template <int BITS>
+StepKernel step_kernel_of(int32_t x_dtype, int32_t g_dtype)
+{
+    return x_dtype == CHOCO_F32 ? step_kernel_of<BITS, float>(g_dtype) : x_dtype == CHOCO_BF16 ? step_kernel_of<BITS, __nv_bfloat16>(g_dtype)
+                                                                                              : step_kernel_of<BITS, __half>(g_dtype);
 }
 
 // 8 elements per thread; the moments are whole blocks.
@@ -351,8 +448,13 @@ __global__ void __launch_bounds__(256) read_state_kernel(State st, void* m_out, 
         if (v_out) { kv = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(st.v) + i); sv = st.v_scale[i / kBlock]; }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            m[e] = moment_m(sbyte((e < 4 ? km.x : km.y) ^ 0x80808080u, e & 3), sm);
-            const float r = root_v(ubyte(e < 4 ? kv.x : kv.y, e & 3), sv);
+            m[e] = byte_bits((e < 4 ? km.x : km.y) ^ 0x80808080u, e & 3);
+            v[e] = byte_bits(e < 4 ? kv.x : kv.y, e & 3);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            m[e] = square_m(m[e]) * sm;
+            const float r = square_v(v[e]) * sv;
             v[e] = r * r;
         }
     }
@@ -367,32 +469,45 @@ __global__ void __launch_bounds__(kNormThreads) norm_partial_kernel(const Tensor
                                                                     double* __restrict__ partial)
 {
     __shared__ double red[kNormThreads / 32];
-    wait_for_previous_kernel();
-    allow_next_kernel();
     const Chunk u = units[blockIdx.x];
     const Tensor t = tensors[u.tensor];
+    wait_for_previous_kernel();
+    allow_next_kernel();
     const int64_t end = min(u.begin + unit_elems, t.numel);
     double acc = 0.0;
     int64_t done = u.begin;
     if (t.aligned) {
         constexpr int kAhead = 4;           // vectors of a thread in flight
         constexpr int kSpanElems = kNormThreads * 8;
-        for (; done + kAhead * kSpanElems <= end; done += kAhead * kSpanElems) {
-            Raw8 r[kAhead];
+        auto span = [&](auto vectors) {
+            constexpr int N = decltype(vectors)::value;
+            Raw8 r[N];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) r[k] = load8(t.g, done + k * kSpanElems + threadIdx.x * 8, t.g_dtype);
+            for (int k = 0; k < N; ++k) r[k] = load8(t.g, done + k * kSpanElems + threadIdx.x * 8, t.g_dtype);
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
+            for (int k = 0; k < N; ++k) {
                 float g[8];
                 unpack8(r[k], t.g_dtype, g);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc = __fma_rn((double)g[e], (double)g[e], acc);
             }
-        }
+            done += N * kSpanElems;
+        };
+        while (done + kAhead * kSpanElems <= end) span(std::integral_constant<int, kAhead>());
+        while (done + kSpanElems <= end) span(std::integral_constant<int, 1>());
     }
-    for (int64_t e = done + threadIdx.x; e < end; e += kNormThreads) {
-        const double g = (double)load_as_float(t.g, e, t.g_dtype);
-        acc = __fma_rn(g, g, acc);
+    for (; done < end; done += 8 * kNormThreads) { // single elements, eight of a thread in flight
+        uint32_t g[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t e = done + k * kNormThreads + threadIdx.x;
+            g[k] = e < end ? load_bits(t.g, e, t.g_dtype) : 0u;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const double d = (double)bits_to_float(g[k], t.g_dtype);
+            acc = __fma_rn(d, d, acc);
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
@@ -440,10 +555,13 @@ struct choco_adamw {
     std::vector<Tensor> tensors;   // as on the device
     std::vector<int64_t> offsets;
     int64_t elements;              // of m and v
-    int64_t nchunks, nunits, unit_elems;
+    std::vector<int32_t> by_group;  // tensors with elements, group after group
+    int64_t most_chunks, nrest, nunits, unit_elems;
+    int64_t pair_begin[10];        // chunks of every pair of types (3 x_dtype + g_dtype), in d_chunks
     int64_t t;                     // step calls so far; a group has taken t - skipped[group] steps
     Tensor* d_tensors;
-    Chunk* d_chunks;
+    Chunk* d_chunks;               // whole blocks of aligned tensors
+    Chunk* d_rest;                 // every other block
     Chunk* d_units;
     int64_t* d_unit_begin;         // [groups + 1]
     int64_t* d_skipped;            // [groups]
@@ -459,10 +577,10 @@ bool on_device(const choco_adamw* o)
 }
 
 template <typename T>
-bool upload(T** out, const T* src, size_t count)
+bool upload(T** out, const T* src, size_t count, size_t room = 1)
 {
     *out = nullptr;
-    const size_t bytes = sizeof(T) * (count ? count : 1);
+    const size_t bytes = sizeof(T) * (count > room ? count : room);
     if (cudaMalloc((void**)out, bytes) != cudaSuccess) { *out = nullptr; return false; }
     if (!src) return cudaMemset(*out, 0, bytes) == cudaSuccess;
     return count == 0 || cudaMemcpy(*out, src, sizeof(T) * count, cudaMemcpyHostToDevice) == cudaSuccess;
@@ -479,6 +597,7 @@ void free_all(choco_adamw* o)
 {
     cudaFree(o->d_tensors);
     cudaFree(o->d_chunks);
+    cudaFree(o->d_rest);
     cudaFree(o->d_units);
     cudaFree(o->d_unit_begin);
     cudaFree(o->d_skipped);
@@ -489,8 +608,7 @@ void free_all(choco_adamw* o)
 bool all_aligned(const Tensor& t) { return aligned_to(t.x, 16) && aligned_to(t.g, 16) && aligned_to(t.copy, 16); }
 
 // Fills the host tables of `o`.  Throws std::bad_alloc.
-int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Chunk>& chunks, std::vector<Chunk>& units,
-         std::vector<int64_t>& unit_begin)
+int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Chunk>& units, std::vector<int64_t>& unit_begin)
 {
     const int32_t groups = o->params.groups;
     std::vector<std::vector<int32_t>> members(groups);
@@ -524,21 +642,46 @@ int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Ch
         if (t.numel > 0) members[t.group].push_back(i);
     }
     o->elements = at;
-    o->unit_elems = 16384;
+    // units of 16384 elements, 4096 where the whole list has fewer than four of the longer ones for each SM
+    o->unit_elems = total >= (int64_t)16384 * 4 * 148 ? 16384 : 4096;
     for (int32_t k = 0; k < groups; ++k) {
         unit_begin.push_back((int64_t)units.size());
-        bool first = true;
         for (int32_t i : members[k]) {
-            const int64_t len = o->tensors[i].numel;
-            for (int64_t b = 0; b < len; b += kChunkElems) { chunks.push_back({i, first ? 1 : 0, b}); first = false; }
-            for (int64_t b = 0; b < len; b += o->unit_elems) units.push_back({i, 0, b});
+            o->by_group.push_back(i);
+            o->most_chunks += o->tensors[i].numel / kChunkElems + 1;
+            for (int64_t b = 0; b < o->tensors[i].numel; b += o->unit_elems) units.push_back({i, 0, b});
         }
     }
     unit_begin.push_back((int64_t)units.size());
-    o->nchunks = (int64_t)chunks.size();
     o->nunits = (int64_t)units.size();
-    if (o->nchunks > 0x7fffffff) return CHOCO_ERR_TOO_LARGE;
-    return CHOCO_OK;
+    return o->most_chunks > 0x7fffffff || o->nunits > 0x7fffffff ? CHOCO_ERR_TOO_LARGE : CHOCO_OK;
+}
+
+// Cuts the tensors into chunks of whole blocks that can be moved in 128-bit accesses, and the rest.
+// Neither list is longer than most_chunks.  Throws std::bad_alloc.
+void cut(choco_adamw* o, std::vector<Chunk>& chunks, std::vector<Chunk>& rest)
+{
+    std::vector<char> seen((size_t)o->params.groups, 0);
+    auto first = [&](int32_t group) {
+        const int32_t f = !seen[group];
+        seen[group] = 1;
+        return f;
+    };
+    auto whole = [&](const Tensor& t) { return t.aligned ? t.numel / kBlock * kBlock : 0; };
+    for (int32_t i : o->by_group) {
+        const Tensor& t = o->tensors[i];
+        for (int64_t b = whole(t); b < t.numel; b += kChunkElems) rest.push_back({i, first(t.group), b});
+    }
+    o->nrest = (int64_t)rest.size();
+    for (int32_t pair = 0; pair < 9; ++pair) {
+        o->pair_begin[pair] = (int64_t)chunks.size();
+        for (int32_t i : o->by_group) {
+            const Tensor& t = o->tensors[i];
+            if (t.x_dtype * 3 + t.g_dtype != pair) continue;
+            for (int64_t b = 0; b < whole(t); b += kChunkElems) chunks.push_back({i, first(t.group), b});
+        }
+    }
+    o->pair_begin[9] = (int64_t)chunks.size();
 }
 
 } // namespace
@@ -558,13 +701,15 @@ int choco_adamw_init(choco_adamw** out, int32_t n_tensors, const choco_adamw_ten
     o->params = *p;
     int rc = CHOCO_OK;
     try {
-        std::vector<Chunk> chunks, units;
+        std::vector<Chunk> chunks, rest, units;
         std::vector<int64_t> unit_begin;
-        rc = plan(o, n_tensors, tensors, chunks, units, unit_begin);
+        rc = plan(o, n_tensors, tensors, units, unit_begin);
+        if (rc == CHOCO_OK) cut(o, chunks, rest);
         if (rc == CHOCO_OK && cudaGetDevice(&o->device) != cudaSuccess) rc = CHOCO_ERR_CUDA;
         if (rc == CHOCO_OK &&
-            !(upload(&o->d_tensors, o->tensors.data(), o->tensors.size()) && upload(&o->d_chunks, chunks.data(), chunks.size()) &&
-              upload(&o->d_units, units.data(), units.size()) && upload(&o->d_unit_begin, unit_begin.data(), unit_begin.size()) &&
+            !(upload(&o->d_tensors, o->tensors.data(), o->tensors.size()) && upload(&o->d_chunks, chunks.data(), chunks.size(), o->most_chunks) &&
+              upload(&o->d_rest, rest.data(), rest.size(), o->most_chunks) && upload(&o->d_units, units.data(), units.size()) &&
+              upload(&o->d_unit_begin, unit_begin.data(), unit_begin.size()) &&
               upload(&o->d_skipped, (const int64_t*)nullptr, (size_t)p->groups) &&
               upload(&o->d_partial, (const double*)nullptr, units.size())))
             rc = CHOCO_ERR_ALLOC;
@@ -603,15 +748,28 @@ int choco_adamw_set_grads(choco_adamw* opt, const void* const* g, void* stream)
         if (!aligned_to(g[i], dtype_size(opt->tensors[i].g_dtype))) return CHOCO_ERR_MISALIGNED;
     }
     cudaStream_t st = (cudaStream_t)stream;
-    if (cudaStreamSynchronize(st) != cudaSuccess) return CHOCO_ERR_CUDA;
-    for (size_t i = 0; i < opt->tensors.size(); ++i) {
-        opt->tensors[i].g = g[i];
-        opt->tensors[i].aligned = all_aligned(opt->tensors[i]);
+    auto send = [&](auto* to, const auto& from) {
+        return from.empty() || cudaMemcpyAsync(to, from.data(), sizeof(from[0]) * from.size(), cudaMemcpyHostToDevice, st) == cudaSuccess;
+    };
+    try {
+        std::vector<Chunk> chunks, rest;
+        chunks.reserve((size_t)opt->most_chunks);
+        rest.reserve((size_t)opt->most_chunks); // nothing below allocates
+        if (cudaStreamSynchronize(st) != cudaSuccess) return CHOCO_ERR_CUDA;
+        bool moved = false; // a tensor's accesses change width with its gradient's alignment
+        for (size_t i = 0; i < opt->tensors.size(); ++i) {
+            Tensor& t = opt->tensors[i];
+            t.g = g[i];
+            moved |= (bool)t.aligned != all_aligned(t);
+            t.aligned = all_aligned(t);
+        }
+        if (moved) cut(opt, chunks, rest);
+        if (!send(opt->d_tensors, opt->tensors) || !send(opt->d_chunks, chunks) || !send(opt->d_rest, rest) ||
+            cudaStreamSynchronize(st) != cudaSuccess)
+            return CHOCO_ERR_CUDA;
+    } catch (const std::exception&) {
+        return CHOCO_ERR_ALLOC;
     }
-    if (cudaMemcpyAsync(opt->d_tensors, opt->tensors.data(), sizeof(Tensor) * opt->tensors.size(), cudaMemcpyHostToDevice, st) !=
-            cudaSuccess ||
-        cudaStreamSynchronize(st) != cudaSuccess)
-        return CHOCO_ERR_CUDA;
     return CHOCO_OK;
 }
 
@@ -647,18 +805,28 @@ int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* 
     sc.beta1 = (float)p.beta1; sc.beta2 = (float)p.beta2;
     sc.omb1 = (float)(1.0 - p.beta1); sc.omb2 = (float)(1.0 - p.beta2);
     sc.eps = (float)p.eps;
+    sc.root_beta2 = (float)std::sqrt(p.beta2);
+    sc.root_omb2 = (float)std::sqrt(1.0 - p.beta2);
     sc.lr = (float)lr;
-    sc.beta1d = p.beta1; sc.beta2d = p.beta2; sc.lrd = lr;
+    sc.log_beta1 = (float)std::log(p.beta1); sc.log_beta2 = (float)std::log(p.beta2);
     sc.step_size = (float)(lr / (1.0 - pow_int(p.beta1, sc.t)));
     sc.rsqrt_bc2 = (float)(1.0 / std::sqrt(1.0 - pow_int(p.beta2, sc.t)));
     cudaStream_t st = (cudaStream_t)stream;
-    if (opt->nchunks > 0) {
-        const State state = {m, v, m_scale, v_scale};
-        const int rc = status_of(launch_overlapped(eight ? step_kernel<8> : step_kernel<32>, dim3((unsigned)opt->nchunks),
-                                                   dim3(kStepThreads), 0, st, HotRange{}, opt->d_tensors, opt->d_chunks, factor,
-                                                   opt->d_skipped, state, sc));
-        if (rc != CHOCO_OK) return rc;
+    const State state = {m, v, m_scale, v_scale};
+    cudaError_t err = cudaSuccess;
+    if (opt->nrest > 0)
+        err = launch_overlapped(eight ? step_rest_kernel<8> : step_rest_kernel<32>, dim3((unsigned)opt->nrest), dim3(kStepThreads), 0, st,
+                                HotRange{}, opt->d_tensors, opt->d_rest, factor, opt->d_skipped, state, sc);
+    int32_t beside = opt->nrest > 0;
+    for (int32_t pair = 0; pair < 9 && err == cudaSuccess; ++pair) {
+        const int32_t count = (int32_t)(opt->pair_begin[pair + 1] - opt->pair_begin[pair]);
+        if (count == 0) continue;
+        err = launch_overlapped(eight ? step_kernel_of<8>(pair / 3, pair % 3) : step_kernel_of<32>(pair / 3, pair % 3), dim3((unsigned)count),
+                                dim3(kStepThreads), 0, st, HotRange{}, opt->d_tensors, opt->d_chunks + opt->pair_begin[pair], factor,
+                                opt->d_skipped, state, sc, beside);
+        beside = 1;
     }
+    if (status_of(err) != CHOCO_OK) return CHOCO_ERR_CUDA;
     opt->t += 1;
     return CHOCO_OK;
 }

@@ -37,6 +37,17 @@ __device__ __forceinline__ float load_as_float(const void* p, int64_t i, int32_t
     if (dtype == CHOCO_BF16) return to_float(static_cast<const __nv_bfloat16*>(p)[i]);
     return to_float(static_cast<const __half*>(p)[i]);
 }
+// the same in two halves, so that several loads can be under way before the first is converted
+__device__ __forceinline__ uint32_t load_bits(const void* p, int64_t i, int32_t dtype)
+{
+    return dtype == CHOCO_F32 ? static_cast<const uint32_t*>(p)[i] : (uint32_t)static_cast<const unsigned short*>(p)[i];
+}
+__device__ __forceinline__ float bits_to_float(uint32_t b, int32_t dtype)
+{
+    if (dtype == CHOCO_F32) return __uint_as_float(b);
+    if (dtype == CHOCO_BF16) return __uint_as_float(b << 16);
+    return __half2float(__ushort_as_half((unsigned short)b));
+}
 __device__ __forceinline__ void store_from_float(void* p, int64_t i, int32_t dtype, float v)
 {
     if (dtype == CHOCO_F32) static_cast<float*>(p)[i] = v;
