@@ -103,7 +103,6 @@ __device__ __forceinline__ void store_vec(T* p, const float* f)
         for (int e = 0; e < V; ++e) w[e] = __float_as_uint(f[e]);
     } else if constexpr (V == 1) {
         *p = from_float<T>(f[0]);
-        return;
     } else {
 #pragma unroll
         for (int e = 0; e < V; e += 2) {
@@ -122,7 +121,7 @@ __device__ __forceinline__ void store_vec(T* p, const float* f)
             reinterpret_cast<uint4*>(p)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
     } else if constexpr (b == 8) {
         *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-    } else {
+    } else if constexpr (b == 4) {
         *reinterpret_cast<uint32_t*>(p) = w[0];
     }
 }

@@ -23,12 +23,11 @@ constexpr int kDigits = 1 << kDigitBits;
 constexpr int kSortTile = 2048;             // keys a block of the sort takes
 constexpr int kSortRounds = kSortTile / kEmbThreads;
 constexpr int kTileLong = 32;               // sorted entries per tile of the sums, many rows ...
-constexpr int kTileShort = 8;               // ... and few: more warps, shorter chains of loads
-constexpr int64_t kShortRows = 16384;
-constexpr int kRankKeys = 64;               // keys a block of the rank kernel places
-constexpr int64_t kRankPairs = (int64_t)1 << 27; // n count^2 up to which tokens are ordered by ranks
+constexpr int kTileMid = 16;                // ... and fewer: more warps, shorter chains of loads
+constexpr int kTileShort = 8;
+constexpr int64_t kMidRows = 65536, kShortRows = 16384;
 constexpr uint32_t kNoKey = 0xffffffffu;
-constexpr int kChainOfWarp = 32;            // chains of partial sums up to this length are added by one warp
+constexpr int kChainOfWarp = 4;             // chains of partial sums up to this length are added by one warp
 
 struct EmbShape {
     int64_t vocab, dim, table_row, table_ld, padding;
@@ -48,31 +47,32 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, int32_t bits, in
 // lookup
 // ---------------------------------------------------------------------------------------
 
-constexpr int kLookupVecs = 4;              // vectors a lane moves: a warp serves 128 V columns of one row
-
-template <typename TT, typename TO, int V>
+// A warp serves one row, or 32 N V columns of it, with all its loads in flight together: N vectors of
+// V elements a lane.  The row of the table is known only when the token has arrived, so the bytes in
+// flight have to come from many warps.
+template <typename TT, typename TO, int V, int N>
 __global__ void __launch_bounds__(kEmbThreads)
 lookup_kernel(EmbShape s, const TT* __restrict__ table, const void* __restrict__ tokens, int32_t index_bits, int64_t tokens_ld,
               TO* __restrict__ out, int64_t out_row, int64_t out_ld, uint32_t slabs)
 {
-    const uint64_t item = (uint64_t)blockIdx.x * kEmbWarps + (threadIdx.x >> 5);
-    const uint32_t row = (uint32_t)(item / slabs), slab = (uint32_t)(item - (uint64_t)row * slabs);
-    if (row >= (uint32_t)((int64_t)s.n * s.count)) return;
-    const uint32_t i = row / (uint32_t)s.count, t = row - i * (uint32_t)s.count;
+    const uint32_t item = blockIdx.x * kEmbWarps + (threadIdx.x >> 5);
+    const uint32_t t = slabs == 1 ? item : item / slabs, slab = slabs == 1 ? 0 : item - t * slabs;
+    wait_for_previous_kernel();
+    allow_next_kernel();
+    if (t >= (uint32_t)s.count) return;
+    const int64_t i = blockIdx.y;
     const int64_t tok = token_at(tokens, index_bits, i * tokens_ld + t, s.vocab);
-    const int64_t c0 = (int64_t)slab * (32 * V * kLookupVecs) + (threadIdx.x & 31) * V;
+    const int32_t c0 = (int32_t)slab * (32 * V * N) + (threadIdx.x & 31) * V, dim = (int32_t)s.dim;
     TO* o = out + i * out_ld + t * out_row;
     const TT* w = table + i * s.table_ld + (tok < 0 ? 0 : tok) * s.table_row;
-    Raw<TT, V> raw[kLookupVecs];
+    Raw<TT, V> raw[N];
 #pragma unroll
-    for (int k = 0; k < kLookupVecs; ++k) {
-        const int64_t c = c0 + k * 32 * V;
-        if (tok >= 0 && c < s.dim) load_raw(raw[k], w + c);
-    }
+    for (int k = 0; k < N; ++k)
+        if (tok >= 0 && c0 + k * 32 * V < dim) load_raw(raw[k], w + c0 + k * 32 * V);
 #pragma unroll
-    for (int k = 0; k < kLookupVecs; ++k) {
-        const int64_t c = c0 + k * 32 * V;
-        if (c >= s.dim) continue;
+    for (int k = 0; k < N; ++k) {
+        const int32_t c = c0 + k * 32 * V;
+        if (c >= dim) continue;
         float f[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) f[e] = tok >= 0 ? raw_get(raw[k], e) * s.scale : 0.f;
@@ -91,102 +91,264 @@ __device__ __forceinline__ uint32_t sort_key(const EmbShape& s, const void* toke
     return t < 0 || t == s.padding ? (uint32_t)s.vocab : (uint32_t)t;
 }
 
-// Which rows of the tables some token names: a bit per row, a multiple of four bytes per worker.  All
-// zeros between calls: whoever zeroes a byte's rows of the gradient clears it.
-struct Presence {
-    uint8_t* bits;               // nullptr: not wanted (the sums are added to the gradient)
-    int64_t bytes;               // per worker
-};
-__device__ __forceinline__ void mark_present(const Presence& p, int32_t worker, uint32_t key)
+// ---------------------------------------------------------------------------------------
+// zeros
+// ---------------------------------------------------------------------------------------
+
+// `bytes` bytes from p on (both even), by `of` threads, this one the i-th
+__device__ __forceinline__ void zero_run(char* p, int64_t bytes, int i, int of)
 {
-    uint32_t* w = reinterpret_cast<uint32_t*>(p.bits + worker * p.bytes) + (key >> 5);
-    const uint32_t bit = 1u << (key & 31);
-    if (!(*reinterpret_cast<volatile uint32_t*>(w) & bit)) atomicOr(w, bit);
+    char* const end = p + bytes;
+    char* const body = p + ((16 - ((uintptr_t)p & 15)) & 15);
+    if (body >= end) {
+        for (char* q = p + 2 * i; q < end; q += 2 * of) *reinterpret_cast<unsigned short*>(q) = 0;
+        return;
+    }
+    char* const tail = end - ((uintptr_t)end & 15);
+    for (char* q = body + 16 * i; q < tail; q += 16 * of) *reinterpret_cast<uint4*>(q) = make_uint4(0, 0, 0, 0);
+    if (p + 2 * i < body) *reinterpret_cast<unsigned short*>(p + 2 * i) = 0; // (at most seven each)
+    if (tail + 2 * i < end) *reinterpret_cast<unsigned short*>(tail + 2 * i) = 0;
 }
 
-// A share of the rows that no token names becomes zeros: bytes of the map [begin, end), a warp each.
-struct ZeroWork {
-    Presence pres;
-    void* grad;
-    int32_t dtype;
-    int32_t wide;                // bytes a store may have: the alignment of every row
-    int64_t begin, end;          // of n * pres.bytes
-    int32_t blocks;              // blocks of the launch that do this, behind the others
-};
+constexpr int kZeroSpan = 8192;             // bytes of a block
 
-__device__ __forceinline__ void zero_run(char* p, int64_t bytes, int wide, int lane)
+// All rows of the gradient, before the sums are written to those that tokens name.  Runs beside the
+// kernel that puts the tokens in order, which leaves the memory and most SMs idle: that kernel
+// lets this one start as soon as all that came before has ended, and the last block here waits for
+// it, so that what follows finds both done.  Knowing the named rows first would save their bytes,
+// and cost the time the ordering takes.  Short blocks in order reach the memory's rate; a resident
+// grid that walks over the table got 5.5 TB/s of 7.3.
+__global__ void __launch_bounds__(kEmbThreads) zero_kernel(EmbShape s, char* grad, int32_t size, uint32_t blocks_per_row, int32_t beside)
 {
-    if (wide == 16) for (int64_t b = lane * 16; b < bytes; b += 512) *reinterpret_cast<uint4*>(p + b) = make_uint4(0, 0, 0, 0);
-    else if (wide == 8) for (int64_t b = lane * 8; b < bytes; b += 256) *reinterpret_cast<uint2*>(p + b) = make_uint2(0, 0);
-    else if (wide == 4) for (int64_t b = lane * 4; b < bytes; b += 128) *reinterpret_cast<uint32_t*>(p + b) = 0;
-    else for (int64_t b = lane * 2; b < bytes; b += 64) *reinterpret_cast<unsigned short*>(p + b) = 0;
+    if (!beside) wait_for_previous_kernel();
+    allow_next_kernel();
+    char* const table = grad + blockIdx.y * s.table_ld * size;
+    if (s.table_row == s.dim) { // one run of bytes
+        const int64_t all = s.vocab * s.dim * size, from = (int64_t)blockIdx.x * kZeroSpan;
+        zero_run(table + from, min((int64_t)kZeroSpan, all - from), threadIdx.x, kEmbThreads);
+    } else {
+        const int64_t row = blockIdx.x / blocks_per_row, from = (int64_t)(blockIdx.x - row * blocks_per_row) * kZeroSpan;
+        zero_run(table + row * s.table_row * size + from, min((int64_t)kZeroSpan, s.dim * size - from), threadIdx.x, kEmbThreads);
+    }
+    if (beside && blockIdx.x + 1 == gridDim.x && blockIdx.y + 1 == gridDim.y) wait_for_previous_kernel();
 }
 
-__device__ __forceinline__ void zero_share(const EmbShape& s, const ZeroWork& z, int32_t block)
+// For each of N keys of a lane the lanes whose key has the same digit, a ballot per bit; the keys' votes do
+// not wait for one another.  Keys that are none are alike with nobody that is one.  (The match
+// instruction takes longer where most digits differ.)
+template <int N>
+__device__ __forceinline__ void lanes_alike(uint32_t (&alike)[N], const uint32_t (&key)[N], int shift, int bits, int rounds)
 {
-    const int lane = threadIdx.x & 31;
-    const int64_t size = z.dtype == CHOCO_F32 ? 4 : 2;
-    const int64_t step = (int64_t)z.blocks * (blockDim.x >> 5);
-    for (int64_t u = z.begin + (int64_t)block * (blockDim.x >> 5) + (threadIdx.x >> 5); u < z.end; u += step) {
-        const int64_t worker = u / z.pres.bytes, r0 = (u - worker * z.pres.bytes) * 8;
-        const uint32_t have = z.pres.bits[u];
-        __syncwarp();
-        if (have && lane == 0) z.pres.bits[u] = 0;
-        if (r0 >= s.vocab) continue;
-        const int rows = (int)min((int64_t)8, s.vocab - r0);
-        char* p = static_cast<char*>(z.grad) + (worker * s.table_ld + r0 * s.table_row) * size;
-        if (!have && s.table_row == s.dim) {
-            const int64_t bytes = rows * s.dim * size;
-            // eight rows start on 16 bytes if the table does, whatever their length in float32
-            const int wide = ((uintptr_t)p | (uint64_t)bytes) % 16 == 0 ? 16 : z.wide;
-            zero_run(p, bytes, wide, lane);
-        } else {
-            for (int r = 0; r < rows; ++r)
-                if (!(have >> r & 1)) zero_run(p + r * s.table_row * size, s.dim * size, z.wide, lane);
+#pragma unroll
+    for (int r = 0; r < N; ++r) alike[r] = __ballot_sync(0xffffffffu, key[r] != kNoKey);
+    for (int b = 0; b < bits; ++b) {
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+            if (r >= rounds) break;
+            const bool one = key[r] >> (shift + b) & 1;
+            const uint32_t ones = __ballot_sync(0xffffffffu, one);
+            alike[r] &= one ? ones : ~ones;
         }
     }
 }
 
-// Few tokens: every key counts the keys before it in order of (token, position).  The pair is
-// one 32-bit number, so that is one comparison; all SMs share the count^2 of them.
-__global__ void __launch_bounds__(kEmbThreads)
-rank_kernel(EmbShape s, const void* __restrict__ tokens, int64_t tokens_ld, int32_t index_bits, int32_t pos_bits, Presence pres,
-            uint32_t* __restrict__ keys, uint32_t* __restrict__ pos)
+// Up to 16 x 8192 tokens per worker: a cluster of blocks keeps a worker's keys and positions in its
+// shared memory and sorts them there, digit by digit (stable, from the lowest).  Every block counts
+// and ranks its part of the list and puts it in order for itself, the blocks add up each other's
+// counts, and each pair goes to its place in the shared memory of the block that holds it next, in
+// the last round to global memory.  One launch where a sort in global memory takes three per digit
+// (131072 tokens of 16 bits: 27 us against 45 us; 8 x 2240: 12 us), and most SMs stay free for the
+// zeros.  What it takes is latency: per digit about 2 us of barriers and exchanged counts, and
+// 4 us for 8192 keys to be ranked and sent.
+constexpr int kOrderThreads = 1024;
+constexpr int kOrderWarps = kOrderThreads / 32;
+constexpr int kOrderDigitBits = 9;
+constexpr int kOrderDigits = 1 << kOrderDigitBits;
+constexpr int kOrderMost = 8192;            // keys of a block
+constexpr int kOrderFew = 2048;             // keys that are not worth a second block
+constexpr int kOrderCluster = 16;           // blocks of a cluster, at most
+
+struct Order {
+    const void* tokens;
+    int64_t tokens_ld;
+    int32_t index_bits;
+    int32_t cluster_log, part_log;          // blocks of a cluster, keys of a block
+    int32_t digit_bits, passes;
+    uint32_t *keys, *pos;                   // out: [n, count]
+};
+
+struct OrderSmem {
+    uint16_t cnt[kOrderWarps][kOrderDigits];
+    uint32_t hist[kOrderDigits];            // read by the other blocks
+    uint32_t base[kOrderDigits];
+    uint32_t ws[kOrderWarps];
+};
+
+__device__ __forceinline__ uint32_t cluster_address(const void* p, uint32_t block) // of block's copy of a shared variable
 {
-    constexpr int kParts = kEmbThreads / kRankKeys;
-    extern __shared__ uint32_t all[];       // count pairs, then a multiple of 16 filled up with the largest
-    __shared__ uint32_t sums[kParts][kRankKeys];
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(block));
+    return a;
+}
+__device__ __forceinline__ uint32_t load_cluster(uint32_t a)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void store_cluster(uint32_t a, uint32_t x, uint32_t y)
+{
+    asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+__global__ void __launch_bounds__(kOrderThreads, 1) order_kernel(EmbShape s, Order o)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    OrderSmem& m = *reinterpret_cast<OrderSmem*>(smem);
+    uint2* buf = reinterpret_cast<uint2*>(smem + sizeof(OrderSmem)); // two buffers of (key, position)
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int32_t worker = blockIdx.x >> o.cluster_log;
     wait_for_previous_kernel();
-    const int32_t worker = blockIdx.y;
-    const int count = (int)s.count, padded = (count + 15) / 16 * 16;
-    for (int j = threadIdx.x; j < padded; j += kEmbThreads)
-        all[j] = j < count ? sort_key(s, tokens, index_bits, worker * tokens_ld + j) << pos_bits | (uint32_t)j : kNoKey;
-    __syncthreads();
     allow_next_kernel();
-    const int mine = threadIdx.x % kRankKeys, part = threadIdx.x / kRankKeys;
-    const int i = blockIdx.x * kRankKeys + mine;
-    const uint32_t key = i < count ? all[i] : 0u;
-    const uint4* quads = reinterpret_cast<const uint4*>(all);
-    const int per = padded / 4 / kParts;
-    uint32_t before = 0;
-#pragma unroll 4
-    for (int q = part * per; q < (part + 1) * per; ++q) {
-        const uint4 v = quads[q];
-        before += (v.x < key) + (v.y < key) + (v.z < key) + (v.w < key);
-    }
-    sums[part][mine] = before;
-    __syncthreads();
-    if (part == 0 && i < count) {
+    const uint32_t rank = blockIdx.x & ((1u << o.cluster_log) - 1u), blocks = 1u << o.cluster_log;
+    const uint32_t part = 1u << o.part_log;
+    const uint32_t first = rank << o.part_log;
+    const int have = (int)min((int64_t)part, max((int64_t)0, s.count - (int64_t)first));
+    const int rounds = part / kOrderThreads, slice = part / kOrderWarps;
+    constexpr int kRounds = kOrderMost / kOrderThreads;
+    uint32_t key[kRounds], pos[kRounds];
+    uint16_t place[kRounds];
 #pragma unroll
-        for (int k = 1; k < kParts; ++k) before += sums[k][mine];
-        const uint32_t tok = key >> pos_bits;
-        keys[worker * s.count + before] = tok;
-        pos[worker * s.count + before] = key & ((1u << pos_bits) - 1u);
-        if (pres.bits && tok < (uint32_t)s.vocab) mark_present(pres, worker, tok);
+    for (int r = 0; r < kRounds; ++r) {
+        const int j = w * slice + r * 32 + lane;
+        key[r] = kNoKey;
+        if (r < rounds && j < have) {
+            key[r] = sort_key(s, o.tokens, o.index_bits, worker * o.tokens_ld + first + j);
+            pos[r] = first + j;
+        }
+    }
+    const uint32_t digits = 1u << o.digit_bits;
+    for (int pass = 0; pass < o.passes; ++pass) {
+        const int shift = pass * o.digit_bits;
+        uint2* in = buf + (pass & 1) * part;
+        uint2* out = buf + ((pass & 1) ^ 1) * part;
+        for (uint32_t d = lane; d < digits; d += 32) m.cnt[w][d] = 0;
+        if (pass > 0) {
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) {
+                const int j = w * slice + r * 32 + lane;
+                if (r < rounds && j < have) { key[r] = in[j].x; pos[r] = in[j].y; }
+            }
+        }
+        __syncwarp();
+        uint32_t alike[kRounds];
+        lanes_alike<kRounds>(alike, key, shift, o.digit_bits, rounds);
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            if (r >= rounds) break;
+            const bool live = key[r] != kNoKey;
+            const uint32_t d = (key[r] >> shift) & (digits - 1);
+            const uint32_t before = live ? m.cnt[w][d] : 0u;
+            __syncwarp();
+            place[r] = (uint16_t)(before + __popc(alike[r] & ((1u << lane) - 1u)));
+            if (live && lane == __ffs(alike[r]) - 1) m.cnt[w][d] = (uint16_t)(before + __popc(alike[r]));
+            __syncwarp();
+        }
+        __syncthreads();
+        // exclusive sums over the digits, one digit per thread
+        auto scan = [&](uint32_t mine) {
+            uint32_t incl = mine;
+#pragma unroll
+            for (int q = 1; q < 32; q <<= 1) {
+                const uint32_t u = __shfl_up_sync(0xffffffffu, incl, q);
+                if (lane >= q) incl += u;
+            }
+            if (lane == 31) m.ws[w] = incl;
+            __syncthreads();
+            uint32_t v = m.ws[lane];
+#pragma unroll
+            for (int q = 1; q < 32; q <<= 1) {
+                const uint32_t u = __shfl_up_sync(0xffffffffu, v, q);
+                if (lane >= q) v += u;
+            }
+            const uint32_t before = __shfl_sync(0xffffffffu, v, (w + 31) & 31);
+            __syncthreads();
+            return incl - mine + (w ? before : 0u);
+        };
+        uint32_t own = 0;
+        if (threadIdx.x < digits) {
+#pragma unroll
+            for (int k = 0; k < kOrderWarps; ++k) own += m.cnt[k][threadIdx.x];
+            m.hist[threadIdx.x] = own;
+        }
+        if (blocks > 1) cluster_arrive();
+        const uint32_t start = scan(own); // where this block's keys with the digit start in its own order
+        if (threadIdx.x < digits) {
+            uint32_t at = start;
+#pragma unroll
+            for (int k = 0; k < kOrderWarps; ++k) {
+                const uint32_t c = m.cnt[k][threadIdx.x];
+                m.cnt[k][threadIdx.x] = (uint16_t)at;
+                at += c;
+            }
+        }
+        __syncthreads();
+        // the block's pairs in its own order, so that what goes to one place goes there in runs
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            if (r >= rounds || key[r] == kNoKey) continue;
+            in[m.cnt[w][(key[r] >> shift) & (digits - 1)] + place[r]] = make_uint2(key[r], pos[r]);
+        }
+        uint32_t earlier = 0, total = 0;
+        if (blocks > 1) cluster_wait();
+        if (blocks > 1 && threadIdx.x < digits) {
+            for (uint32_t b = 0; b < blocks; b += 8) {
+                uint32_t c[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) c[k] = b + k < blocks ? load_cluster(cluster_address(&m.hist[threadIdx.x], b + k)) : 0u;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (b + k < rank) earlier += c[k];
+                    total += c[k];
+                }
+            }
+        }
+        if (blocks > 1) {
+            const uint32_t base = scan(total);
+            if (threadIdx.x < digits) m.base[threadIdx.x] = base + earlier - start;
+        } else if (threadIdx.x < digits) {
+            m.base[threadIdx.x] = 0; // the block's own order is all
+        }
+        __syncthreads();
+        const bool last = pass + 1 == o.passes;
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int j = r * kOrderThreads + threadIdx.x;
+            if (r >= rounds || j >= have) break;
+            const uint2 kp = in[j];
+            const uint32_t to = m.base[(kp.x >> shift) & (digits - 1)] + j;
+            if (last) {
+                o.keys[worker * s.count + to] = kp.x;
+                o.pos[worker * s.count + to] = kp.y;
+            } else if (blocks > 1) {
+                store_cluster(cluster_address(out + (to & (part - 1)), to >> o.part_log), kp.x, kp.y);
+            } else {
+                out[to] = kp;
+            }
+        }
+        // what was sent has arrived, and nobody reads these counts any more (nor, at the end, this block's memory)
+        if (blocks > 1) {
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
     }
 }
 
-// Many tokens: a stable radix sort, three launches per digit.
+// More tokens: a stable radix sort in global memory, three launches per digit.
 struct SortPass {
     const void* tokens;          // first pass: the tokens themselves
     int64_t tokens_ld;
@@ -196,7 +358,6 @@ struct SortPass {
     uint32_t *key_out, *pos_out;
     uint32_t* hist;              // [n, kDigits, tiles]
     uint32_t* total;             // [n, kDigits]
-    Presence pres;
 };
 
 __device__ __forceinline__ uint32_t pass_key(const EmbShape& s, const SortPass& p, int32_t worker, int64_t j)
@@ -204,13 +365,11 @@ __device__ __forceinline__ uint32_t pass_key(const EmbShape& s, const SortPass& 
     return p.first ? sort_key(s, p.tokens, p.index_bits, worker * p.tokens_ld + j) : p.key_in[worker * s.count + j];
 }
 
-__global__ void __launch_bounds__(kEmbThreads) sort_count_kernel(EmbShape s, SortPass p, ZeroWork z)
+__global__ void __launch_bounds__(kEmbThreads) sort_count_kernel(EmbShape s, SortPass p)
 {
     __shared__ uint32_t h[kDigits];
     wait_for_previous_kernel();
     allow_next_kernel();
-    const int32_t blocks = p.tiles * s.n;
-    if ((int32_t)blockIdx.x >= blocks) return zero_share(s, z, blockIdx.x - blocks);
     const int32_t worker = blockIdx.x / p.tiles, tile = blockIdx.x - worker * p.tiles;
     h[threadIdx.x] = 0;
     __syncthreads();
@@ -224,47 +383,54 @@ __global__ void __launch_bounds__(kEmbThreads) sort_count_kernel(EmbShape s, Sor
     for (int r = 0; r < kSortRounds; ++r) {
         if (key[r] == kNoKey) continue;
         atomicAdd(&h[(key[r] >> p.shift) & (kDigits - 1)], 1u);
-        if (p.first && p.pres.bits && key[r] < (uint32_t)s.vocab) mark_present(p.pres, worker, key[r]);
     }
     __syncthreads();
     p.hist[((int64_t)worker * kDigits + threadIdx.x) * p.tiles + tile] = h[threadIdx.x];
 }
 
 // One warp per digit: exclusive sums of its counts over the tiles, and their total.
-__global__ void __launch_bounds__(kEmbThreads) sort_scan_kernel(EmbShape s, SortPass p, ZeroWork z)
+__global__ void __launch_bounds__(kEmbThreads) sort_scan_kernel(EmbShape s, SortPass p)
 {
     wait_for_previous_kernel();
     allow_next_kernel();
-    const int32_t blocks = s.n * (kDigits / kEmbWarps);
-    if ((int32_t)blockIdx.x >= blocks) return zero_share(s, z, blockIdx.x - blocks);
     const int lane = threadIdx.x & 31;
     const int64_t row = (int64_t)blockIdx.x * kEmbWarps + (threadIdx.x >> 5);
     uint32_t* h = p.hist + row * p.tiles;
     uint32_t carry = 0;
-    for (int32_t b = 0; b < p.tiles; b += 32) {
-        const int32_t j = b + lane;
-        const uint32_t mine = j < p.tiles ? h[j] : 0u;
-        uint32_t v = mine;
+    for (int32_t b = 0; b < p.tiles; b += 32 * 8) { // a lane has eight tiles in a row
+        uint32_t c[8], sum = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int32_t j = b + lane * 8 + k;
+            c[k] = j < p.tiles ? h[j] : 0u;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += c[k];
+        uint32_t v = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t u = __shfl_up_sync(0xffffffffu, v, o);
             if (lane >= o) v += u;
         }
-        if (j < p.tiles) h[j] = carry + v - mine;
+        uint32_t at = carry + v - sum;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int32_t j = b + lane * 8 + k;
+            if (j < p.tiles) h[j] = at;
+            at += c[k];
+        }
         carry += __shfl_sync(0xffffffffu, v, 31);
     }
     if (lane == 0) p.total[row] = carry;
 }
 
 // Every warp ranks its slice of the tile in order; equal digits keep their order.
-__global__ void __launch_bounds__(kEmbThreads) sort_scatter_kernel(EmbShape s, SortPass p, ZeroWork z)
+__global__ void __launch_bounds__(kEmbThreads) sort_scatter_kernel(EmbShape s, SortPass p)
 {
     __shared__ uint32_t cnt[kEmbWarps][kDigits];
     __shared__ uint32_t ws[kEmbWarps];
     wait_for_previous_kernel();
     allow_next_kernel();
-    const int32_t blocks = p.tiles * s.n;
-    if ((int32_t)blockIdx.x >= blocks) return zero_share(s, z, blockIdx.x - blocks);
     const int32_t worker = blockIdx.x / p.tiles, tile = blockIdx.x - worker * p.tiles;
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     // thread d: where digit d of this tile starts = keys with smaller digits + this digit in earlier tiles
@@ -287,11 +453,13 @@ __global__ void __launch_bounds__(kEmbThreads) sort_scatter_kernel(EmbShape s, S
         key[r] = j < s.count ? pass_key(s, p, worker, j) : kNoKey;
         pos[r] = p.first ? (uint32_t)j : j < s.count ? p.pos_in[worker * s.count + j] : 0u;
     }
+    uint32_t alike[kSortRounds];
+    lanes_alike<kSortRounds>(alike, key, p.shift, kDigitBits, kSortRounds);
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r) {
         const bool in = key[r] != kNoKey;
         const uint32_t d = (key[r] >> p.shift) & (kDigits - 1);
-        const uint32_t same = __match_any_sync(0xffffffffu, in ? d : kNoKey);
+        const uint32_t same = alike[r];
         const uint32_t before = in ? cnt[w][d] : 0u;
         __syncwarp();
         rank[r] = before + __popc(same & ((1u << lane) - 1u));
@@ -339,9 +507,27 @@ struct Sums {
     uint32_t slabs;              // groups of columns
 };
 
+// Adds to float32 in memory without reading it first.  Every element gets at most one such addition
+// in a call, so their order does not matter (subnormal results become zeros).
+template <int V>
+__device__ __forceinline__ void add_in_memory(float* p, const float* f)
+{
+    if constexpr (V >= 4) {
+#pragma unroll
+        for (int k = 0; k < V; k += 4)
+            asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p + k), "f"(f[k]), "f"(f[k + 1]), "f"(f[k + 2]), "f"(f[k + 3])
+                         : "memory");
+    } else if constexpr (V == 2) {
+        asm volatile("red.global.add.v2.f32 [%0], {%1, %2};" ::"l"(p), "f"(f[0]), "f"(f[1]) : "memory");
+    } else {
+        asm volatile("red.global.add.f32 [%0], %1;" ::"l"(p), "f"(f[0]) : "memory");
+    }
+}
+
 // scale * acc (+ what is there) to V columns of a row of the gradient, whose type is known at run time
 template <int V>
-__device__ __forceinline__ void store_grad(const EmbShape& s, const Sums& a, int32_t worker, uint32_t key, int64_t c, const float* acc)
+__device__ __forceinline__ void store_grad(const EmbShape& s, void* grad, int32_t dtype, bool accumulate, int32_t worker, uint32_t key,
+                                           int64_t c, const float* acc)
 {
     const int64_t at = worker * s.table_ld + (int64_t)key * s.table_row + c;
     float f[V];
@@ -349,24 +535,24 @@ __device__ __forceinline__ void store_grad(const EmbShape& s, const Sums& a, int
     for (int e = 0; e < V; ++e) f[e] = acc[e] * s.scale;
     auto put = [&](auto* g) {
         using TG = std::remove_pointer_t<decltype(g)>;
-        if (a.accumulate) {
+        if (accumulate) {
+            if constexpr (std::is_same_v<TG, float>) return add_in_memory<V>(g + at, f);
 #pragma unroll
             for (int e = 0; e < V; ++e) f[e] += to_float(g[at + e]);
         }
         store_vec<TG, V>(g + at, f);
     };
-    if (a.grad_dtype == CHOCO_F32) put(static_cast<float*>(a.grad));
-    else if (a.grad_dtype == CHOCO_BF16) put(static_cast<__nv_bfloat16*>(a.grad));
-    else put(static_cast<__half*>(a.grad));
+    if (dtype == CHOCO_F32) put(static_cast<float*>(grad));
+    else if (dtype == CHOCO_BF16) put(static_cast<__nv_bfloat16*>(grad));
+    else put(static_cast<__half*>(grad));
 }
 
 // One warp per tile and group of 32 V C columns; B entries' loads are in flight together.
 template <typename TD, int V, int C, int B>
-__global__ void __launch_bounds__(kEmbThreads) sum_tiles_kernel(EmbShape s, Sums a, ZeroWork z, uint32_t sum_blocks)
+__global__ void __launch_bounds__(kEmbThreads) sum_tiles_kernel(EmbShape s, Sums a)
 {
     wait_for_previous_kernel();
     allow_next_kernel();
-    if (blockIdx.x >= sum_blocks) return zero_share(s, z, blockIdx.x - sum_blocks);
     const int lane = threadIdx.x & 31;
     const uint64_t item = (uint64_t)blockIdx.x * kEmbWarps + (threadIdx.x >> 5);
     const uint32_t gt = (uint32_t)(item / a.slabs), slab = (uint32_t)(item - (uint64_t)gt * a.slabs);
@@ -398,7 +584,8 @@ __global__ void __launch_bounds__(kEmbThreads) sum_tiles_kernel(EmbShape s, Sums
         } else {
 #pragma unroll
             for (int c = 0; c < C; ++c)
-                if (c0 + c * 32 * V < s.dim) store_grad<V>(s, a, worker, cur, c0 + c * 32 * V, acc[c]);
+                if (c0 + c * 32 * V < s.dim)
+                    store_grad<V>(s, a.grad, a.grad_dtype, a.accumulate, worker, cur, c0 + c * 32 * V, acc[c]);
         }
     };
     for (int b = 0; b < live; b += B) {
@@ -436,19 +623,23 @@ __global__ void __launch_bounds__(kEmbThreads) sum_tiles_kernel(EmbShape s, Sums
 }
 
 // Runs that cross tiles: the tile in which one starts adds up the partial sums of all its tiles, in
-// order.  A chain of up to kChainOfWarp tiles is one warp's work; longer ones (frequent
-// tokens) are shared by the block's warps, a contiguous part each.
-constexpr int kJoinCols = 128;              // columns of a warp, four per lane
+// order, kJoinCols columns to a warp.  Most chains are two or three tiles long and one warp's work;
+// those of more than kChainOfWarp tiles (frequent tokens) are shared by a block's warps, a
+// contiguous part each.  The parts a warp adds are on their way together: one after the other they
+// took 44 us instead of 24 us for 131072 rows of 1024.
+constexpr int kJoinCols = 128;              // four a lane
+constexpr int kLongAtOnce = 8;              // parts that a warp of a long chain has in flight
 
-__global__ void __launch_bounds__(kEmbThreads) join_kernel(EmbShape s, Sums a)
+template <int V>
+__global__ void __launch_bounds__(kEmbThreads) join_kernel(EmbShape s, Sums a, uint32_t slabs)
 {
     __shared__ float4 sub[kEmbWarps][32];
     __shared__ uint32_t long_tile[kEmbWarps], long_len[kEmbWarps], long_key[kEmbWarps];
     wait_for_previous_kernel();
     allow_next_kernel();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const uint32_t gt = blockIdx.x * kEmbWarps + w;
-    const int64_t c0 = (int64_t)blockIdx.y * kJoinCols + lane * 4;
+    const uint32_t group = blockIdx.x / slabs, slab = blockIdx.x - group * slabs;
+    const uint32_t gt = group * kEmbWarps + w;
     uint32_t key = kNoKey, len = 0;
     if (gt < (uint32_t)a.tiles * (uint32_t)s.n) {
         const int32_t worker = gt / (uint32_t)a.tiles, tile = gt - worker * a.tiles;
@@ -471,45 +662,152 @@ __global__ void __launch_bounds__(kEmbThreads) join_kernel(EmbShape s, Sums a)
         long_tile[w] = gt;
         long_key[w] = key;
     }
-    auto part_of = [&](uint32_t t, int slot) {
-        return *reinterpret_cast<const float4*>(a.part + ((int64_t)t * 2 + slot) * a.pitch + c0);
+    auto part_of = [&](uint32_t t, int slot, int64_t c) {
+        return *reinterpret_cast<const float4*>(a.part + ((int64_t)t * 2 + slot) * a.pitch + c);
     };
     auto add = [](float4& x, const float4 y) { x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w; };
-    auto sum_of = [&](uint32_t t0, uint32_t from, uint32_t to, float4 sum) {  // slots 0 of tiles t0 + [from, to)
-        for (uint32_t j = from; j < to; j += 8) {
-            float4 v[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = j + u < to ? part_of(t0 + j + u, 0) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) add(sum, v[u]);
-        }
-        return sum;
-    };
-    auto put = [&](uint32_t t, uint32_t k, const float4 sum) {
+    auto put = [&](uint32_t t, uint32_t k, int64_t c, const float4 sum) {
         const float f[4] = {sum.x, sum.y, sum.z, sum.w};
         const int32_t worker = t / (uint32_t)a.tiles;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (c0 + e < s.dim) store_grad<1>(s, a, worker, k, c0 + e, f + e);
+        for (int e = 0; e < 4; e += V)
+            if (c + e < s.dim) store_grad<V>(s, a.grad, a.grad_dtype, a.accumulate, worker, k, c + e, f + e);
     };
-    if (len > 0 && len <= kChainOfWarp && c0 < s.dim) put(gt, key, sum_of(gt + 1, 0, len, part_of(gt, 1)));
+    const int64_t c = (int64_t)slab * kJoinCols + lane * 4;
+    // sum += slots 0 of the tiles t + [from, to), N tiles at a time
+    auto add_parts = [&](auto at_once, float4& sum, uint32_t t, uint32_t from, uint32_t to) {
+        constexpr int N = decltype(at_once)::value;
+        for (uint32_t j = from; j < to; j += N) {
+            float4 v[N];
+#pragma unroll
+            for (int u = 0; u < N; ++u) v[u] = j + u < to && c < s.dim ? part_of(t + j + u, 0, c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int u = 0; u < N; ++u) add(sum, v[u]);
+        }
+    };
+    if (len > 0 && len <= kChainOfWarp && c < s.dim) {
+        float4 sum = part_of(gt, 1, c);
+        add_parts(std::integral_constant<int, kChainOfWarp>(), sum, gt + 1, 0, len);
+        put(gt, key, c, sum);
+    }
     __syncthreads();
-    for (int q = 0; q < kEmbWarps; ++q) {
-        const uint32_t n = long_len[q]; // the same for all threads
+    for (int k = 0; k < kEmbWarps; ++k) {
+        const uint32_t n = long_len[k]; // the same for all threads
         if (n == 0) continue;
-        const uint32_t t = long_tile[q], each = (n + kEmbWarps - 1) / kEmbWarps;
+        const uint32_t t = long_tile[k], each = (n + kEmbWarps - 1) / kEmbWarps;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c0 < s.dim) sum = sum_of(t + 1, min(n, w * each), min(n, (w + 1) * each), sum);
+        add_parts(std::integral_constant<int, kLongAtOnce>(), sum, t + 1, min(n, w * each), min(n, (w + 1) * each));
         sub[w][lane] = sum;
         __syncthreads();
-        if (w == 0 && c0 < s.dim) {
-            sum = part_of(t, 1);
+        if (w == 0 && c < s.dim) {
+            sum = part_of(t, 1, c);
 #pragma unroll
-            for (int k = 0; k < kEmbWarps; ++k) add(sum, sub[k][lane]);
-            put(t, long_key[q], sum);
+            for (int p = 0; p < kEmbWarps; ++p) add(sum, sub[p][lane]);
+            put(t, long_key[k], c, sum);
         }
         __syncthreads();
     }
+}
+
+// ---------------------------------------------------------------------------------------
+// a few tokens: everything in one launch
+// ---------------------------------------------------------------------------------------
+
+constexpr int kDirectTokens = 256;          // per worker
+
+struct Direct {
+    const void* tokens;
+    int64_t tokens_ld;
+    int32_t index_bits;
+    const void* dout;
+    int64_t dout_row, dout_ld;
+    void* grad;
+    int32_t grad_dtype, accumulate;
+    uint32_t groups, slabs;      // groups of kEmbWarps positions, of columns
+    int64_t eights;              // groups of eight rows of a table, if rows nobody names become zeros, else 0
+    uint32_t zero_blocks;        // per worker
+};
+
+// Every warp takes one position.  If its token occurs earlier there is nothing to do; otherwise it
+// adds up the rows of all later positions with that token, 32 V C columns.  Blocks behind those zero
+// rows: a warp compares eight rows with all tokens.
+template <typename TD, int V, int C>
+__global__ void __launch_bounds__(kEmbThreads) direct_kernel(EmbShape s, Direct d)
+{
+    __shared__ uint32_t keys[kDirectTokens];
+    __shared__ uint8_t list[kEmbWarps][kDirectTokens];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int32_t worker = blockIdx.y;
+    const int count = (int)s.count;
+    wait_for_previous_kernel();
+    allow_next_kernel();
+    if (threadIdx.x < count) keys[threadIdx.x] = sort_key(s, d.tokens, d.index_bits, worker * d.tokens_ld + threadIdx.x);
+    __syncthreads();
+    const uint32_t sum_blocks = d.groups * d.slabs;
+    if (blockIdx.x >= sum_blocks) {
+        const int64_t step = (int64_t)d.zero_blocks * kEmbWarps;
+        for (int64_t u = (int64_t)(blockIdx.x - sum_blocks) * kEmbWarps + w; u < d.eights; u += step) {
+            uint32_t named = 0;
+            for (int j = lane; j < count; j += 32) {
+                const uint32_t r = keys[j] - (uint32_t)(u * 8);
+                if (keys[j] < (uint32_t)s.vocab && r < 8) named |= 1u << r;
+            }
+            named = __reduce_or_sync(0xffffffffu, named);
+            const int64_t size = d.grad_dtype == CHOCO_F32 ? 4 : 2;
+            char* p = static_cast<char*>(d.grad) + (worker * s.table_ld + u * 8 * s.table_row) * size;
+            const int left = (int)min((int64_t)8, s.vocab - u * 8);
+            if (named == 0 && s.table_row == s.dim) zero_run(p, left * s.dim * size, lane, 32);
+            else
+                for (int r = 0; r < left; ++r)
+                    if (!(named >> r & 1)) zero_run(p + r * s.table_row * size, s.dim * size, lane, 32);
+        }
+        return;
+    }
+    const uint32_t group = blockIdx.x / d.slabs, slab = blockIdx.x - group * d.slabs;
+    const int mine = (int)group * kEmbWarps + w;
+    if (mine >= count) return;
+    const uint32_t key = keys[mine];
+    if (key >= (uint32_t)s.vocab) return;
+    for (int j = 0; j < mine; j += 32)
+        if (__any_sync(0xffffffffu, j + lane < mine && keys[j + lane] == key)) return;
+    int n = 0;
+    for (int j = mine & ~31; j < count; j += 32) {
+        const bool is = j + lane >= mine && j + lane < count && keys[j + lane] == key;
+        const uint32_t all = __ballot_sync(0xffffffffu, is);
+        if (is) list[w][n + __popc(all & ((1u << lane) - 1u))] = (uint8_t)(j + lane);
+        n += __popc(all);
+    }
+    __syncwarp();
+    const TD* rows = static_cast<const TD*>(d.dout) + worker * d.dout_ld;
+    const int64_t c0 = (int64_t)slab * (32 * V * C) + lane * V;
+    float acc[C][V];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[c][e] = 0.f;
+    constexpr int B = 8;
+    for (int b = 0; b < n; b += B) {
+        Raw<TD, V> raw[B][C];
+#pragma unroll
+        for (int j = 0; j < B; ++j)
+            if (b + j < n) {
+                const TD* r = rows + list[w][b + j] * d.dout_row;
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    if (c0 + c * 32 * V < s.dim) load_raw(raw[j][c], r + c0 + c * 32 * V);
+            }
+#pragma unroll
+        for (int j = 0; j < B; ++j)
+            if (b + j < n)
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[c][e] += raw_get(raw[j][c], e);
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (c0 + c * 32 * V < s.dim)
+            store_grad<V>(s, d.grad, d.grad_dtype, d.accumulate, worker, key, c0 + c * 32 * V, acc[c]);
 }
 
 template <typename F>
@@ -520,7 +818,12 @@ int with_type(int32_t dtype, F f)
     return f((__half*)nullptr);
 }
 
-int status_of_launch() { return cudaGetLastError() == cudaSuccess ? CHOCO_OK : CHOCO_ERR_CUDA; }
+int status_of(cudaError_t e)
+{
+    if (e == cudaSuccess) return CHOCO_OK;
+    cudaGetLastError();
+    return CHOCO_ERR_CUDA;
+}
 
 // The largest number of elements (a power of two, at most `most`) by which every row of an array
 // can be cut into aligned vectors.
@@ -542,9 +845,6 @@ struct choco_embedding {
     uint32_t* pos[2];
     uint32_t* hist;
     uint32_t* total;
-    uint8_t* present;
-    int64_t present_bytes;       // per worker
-    bool dirty;                  // a call failed half-way: the map may not be clear
     float* part;
     int64_t pitch;
 };
@@ -562,7 +862,6 @@ void free_all(choco_embedding* e)
     for (int k = 0; k < 2; ++k) { cudaFree(e->key[k]); cudaFree(e->pos[k]); }
     cudaFree(e->hist);
     cudaFree(e->total);
-    cudaFree(e->present);
     cudaFree(e->part);
     delete e;
 }
@@ -582,38 +881,87 @@ int check_tokens(const choco_embedding* e, const void* tokens, int32_t bits, int
     return CHOCO_OK;
 }
 
-int tile_of(int64_t rows) { return rows <= kShortRows ? kTileShort : kTileLong; }
+// (8 x 2240 rows of 650 added: 33.6 us in tiles of 16, 35.5 us of 32; 4 x 1000 rows of 200: 17.4 us of 8, 18.9 us of 16)
+int tile_of(int64_t rows) { return rows <= kShortRows ? kTileShort : rows <= kMidRows ? kTileMid : kTileLong; }
 
-// number of bits for positions, if (token, position) pairs fit 32 bits and ordering by ranks pays; else 0
-int rank_bits(const EmbShape& s)
+// How a cluster of blocks orders the tokens, or false if there are too many for that.
+bool plan_order(const EmbShape& s, Order& o)
 {
-    int b = 1;
-    while (((int64_t)1 << b) < s.count) ++b;
-    if ((int64_t)s.n * s.count * s.count > kRankPairs || ((s.vocab + 1) << b) > (int64_t)1 << 32 || s.count > 8192) return 0;
-    return b;
+    if (s.count > (int64_t)kOrderCluster * kOrderMost) return false;
+    // a block for every kOrderFew keys, while all workers' clusters run at once, or as many as their memory needs
+    o.cluster_log = 0;
+    while ((1 << o.cluster_log) < kOrderCluster && ((int64_t)kOrderFew << o.cluster_log) < s.count &&
+           (((int64_t)kOrderMost << o.cluster_log) < s.count || ((int64_t)s.n << (o.cluster_log + 1)) <= 148))
+        ++o.cluster_log;
+    o.part_log = 10;
+    while (((int64_t)1 << (o.part_log + o.cluster_log)) < s.count) ++o.part_log;
+    int bits = 1;
+    while ((s.vocab >> bits) != 0) ++bits; // keys go up to vocab
+    o.passes = (bits + kOrderDigitBits - 1) / kOrderDigitBits;
+    o.digit_bits = (bits + o.passes - 1) / o.passes;
+    return true;
+}
+
+cudaError_t launch_order(const EmbShape& s, const Order& o, cudaStream_t st)
+{
+    const size_t smem = sizeof(OrderSmem) + ((size_t)2 * sizeof(uint2) << o.part_log);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(s.n << o.cluster_log));
+    cfg.blockDim = dim3(kOrderThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1u << o.cluster_log;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, order_kernel, s, o);
 }
 
 template <typename TD, int V, int C, int B>
-cudaError_t launch_sums(const EmbShape& s, Sums a, const ZeroWork& z, cudaStream_t st)
+cudaError_t launch_sums(const EmbShape& s, Sums a, cudaStream_t st)
 {
     a.slabs = (uint32_t)((s.dim + 32 * V * C - 1) / (32 * V * C));
     const uint64_t warps = (uint64_t)a.slabs * a.tiles * s.n;
     const uint64_t blocks = (warps + kEmbWarps - 1) / kEmbWarps;
-    if (blocks + z.blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    return launch_overlapped(sum_tiles_kernel<TD, V, C, B>, dim3((unsigned)(blocks + z.blocks)), dim3(kEmbThreads), 0, st, HotRange{}, s, a,
-                             z, (uint32_t)blocks);
+    if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+    return launch_overlapped(sum_tiles_kernel<TD, V, C, B>, dim3((unsigned)blocks), dim3(kEmbThreads), 0, st, HotRange{}, s, a);
 }
 
 template <typename TD>
-cudaError_t launch_sums_for(const EmbShape& s, const Sums& a, const ZeroWork& z, int v, cudaStream_t st)
+cudaError_t launch_sums_for(const EmbShape& s, const Sums& a, int v, cudaStream_t st)
 {
     // 256 columns of a row to a warp, 128 where one element at a time is all that alignment leaves;
     // narrow rows take fewer vectors per lane
     if constexpr (sizeof(TD) == 2)
-        if (v == 8) return launch_sums<TD, 8, 1, 8>(s, a, z, st);
-    if (v >= 4) return s.dim <= 128 ? launch_sums<TD, 4, 1, 8>(s, a, z, st) : launch_sums<TD, 4, 2, 4>(s, a, z, st);
-    if (v == 2) return s.dim <= 64 ? launch_sums<TD, 2, 1, 8>(s, a, z, st) : launch_sums<TD, 2, 4, 4>(s, a, z, st);
-    return launch_sums<TD, 1, 4, 4>(s, a, z, st);
+        if (v == 8) return launch_sums<TD, 8, 1, 8>(s, a, st);
+    if (v >= 4) return s.dim <= 128 ? launch_sums<TD, 4, 1, 8>(s, a, st) : launch_sums<TD, 4, 2, 4>(s, a, st);
+    if (v == 2) return s.dim <= 64 ? launch_sums<TD, 2, 1, 8>(s, a, st) : launch_sums<TD, 2, 4, 4>(s, a, st);
+    return launch_sums<TD, 1, 4, 4>(s, a, st);
+}
+
+template <typename TD, int V, int C>
+cudaError_t launch_direct(const EmbShape& s, Direct d, cudaStream_t st)
+{
+    d.groups = (uint32_t)((s.count + kEmbWarps - 1) / kEmbWarps);
+    d.slabs = (uint32_t)((s.dim + 32 * V * C - 1) / (32 * V * C));
+    d.zero_blocks = (uint32_t)std::min<int64_t>((d.eights + kEmbWarps - 1) / kEmbWarps, std::max<int64_t>(1, 148 * 8 / s.n));
+    return launch_overlapped(direct_kernel<TD, V, C>, dim3(d.groups * d.slabs + d.zero_blocks, (unsigned)s.n), dim3(kEmbThreads), 0, st,
+                             HotRange{}, s, d);
+}
+
+template <typename TD>
+cudaError_t launch_direct_for(const EmbShape& s, const Direct& d, int v, cudaStream_t st)
+{
+    if constexpr (sizeof(TD) == 2)
+        if (v == 8) return launch_direct<TD, 8, 1>(s, d, st);
+    if (v >= 4) return launch_direct<TD, 4, 1>(s, d, st);
+    if (v == 2) return launch_direct<TD, 2, 2>(s, d, st);
+    return launch_direct<TD, 1, 2>(s, d, st);
 }
 
 } // namespace
@@ -638,12 +986,11 @@ int choco_embedding_init(choco_embedding** out, const choco_embedding_params* p)
     cudaError_t err = cudaGetDevice(&e->device);
     const int64_t total = q.n * q.max_tokens;
     e->pitch = (q.dim + 7) / 8 * 8;
-    e->present_bytes = (q.vocab + 31) / 32 * 4;
     if (total > 0) {
         const int64_t sort_tiles = (q.max_tokens + kSortTile - 1) / kSortTile;
-        // batches of every size up to the largest have to fit, in tiles of either length
-        const int64_t few = std::min(total, kShortRows);
-        const int64_t tiles = std::max<int64_t>((q.max_tokens + kTileLong - 1) / kTileLong * q.n, (few + kTileShort - 1) / kTileShort + q.n);
+        // batches of every size up to the largest have to fit, in tiles of any length
+        const int64_t few = std::min(total, kShortRows), mid = std::min(total, kMidRows);
+        const int64_t tiles = std::max({(q.max_tokens + kTileLong - 1) / kTileLong * q.n, mid / kTileMid + q.n, few / kTileShort + q.n});
         auto get = [&](auto** ptr, int64_t count) {
             if (err == cudaSuccess) err = cudaMalloc((void**)ptr, (size_t)count * sizeof(**ptr));
         };
@@ -653,8 +1000,9 @@ int choco_embedding_init(choco_embedding** out, const choco_embedding_params* p)
         get(&e->part, tiles * 2 * e->pitch);
     }
     if (q.max_tokens > 0 && err == cudaSuccess) {
-        err = cudaMalloc((void**)&e->present, (size_t)(q.n * e->present_bytes));
-        if (err == cudaSuccess) err = cudaMemset(e->present, 0, (size_t)(q.n * e->present_bytes));
+        err = cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                   (int)(sizeof(OrderSmem) + 2 * sizeof(uint2) * kOrderMost));
+        if (err == cudaSuccess) err = cudaFuncSetAttribute(order_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     }
     if (err != cudaSuccess) {
         cudaGetLastError();
@@ -691,15 +1039,21 @@ int choco_embedding_forward(choco_embedding* emb, const void* table, int32_t tab
         return with_type(out_dtype, [&](auto* to) {
             using TT = std::remove_pointer_t<decltype(tt)>;
             using TO = std::remove_pointer_t<decltype(to)>;
+            auto launch = [&](auto vec, auto vectors) {
+                constexpr int V = decltype(vec)::value, N = decltype(vectors)::value;
+                const int64_t slabs = (s.dim + 32 * V * N - 1) / (32 * V * N);
+                const int64_t blocks = (count * slabs + kEmbWarps - 1) / kEmbWarps;
+                if (blocks > 0x1fffffff) return (int)CHOCO_ERR_TOO_LARGE; // (more than the output can have in memory)
+                return status_of(launch_overlapped(lookup_kernel<TT, TO, V, N>, dim3((unsigned)blocks, (unsigned)s.n), dim3(kEmbThreads), 0,
+                                                   st, HotRange{}, s, static_cast<const TT*>(table), tokens, index_bits, tokens_ld,
+                                                   static_cast<TO*>(out), out_row, out_ld, (uint32_t)slabs));
+            };
+            // 4 or 6 vectors a lane, whichever leaves fewer of them idle
             auto go = [&](auto vec) {
                 constexpr int V = decltype(vec)::value;
-                const int64_t slabs = (s.dim + 32 * V * kLookupVecs - 1) / (32 * V * kLookupVecs);
-                const int64_t blocks = (count * s.n * slabs + kEmbWarps - 1) / kEmbWarps;
-                if (blocks > 0x7fffffff) return (int)CHOCO_ERR_TOO_LARGE;
-                lookup_kernel<TT, TO, V><<<(unsigned)blocks, kEmbThreads, 0, st>>>(
-                    s, static_cast<const TT*>(table), tokens, index_bits, tokens_ld, static_cast<TO*>(out), out_row, out_ld,
-                    (uint32_t)slabs);
-                return status_of_launch();
+                auto idle = [&](int64_t cols) { return (s.dim + cols - 1) / cols * cols - s.dim; };
+                if (idle(32 * V * 6) < idle(32 * V * 4)) return launch(vec, std::integral_constant<int, 6>());
+                return launch(vec, std::integral_constant<int, 4>());
             };
             if constexpr (sizeof(TT) == 2 || sizeof(TO) == 2)
                 if (v == 8) return go(std::integral_constant<int, 8>());
@@ -723,67 +1077,56 @@ int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t i
     if (count == 0 && accumulate) return CHOCO_OK;
     const EmbShape s = shape_of(emb, count);
     cudaStream_t st = (cudaStream_t)stream;
-    const int64_t sort_tiles = (count + kSortTile - 1) / kSortTile;
-
-    Presence pres = {accumulate ? nullptr : emb->present, emb->present_bytes};
-    ZeroWork z = {};
-    z.pres = pres;
-    z.grad = grad;
-    z.dtype = grad_dtype;
-    z.wide = vector_of(grad, grad_dtype, s.table_row, s.table_ld, s.dim, s.n, 8) * (int)dtype_size(grad_dtype);
-    z.wide = std::min(z.wide, 16);
-    const int64_t map = accumulate ? 0 : emb->present_bytes * s.n;
-    // `part` of `parts` of the rows nobody names, done by blocks behind those of a launch
-    auto share = [&](int part, int parts) {
-        z.begin = map * part / parts;
-        z.end = map * (part + 1) / parts;
-        z.blocks = (int32_t)std::min<int64_t>((z.end - z.begin + kEmbWarps - 1) / kEmbWarps, 148 * 8);
-    };
+    const int v = std::min(vector_of(dout, dout_dtype, dout_row, dout_ld, s.dim, s.n, 8),
+                           vector_of(grad, grad_dtype, s.table_row, s.table_ld, s.dim, s.n, 8));
     cudaError_t err = cudaSuccess;
-    if (!accumulate) {
-        if (emb->dirty) err = cudaMemsetAsync(emb->present, 0, (size_t)map, st);
-        emb->dirty = true;
+
+    if (count <= kDirectTokens) {
+        const Direct d = {tokens, tokens_ld, index_bits, dout, dout_row, dout_ld, grad, grad_dtype, accumulate, 0, 0,
+                          accumulate ? 0 : (s.vocab + 7) / 8, 0};
+        with_type(dout_dtype, [&](auto* td) {
+            err = launch_direct_for<std::remove_pointer_t<decltype(td)>>(s, d, v, st);
+            return 0;
+        });
+        return status_of(err);
     }
-    int cur = 0;
+
+    auto zero = [&](int32_t beside) {
+        if (accumulate || err != cudaSuccess) return;
+        const int32_t size = (int32_t)dtype_size(grad_dtype);
+        const int64_t per_row = (s.dim * size + kZeroSpan - 1) / kZeroSpan;
+        const int64_t blocks = s.table_row == s.dim ? (s.vocab * s.dim * size + kZeroSpan - 1) / kZeroSpan : s.vocab * per_row;
+        if (blocks > 0x7fffffff) err = cudaErrorInvalidValue;
+        else
+            err = launch_overlapped(zero_kernel, dim3((unsigned)blocks, (unsigned)s.n), dim3(kEmbThreads), 0, st, HotRange{}, s,
+                                    static_cast<char*>(grad), size, (uint32_t)per_row, beside);
+    };
     const dim3 threads(kEmbThreads);
-    const int bits = rank_bits(s);
-    if (count > 0 && bits > 0) {
-        const size_t smem = (size_t)(count + 15) / 16 * 16 * 4;
-        const dim3 grid((unsigned)((count + kRankKeys - 1) / kRankKeys), (unsigned)s.n);
-        if (err == cudaSuccess)
-            err = launch_overlapped(rank_kernel, grid, threads, smem, st, HotRange{}, s, tokens, tokens_ld, index_bits, bits, pres,
-                                    emb->key[0], emb->pos[0]);
-        share(0, 1);
-    } else if (count > 0) {
+    int cur = 0;
+    Order o = {};
+    if (plan_order(s, o)) {
+        o.tokens = tokens; o.tokens_ld = tokens_ld; o.index_bits = index_bits;
+        o.keys = emb->key[0]; o.pos = emb->pos[0];
+        err = launch_order(s, o, st);
+        zero(1);
+    } else {
         SortPass p = {};
         p.tokens = tokens; p.tokens_ld = tokens_ld; p.index_bits = index_bits;
-        p.tiles = (int32_t)sort_tiles;
+        p.tiles = (int32_t)((count + kSortTile - 1) / kSortTile);
         p.hist = emb->hist;
         p.total = emb->total;
-        p.pres = pres;
         p.first = 1;
-        int passes = 1;
-        while ((s.vocab >> (passes * kDigitBits)) != 0) ++passes;
-        const int shares = 3 * passes - 1; // every launch but the first, which finds out what is present, zeroes a share
-        int done = 0;
-        for (int k = 0; k < passes; ++k) {
-            p.shift = k * kDigitBits;
+        zero(0);
+        for (p.shift = 0; p.shift == 0 || (s.vocab >> p.shift) != 0; p.shift += kDigitBits) {
             p.key_in = emb->key[cur]; p.pos_in = emb->pos[cur];
             p.key_out = emb->key[cur ^ 1]; p.pos_out = emb->pos[cur ^ 1];
-            const unsigned tiles = (unsigned)(sort_tiles * s.n), digits = (unsigned)(s.n * (kDigits / kEmbWarps));
-            if (k == 0) z.begin = z.end = z.blocks = 0;
-            else share(done++, shares);
-            if (err == cudaSuccess) err = launch_overlapped(sort_count_kernel, dim3(tiles + z.blocks), threads, 0, st, HotRange{}, s, p, z);
-            share(done++, shares);
-            if (err == cudaSuccess) err = launch_overlapped(sort_scan_kernel, dim3(digits + z.blocks), threads, 0, st, HotRange{}, s, p, z);
-            share(done++, shares);
-            if (err == cudaSuccess) err = launch_overlapped(sort_scatter_kernel, dim3(tiles + z.blocks), threads, 0, st, HotRange{}, s, p, z);
+            const unsigned tiles = (unsigned)(p.tiles * s.n), digits = (unsigned)(s.n * (kDigits / kEmbWarps));
+            if (err == cudaSuccess) err = launch_overlapped(sort_count_kernel, dim3(tiles), threads, 0, st, HotRange{}, s, p);
+            if (err == cudaSuccess) err = launch_overlapped(sort_scan_kernel, dim3(digits), threads, 0, st, HotRange{}, s, p);
+            if (err == cudaSuccess) err = launch_overlapped(sort_scatter_kernel, dim3(tiles), threads, 0, st, HotRange{}, s, p);
             p.first = 0;
             cur ^= 1;
         }
-        z.begin = z.end = z.blocks = 0;
-    } else {
-        share(0, 1);
     }
     Sums a = {};
     a.keys = emb->key[cur]; a.pos = emb->pos[cur];
@@ -792,23 +1135,20 @@ int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t i
     a.part = emb->part; a.pitch = emb->pitch;
     a.tile = tile_of(count * s.n);
     a.tiles = (int32_t)((count + a.tile - 1) / a.tile);
-    const int v = std::min(vector_of(dout, dout_dtype, dout_row, dout_ld, s.dim, s.n, 8),
-                           vector_of(grad, grad_dtype, s.table_row, s.table_ld, s.dim, s.n, 8));
     if (err == cudaSuccess)
         with_type(dout_dtype, [&](auto* td) {
-            err = launch_sums_for<std::remove_pointer_t<decltype(td)>>(s, a, z, v, st);
+            err = launch_sums_for<std::remove_pointer_t<decltype(td)>>(s, a, v, st);
             return 0;
         });
-    if (err == cudaSuccess && a.tiles > 1) {
-        const dim3 grid((unsigned)(((int64_t)a.tiles * s.n + kEmbWarps - 1) / kEmbWarps), (unsigned)((s.dim + kJoinCols - 1) / kJoinCols));
-        err = launch_overlapped(join_kernel, grid, threads, 0, st, HotRange{}, s, a);
+    if (err == cudaSuccess) {
+        const uint32_t slabs = (uint32_t)((s.dim + kJoinCols - 1) / kJoinCols);
+        const int64_t blocks = ((int64_t)a.tiles * s.n + kEmbWarps - 1) / kEmbWarps * slabs;
+        if (blocks > 0x7fffffff) err = cudaErrorInvalidValue;
+        else
+            err = launch_overlapped(v >= 4 ? join_kernel<4> : v == 2 ? join_kernel<2> : join_kernel<1>, dim3((unsigned)blocks), threads, 0, st,
+                                    HotRange{}, s, a, slabs);
     }
-    if (err != cudaSuccess || status_of_launch() != CHOCO_OK) {
-        cudaGetLastError();
-        return CHOCO_ERR_CUDA;
-    }
-    emb->dirty = false;
-    return CHOCO_OK;
+    return status_of(err);
 }
 
 } // extern "C"
