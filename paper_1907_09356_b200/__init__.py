@@ -166,11 +166,20 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+_current_stream = None
+
+
 def _stream(stream) -> Optional[int]:
-    if stream is None:
+    if stream is not None:
+        return stream.cuda_stream or None
+    global _current_stream
+    if _current_stream is None:
         import torch
-        stream = torch.cuda.current_stream()
-    return stream.cuda_stream or None
+        # the handle itself where torch gives it (0.1 us); its Stream object takes 3 us to make
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _current_stream = ((lambda: raw(torch.cuda.current_device())) if raw is not None and torch.cuda.is_available()
+                           else (lambda: torch.cuda.current_stream().cuda_stream))
+    return _current_stream() or None
 
 
 # --------------------------------------------------------------------------- C names
@@ -399,26 +408,45 @@ def choco_layers_set_nesterov(layers, enable: bool) -> None:
     _check(load().choco_layers_set_nesterov(layers, 1 if enable else 0))
 
 
+_dtype_codes: dict = {}    # by torch dtype, filled as they are met
+_index_codes: dict = {}
+
+
 def _dtype(t) -> int:
     """choco_dtype of a tensor (or of a torch dtype)."""
-    name = str(getattr(t, "dtype", t)).rpartition(".")[2]
-    if name not in DTYPES:
-        raise ChocoError(f"libchoco: {name} arrays are not supported (float32, bfloat16 or float16)", -1)
-    return DTYPES[name]
+    dtype = getattr(t, "dtype", t)
+    code = _dtype_codes.get(dtype)
+    if code is None:
+        name = str(dtype).rpartition(".")[2]
+        if name not in DTYPES:
+            raise ChocoError(f"libchoco: {name} arrays are not supported (float32, bfloat16 or float16)", -1)
+        code = _dtype_codes[dtype] = DTYPES[name]
+    return code
 
 
 def _index_bits(t) -> int:
-    name = str(t.dtype).rpartition(".")[2]
-    if name not in ("int32", "int64"):
-        raise ChocoError(f"libchoco: tokens are int32 or int64, not {name}", -1)
-    return 32 if name == "int32" else 64
+    code = _index_codes.get(t.dtype)
+    if code is None:
+        name = str(t.dtype).rpartition(".")[2]
+        if name not in ("int32", "int64"):
+            raise ChocoError(f"libchoco: tokens are int32 or int64, not {name}", -1)
+        code = _index_codes[t.dtype] = 32 if name == "int32" else 64
+    return code
 
 
-def _rows3(t, what: str, n: int, count: int, dim: int) -> tuple[int, int]:
-    """(row, worker) strides of an [n, count, dim] tensor with unit stride inside a row."""
-    if tuple(t.shape) != (n, count, dim) or (dim > 1 and count and t.stride(2) != 1):
-        raise ChocoError(f"libchoco: {what} must be [{n}, {count}, {dim}] with contiguous rows, not {tuple(t.shape)}", -1)
-    return (t.stride(1) if count > 1 else max(dim, t.stride(1))), t.stride(0)
+def _token_rows(tokens, rows, what: str) -> tuple:
+    """(tokens per worker, stride of the tokens' rows, strides of `rows` from token to token and from
+    worker to worker) for tokens [n, T] and rows [n, T, dim] with unit stride inside their rows."""
+    shape, (n, count) = rows.shape, tokens.shape
+    ld, inside = tokens.stride()
+    if count > 1 and inside != 1:
+        raise ChocoError("libchoco: tokens must be contiguous inside a worker's row", -1)
+    if len(shape) != 3 or shape[0] != n or shape[1] != count:
+        raise ChocoError(f"libchoco: {what} must be [{n}, {count}, dim], not {list(shape)}", -1)
+    worker, row, inside = rows.stride()
+    if shape[2] > 1 and count and inside != 1:
+        raise ChocoError(f"libchoco: {what} must have contiguous rows", -1)
+    return count, ld, (row if count > 1 else max(shape[2], row)), worker
 
 
 def choco_embedding_init(n: int, vocab: int, dim: int, max_tokens: int, table_row: int = 0, table_ld: int = 0,
@@ -437,22 +465,16 @@ def choco_embedding_destroy(emb) -> None:
 def choco_embedding_forward(emb, table, tokens, out, stream=None) -> None:
     """out[i, t] = scale * table_i[tokens[i, t]].  `table` is a tensor that starts at worker 0's first
     row; tokens [n, T] int32 or int64; out [n, T, dim]."""
-    n, count = tokens.shape
-    if count > 1 and tokens.stride(1) != 1:
-        raise ChocoError("libchoco: tokens must be contiguous inside a worker's row", -1)
-    row, ld = _rows3(out, "out", n, count, out.shape[2])
-    _check(load().choco_embedding_forward(emb, _ptr(table), _dtype(table), _ptr(tokens), _index_bits(tokens), count,
-                                          tokens.stride(0), _ptr(out), _dtype(out), row, ld, _stream(stream)))
+    count, tokens_ld, row, ld = _token_rows(tokens, out, "out")
+    _check(load().choco_embedding_forward(emb, table.data_ptr(), _dtype(table), tokens.data_ptr(), _index_bits(tokens), count,
+                                          tokens_ld, out.data_ptr(), _dtype(out), row, ld, _stream(stream)))
 
 
 def choco_embedding_backward(emb, tokens, dout, grad, accumulate: bool = False, stream=None) -> None:
     """grad_i[r] (+)= scale * sum of dout[i, t] over the t with tokens[i, t] = r, in the table's layout."""
-    n, count = tokens.shape
-    if count > 1 and tokens.stride(1) != 1:
-        raise ChocoError("libchoco: tokens must be contiguous inside a worker's row", -1)
-    row, ld = _rows3(dout, "dout", n, count, dout.shape[2])
-    _check(load().choco_embedding_backward(emb, _ptr(tokens), _index_bits(tokens), count, tokens.stride(0), _ptr(dout),
-                                           _dtype(dout), row, ld, _ptr(grad), _dtype(grad), 1 if accumulate else 0,
+    count, tokens_ld, row, ld = _token_rows(tokens, dout, "dout")
+    _check(load().choco_embedding_backward(emb, tokens.data_ptr(), _index_bits(tokens), count, tokens_ld, dout.data_ptr(),
+                                           _dtype(dout), row, ld, grad.data_ptr(), _dtype(grad), 1 if accumulate else 0,
                                            _stream(stream)))
 
 
@@ -595,7 +617,8 @@ class Embedding:
         self.handle = choco_embedding_init(n, vocab, dim, max_tokens, table_row, table_ld, scale, padding)
 
     def _shape(self, tokens, rows):
-        if tokens.dim() != 2 or tokens.shape[0] != self.n or rows.dim() != 3 or rows.shape[2] != self.dim:
+        a, b = tokens.shape, rows.shape
+        if len(a) != 2 or a[0] != self.n or len(b) != 3 or b[2] != self.dim:
             raise ChocoError(f"libchoco: tokens must be [{self.n}, T], rows [{self.n}, T, {self.dim}]", -1)
 
     def forward(self, table, tokens, out, stream=None):
