@@ -47,31 +47,34 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, int32_t bits, in
 // lookup
 // ---------------------------------------------------------------------------------------
 
-// A warp serves one row, or 32 N V columns of it, with all its loads in flight together: N vectors of
-// V elements a lane.  The row of the table is known only when the token has arrived, so the bytes in
-// flight have to come from many warps.
-template <typename TT, typename TO, int V, int N>
+// N vectors of V elements a lane, all its loads in flight together: a warp serves 32 N V columns of
+// a row, or where rows are narrow 32 / lanes of them.  The row of the table is known only when the
+// token has arrived, so the bytes in flight have to come from many warps, and rows too narrow to
+// fill one are served together.
+template <typename TT, typename TO, int V, int N, bool NARROW>
 __global__ void __launch_bounds__(kEmbThreads)
 lookup_kernel(EmbShape s, const TT* __restrict__ table, const void* __restrict__ tokens, int32_t index_bits, int64_t tokens_ld,
-              TO* __restrict__ out, int64_t out_row, int64_t out_ld, uint32_t slabs)
+              TO* __restrict__ out, int64_t out_row, int64_t out_ld, uint32_t slabs, uint32_t narrow_log)
 {
-    const uint32_t item = blockIdx.x * kEmbWarps + (threadIdx.x >> 5);
+    const uint32_t lanes_log = NARROW ? narrow_log : 5; // lanes of a row
+    const uint32_t lane = threadIdx.x & 31, lanes = 1u << lanes_log, mine = lane & (lanes - 1);
+    const uint32_t item = ((blockIdx.x * kEmbWarps + (threadIdx.x >> 5)) << (5 - lanes_log)) + (lane >> lanes_log);
     const uint32_t t = slabs == 1 ? item : item / slabs, slab = slabs == 1 ? 0 : item - t * slabs;
     wait_for_previous_kernel();
     allow_next_kernel();
     if (t >= (uint32_t)s.count) return;
     const int64_t i = blockIdx.y;
     const int64_t tok = token_at(tokens, index_bits, i * tokens_ld + t, s.vocab);
-    const int32_t c0 = (int32_t)slab * (32 * V * N) + (threadIdx.x & 31) * V, dim = (int32_t)s.dim;
+    const int32_t step = (int32_t)lanes * V, c0 = (int32_t)slab * step * N + (int32_t)mine * V, dim = (int32_t)s.dim;
     TO* o = out + i * out_ld + t * out_row;
     const TT* w = table + i * s.table_ld + (tok < 0 ? 0 : tok) * s.table_row;
     Raw<TT, V> raw[N];
 #pragma unroll
     for (int k = 0; k < N; ++k)
-        if (tok >= 0 && c0 + k * 32 * V < dim) load_raw(raw[k], w + c0 + k * 32 * V);
+        if (tok >= 0 && c0 + k * step < dim) load_raw(raw[k], w + c0 + k * step);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const int32_t c = c0 + k * 32 * V;
+        const int32_t c = c0 + k * step;
         if (c >= dim) continue;
         float f[V];
 #pragma unroll
@@ -1041,18 +1044,21 @@ int choco_embedding_forward(choco_embedding* emb, const void* table, int32_t tab
             using TO = std::remove_pointer_t<decltype(to)>;
             auto launch = [&](auto vec, auto vectors) {
                 constexpr int V = decltype(vec)::value, N = decltype(vectors)::value;
-                const int64_t slabs = (s.dim + 32 * V * N - 1) / (32 * V * N);
-                const int64_t blocks = (count * slabs + kEmbWarps - 1) / kEmbWarps;
+                uint32_t lanes_log = 5;
+                while (lanes_log > 2 && ((int64_t)V * N << (lanes_log - 1)) >= s.dim) --lanes_log;
+                auto* kernel = lanes_log < 5 ? lookup_kernel<TT, TO, V, N, true> : lookup_kernel<TT, TO, V, N, false>;
+                const int64_t slabs = (s.dim + 32 * V * N - 1) / (32 * V * N), per_block = (int64_t)kEmbWarps << (5 - lanes_log);
+                const int64_t blocks = (count * slabs + per_block - 1) / per_block;
                 if (blocks > 0x1fffffff) return (int)CHOCO_ERR_TOO_LARGE; // (more than the output can have in memory)
-                return status_of(launch_overlapped(lookup_kernel<TT, TO, V, N>, dim3((unsigned)blocks, (unsigned)s.n), dim3(kEmbThreads), 0,
+                return status_of(launch_overlapped(kernel, dim3((unsigned)blocks, (unsigned)s.n), dim3(kEmbThreads), 0,
                                                    st, HotRange{}, s, static_cast<const TT*>(table), tokens, index_bits, tokens_ld,
-                                                   static_cast<TO*>(out), out_row, out_ld, (uint32_t)slabs));
+                                                   static_cast<TO*>(out), out_row, out_ld, (uint32_t)slabs, lanes_log));
             };
             // 4 or 6 vectors a lane, whichever leaves fewer of them idle
             auto go = [&](auto vec) {
                 constexpr int V = decltype(vec)::value;
                 auto idle = [&](int64_t cols) { return (s.dim + cols - 1) / cols * cols - s.dim; };
-                if (idle(32 * V * 6) < idle(32 * V * 4)) return launch(vec, std::integral_constant<int, 6>());
+                if (s.dim > 32 * V * 4 && idle(32 * V * 6) < idle(32 * V * 4)) return launch(vec, std::integral_constant<int, 6>());
                 return launch(vec, std::integral_constant<int, 4>());
             };
             if constexpr (sizeof(TT) == 2 || sizeof(TO) == 2)
