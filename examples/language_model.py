@@ -20,9 +20,11 @@ import paper_1907_09356_b200 as choco  # noqa: E402
 import workloads  # noqa: E402
 
 
-def train(workers=8, steps=200, bits=32, q="topk", vocab=512, dim=64, batch=16, length=33, lr=3e-3, gamma=0.4, clip=1.0, seed=0,
+def train(workers=8, steps=200, bits=32, q="topk", vocab=512, dim=64, batch=16, length=33, lr=3e-3, gamma=None, clip=1.0, seed=0,
           log=None):
     """Returns (mean loss per step, consensus distance per step)."""
+    if gamma is None:       # consensus stepsizes in the stable range of each operator
+        gamma = {"topk": 0.1, "randk": 0.03, "qsgd": 0.1, "sign": 0.4, "identity": 1.0}[q]
     dev = torch.device("cuda")
     gen = torch.Generator(device=dev).manual_seed(seed)
     w = workloads.ring(workers)

@@ -22,7 +22,7 @@ constexpr int kStepThreads = 128;            // short blocks: 256 threads took 5
 constexpr int kStepWarps = kStepThreads / 32;
 constexpr int kChunkElems = kStepWarps * kBlock;
 // blocks on an SM: 64 registers a thread with 32-bit moments, 48 with codes, where more warps pay (552 us against 579)
-constexpr int kStepBlocks32 = 8, kStepBlocks8 = 10;
+constexpr int kStepBlocks32 = 8, kStepBlocks8 = 10, kStepBlocksRest = 6;
 constexpr int kNormThreads = 256;
 constexpr float kCodesM = 127.0f;           // codes k stand for s k^2, k up to 127 (m) and 255 (sqrt v)
 constexpr float kCodesV = 255.0f;
@@ -274,31 +274,33 @@ __device__ __forceinline__ void finish_block(Loaded<BITS, XT, GT>& l, const Tens
 
 // Any block: a lane owns every 32nd element, so that single elements still make whole lines; the
 // last block of a tensor and tensors that do not start on 16 bytes.
-template <int BITS>
+template <int BITS, typename XT, typename GT>
 struct LoadedAny {
-    uint32_t g[8], x[8];
+    Raw<GT, 1> g[8];
+    Raw<XT, 1> x[8];
     float m[8], v[8], sm, sv;
 };
-template <int BITS>
-__device__ __forceinline__ void load_block_any(LoadedAny<BITS>& l, const Tensor& t, const State& st, int64_t base, int count)
+template <int BITS, typename XT, typename GT>
+__device__ __forceinline__ void load_block_any(LoadedAny<BITS, XT, GT>& l, const Tensor& t, const State& st, int64_t base, int count)
 {
     const int lane = threadIdx.x & 31;
     const int64_t s0 = t.state + base;
+    const GT* g = static_cast<const GT*>(t.g) + base + lane;
+    const XT* x = static_cast<const XT*>(t.x) + base + lane;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const int e = j * 32 + lane;
-        l.g[j] = l.x[j] = 0;
+        l.g[j].w[0] = l.x[j].w[0] = 0;
         l.m[j] = BITS == 32 ? 0.f : 8388736.0f; // code 0
         l.v[j] = BITS == 32 ? 0.f : 8388608.0f;
-        if (e >= count) continue;
-        l.g[j] = load_bits(t.g, base + e, t.g_dtype);
-        l.x[j] = load_bits(t.x, base + e, t.x_dtype);
+        if (j * 32 + lane >= count) continue;
+        load_raw(l.g[j], g + j * 32);
+        load_raw(l.x[j], x + j * 32);
         if constexpr (BITS == 32) {
-            l.m[j] = static_cast<const float*>(st.m)[s0 + e];
-            l.v[j] = static_cast<const float*>(st.v)[s0 + e];
+            l.m[j] = static_cast<const float*>(st.m)[s0 + j * 32 + lane];
+            l.v[j] = static_cast<const float*>(st.v)[s0 + j * 32 + lane];
         } else {
-            l.m[j] = byte_bits(static_cast<const uint8_t*>(st.m)[s0 + e] ^ 0x80u, 0);
-            l.v[j] = byte_bits(static_cast<const uint8_t*>(st.v)[s0 + e], 0);
+            l.m[j] = byte_bits(static_cast<const uint8_t*>(st.m)[s0 + j * 32 + lane] ^ 0x80u, 0);
+            l.v[j] = byte_bits(static_cast<const uint8_t*>(st.v)[s0 + j * 32 + lane], 0);
         }
     }
     if constexpr (BITS == 8) {
@@ -306,8 +308,8 @@ __device__ __forceinline__ void load_block_any(LoadedAny<BITS>& l, const Tensor&
         l.sv = st.v_scale[s0 / kBlock];
     }
 }
-template <int BITS>
-__device__ __forceinline__ void finish_block_any(LoadedAny<BITS>& l, const Tensor& t, const State& st, const StepScalars& sc,
+template <int BITS, typename XT, typename GT>
+__device__ __forceinline__ void finish_block_any(LoadedAny<BITS, XT, GT>& l, const Tensor& t, const State& st, const StepScalars& sc,
                                                  const Factors& f, int64_t base, int count)
 {
     const int lane = threadIdx.x & 31;
@@ -315,8 +317,8 @@ __device__ __forceinline__ void finish_block_any(LoadedAny<BITS>& l, const Tenso
     float g[8], x[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        g[j] = bits_to_float(l.g[j], t.g_dtype);
-        x[j] = bits_to_float(l.x[j], t.x_dtype);
+        g[j] = raw_get(l.g[j], 0);
+        x[j] = raw_get(l.x[j], 0);
     }
     if constexpr (BITS == 32) {
         update8(sc, f, g, x, l.m, l.v);
@@ -331,7 +333,7 @@ __device__ __forceinline__ void finish_block_any(LoadedAny<BITS>& l, const Tenso
     for (int j = 0; j < 8; ++j) {
         const int e = j * 32 + lane;
         if (e >= count) continue;
-        store_from_float(t.x, base + e, t.x_dtype, x[j]);
+        static_cast<XT*>(t.x)[base + e] = from_float<XT>(x[j]);
         if (t.copy) store_from_float(t.copy, base + e, t.copy_dtype, x[j]);
         if constexpr (BITS == 32) {
             static_cast<float*>(st.m)[s0 + e] = l.m[j];
@@ -359,8 +361,8 @@ __device__ __forceinline__ bool factors_of(Factors& f, const Tensor& t, float c,
     return isfinite(c);
 }
 
-// A step is a launch of `step_rest_kernel` for the blocks that need single accesses and one of
-// `step_kernel` for each pair of types whose tensors have whole aligned blocks; most lists need one
+// A step is, for each pair of types in the list, a launch of `step_rest_kernel` for the blocks that
+// need single accesses and one of `step_kernel` for whole blocks of aligned tensors; most lists need one
 // or two.  (In one kernel the first would set the registers of the others; a stack frame of 160
 // bytes alone cost 40 % of their speed.)  They touch different elements and run side by side: each
 // lets the next start as soon as all that came before the step has ended, and waits for the
@@ -368,23 +370,25 @@ __device__ __forceinline__ bool factors_of(Factors& f, const Tensor& t, float c,
 // Nobody but the thread that finds `first` looks at the count of a group that sits a step out.
 
 // one block of threads per chunk, one warp per block of elements
-template <int BITS>
-__global__ void __launch_bounds__(kStepThreads)
+template <int BITS, typename XT, typename GT>
+__global__ void __launch_bounds__(kStepThreads, kStepBlocksRest)
 step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
-                 int64_t* skipped, State st, StepScalars sc)
+                 int64_t* skipped, State st, StepScalars sc, int32_t beside)
 {
     const Chunk ch = chunks[blockIdx.x];
     const Tensor t = tensors[ch.tensor];
-    wait_for_previous_kernel();
+    if (!beside) wait_for_previous_kernel();
     allow_next_kernel();
     const int64_t base = ch.begin + (int64_t)(threadIdx.x >> 5) * kBlock;
-    if (base >= t.numel) return;
-    const int count = (int)min((int64_t)kBlock, t.numel - base);
-    LoadedAny<BITS> l;
-    load_block_any<BITS>(l, t, st, base, count);
-    Factors f;
-    if (factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc)) finish_block_any<BITS>(l, t, st, sc, f, base, count);
-    else if (ch.first && threadIdx.x == 0) skipped[t.group] += 1;
+    if (base < t.numel) {
+        const int count = (int)min((int64_t)kBlock, t.numel - base);
+        LoadedAny<BITS, XT, GT> l;
+        load_block_any(l, t, st, base, count);
+        Factors f;
+        if (factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc)) finish_block_any(l, t, st, sc, f, base, count);
+        else if (ch.first && threadIdx.x == 0) skipped[t.group] += 1;
+    }
+    if (beside) wait_for_previous_kernel();
 }
 
 // One block of threads per chunk, one warp per block of elements.  The chunks are taken from the
@@ -416,17 +420,19 @@ step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks
 }
 
 using StepKernel = void (*)(const Tensor*, const Chunk*, const float*, int64_t*, State, StepScalars, int32_t);
+template <int BITS, typename XT, typename GT>
+StepKernel step_kernel_of(bool rest) { return rest ? step_rest_kernel<BITS, XT, GT> : step_kernel<BITS, XT, GT>; }
 template <int BITS, typename XT>
-StepKernel step_kernel_of(int32_t g_dtype)
+StepKernel step_kernel_of(int32_t g, bool rest)
 {
-    return g_dtype == CHOCO_F32 ? step_kernel<BITS, XT, float> : g_dtype == CHOCO_BF16 ? step_kernel<BITS, XT, __nv_bfloat16>
-                                                                                       : step_kernel<BITS, XT, __half>;
+    return g == CHOCO_F32 ? step_kernel_of<BITS, XT, float>(rest) : g == CHOCO_BF16 ? step_kernel_of<BITS, XT, __nv_bfloat16>(rest)
+                                                                                    : step_kernel_of<BITS, XT, __half>(rest);
 }
 template <int BITS>
-StepKernel step_kernel_of(int32_t x_dtype, int32_t g_dtype)
+StepKernel step_kernel_of(int32_t x, int32_t g, bool rest)
 {
-    return x_dtype == CHOCO_F32 ? step_kernel_of<BITS, float>(g_dtype) : x_dtype == CHOCO_BF16 ? step_kernel_of<BITS, __nv_bfloat16>(g_dtype)
-                                                                                              : step_kernel_of<BITS, __half>(g_dtype);
+    return x == CHOCO_F32 ? step_kernel_of<BITS, float>(g, rest) : x == CHOCO_BF16 ? step_kernel_of<BITS, __nv_bfloat16>(g, rest)
+                                                                                  : step_kernel_of<BITS, __half>(g, rest);
 }
 
 // 8 elements per thread; the moments are whole blocks.
@@ -548,20 +554,22 @@ __global__ void __launch_bounds__(kNormThreads) norm_finish_kernel(const double*
 
 } // namespace
 
+constexpr int kPairs = 9;               // of types: 3 x_dtype + g_dtype
+
 struct choco_adamw {
     choco_adamw_params params;
     int device;
     bool norm_only;                // no parameters: the list serves choco_adamw_grad_norm alone
+    bool broken;                   // the tables on the device may be half written (a copy of new ones failed)
     std::vector<Tensor> tensors;   // as on the device
     std::vector<int64_t> offsets;
     int64_t elements;              // of m and v
     std::vector<int32_t> by_group;  // tensors with elements, group after group
-    int64_t most_chunks, nrest, nunits, unit_elems;
-    int64_t pair_begin[10];        // chunks of every pair of types (3 x_dtype + g_dtype), in d_chunks
+    int64_t most_chunks, nunits, unit_elems;
+    int64_t begin[2 * kPairs + 1]; // in d_chunks, for every pair of types: other blocks, whole blocks of aligned tensors
     int64_t t;                     // step calls so far; a group has taken t - skipped[group] steps
     Tensor* d_tensors;
-    Chunk* d_chunks;               // whole blocks of aligned tensors
-    Chunk* d_rest;                 // every other block
+    Chunk* d_chunks;
     Chunk* d_units;
     int64_t* d_unit_begin;         // [groups + 1]
     int64_t* d_skipped;            // [groups]
@@ -597,7 +605,6 @@ void free_all(choco_adamw* o)
 {
     cudaFree(o->d_tensors);
     cudaFree(o->d_chunks);
-    cudaFree(o->d_rest);
     cudaFree(o->d_units);
     cudaFree(o->d_unit_begin);
     cudaFree(o->d_skipped);
@@ -648,7 +655,7 @@ int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Ch
         unit_begin.push_back((int64_t)units.size());
         for (int32_t i : members[k]) {
             o->by_group.push_back(i);
-            o->most_chunks += o->tensors[i].numel / kChunkElems + 1;
+            o->most_chunks += o->tensors[i].numel / kChunkElems + 2;
             for (int64_t b = 0; b < o->tensors[i].numel; b += o->unit_elems) units.push_back({i, 0, b});
         }
     }
@@ -657,31 +664,26 @@ int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Ch
     return o->most_chunks > 0x7fffffff || o->nunits > 0x7fffffff ? CHOCO_ERR_TOO_LARGE : CHOCO_OK;
 }
 
-// Cuts the tensors into chunks of whole blocks that can be moved in 128-bit accesses, and the rest.
-// Neither list is longer than most_chunks.  Throws std::bad_alloc.
-void cut(choco_adamw* o, std::vector<Chunk>& chunks, std::vector<Chunk>& rest)
+// Cuts the tensors into chunks, never more than most_chunks; begin: where each range starts.  Throws
+// std::bad_alloc.
+std::vector<Chunk> cut(const choco_adamw* o, const std::vector<Tensor>& tensors, int64_t* begin)
 {
+    std::vector<Chunk> chunks;
     std::vector<char> seen((size_t)o->params.groups, 0);
-    auto first = [&](int32_t group) {
-        const int32_t f = !seen[group];
-        seen[group] = 1;
-        return f;
-    };
-    auto whole = [&](const Tensor& t) { return t.aligned ? t.numel / kBlock * kBlock : 0; };
-    for (int32_t i : o->by_group) {
-        const Tensor& t = o->tensors[i];
-        for (int64_t b = whole(t); b < t.numel; b += kChunkElems) rest.push_back({i, first(t.group), b});
-    }
-    o->nrest = (int64_t)rest.size();
-    for (int32_t pair = 0; pair < 9; ++pair) {
-        o->pair_begin[pair] = (int64_t)chunks.size();
+    for (int32_t k = 0; k < 2 * kPairs; ++k) {
+        begin[k] = (int64_t)chunks.size();
         for (int32_t i : o->by_group) {
-            const Tensor& t = o->tensors[i];
-            if (t.x_dtype * 3 + t.g_dtype != pair) continue;
-            for (int64_t b = 0; b < whole(t); b += kChunkElems) chunks.push_back({i, first(t.group), b});
+            const Tensor& t = tensors[i];
+            if (t.x_dtype * 3 + t.g_dtype != k / 2) continue;
+            const int64_t whole = t.aligned ? t.numel / kBlock * kBlock : 0;
+            for (int64_t b = k % 2 ? 0 : whole; b < (k % 2 ? whole : t.numel); b += kChunkElems) {
+                chunks.push_back({i, !seen[t.group], b});
+                seen[t.group] = 1;
+            }
         }
     }
-    o->pair_begin[9] = (int64_t)chunks.size();
+    begin[2 * kPairs] = (int64_t)chunks.size();
+    return chunks;
 }
 
 } // namespace
@@ -701,15 +703,14 @@ int choco_adamw_init(choco_adamw** out, int32_t n_tensors, const choco_adamw_ten
     o->params = *p;
     int rc = CHOCO_OK;
     try {
-        std::vector<Chunk> chunks, rest, units;
+        std::vector<Chunk> chunks, units;
         std::vector<int64_t> unit_begin;
         rc = plan(o, n_tensors, tensors, units, unit_begin);
-        if (rc == CHOCO_OK) cut(o, chunks, rest);
+        if (rc == CHOCO_OK) chunks = cut(o, o->tensors, o->begin);
         if (rc == CHOCO_OK && cudaGetDevice(&o->device) != cudaSuccess) rc = CHOCO_ERR_CUDA;
         if (rc == CHOCO_OK &&
             !(upload(&o->d_tensors, o->tensors.data(), o->tensors.size()) && upload(&o->d_chunks, chunks.data(), chunks.size(), o->most_chunks) &&
-              upload(&o->d_rest, rest.data(), rest.size(), o->most_chunks) && upload(&o->d_units, units.data(), units.size()) &&
-              upload(&o->d_unit_begin, unit_begin.data(), unit_begin.size()) &&
+              upload(&o->d_units, units.data(), units.size()) && upload(&o->d_unit_begin, unit_begin.data(), unit_begin.size()) &&
               upload(&o->d_skipped, (const int64_t*)nullptr, (size_t)p->groups) &&
               upload(&o->d_partial, (const double*)nullptr, units.size())))
             rc = CHOCO_ERR_ALLOC;
@@ -752,21 +753,24 @@ int choco_adamw_set_grads(choco_adamw* opt, const void* const* g, void* stream)
         return from.empty() || cudaMemcpyAsync(to, from.data(), sizeof(from[0]) * from.size(), cudaMemcpyHostToDevice, st) == cudaSuccess;
     };
     try {
-        std::vector<Chunk> chunks, rest;
-        chunks.reserve((size_t)opt->most_chunks);
-        rest.reserve((size_t)opt->most_chunks); // nothing below allocates
-        if (cudaStreamSynchronize(st) != cudaSuccess) return CHOCO_ERR_CUDA;
+        std::vector<Tensor> tensors = opt->tensors;
+        std::vector<Chunk> chunks;
+        int64_t begin[2 * kPairs + 1];
         bool moved = false; // a tensor's accesses change width with its gradient's alignment
-        for (size_t i = 0; i < opt->tensors.size(); ++i) {
-            Tensor& t = opt->tensors[i];
-            t.g = g[i];
-            moved |= (bool)t.aligned != all_aligned(t);
-            t.aligned = all_aligned(t);
+        for (size_t i = 0; i < tensors.size(); ++i) {
+            tensors[i].g = g[i];
+            tensors[i].aligned = all_aligned(tensors[i]);
+            moved |= tensors[i].aligned != opt->tensors[i].aligned;
         }
-        if (moved) cut(opt, chunks, rest);
-        if (!send(opt->d_tensors, opt->tensors) || !send(opt->d_chunks, chunks) || !send(opt->d_rest, rest) ||
-            cudaStreamSynchronize(st) != cudaSuccess)
+        if (moved) chunks = cut(opt, tensors, begin);
+        if (cudaStreamSynchronize(st) != cudaSuccess) return CHOCO_ERR_CUDA;
+        // the tables on the device have to agree with each other and with the host's: if one copy fails, no call may use them
+        opt->broken = true;
+        if (!send(opt->d_tensors, tensors) || !send(opt->d_chunks, chunks) || cudaStreamSynchronize(st) != cudaSuccess)
             return CHOCO_ERR_CUDA;
+        opt->tensors.swap(tensors);
+        if (moved) std::memcpy(opt->begin, begin, sizeof(begin));
+        opt->broken = false;
     } catch (const std::exception&) {
         return CHOCO_ERR_ALLOC;
     }
@@ -779,6 +783,7 @@ int choco_adamw_grad_norm(choco_adamw* opt, float max_norm, float unscale, float
         !std::isfinite(unscale) || !on_device(opt))
         return CHOCO_ERR_INVALID_ARG;
     if (!aligned_to(norm, 4) || !aligned_to(factor, 4)) return CHOCO_ERR_MISALIGNED;
+    if (opt->broken) return CHOCO_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)stream;
     const dim3 threads(kNormThreads);
     cudaError_t err = cudaSuccess;
@@ -799,6 +804,7 @@ int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* 
     if (opt->elements > 0 && (!m || !v || (eight && (!m_scale || !v_scale)))) return CHOCO_ERR_INVALID_ARG;
     if (!aligned_to(m, 16) || !aligned_to(v, 16) || !aligned_to(m_scale, 4) || !aligned_to(v_scale, 4) || !aligned_to(factor, 4))
         return CHOCO_ERR_MISALIGNED;
+    if (opt->broken) return CHOCO_ERR_CUDA;
     const choco_adamw_params& p = opt->params;
     StepScalars sc;
     sc.t = opt->t + 1;
@@ -814,15 +820,13 @@ int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* 
     cudaStream_t st = (cudaStream_t)stream;
     const State state = {m, v, m_scale, v_scale};
     cudaError_t err = cudaSuccess;
-    if (opt->nrest > 0)
-        err = launch_overlapped(eight ? step_rest_kernel<8> : step_rest_kernel<32>, dim3((unsigned)opt->nrest), dim3(kStepThreads), 0, st,
-                                HotRange{}, opt->d_tensors, opt->d_rest, factor, opt->d_skipped, state, sc);
-    int32_t beside = opt->nrest > 0;
-    for (int32_t pair = 0; pair < 9 && err == cudaSuccess; ++pair) {
-        const int32_t count = (int32_t)(opt->pair_begin[pair + 1] - opt->pair_begin[pair]);
+    int32_t beside = 0;
+    for (int32_t k = 0; k < 2 * kPairs && err == cudaSuccess; ++k) {
+        const int64_t count = opt->begin[k + 1] - opt->begin[k];
         if (count == 0) continue;
-        err = launch_overlapped(eight ? step_kernel_of<8>(pair / 3, pair % 3) : step_kernel_of<32>(pair / 3, pair % 3), dim3((unsigned)count),
-                                dim3(kStepThreads), 0, st, HotRange{}, opt->d_tensors, opt->d_chunks + opt->pair_begin[pair], factor,
+        const int32_t x = k / 2 / 3, g = k / 2 % 3;
+        err = launch_overlapped(eight ? step_kernel_of<8>(x, g, k % 2 == 0) : step_kernel_of<32>(x, g, k % 2 == 0), dim3((unsigned)count),
+                                dim3(kStepThreads), 0, st, HotRange{}, opt->d_tensors, opt->d_chunks + opt->begin[k], factor,
                                 opt->d_skipped, state, sc, beside);
         beside = 1;
     }

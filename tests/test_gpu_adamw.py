@@ -355,6 +355,26 @@ def test_separate_tensors_groups_in_any_order_and_new_gradients():
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_new_gradients_at_other_alignments(bits):
+    """A gradient that moves to an address off a 16-byte boundary, and back: other accesses, same results."""
+    r = Run(1, [5000], bits, step=1)
+    r.randomise()
+    store = torch.randn(5008, device=DEV)
+    for shift in (0, 1, 2, 4, 3, 0):
+        g = store[shift:shift + 5000]
+        choco.choco_adamw_set_grads(r.opt.handle, [g.data_ptr()])
+        r.G[0, :5000] = g                                        # what ref() looks at
+        t = int(r.opt.get_steps()[0]) + 1
+        want = r.ref(1e-3, t)
+        r.opt.step(1e-3)
+        r.check(None, want)
+    norm, factor = torch.zeros(1, device=DEV), torch.zeros(1, device=DEV)
+    r.opt.grad_norm(1.0, norm, factor)
+    assert abs(float(norm) / float(store[:5000].double().norm()) - 1) <= 2 * U
+    r.opt.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_read_state(bits, dtype):
     r = Run(2, [300, 4096, 7], bits, step=3)
