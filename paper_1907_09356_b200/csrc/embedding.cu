@@ -27,7 +27,8 @@ constexpr int kTileMid = 16;                // ... and fewer: more warps, shorte
 constexpr int kTileShort = 8;
 constexpr int64_t kMidRows = 65536, kShortRows = 16384;
 constexpr uint32_t kNoKey = 0xffffffffu;
-constexpr int kChainOfWarp = 4;             // chains of partial sums up to this length are added by one warp
+constexpr int kShortChain = 8;              // tiles behind the first that a run's partial sums are in, for one warp to add
+constexpr int64_t kJoinBlocks = 148 * 5;
 
 struct EmbShape {
     int64_t vocab, dim, table_row, table_ld, padding;
@@ -178,6 +179,7 @@ struct Order {
     int32_t cluster_log, part_log;          // blocks of a cluster, keys of a block
     int32_t digit_bits, passes;
     uint32_t *keys, *pos;                   // out: [n, count]
+    uint32_t* chain_count;                  // set to 0 (see Sums)
 };
 
 struct OrderSmem {
@@ -215,6 +217,7 @@ __global__ void __launch_bounds__(kOrderThreads, 1) order_kernel(EmbShape s, Ord
     const int32_t worker = blockIdx.x >> o.cluster_log;
     wait_for_previous_kernel();
     allow_next_kernel();
+    if (blockIdx.x == 0 && threadIdx.x < 2) o.chain_count[threadIdx.x] = 0;
     const uint32_t rank = blockIdx.x & ((1u << o.cluster_log) - 1u), blocks = 1u << o.cluster_log;
     const uint32_t part = 1u << o.part_log;
     const uint32_t first = rank << o.part_log;
@@ -361,6 +364,7 @@ struct SortPass {
     uint32_t *key_out, *pos_out;
     uint32_t* hist;              // [n, kDigits, tiles]
     uint32_t* total;             // [n, kDigits]
+    uint32_t* chain_count;       // set to 0 (see Sums)
 };
 
 __device__ __forceinline__ uint32_t pass_key(const EmbShape& s, const SortPass& p, int32_t worker, int64_t j)
@@ -374,6 +378,7 @@ __global__ void __launch_bounds__(kEmbThreads) sort_count_kernel(EmbShape s, Sor
     wait_for_previous_kernel();
     allow_next_kernel();
     const int32_t worker = blockIdx.x / p.tiles, tile = blockIdx.x - worker * p.tiles;
+    if (blockIdx.x == 0 && threadIdx.x < 2) p.chain_count[threadIdx.x] = 0;
     h[threadIdx.x] = 0;
     __syncthreads();
     uint32_t key[kSortRounds];
@@ -504,6 +509,9 @@ struct Sums {
     void* grad;
     int32_t grad_dtype, accumulate;
     float* part;                 // [n * tiles, 2, pitch]: a run that comes from the tile before; one that starts here and goes on
+    uint32_t* chains;            // [n * tiles] tiles with a run of the second kind, in no order: those of few tiles from the
+    uint32_t chain_room;         // front, long ones from the back
+    uint32_t* chain_count;       // [2] their numbers
     int64_t pitch;
     int32_t tile;                // entries per tile
     int32_t tiles;               // per worker
@@ -550,14 +558,22 @@ __device__ __forceinline__ void store_grad(const EmbShape& s, void* grad, int32_
     else put(static_cast<__half*>(grad));
 }
 
-// One warp per tile and group of 32 V C columns; B entries' loads are in flight together.
+// One warp per tile and group of 32 V C columns; B entries' loads are in flight together.  A run that
+// starts in the tile and reaches at most half a tile into the next one is added up here (and left out
+// there); what reaches further leaves a partial sum for every tile it is in.  What bounds it is the
+// memory (131072 rows of 1024 bf16 into 27000 rows of floats: 350 MB in 55 us); the registers are kept
+// below 85 so that 24 warps share an SM.
+constexpr int kSumThreads = 128, kSumBlocks = 6;
+
 template <typename TD, int V, int C, int B>
-__global__ void __launch_bounds__(kEmbThreads) sum_tiles_kernel(EmbShape s, Sums a)
+__global__ void __launch_bounds__(kSumThreads, kSumBlocks) sum_tiles_kernel(EmbShape s, Sums a)
 {
     wait_for_previous_kernel();
     allow_next_kernel();
-    const int lane = threadIdx.x & 31;
-    const uint64_t item = (uint64_t)blockIdx.x * kEmbWarps + (threadIdx.x >> 5);
+    // the tile's entries, what is taken from the next one, and room for a batch to look past the end
+    __shared__ uint32_t entry_key[kSumThreads / 32][kTileLong * 3 / 2 + B], entry_pos[kSumThreads / 32][kTileLong * 3 / 2 + B];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const uint64_t item = (uint64_t)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);
     const uint32_t gt = (uint32_t)(item / a.slabs), slab = (uint32_t)(item - (uint64_t)gt * a.slabs);
     if (gt >= (uint32_t)a.tiles * (uint32_t)s.n) return;
     const int32_t worker = gt / (uint32_t)a.tiles, tile = gt - worker * a.tiles;
@@ -566,11 +582,52 @@ __global__ void __launch_bounds__(kEmbThreads) sum_tiles_kernel(EmbShape s, Sums
     const uint32_t key = lane < cnt ? a.keys[e0 + lane] : kNoKey;
     const uint32_t pos = lane < cnt ? a.pos[e0 + lane] : 0u;
     const uint32_t prev = tile > 0 ? a.keys[e0 - 1] : kNoKey;
-    const uint32_t next = first + cnt < s.count ? a.keys[e0 + cnt] : kNoKey;
+    // what follows the tile, for its last run
+    const bool there = first + cnt + lane < s.count;
+    const uint32_t more_key = there ? a.keys[e0 + cnt + lane] : kNoKey, more_pos = there ? a.pos[e0 + cnt + lane] : 0u;
+    const int64_t far_on = first + (kShortChain + 1) * a.tile;
+    const uint32_t far_key = far_on < s.count ? a.keys[worker * s.count + far_on] : kNoKey;
     const int live = __popc(__ballot_sync(0xffffffffu, key < (uint32_t)s.vocab));
     if (live == 0) return;
-    uint32_t cur = __shfl_sync(0xffffffffu, key, 0);
-    bool head = cur == prev;
+    // Does the run that ends the tile before start there, and reach at most half a tile into this
+    // one?  Then that tile's warp has added it up.
+    const int reach = a.tile / 2;
+    int from = 0;
+    bool head = __shfl_sync(0xffffffffu, key, 0) == prev;
+    if (head) {
+        const uint32_t before = a.keys[e0 - a.tile], far = tile > 1 ? a.keys[e0 - a.tile - 1] : kNoKey;
+        const int lead = __ffs(~__ballot_sync(0xffffffffu, lane < cnt && key == prev)) - 1; // (cnt < 32 or a later key differs, or -1)
+        if (lead >= 0 && lead <= reach && !(before == prev && far == prev)) {
+            if (lead >= live) return;
+            from = lead;
+            head = false;
+        }
+    }
+    uint32_t cur = __shfl_sync(0xffffffffu, key, from);
+    // And does the last run go on, and if it started here, not further than that?  Then what
+    // follows the tile of it is this warp's too.
+    const uint32_t last = __shfl_sync(0xffffffffu, key, live - 1);
+    bool goes_on = live == cnt && __shfl_sync(0xffffffffu, more_key, 0) == last;
+    int end = live;
+    if (goes_on && !(head && cur == last)) {
+        const int more = __ffs(~__ballot_sync(0xffffffffu, more_key == last)) - 1;
+        if (more >= 0 && more <= reach) {
+            end += more;
+            goes_on = false;
+        } else if (slab == 0 && lane == 0) {
+            if (far_key == last) a.chains[a.chain_room - 1 - atomicAdd(a.chain_count + 1, 1u)] = gt;
+            else a.chains[atomicAdd(a.chain_count, 1u)] = gt;
+        }
+    }
+    if (lane < cnt) {
+        entry_key[w][lane] = key;
+        entry_pos[w][lane] = pos;
+    }
+    if (lane < end - cnt) {
+        entry_key[w][cnt + lane] = more_key;
+        entry_pos[w][cnt + lane] = more_pos;
+    }
+    __syncwarp();
     const TD* d = static_cast<const TD*>(a.dout) + worker * a.dout_ld;
     const int64_t c0 = (int64_t)slab * (32 * V * C) + lane * V;
     float acc[C][V];
@@ -578,8 +635,8 @@ __global__ void __launch_bounds__(kEmbThreads) sum_tiles_kernel(EmbShape s, Sums
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[c][e] = 0.f;
-    auto flush = [&](bool goes_on) {
-        if (head || goes_on) {
+    auto flush = [&](bool unfinished) {
+        if (head || unfinished) {
             float* p = a.part + ((int64_t)gt * 2 + (head ? 0 : 1)) * a.pitch;
 #pragma unroll
             for (int c = 0; c < C; ++c)
@@ -591,12 +648,12 @@ __global__ void __launch_bounds__(kEmbThreads) sum_tiles_kernel(EmbShape s, Sums
                     store_grad<V>(s, a.grad, a.grad_dtype, a.accumulate, worker, cur, c0 + c * 32 * V, acc[c]);
         }
     };
-    for (int b = 0; b < live; b += B) {
+    for (int b = from; b < end; b += B) {
         Raw<TD, V> raw[B][C];
 #pragma unroll
         for (int j = 0; j < B; ++j) {
-            const uint32_t p = __shfl_sync(0xffffffffu, pos, (b + j) & 31);
-            if (b + j < live) {
+            const uint32_t p = entry_pos[w][b + j];
+            if (b + j < end) {
                 const TD* r = d + p * a.dout_row;
 #pragma unroll
                 for (int c = 0; c < C; ++c)
@@ -605,8 +662,8 @@ __global__ void __launch_bounds__(kEmbThreads) sum_tiles_kernel(EmbShape s, Sums
         }
 #pragma unroll
         for (int j = 0; j < B; ++j) {
-            const uint32_t k = __shfl_sync(0xffffffffu, key, (b + j) & 31);
-            if (b + j >= live) break;
+            if (b + j >= end) break;
+            const uint32_t k = entry_key[w][b + j];
             if (k != cur) {
                 flush(false);
                 head = false;
@@ -622,93 +679,85 @@ __global__ void __launch_bounds__(kEmbThreads) sum_tiles_kernel(EmbShape s, Sums
                 for (int e = 0; e < V; ++e) acc[c][e] += raw_get(raw[j][c], e);
         }
     }
-    flush(live == cnt && next == cur);
+    flush(goes_on);
 }
 
-// Runs that cross tiles: the tile in which one starts adds up the partial sums of all its tiles, in
-// order, kJoinCols columns to a warp.  Most chains are two or three tiles long and one warp's work;
-// those of more than kChainOfWarp tiles (frequent tokens) are shared by a block's warps, a
-// contiguous part each.  The parts a warp adds are on their way together: one after the other they
-// took 44 us instead of 24 us for 131072 rows of 1024.
+// Runs that reach further than half a tile into the next one: the partial sums of all their tiles,
+// in order, 128 columns at a time.  Chains of up to kShortChain tiles are a warp's work, all parts in
+// flight together; of longer ones (frequent tokens) a block takes one, a warp a contiguous part.
 constexpr int kJoinCols = 128;              // four a lane
-constexpr int kLongAtOnce = 8;              // parts that a warp of a long chain has in flight
 
 template <int V>
 __global__ void __launch_bounds__(kEmbThreads) join_kernel(EmbShape s, Sums a, uint32_t slabs)
 {
     __shared__ float4 sub[kEmbWarps][32];
-    __shared__ uint32_t long_tile[kEmbWarps], long_len[kEmbWarps], long_key[kEmbWarps];
     wait_for_previous_kernel();
     allow_next_kernel();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const uint32_t group = blockIdx.x / slabs, slab = blockIdx.x - group * slabs;
-    const uint32_t gt = group * kEmbWarps + w;
-    uint32_t key = kNoKey, len = 0;
-    if (gt < (uint32_t)a.tiles * (uint32_t)s.n) {
-        const int32_t worker = gt / (uint32_t)a.tiles, tile = gt - worker * a.tiles;
-        const uint32_t* k = a.keys + worker * s.count;
-        const int64_t first = (int64_t)tile * a.tile, after = first + a.tile;
-        if (after < s.count) {
-            const uint32_t last = k[after - 1], next = k[after], head = k[first], prev = tile > 0 ? k[first - 1] : kNoKey;
-            if (last == next && last < (uint32_t)s.vocab && !(head == last && prev == last)) {
-                key = last;
-                // further tiles that begin with it
-                for (uint32_t all = 0xffffffffu; all == 0xffffffffu; len += __popc(all)) {
-                    const int64_t j = after + (int64_t)(len + lane) * a.tile;
-                    all = __ballot_sync(0xffffffffu, j < s.count && k[j < s.count ? j : 0] == key);
-                }
-            }
-        }
-    }
-    if (lane == 0) {
-        long_len[w] = len > kChainOfWarp ? len : 0;
-        long_tile[w] = gt;
-        long_key[w] = key;
-    }
+    const uint32_t few = a.chain_count[0], many = a.chain_count[1];
+    auto add = [](float4& x, const float4 y) { x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w; };
     auto part_of = [&](uint32_t t, int slot, int64_t c) {
         return *reinterpret_cast<const float4*>(a.part + ((int64_t)t * 2 + slot) * a.pitch + c);
     };
-    auto add = [](float4& x, const float4 y) { x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w; };
-    auto put = [&](uint32_t t, uint32_t k, int64_t c, const float4 sum) {
-        const float f[4] = {sum.x, sum.y, sum.z, sum.w};
-        const int32_t worker = t / (uint32_t)a.tiles;
+    // sum += slots 0 of the tiles t + [from, to)
+    auto add_parts = [&](float4& sum, uint32_t t, uint32_t from, uint32_t to, int64_t c) {
+        for (uint32_t j = from; j < to; j += kShortChain) {
+            float4 v[kShortChain];
 #pragma unroll
-        for (int e = 0; e < 4; e += V)
-            if (c + e < s.dim) store_grad<V>(s, a.grad, a.grad_dtype, a.accumulate, worker, k, c + e, f + e);
-    };
-    const int64_t c = (int64_t)slab * kJoinCols + lane * 4;
-    // sum += slots 0 of the tiles t + [from, to), N tiles at a time
-    auto add_parts = [&](auto at_once, float4& sum, uint32_t t, uint32_t from, uint32_t to) {
-        constexpr int N = decltype(at_once)::value;
-        for (uint32_t j = from; j < to; j += N) {
-            float4 v[N];
+            for (int u = 0; u < kShortChain; ++u) v[u] = j + u < to ? part_of(t + j + u, 0, c) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int u = 0; u < N; ++u) v[u] = j + u < to && c < s.dim ? part_of(t + j + u, 0, c) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int u = 0; u < N; ++u) add(sum, v[u]);
+            for (int u = 0; u < kShortChain; ++u) add(sum, v[u]);
         }
     };
-    if (len > 0 && len <= kChainOfWarp && c < s.dim) {
-        float4 sum = part_of(gt, 1, c);
-        add_parts(std::integral_constant<int, kChainOfWarp>(), sum, gt + 1, 0, len);
-        put(gt, key, c, sum);
-    }
-    __syncthreads();
-    for (int k = 0; k < kEmbWarps; ++k) {
-        const uint32_t n = long_len[k]; // the same for all threads
-        if (n == 0) continue;
-        const uint32_t t = long_tile[k], each = (n + kEmbWarps - 1) / kEmbWarps;
+    auto put = [&](int32_t worker, uint32_t key, int64_t c, const float4 sum) {
+        const float f[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+        for (int e = 0; e < 4; e += V)
+            if (c + e < s.dim) store_grad<V>(s, a.grad, a.grad_dtype, a.accumulate, worker, key, c + e, f + e);
+    };
+    for (uint64_t task = blockIdx.x; task < (uint64_t)many * slabs; task += gridDim.x) {
+        const uint32_t at = (uint32_t)(task / slabs), gt = a.chains[a.chain_room - 1 - at];
+        const int64_t c = (int64_t)(task - (uint64_t)at * slabs) * kJoinCols + lane * 4;
+        const int32_t worker = gt / (uint32_t)a.tiles, tile = gt - worker * a.tiles;
+        const uint32_t* k = a.keys + worker * s.count;
+        const uint32_t key = k[(int64_t)(tile + 1) * a.tile - 1];
+        // The tiles that begin with this key follow one another: tile + 1 is one, the last is in
+        // [lo, hi); 32 places are looked at together.
+        int32_t lo = tile + 1, hi = a.tiles;
+        while (hi - lo > 1) {
+            const int32_t step = (hi - lo + 31) / 32;
+            const int64_t j = lo + (int64_t)(lane + 1) * step;
+            const int32_t n = __popc(__ballot_sync(0xffffffffu, j < hi && k[(j < hi ? j : lo) * a.tile] == key));
+            hi = min(hi, lo + (n + 1) * step);
+            lo += n * step;
+        }
+        const uint32_t len = lo - tile, each = (len + kEmbWarps - 1) / kEmbWarps;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        add_parts(std::integral_constant<int, kLongAtOnce>(), sum, t + 1, min(n, w * each), min(n, (w + 1) * each));
+        if (w == 0 && c < s.dim) sum = part_of(gt, 1, c);
+        if (c < s.dim) add_parts(sum, gt + 1, min(len, w * each), min(len, (w + 1) * each), c);
         sub[w][lane] = sum;
         __syncthreads();
         if (w == 0 && c < s.dim) {
-            sum = part_of(t, 1, c);
 #pragma unroll
-            for (int p = 0; p < kEmbWarps; ++p) add(sum, sub[p][lane]);
-            put(t, long_key[k], c, sum);
+            for (int p = 1; p < kEmbWarps; ++p) add(sum, sub[p][lane]);
+            put(worker, key, c, sum);
         }
         __syncthreads();
+    }
+    // (the blocks that had nothing above begin here)
+    const uint32_t warps = gridDim.x * kEmbWarps;
+    for (uint64_t task = (gridDim.x - 1 - blockIdx.x) * kEmbWarps + w; task < (uint64_t)few * slabs; task += warps) {
+        const uint32_t at = (uint32_t)(task / slabs), gt = a.chains[at];
+        const int64_t c = (int64_t)(task - (uint64_t)at * slabs) * kJoinCols + lane * 4;
+        const int32_t worker = gt / (uint32_t)a.tiles, tile = gt - worker * a.tiles;
+        const uint32_t* k = a.keys + worker * s.count;
+        const uint32_t key = k[(int64_t)(tile + 1) * a.tile - 1];
+        const int64_t j = (int64_t)(tile + 1 + lane) * a.tile; // the tiles behind that begin with it
+        const uint32_t len = __popc(__ballot_sync(0xffffffffu, lane < kShortChain && j < s.count && k[j < s.count ? j : 0] == key));
+        if (c >= s.dim) continue;
+        float4 sum = part_of(gt, 1, c);
+        add_parts(sum, gt + 1, 0, len, c);
+        put(worker, key, c, sum);
     }
 }
 
@@ -850,6 +899,8 @@ struct choco_embedding {
     uint32_t* total;
     float* part;
     int64_t pitch;
+    uint32_t* chains;            // two counts, then the tiles
+    uint32_t chain_room;
 };
 
 namespace {
@@ -866,6 +917,7 @@ void free_all(choco_embedding* e)
     cudaFree(e->hist);
     cudaFree(e->total);
     cudaFree(e->part);
+    cudaFree(e->chains);
     delete e;
 }
 
@@ -930,9 +982,9 @@ cudaError_t launch_sums(const EmbShape& s, Sums a, cudaStream_t st)
 {
     a.slabs = (uint32_t)((s.dim + 32 * V * C - 1) / (32 * V * C));
     const uint64_t warps = (uint64_t)a.slabs * a.tiles * s.n;
-    const uint64_t blocks = (warps + kEmbWarps - 1) / kEmbWarps;
+    const uint64_t blocks = (warps + kSumThreads / 32 - 1) / (kSumThreads / 32);
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    return launch_overlapped(sum_tiles_kernel<TD, V, C, B>, dim3((unsigned)blocks), dim3(kEmbThreads), 0, st, HotRange{}, s, a);
+    return launch_overlapped(sum_tiles_kernel<TD, V, C, B>, dim3((unsigned)blocks), dim3(kSumThreads), 0, st, HotRange{}, s, a);
 }
 
 template <typename TD>
@@ -1001,6 +1053,8 @@ int choco_embedding_init(choco_embedding** out, const choco_embedding_params* p)
         get(&e->hist, q.n * kDigits * sort_tiles);
         get(&e->total, (int64_t)q.n * kDigits);
         get(&e->part, tiles * 2 * e->pitch);
+        get(&e->chains, tiles + 2);
+        e->chain_room = (uint32_t)tiles;
     }
     if (q.max_tokens > 0 && err == cudaSuccess) {
         err = cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -1113,6 +1167,7 @@ int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t i
     if (plan_order(s, o)) {
         o.tokens = tokens; o.tokens_ld = tokens_ld; o.index_bits = index_bits;
         o.keys = emb->key[0]; o.pos = emb->pos[0];
+        o.chain_count = emb->chains;
         err = launch_order(s, o, st);
         zero(1);
     } else {
@@ -1121,6 +1176,7 @@ int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t i
         p.tiles = (int32_t)((count + kSortTile - 1) / kSortTile);
         p.hist = emb->hist;
         p.total = emb->total;
+        p.chain_count = emb->chains;
         p.first = 1;
         zero(0);
         for (p.shift = 0; p.shift == 0 || (s.vocab >> p.shift) != 0; p.shift += kDigitBits) {
@@ -1139,6 +1195,7 @@ int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t i
     a.dout = dout; a.dout_row = dout_row; a.dout_ld = dout_ld;
     a.grad = grad; a.grad_dtype = grad_dtype; a.accumulate = accumulate;
     a.part = emb->part; a.pitch = emb->pitch;
+    a.chains = emb->chains + 2; a.chain_room = emb->chain_room; a.chain_count = emb->chains;
     a.tile = tile_of(count * s.n);
     a.tiles = (int32_t)((count + a.tile - 1) / a.tile);
     if (err == cudaSuccess)
@@ -1148,11 +1205,10 @@ int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t i
         });
     if (err == cudaSuccess) {
         const uint32_t slabs = (uint32_t)((s.dim + kJoinCols - 1) / kJoinCols);
-        const int64_t blocks = ((int64_t)a.tiles * s.n + kEmbWarps - 1) / kEmbWarps * slabs;
-        if (blocks > 0x7fffffff) err = cudaErrorInvalidValue;
-        else
-            err = launch_overlapped(v >= 4 ? join_kernel<4> : v == 2 ? join_kernel<2> : join_kernel<1>, dim3((unsigned)blocks), threads, 0, st,
-                                    HotRange{}, s, a, slabs);
+        // a resident grid: how many chains there are is known on the device only
+        const int64_t blocks = std::min<int64_t>((int64_t)a.tiles * s.n * slabs, kJoinBlocks);
+        err = launch_overlapped(v >= 4 ? join_kernel<4> : v == 2 ? join_kernel<2> : join_kernel<1>, dim3((unsigned)blocks), threads, 0, st,
+                                HotRange{}, s, a, slabs);
     }
     return status_of(err);
 }
