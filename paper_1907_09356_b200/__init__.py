@@ -616,17 +616,18 @@ class Embedding:
         self.n, self.vocab, self.dim = n, vocab, dim
         self.handle = choco_embedding_init(n, vocab, dim, max_tokens, table_row, table_ld, scale, padding)
 
-    def _shape(self, tokens, rows):
-        a, b = tokens.shape, rows.shape
-        if len(a) != 2 or a[0] != self.n or len(b) != 3 or b[2] != self.dim:
-            raise ChocoError(f"libchoco: tokens must be [{self.n}, T], rows [{self.n}, T, {self.dim}]", -1)
+    def _wrong(self, tokens, rows):
+        raise ChocoError(f"libchoco: tokens must be [{self.n}, T], rows [{self.n}, T, {self.dim}], not {list(tokens.shape)} and "
+                         f"{list(rows.shape)}", -1)
 
     def forward(self, table, tokens, out, stream=None):
-        self._shape(tokens, out)
+        if tokens.dim() != 2 or out.dim() != 3 or tokens.shape[0] != self.n or out.shape[2] != self.dim:
+            self._wrong(tokens, out)
         choco_embedding_forward(self.handle, table, tokens, out, stream)
 
     def backward(self, tokens, dout, grad, accumulate: bool = False, stream=None):
-        self._shape(tokens, dout)
+        if tokens.dim() != 2 or dout.dim() != 3 or tokens.shape[0] != self.n or dout.shape[2] != self.dim:
+            self._wrong(tokens, dout)
         choco_embedding_backward(self.handle, tokens, dout, grad, accumulate, stream)
 
     def close(self):

@@ -427,20 +427,57 @@ step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks
     if (beside) wait_for_previous_kernel();
 }
 
-using StepKernel = void (*)(const Tensor*, const Chunk*, const float*, int64_t*, State, StepScalars, int32_t);
+// Both kinds of chunks in one launch, for lists so short that a second launch takes longer than
+// this kernel's registers cost.
 template <int BITS, typename XT, typename GT>
-StepKernel step_kernel_of(bool rest) { return rest ? step_rest_kernel<BITS, XT, GT> : step_kernel<BITS, XT, GT>; }
-template <int BITS, typename XT>
-StepKernel step_kernel_of(int32_t g, bool rest)
+__global__ void __launch_bounds__(kStepThreads, kStepBlocksRest)
+step_both_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
+                 int64_t* skipped, State st, StepScalars sc, int32_t beside)
 {
-    return g == CHOCO_F32 ? step_kernel_of<BITS, XT, float>(rest) : g == CHOCO_BF16 ? step_kernel_of<BITS, XT, __nv_bfloat16>(rest)
-                                                                                    : step_kernel_of<BITS, XT, __half>(rest);
+    const Chunk ch = chunks[blockIdx.x];
+    const Tensor t = tensors[ch.tensor];
+    if (!beside) wait_for_previous_kernel();
+    allow_next_kernel();
+    const int64_t base = ch.begin + (int64_t)(threadIdx.x >> 5) * kBlock;
+    const int64_t whole = t.aligned ? t.numel / kBlock * kBlock : 0; // where the tensor's other chunks begin
+    Factors f;
+    bool go = true;
+    if (ch.begin < whole) {
+        if (base < whole) {
+            Loaded<BITS, XT, GT> l;
+            load_block(l, t, st, base);
+            go = factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc);
+            if (go) finish_block(l, t, st, sc, f, base);
+        }
+    } else if (base < t.numel) {
+        const int count = (int)min((int64_t)kBlock, t.numel - base);
+        LoadedAny<BITS, XT, GT> l;
+        load_block_any(l, t, st, base, count);
+        go = factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc);
+        if (go) finish_block_any(l, t, st, sc, f, base, count);
+    }
+    if (!go && ch.first && threadIdx.x == 0) skipped[t.group] += 1;
+    if (beside) wait_for_previous_kernel();
+}
+
+using StepKernel = void (*)(const Tensor*, const Chunk*, const float*, int64_t*, State, StepScalars, int32_t);
+enum StepForm { kRest, kWhole, kBoth };
+template <int BITS, typename XT, typename GT>
+StepKernel step_kernel_of(StepForm form)
+{
+    return form == kRest ? step_rest_kernel<BITS, XT, GT> : form == kWhole ? step_kernel<BITS, XT, GT> : step_both_kernel<BITS, XT, GT>;
+}
+template <int BITS, typename XT>
+StepKernel step_kernel_of(int32_t g, StepForm form)
+{
+    return g == CHOCO_F32 ? step_kernel_of<BITS, XT, float>(form) : g == CHOCO_BF16 ? step_kernel_of<BITS, XT, __nv_bfloat16>(form)
+                                                                                    : step_kernel_of<BITS, XT, __half>(form);
 }
 template <int BITS>
-StepKernel step_kernel_of(int32_t x, int32_t g, bool rest)
+StepKernel step_kernel_of(int32_t x, int32_t g, StepForm form)
 {
-    return x == CHOCO_F32 ? step_kernel_of<BITS, float>(g, rest) : x == CHOCO_BF16 ? step_kernel_of<BITS, __nv_bfloat16>(g, rest)
-                                                                                  : step_kernel_of<BITS, __half>(g, rest);
+    return x == CHOCO_F32 ? step_kernel_of<BITS, float>(g, form) : x == CHOCO_BF16 ? step_kernel_of<BITS, __nv_bfloat16>(g, form)
+                                                                                  : step_kernel_of<BITS, __half>(g, form);
 }
 
 // 8 elements per thread; the moments are whole blocks.
@@ -574,6 +611,9 @@ norm_kernel(const Tensor* __restrict__ tensors, const Unit* __restrict__ units, 
 
 } // namespace
 
+// Lists up to this many chunks take one launch for both kinds: 8 x 65 tensors of a ResNet-20, 11.9 us against 12.9;
+// 16 M elements, 68.1 against 68.8.  With codes the registers cost more: 4.4 M elements, 14.8 us against 15.0; 25 M, 83 against 72.
+constexpr int64_t kBothChunks32 = 32768, kBothChunks8 = 4096;
 constexpr int kPairs = 9;               // of types: 3 x_dtype + g_dtype
 
 struct choco_adamw {
@@ -839,14 +879,22 @@ int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* 
     const State state = {m, v, m_scale, v_scale};
     cudaError_t err = cudaSuccess;
     int32_t beside = 0;
-    for (int32_t k = 0; k < 2 * kPairs && err == cudaSuccess; ++k) {
-        const int64_t count = opt->begin[k + 1] - opt->begin[k];
-        if (count == 0) continue;
-        const int32_t x = k / 2 / 3, g = k / 2 % 3;
-        err = launch_overlapped(eight ? step_kernel_of<8>(x, g, k % 2 == 0) : step_kernel_of<32>(x, g, k % 2 == 0), dim3((unsigned)count),
-                                dim3(kStepThreads), 0, st, HotRange{}, opt->d_tensors, opt->d_chunks + opt->begin[k], factor,
-                                opt->d_skipped, state, sc, beside);
+    auto launch = [&](int32_t pair, StepForm form, int64_t begin, int64_t end) {
+        if (begin == end || err != cudaSuccess) return;
+        const int32_t x = pair / 3, g = pair % 3;
+        err = launch_overlapped(eight ? step_kernel_of<8>(x, g, form) : step_kernel_of<32>(x, g, form), dim3((unsigned)(end - begin)),
+                                dim3(kStepThreads), 0, st, HotRange{}, opt->d_tensors, opt->d_chunks + begin, factor, opt->d_skipped,
+                                state, sc, beside);
         beside = 1;
+    };
+    for (int32_t pair = 0; pair < kPairs; ++pair) {
+        const int64_t *b = opt->begin + 2 * pair, rest = b[1] - b[0], whole = b[2] - b[1];
+        if (rest > 0 && whole > 0 && rest + whole <= (eight ? kBothChunks8 : kBothChunks32)) {
+            launch(pair, kBoth, b[0], b[2]);
+        } else {
+            launch(pair, kRest, b[0], b[1]);
+            launch(pair, kWhole, b[1], b[2]);
+        }
     }
     if (status_of(err) != CHOCO_OK) return CHOCO_ERR_CUDA;
     opt->t += 1;
