@@ -52,35 +52,56 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, int32_t bits, in
 // a row, or where rows are narrow 32 / lanes of them.  The row of the table is known only when the
 // token has arrived, so the bytes in flight have to come from many warps, and rows too narrow to
 // fill one are served together.
+// Where a lane's vectors of one row are small, it takes those of up to three rows together (rows of 650
+// bf16: 11.2 us alone, 9.4 us three; of 650 floats: 14.9 and 14.1 us; of 1024 bf16, 16 words of
+// a lane, nothing is gained, and with 32 words much is lost).
+template <typename TT, int V, int N>
+__host__ __device__ constexpr int lookup_rows()
+{
+    constexpr int words = N * ((V * (int)sizeof(TT) + 3) / 4);
+    return words <= 8 ? 3 : words <= 12 ? 2 : 1;
+}
+
 template <typename TT, typename TO, int V, int N, bool NARROW>
 __global__ void __launch_bounds__(kEmbThreads)
 lookup_kernel(EmbShape s, const TT* __restrict__ table, const void* __restrict__ tokens, int32_t index_bits, int64_t tokens_ld,
               TO* __restrict__ out, int64_t out_row, int64_t out_ld, uint32_t slabs, uint32_t narrow_log)
 {
+    constexpr int R = NARROW ? 1 : lookup_rows<TT, V, N>();
     const uint32_t lanes_log = NARROW ? narrow_log : 5; // lanes of a row
     const uint32_t lane = threadIdx.x & 31, lanes = 1u << lanes_log, mine = lane & (lanes - 1);
     const uint32_t item = ((blockIdx.x * kEmbWarps + (threadIdx.x >> 5)) << (5 - lanes_log)) + (lane >> lanes_log);
-    const uint32_t t = slabs == 1 ? item : item / slabs, slab = slabs == 1 ? 0 : item - t * slabs;
+    const uint32_t tr = slabs == 1 ? item : item / slabs, slab = slabs == 1 ? 0 : item - tr * slabs;
+    const uint32_t t = tr * R;
     wait_for_previous_kernel();
     allow_next_kernel();
     if (t >= (uint32_t)s.count) return;
     const int64_t i = blockIdx.y;
-    const int64_t tok = token_at(tokens, index_bits, i * tokens_ld + t, s.vocab);
+    int64_t tok[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) tok[r] = t + r < (uint32_t)s.count ? token_at(tokens, index_bits, i * tokens_ld + t + r, s.vocab) : -1;
     const int32_t step = (int32_t)lanes * V, c0 = (int32_t)slab * step * N + (int32_t)mine * V, dim = (int32_t)s.dim;
-    TO* o = out + i * out_ld + t * out_row;
-    const TT* w = table + i * s.table_ld + (tok < 0 ? 0 : tok) * s.table_row;
-    Raw<TT, V> raw[N];
+    Raw<TT, V> raw[R][N];
 #pragma unroll
-    for (int k = 0; k < N; ++k)
-        if (tok >= 0 && c0 + k * step < dim) load_raw(raw[k], w + c0 + k * step);
+    for (int r = 0; r < R; ++r) {
+        const TT* w = table + i * s.table_ld + (tok[r] < 0 ? 0 : tok[r]) * s.table_row;
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        const int32_t c = c0 + k * step;
-        if (c >= dim) continue;
-        float f[V];
+        for (int k = 0; k < N; ++k)
+            if (tok[r] >= 0 && c0 + k * step < dim) load_raw(raw[r][k], w + c0 + k * step);
+    }
 #pragma unroll
-        for (int e = 0; e < V; ++e) f[e] = tok >= 0 ? raw_get(raw[k], e) * s.scale : 0.f;
-        store_vec<TO, V>(o + c, f);
+    for (int r = 0; r < R; ++r) {
+        if (t + r >= (uint32_t)s.count) break;
+        TO* o = out + i * out_ld + (int64_t)(t + r) * out_row;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int32_t c = c0 + k * step;
+            if (c >= dim) continue;
+            float f[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = tok[r] >= 0 ? raw_get(raw[r][k], e) * s.scale : 0.f;
+            store_vec<TO, V>(o + c, f);
+        }
     }
 }
 
@@ -1102,7 +1123,8 @@ int choco_embedding_forward(choco_embedding* emb, const void* table, int32_t tab
                 while (lanes_log > 2 && ((int64_t)V * N << (lanes_log - 1)) >= s.dim) --lanes_log;
                 auto* kernel = lanes_log < 5 ? lookup_kernel<TT, TO, V, N, true> : lookup_kernel<TT, TO, V, N, false>;
                 const int64_t slabs = (s.dim + 32 * V * N - 1) / (32 * V * N), per_block = (int64_t)kEmbWarps << (5 - lanes_log);
-                const int64_t blocks = (count * slabs + per_block - 1) / per_block;
+                const int64_t rows_a_warp = lanes_log < 5 ? 1 : lookup_rows<TT, V, N>();
+                const int64_t blocks = ((count + rows_a_warp - 1) / rows_a_warp * slabs + per_block - 1) / per_block;
                 if (blocks > 0x1fffffff) return (int)CHOCO_ERR_TOO_LARGE; // (more than the output can have in memory)
                 return status_of(launch_overlapped(kernel, dim3((unsigned)blocks, (unsigned)s.n), dim3(kEmbThreads), 0,
                                                    st, HotRange{}, s, static_cast<const TT*>(table), tokens, index_bits, tokens_ld,
