@@ -166,20 +166,42 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-_current_stream = None
+_raw_stream = None
+
+
+def _find_raw_stream():
+    """Current stream's handle by device index."""
+    global _raw_stream
+    import torch
+    # the handle itself where torch gives it (0.1 us); its Stream object takes 3 us to make
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if _raw_stream is None:
+        _raw_stream = lambda device: torch.cuda.current_stream(device).cuda_stream  # noqa: E731
+    return _raw_stream
 
 
 def _stream(stream) -> Optional[int]:
-    if stream is not None:
-        return stream.cuda_stream or None
-    global _current_stream
-    if _current_stream is None:
+    if stream is None:
         import torch
-        # the handle itself where torch gives it (0.1 us); its Stream object takes 3 us to make
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        _current_stream = ((lambda: raw(torch.cuda.current_device())) if raw is not None and torch.cuda.is_available()
-                           else (lambda: torch.cuda.current_stream().cuda_stream))
-    return _current_stream() or None
+        stream = (_raw_stream or _find_raw_stream())(torch.cuda.current_device())
+        return stream or None
+    return stream.cuda_stream or None
+
+
+def _stream_of(stream, device: int) -> Optional[int]:
+    """The same for a call whose tensors are known to be on `device`."""
+    if stream is None:
+        return (_raw_stream or _find_raw_stream())(device) or None
+    return stream.cuda_stream or None
+
+
+def _on_one_device(what: str, *tensors) -> int:
+    """Index of the GPU that all of them are on."""
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() != device or device < 0:
+            raise ChocoError(f"libchoco: {what} must be on one GPU", -1)
+    return device
 
 
 # --------------------------------------------------------------------------- C names
@@ -434,19 +456,21 @@ def _index_bits(t) -> int:
     return code
 
 
-def _token_rows(tokens, rows, what: str) -> tuple:
+def _token_rows(tokens, rows, n, dim) -> tuple:
     """(tokens per worker, stride of the tokens' rows, strides of `rows` from token to token and from
-    worker to worker) for tokens [n, T] and rows [n, T, dim] with unit stride inside their rows."""
-    shape, (n, count) = rows.shape, tokens.shape
-    ld, inside = tokens.stride()
-    if count > 1 and inside != 1:
-        raise ChocoError("libchoco: tokens must be contiguous inside a worker's row", -1)
-    if len(shape) != 3 or shape[0] != n or shape[1] != count:
-        raise ChocoError(f"libchoco: {what} must be [{n}, {count}, dim], not {list(shape)}", -1)
-    worker, row, inside = rows.stride()
-    if shape[2] > 1 and count and inside != 1:
-        raise ChocoError(f"libchoco: {what} must have contiguous rows", -1)
-    return count, ld, (row if count > 1 else max(shape[2], row)), worker
+    worker to worker) for tokens [n, T] and rows [n, T, dim] with unit stride inside their rows;
+    n and dim None: whatever they are."""
+    a, b = tokens.shape, rows.shape
+    if len(a) == 2 and len(b) == 3 and a[0] == b[0] == (n or a[0]) and a[1] == b[1] and b[2] == (dim or b[2]):
+        count = a[1]
+        ld, one = tokens.stride()
+        worker, row, inside = rows.stride()
+        if count == 0:
+            return 0, ld, b[2], 0
+        if (one == 1 or count == 1) and (inside == 1 or b[2] == 1):
+            return count, ld, (row if count > 1 else max(b[2], row)), worker
+    raise ChocoError(f"libchoco: tokens must be [{n or 'n'}, T] and the rows [{n or 'n'}, T, {dim or 'dim'}], both contiguous inside "
+                     f"their rows, not {list(a)} and {list(b)}", -1)
 
 
 def choco_embedding_init(n: int, vocab: int, dim: int, max_tokens: int, table_row: int = 0, table_ld: int = 0,
@@ -462,20 +486,22 @@ def choco_embedding_destroy(emb) -> None:
     _check(load().choco_embedding_destroy(emb))
 
 
-def choco_embedding_forward(emb, table, tokens, out, stream=None) -> None:
+def choco_embedding_forward(emb, table, tokens, out, stream=None, n=None, dim=None) -> None:
     """out[i, t] = scale * table_i[tokens[i, t]].  `table` is a tensor that starts at worker 0's first
     row; tokens [n, T] int32 or int64; out [n, T, dim]."""
-    count, tokens_ld, row, ld = _token_rows(tokens, out, "out")
+    count, tokens_ld, row, ld = _token_rows(tokens, out, n, dim)
+    device = _on_one_device("table, tokens and out", out, tokens, table)
     _check(load().choco_embedding_forward(emb, table.data_ptr(), _dtype(table), tokens.data_ptr(), _index_bits(tokens), count,
-                                          tokens_ld, out.data_ptr(), _dtype(out), row, ld, _stream(stream)))
+                                          tokens_ld, out.data_ptr(), _dtype(out), row, ld, _stream_of(stream, device)))
 
 
-def choco_embedding_backward(emb, tokens, dout, grad, accumulate: bool = False, stream=None) -> None:
+def choco_embedding_backward(emb, tokens, dout, grad, accumulate: bool = False, stream=None, n=None, dim=None) -> None:
     """grad_i[r] (+)= scale * sum of dout[i, t] over the t with tokens[i, t] = r, in the table's layout."""
-    count, tokens_ld, row, ld = _token_rows(tokens, dout, "dout")
+    count, tokens_ld, row, ld = _token_rows(tokens, dout, n, dim)
+    device = _on_one_device("tokens, dout and grad", grad, tokens, dout)
     _check(load().choco_embedding_backward(emb, tokens.data_ptr(), _index_bits(tokens), count, tokens_ld, dout.data_ptr(),
                                            _dtype(dout), row, ld, grad.data_ptr(), _dtype(grad), 1 if accumulate else 0,
-                                           _stream(stream)))
+                                           _stream_of(stream, device)))
 
 
 def choco_adamw_init(tensors, groups: int = 1, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
@@ -510,10 +536,14 @@ def choco_adamw_set_grads(opt, pointers, stream=None) -> None:
 
 
 def choco_adamw_grad_norm(opt, max_norm: float, norm, factor, unscale: float = 1.0, stream=None) -> None:
-    _check(load().choco_adamw_grad_norm(opt, max_norm, unscale, _ptr(norm), _ptr(factor), _stream(stream)))
+    device = _on_one_device("norm and factor", norm, factor)
+    _check(load().choco_adamw_grad_norm(opt, max_norm, unscale, norm.data_ptr(), factor.data_ptr(), _stream_of(stream, device)))
 
 
 def choco_adamw_step(opt, m, v, m_scale, v_scale, lr: float, factor=None, stream=None) -> None:
+    for t in (m, v, m_scale, v_scale, factor):
+        if t is not None and not t.is_cuda:
+            raise ChocoError("libchoco: moments and factor must be on the GPU", -1)
     _check(load().choco_adamw_step(opt, _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), lr, _ptr(factor), _stream(stream)))
 
 
@@ -522,6 +552,9 @@ def choco_adamw_read_state(opt, m, v, m_scale, v_scale, m_out, v_out, stream=Non
     out = m_out if m_out is not None else v_out
     if m_out is not None and v_out is not None and m_out.dtype != v_out.dtype:
         raise ChocoError("libchoco: m_out and v_out have one type", -1)
+    for t in (m, v, m_scale, v_scale, m_out, v_out):
+        if t is not None and not t.is_cuda:
+            raise ChocoError("libchoco: moments and outputs must be on the GPU", -1)
     _check(load().choco_adamw_read_state(opt, _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), _ptr(m_out), _ptr(v_out),
                                          0 if out is None else _dtype(out), _stream(stream)))
 
@@ -557,8 +590,8 @@ def adamw_layer_tensors(X, G, layer_off, weight_decay=0.0, lr_scale=1.0, copy=No
     for name, a in (("x", X), ("g", G), ("copy", copy)):
         if a is None:
             continue
-        if a.dim() != 2 or a.shape[0] != n or a.shape[1] < off[-1] or (a.shape[1] > 1 and a.stride(1) != 1):
-            raise ChocoError(f"libchoco: {name} must be [{n}, >= {int(off[-1])}] with contiguous rows", -1)
+        if not a.is_cuda or a.dim() != 2 or a.shape[0] != n or a.shape[1] < off[-1] or (a.shape[1] > 1 and a.stride(1) != 1):
+            raise ChocoError(f"libchoco: {name} must be [{n}, >= {int(off[-1])}] on the GPU with contiguous rows", -1)
         t[name] = (a.data_ptr() + (rows * a.stride(0) + off[None, :-1]) * a.element_size()).astype(np.uint64)
         t[name + "_dtype"] = _dtype(a)
     t["numel"] = np.diff(off)[None]
@@ -616,19 +649,11 @@ class Embedding:
         self.n, self.vocab, self.dim = n, vocab, dim
         self.handle = choco_embedding_init(n, vocab, dim, max_tokens, table_row, table_ld, scale, padding)
 
-    def _wrong(self, tokens, rows):
-        raise ChocoError(f"libchoco: tokens must be [{self.n}, T], rows [{self.n}, T, {self.dim}], not {list(tokens.shape)} and "
-                         f"{list(rows.shape)}", -1)
-
     def forward(self, table, tokens, out, stream=None):
-        if tokens.dim() != 2 or out.dim() != 3 or tokens.shape[0] != self.n or out.shape[2] != self.dim:
-            self._wrong(tokens, out)
-        choco_embedding_forward(self.handle, table, tokens, out, stream)
+        choco_embedding_forward(self.handle, table, tokens, out, stream, self.n, self.dim)
 
     def backward(self, tokens, dout, grad, accumulate: bool = False, stream=None):
-        if tokens.dim() != 2 or dout.dim() != 3 or tokens.shape[0] != self.n or dout.shape[2] != self.dim:
-            self._wrong(tokens, dout)
-        choco_embedding_backward(self.handle, tokens, dout, grad, accumulate, stream)
+        choco_embedding_backward(self.handle, tokens, dout, grad, accumulate, stream, self.n, self.dim)
 
     def close(self):
         if getattr(self, "handle", None) is not None:

@@ -498,4 +498,8 @@ def test_refusals():
         choco.AdamW(r.X, r.G, [0, 100_000])
     with pytest.raises(choco.ChocoError):
         o.read_state(torch.empty(10, device=DEV), None)
+    for call in (lambda: choco.AdamW(r.X.cpu(), r.G, r.off), lambda: choco.AdamW(r.X, r.G.cpu(), r.off),
+                 lambda: o.step(1e-3, f.cpu()), lambda: o.grad_norm(1.0, f, f.cpu())):   # nothing of them reaches a kernel
+        with pytest.raises(choco.ChocoError):
+            call()
     o.close()

@@ -362,5 +362,10 @@ def test_refusals():
         emb.forward(X, tok.to(torch.int16), out)
     with pytest.raises(choco.ChocoError):
         emb.backward(tok, out[:, :3], X)
+    for bad in ((X.cpu(), tok, out), (X, tok.cpu(), out), (X, tok, out.cpu())):   # nothing of them reaches a kernel
+        with pytest.raises(choco.ChocoError):
+            emb.forward(*bad)
+        with pytest.raises(choco.ChocoError):
+            emb.backward(bad[1], bad[2], bad[0])
     torch.cuda.synchronize()
     emb.close()
