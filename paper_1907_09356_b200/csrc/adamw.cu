@@ -23,7 +23,7 @@ constexpr int kStepWarps = kStepThreads / 32;
 constexpr int kChunkElems = kStepWarps * kBlock;
 // blocks on an SM: 64 registers a thread with 32-bit moments, 48 with codes, where more warps pay (552 us against 579)
 constexpr int kStepBlocks32 = 8, kStepBlocks8 = 10, kStepBlocksRest = 6;
-constexpr int kNormThreads = 128;            // (8 x 65 small tensors: 6.1 us, 7.2 us with 256; long lists 260 us against 257)
+constexpr int kNormThreads = 128, kNormThreadsLong = 256; // 8 x 65 small tensors 6.1 us and 7.2 us, 16 x 28.95 M elements 262 us and 256 us
 constexpr int64_t kUnitLong = 16384, kUnitShort = 2048; // elements of a unit of the norms
 constexpr float kCodesM = 127.0f;           // codes k stand for s k^2, k up to 127 (m) and 255 (sqrt v)
 constexpr float kCodesV = 255.0f;
@@ -517,6 +517,7 @@ __global__ void __launch_bounds__(256) read_state_kernel(State st, void* m_out, 
 // takes one unit (a run of one tensor's gradient); the last block of a group to finish adds up the
 // group's units in their order and forms its norm and factor.  What bounds it is the memory
 // (16 x 28.95 M float32: 255 us, 7.3 TB/s).
+template <int THREADS>
 __device__ __forceinline__ double sum_of_block(double acc, double* red) // thread 0 has the sum
 {
 #pragma unroll
@@ -524,7 +525,7 @@ __device__ __forceinline__ double sum_of_block(double acc, double* red) // threa
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = acc;
     __syncthreads();
     if (threadIdx.x == 0)
-        for (int w = 1; w < kNormThreads / 32; ++w) acc += red[w];
+        for (int w = 1; w < THREADS / 32; ++w) acc += red[w];
     return acc;
 }
 
@@ -536,10 +537,11 @@ struct NormOut {
     float *norm, *factor;
 };
 
-__global__ void __launch_bounds__(kNormThreads)
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
 norm_kernel(const Tensor* __restrict__ tensors, const Unit* __restrict__ units, int64_t unit_elems, NormOut o)
 {
-    __shared__ double red[kNormThreads / 32];
+    __shared__ double red[THREADS / 32];
     __shared__ bool last;
     const Unit u = units[blockIdx.x];
     const Tensor t = tensors[u.tensor];
@@ -551,7 +553,7 @@ norm_kernel(const Tensor* __restrict__ tensors, const Unit* __restrict__ units, 
     int64_t done = u.begin;
     if (t.aligned) {
         constexpr int kAhead = 4;           // vectors of a thread in flight
-        constexpr int kSpanElems = kNormThreads * 8;
+        constexpr int kSpanElems = THREADS * 8;
         auto span = [&](auto vectors) {
             constexpr int N = decltype(vectors)::value;
             Raw8 r[N];
@@ -571,11 +573,11 @@ norm_kernel(const Tensor* __restrict__ tensors, const Unit* __restrict__ units, 
         if (done + kSpanElems <= end) span(std::integral_constant<int, 1>());
     }
     constexpr int kSingles = 8;             // single elements of a thread in flight
-    for (; done < end; done += kSingles * kNormThreads) {
+    for (; done < end; done += kSingles * THREADS) {
         uint32_t g[kSingles];
 #pragma unroll
         for (int k = 0; k < kSingles; ++k) {
-            const int64_t e = done + k * kNormThreads + threadIdx.x;
+            const int64_t e = done + k * THREADS + threadIdx.x;
             g[k] = e < end ? load_bits(t.g, e, t.g_dtype) : 0u;
         }
 #pragma unroll
@@ -584,7 +586,7 @@ norm_kernel(const Tensor* __restrict__ tensors, const Unit* __restrict__ units, 
             acc = __fma_rn(d, d, acc);
         }
     }
-    acc = sum_of_block(acc, red);
+    acc = sum_of_block<THREADS>(acc, red);
     if (threadIdx.x == 0) {
         o.partial[blockIdx.x] = acc;
         __threadfence(); // before the count, so that the last block finds it
@@ -594,8 +596,8 @@ norm_kernel(const Tensor* __restrict__ tensors, const Unit* __restrict__ units, 
     if (!last) return;
     __threadfence();
     acc = 0.0;
-    for (int64_t k = u0 + threadIdx.x; k < u1; k += kNormThreads) acc += __ldcg(o.partial + k);
-    acc = sum_of_block(acc, red);
+    for (int64_t k = u0 + threadIdx.x; k < u1; k += THREADS) acc += __ldcg(o.partial + k);
+    acc = sum_of_block<THREADS>(acc, red);
     if (threadIdx.x == 0) {
         o.done[u.group] = 0;
         const double nrm = (double)o.unscale * sqrt(acc);
@@ -850,8 +852,10 @@ int choco_adamw_grad_norm(choco_adamw* opt, float max_norm, float unscale, float
     if (!aligned_to(norm, 4) || !aligned_to(factor, 4)) return CHOCO_ERR_MISALIGNED;
     if (opt->broken) return CHOCO_ERR_CUDA;
     const NormOut o = {opt->d_partial, opt->d_unit_begin, opt->d_done, max_norm, unscale, norm, factor};
-    return status_of(launch_overlapped(norm_kernel, dim3((unsigned)opt->nunits), dim3(kNormThreads), 0, (cudaStream_t)stream, HotRange{},
-                                       opt->d_tensors, opt->d_units, opt->unit_elems, o));
+    const bool many = opt->unit_elems == kUnitLong;
+    return status_of(launch_overlapped(many ? norm_kernel<kNormThreadsLong> : norm_kernel<kNormThreads>, dim3((unsigned)opt->nunits),
+                                       dim3(many ? kNormThreadsLong : kNormThreads), 0, (cudaStream_t)stream, HotRange{}, opt->d_tensors,
+                                       opt->d_units, opt->unit_elems, o));
 }
 
 int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* v_scale, double lr, const float* factor,

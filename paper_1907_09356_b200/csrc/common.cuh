@@ -4,7 +4,8 @@
 // float32, round to nearest even, no fused multiply-add (the library is compiled with
 // -fmad=false), IEEE division and square root, norms summed as a pairwise tree over the
 // coordinate index (level 0 = the terms, each level adds elements 2j and 2j+1, missing
-// elements count as +0).
+// elements count as +0).  The one exception is AdamW's update with 8-bit moments (adamw.cu), which
+// says there what it does instead and why; it too gives the same bits every time.
 #pragma once
 
 #include <cuda_runtime.h>

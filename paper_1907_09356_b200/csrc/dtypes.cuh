@@ -30,14 +30,8 @@ __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { re
 template <>
 __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
-// one element of an array whose type is known at run time
-__device__ __forceinline__ float load_as_float(const void* p, int64_t i, int32_t dtype)
-{
-    if (dtype == CHOCO_F32) return static_cast<const float*>(p)[i];
-    if (dtype == CHOCO_BF16) return to_float(static_cast<const __nv_bfloat16*>(p)[i]);
-    return to_float(static_cast<const __half*>(p)[i]);
-}
-// the same in two halves, so that several loads can be under way before the first is converted
+// one element of an array whose type is known at run time, in two halves, so that several loads can be under way before the
+// first is converted
 __device__ __forceinline__ uint32_t load_bits(const void* p, int64_t i, int32_t dtype)
 {
     return dtype == CHOCO_F32 ? static_cast<const uint32_t*>(p)[i] : (uint32_t)static_cast<const unsigned short*>(p)[i];

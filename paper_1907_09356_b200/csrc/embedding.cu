@@ -3,8 +3,9 @@
 // The gradient orders every worker's tokens with their positions, so that the rows of dout that
 // belong to one row of the table follow one another in order of position, cuts that list into tiles
 // of equal length and adds up each tile's rows in registers, in float32.  A run of one token that
-// crosses tiles leaves partial sums, which a last kernel adds in tile order.  No atomics on
-// values: the result depends on the tokens and the sizes alone.
+// goes on for more than half a tile leaves partial sums, which a last kernel adds in tile order.
+// Every element of the gradient is written, or added to, once: the result depends on the tokens
+// and the sizes alone.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -568,9 +569,13 @@ __device__ __forceinline__ void store_grad(const EmbShape& s, void* grad, int32_
     auto put = [&](auto* g) {
         using TG = std::remove_pointer_t<decltype(g)>;
         if (accumulate) {
-            if constexpr (std::is_same_v<TG, float>) return add_in_memory<V>(g + at, f);
+            if constexpr (std::is_same_v<TG, float>) {
+                add_in_memory<V>(g + at, f);
+                return;
+            } else {
 #pragma unroll
-            for (int e = 0; e < V; ++e) f[e] += to_float(g[at + e]);
+                for (int e = 0; e < V; ++e) f[e] += to_float(g[at + e]);
+            }
         }
         store_vec<TG, V>(g + at, f);
     };
