@@ -437,7 +437,8 @@ int choco_embedding_destroy(choco_embedding* emb);
  * choco_embedding_forward -- out[i, t, :] = scale * table_i[tokens[i, t], :], formed in float32
  * and rounded once to the output's type.
  *   tokens     DEVICE, int32 (index_bits = 32) or int64 (64), `count` >= 0 per worker (no limit
- *              but n count < 2^31), rows `tokens_ld` >= count elements apart.
+ *              but n count < 2^31), rows `tokens_ld` >= count elements apart, or 0: the same tokens
+ *              for all workers.
  *   out        DEVICE; element (i, t, c) at i out_ld + t out_row + c; out_row >= dim.
  * Table, tokens and out do not overlap.
  */
@@ -455,7 +456,8 @@ int choco_embedding_forward(choco_embedding* emb, const void* table, int32_t tab
  * and the sizes alone, and the result is rounded once.
  * What dout holds at tokens outside [0, vocab) is not read into any sum.
  *   count      <= max_tokens (CHOCO_ERR_TOO_LARGE); 0 writes zeros (or nothing).
- *   dout       DEVICE; element (i, t, c) at i dout_ld + t dout_row + c.
+ *   dout       DEVICE; element (i, t, c) at i dout_ld + t dout_row + c; dout_row >= dim, or 0: one row
+ *              for all tokens; dout_ld >= 0 (0: one batch for all workers).  Does not overlap grad.
  * Elements of grad between rows (table_row > dim) and between tables are not touched.
  */
 int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t index_bits, int64_t count,
@@ -502,7 +504,8 @@ typedef struct {
  *                     divides by eps alone).  Codes and scales of zero are moments of zero: a
  *                     fresh run starts from zeroed arrays.
  * m and v (and the 8-bit codes) are 16-byte aligned, the scales 4-byte.
- * The list is copied; the tensors it points to have to stay where they are.
+ * The list is copied; the tensors it points to have to stay where they are and not overlap (but for
+ * gradients, which are only read).
  */
 int choco_adamw_init(choco_adamw** out, int32_t n_tensors, const choco_adamw_tensor* tensors,
                      const choco_adamw_params* p);
@@ -525,7 +528,8 @@ int choco_adamw_grad_norm(choco_adamw* opt, float max_norm, float unscale, float
  * choco_adamw_step -- one step of all tensors.  factor: DEVICE float [groups], the gradient
  * factors c, or NULL for 1.  A group whose factor is infinite or NaN is left as it is, parameters,
  * moments, copy and step number, so that a step with overflowed gradients is skipped without a
- * host synchronisation.  After it, X has changed outside the gossip step: call choco_invalidate
+ * host synchronisation.  Infinite or NaN gradients that no factor keeps out leave the elements they
+ * are in, and with 8-bit moments the blocks, without meaning.  After a step, X has changed outside the gossip step: call choco_invalidate
  * (or run with choco_set_carry(ctx, 0)) before the next choco_gossip_step.
  */
 int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* v_scale, double lr,

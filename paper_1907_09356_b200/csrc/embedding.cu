@@ -955,7 +955,7 @@ EmbShape shape_of(const choco_embedding* e, int64_t count)
 
 int check_tokens(const choco_embedding* e, const void* tokens, int32_t bits, int64_t count, int64_t ld)
 {
-    if (!on_device(e) || (bits != 32 && bits != 64) || count < 0 || (e->p.n > 1 && ld < count)) return CHOCO_ERR_INVALID_ARG;
+    if (!on_device(e) || (bits != 32 && bits != 64) || count < 0 || (e->p.n > 1 && ld < count && ld != 0)) return CHOCO_ERR_INVALID_ARG;
     if (count > 0 && !tokens) return CHOCO_ERR_INVALID_ARG;
     if (!aligned_to(tokens, bits / 8)) return CHOCO_ERR_MISALIGNED;
     if (count >= ((int64_t)1 << 31) || count * e->p.n >= ((int64_t)1 << 31)) return CHOCO_ERR_TOO_LARGE;
@@ -1159,7 +1159,7 @@ int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t i
     const int rc = check_tokens(emb, tokens, index_bits, count, tokens_ld);
     if (rc != CHOCO_OK) return rc;
     if (emb->p.max_tokens == 0 || count > emb->p.max_tokens) return CHOCO_ERR_TOO_LARGE;
-    if (count > 0 && (!dout || dout_row < emb->p.dim || (emb->p.n > 1 && dout_ld < 0))) return CHOCO_ERR_INVALID_ARG;
+    if (count > 0 && (!dout || (dout_row < emb->p.dim && dout_row != 0) || (emb->p.n > 1 && dout_ld < 0))) return CHOCO_ERR_INVALID_ARG;
     if (!aligned_to(grad, dtype_size(grad_dtype)) || !aligned_to(dout, dtype_size(dout_dtype))) return CHOCO_ERR_MISALIGNED;
     if (count == 0 && accumulate) return CHOCO_OK;
     const EmbShape s = shape_of(emb, count);

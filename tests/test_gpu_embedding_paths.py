@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_1907_09356_b200 as choco
-from test_gpu_embedding import DEV, F32, BF16, check_grad, table_in, tokens_of
+from test_gpu_embedding import DEV, F32, BF16, check_grad, ref_lookup, table_in, tokens_of
 
 pytestmark = pytest.mark.gpu
 
@@ -63,4 +63,29 @@ def test_vocabularies_at_the_digits_limits(vocab):
     emb = choco.Embedding(1, vocab, 4, 5000)
     one(emb, 1, vocab, 4, 5000, "uniform", False)
     one(emb, 1, vocab, 4, 5000, "outside", False)
+    emb.close()
+
+
+@pytest.mark.parametrize("count", [1, 40, 300, 9000])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_broadcast_gradients_and_shared_tokens(count, accumulate):
+    """One row of dout for every token (a mean's gradient), one batch for all workers, the same tokens for
+    all workers: expanded tensors, with strides of zero."""
+    n, vocab, dim = 3, 50, 24
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    tok = tokens_of(n, count, vocab, "zipf", count)
+    shared = tokens_of(1, count, vocab, "ragged", count).expand(n, count)
+    row = torch.randn((n, 1, dim), generator=gen, device=DEV).expand(n, count, dim)
+    batch = torch.randn((1, count, dim), generator=gen, device=DEV).expand(n, count, dim)
+    emb = choco.Embedding(n, vocab, dim, count)
+    for t in (tok, shared):
+        for dout in (row, batch):
+            G, view = table_in(n, vocab, dim, dim, vocab * dim, 0, F32, 6)
+            before = view.clone()
+            emb.backward(t, dout, G, accumulate=accumulate)
+            check_grad(view, t, dout, 1.0, before if accumulate else None)
+        X, xview = table_in(n, vocab, dim, dim, vocab * dim, 0, F32, 7)
+        out = torch.empty((n, count, dim), device=DEV)
+        emb.forward(X, t, out)
+        assert torch.equal(out.double(), ref_lookup(xview, t, 1.0))
     emb.close()
