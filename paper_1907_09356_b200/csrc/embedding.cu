@@ -792,6 +792,9 @@ __global__ void __launch_bounds__(kEmbThreads) join_kernel(EmbShape s, Sums a, u
 // ---------------------------------------------------------------------------------------
 
 constexpr int kDirectTokens = 256;          // per worker
+// Tables up to this are zeroed by the same launch (13 MB: 5.6 us, 6.6 us apart); beyond, a kernel of its own reaches the
+// memory's rate (692 MB: 98 us, 120 us together).
+constexpr int64_t kDirectZeroBytes = (int64_t)16 << 20;
 
 struct Direct {
     const void* tokens;
@@ -1168,16 +1171,6 @@ int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t i
                            vector_of(grad, grad_dtype, s.table_row, s.table_ld, s.dim, s.n, 8));
     cudaError_t err = cudaSuccess;
 
-    if (count <= kDirectTokens) {
-        const Direct d = {tokens, tokens_ld, index_bits, dout, dout_row, dout_ld, grad, grad_dtype, accumulate, 0, 0,
-                          accumulate ? 0 : (s.vocab + 7) / 8, 0};
-        with_type(dout_dtype, [&](auto* td) {
-            err = launch_direct_for<std::remove_pointer_t<decltype(td)>>(s, d, v, st);
-            return 0;
-        });
-        return status_of(err);
-    }
-
     auto zero = [&](int32_t beside) {
         if (accumulate || err != cudaSuccess) return;
         const int32_t size = (int32_t)dtype_size(grad_dtype);
@@ -1188,6 +1181,19 @@ int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t i
             err = launch_overlapped(zero_kernel, dim3((unsigned)blocks, (unsigned)s.n), dim3(kEmbThreads), 0, st, HotRange{}, s,
                                     static_cast<char*>(grad), size, (uint32_t)per_row, beside);
     };
+    if (count <= kDirectTokens) {
+        const bool apart = !accumulate && s.n * s.vocab * s.dim * dtype_size(grad_dtype) > kDirectZeroBytes;
+        if (apart) zero(0);
+        const Direct d = {tokens, tokens_ld, index_bits, dout, dout_row, dout_ld, grad, grad_dtype, accumulate, 0, 0,
+                          accumulate || apart ? 0 : (s.vocab + 7) / 8, 0};
+        if (err == cudaSuccess && (count > 0 || d.eights > 0))
+            with_type(dout_dtype, [&](auto* td) {
+                err = launch_direct_for<std::remove_pointer_t<decltype(td)>>(s, d, v, st);
+                return 0;
+            });
+        return status_of(err);
+    }
+
     const dim3 threads(kEmbThreads);
     int cur = 0;
     Order o = {};
