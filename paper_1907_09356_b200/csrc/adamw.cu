@@ -630,8 +630,9 @@ struct choco_adamw {
     int64_t most_chunks, nunits, unit_elems;
     int64_t begin[2 * kPairs + 1]; // in d_chunks, for every pair of types: other blocks, whole blocks of aligned tensors
     int64_t t;                     // step calls so far; a group has taken t - skipped[group] steps
+    void* memory;                  // all that follows
     Tensor* d_tensors;
-    Chunk* d_chunks;
+    Chunk* d_chunks;               // room for most_chunks
     Unit* d_units;
     int64_t* d_unit_begin;         // [groups + 1]
     int64_t* d_skipped;            // [groups]
@@ -647,14 +648,39 @@ bool on_device(const choco_adamw* o)
     return cudaGetDevice(&dev) == cudaSuccess && dev == o->device;
 }
 
-template <typename T>
-bool upload(T** out, const T* src, size_t count, size_t room = 1)
+// Device memory for everything, in one allocation, and what of it has a first value in one copy.
+// Throws std::bad_alloc.
+int allocate(choco_adamw* o, const std::vector<Chunk>& chunks, const std::vector<Unit>& units, const std::vector<int64_t>& unit_begin)
 {
-    *out = nullptr;
-    const size_t bytes = sizeof(T) * (count > room ? count : room);
-    if (cudaMalloc((void**)out, bytes) != cudaSuccess) { *out = nullptr; return false; }
-    if (!src) return cudaMemset(*out, 0, bytes) == cudaSuccess;
-    return count == 0 || cudaMemcpy(*out, src, sizeof(T) * count, cudaMemcpyHostToDevice) == cudaSuccess;
+    const size_t groups = (size_t)o->params.groups;
+    std::vector<char> first;
+    size_t at[7];
+    auto place = [&](int k, const void* from, size_t bytes, size_t room) {
+        at[k] = (first.size() + 255) / 256 * 256;
+        first.resize(at[k] + (room > bytes ? room : bytes), 0);
+        if (bytes) std::memcpy(first.data() + at[k], from, bytes);
+    };
+    place(0, o->tensors.data(), sizeof(Tensor) * o->tensors.size(), 0);
+    place(1, chunks.data(), sizeof(Chunk) * chunks.size(), sizeof(Chunk) * (size_t)o->most_chunks);
+    place(2, units.data(), sizeof(Unit) * units.size(), 0);
+    place(3, unit_begin.data(), sizeof(int64_t) * unit_begin.size(), 0);
+    place(4, nullptr, 0, sizeof(int64_t) * groups);
+    place(5, nullptr, 0, sizeof(uint32_t) * groups);
+    at[6] = (first.size() + 255) / 256 * 256;
+    if (cudaMalloc(&o->memory, at[6] + sizeof(double) * units.size()) != cudaSuccess) {
+        o->memory = nullptr;
+        return CHOCO_ERR_ALLOC;
+    }
+    if (cudaMemcpy(o->memory, first.data(), first.size(), cudaMemcpyHostToDevice) != cudaSuccess) return CHOCO_ERR_CUDA;
+    char* const m = static_cast<char*>(o->memory);
+    o->d_tensors = reinterpret_cast<Tensor*>(m + at[0]);
+    o->d_chunks = reinterpret_cast<Chunk*>(m + at[1]);
+    o->d_units = reinterpret_cast<Unit*>(m + at[2]);
+    o->d_unit_begin = reinterpret_cast<int64_t*>(m + at[3]);
+    o->d_skipped = reinterpret_cast<int64_t*>(m + at[4]);
+    o->d_done = reinterpret_cast<uint32_t*>(m + at[5]);
+    o->d_partial = reinterpret_cast<double*>(m + at[6]);
+    return CHOCO_OK;
 }
 
 int status_of(cudaError_t e)
@@ -666,13 +692,7 @@ int status_of(cudaError_t e)
 
 void free_all(choco_adamw* o)
 {
-    cudaFree(o->d_tensors);
-    cudaFree(o->d_chunks);
-    cudaFree(o->d_units);
-    cudaFree(o->d_unit_begin);
-    cudaFree(o->d_skipped);
-    cudaFree(o->d_partial);
-    cudaFree(o->d_done);
+    cudaFree(o->memory);
     delete o;
 }
 
@@ -726,6 +746,7 @@ int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Un
     }
     unit_begin.push_back((int64_t)units.size());
     o->nunits = (int64_t)units.size();
+    if (o->norm_only) o->most_chunks = 0; // no step
     return o->most_chunks > 0x7fffffff || o->nunits > 0x7fffffff ? CHOCO_ERR_TOO_LARGE : CHOCO_OK;
 }
 
@@ -735,6 +756,7 @@ std::vector<Chunk> cut(const choco_adamw* o, const std::vector<Tensor>& tensors,
 {
     std::vector<Chunk> chunks;
     std::vector<char> seen((size_t)o->params.groups, 0);
+    chunks.reserve((size_t)o->most_chunks);
     for (int32_t k = 0; k < 2 * kPairs; ++k) {
         begin[k] = (int64_t)chunks.size();
         for (int32_t i : o->by_group) {
@@ -772,15 +794,9 @@ int choco_adamw_init(choco_adamw** out, int32_t n_tensors, const choco_adamw_ten
         std::vector<Unit> units;
         std::vector<int64_t> unit_begin;
         rc = plan(o, n_tensors, tensors, units, unit_begin);
-        if (rc == CHOCO_OK) chunks = cut(o, o->tensors, o->begin);
+        if (rc == CHOCO_OK && !o->norm_only) chunks = cut(o, o->tensors, o->begin);
         if (rc == CHOCO_OK && cudaGetDevice(&o->device) != cudaSuccess) rc = CHOCO_ERR_CUDA;
-        if (rc == CHOCO_OK &&
-            !(upload(&o->d_tensors, o->tensors.data(), o->tensors.size()) && upload(&o->d_chunks, chunks.data(), chunks.size(), o->most_chunks) &&
-              upload(&o->d_units, units.data(), units.size()) && upload(&o->d_unit_begin, unit_begin.data(), unit_begin.size()) &&
-              upload(&o->d_skipped, (const int64_t*)nullptr, 0, (size_t)p->groups) &&
-              upload(&o->d_partial, (const double*)nullptr, 0, units.size()) &&
-              upload(&o->d_done, (const uint32_t*)nullptr, 0, (size_t)p->groups)))
-            rc = CHOCO_ERR_ALLOC;
+        if (rc == CHOCO_OK) rc = allocate(o, chunks, units, unit_begin);
     } catch (const std::exception&) {
         rc = CHOCO_ERR_ALLOC;
     }
@@ -829,6 +845,7 @@ int choco_adamw_set_grads(choco_adamw* opt, const void* const* g, void* stream)
             tensors[i].aligned = all_aligned(tensors[i]);
             moved |= tensors[i].aligned != opt->tensors[i].aligned;
         }
+        moved = moved && !opt->norm_only;
         if (moved) chunks = cut(opt, tensors, begin);
         if (cudaStreamSynchronize(st) != cudaSuccess) return CHOCO_ERR_CUDA;
         // the tables on the device have to agree with each other and with the host's: if one copy fails, no call may use them

@@ -922,7 +922,8 @@ int vector_of(const void* p, int32_t dtype, int64_t row, int64_t ld, int64_t dim
 struct choco_embedding {
     choco_embedding_params p;
     int device;
-    uint32_t* key[2];
+    void* memory;                // all that follows
+    uint32_t* key[2];            // the second ones, hist and total only where a batch may have to be sorted in global memory
     uint32_t* pos[2];
     uint32_t* hist;
     uint32_t* total;
@@ -942,11 +943,7 @@ bool on_device(const choco_embedding* e)
 
 void free_all(choco_embedding* e)
 {
-    for (int k = 0; k < 2; ++k) { cudaFree(e->key[k]); cudaFree(e->pos[k]); }
-    cudaFree(e->hist);
-    cudaFree(e->total);
-    cudaFree(e->part);
-    cudaFree(e->chains);
+    cudaFree(e->memory);
     delete e;
 }
 
@@ -1068,26 +1065,36 @@ int choco_embedding_init(choco_embedding** out, const choco_embedding_params* p)
     if (!e) return CHOCO_ERR_ALLOC;
     e->p = q;
     cudaError_t err = cudaGetDevice(&e->device);
-    const int64_t total = q.n * q.max_tokens;
     e->pitch = (q.dim + 7) / 8 * 8;
-    if (total > 0) {
-        const int64_t sort_tiles = (q.max_tokens + kSortTile - 1) / kSortTile;
+    if (q.max_tokens > kDirectTokens) {
+        const int64_t total = q.n * q.max_tokens;
+        const bool sorts = q.max_tokens > (int64_t)kOrderCluster * kOrderMost;
         // batches of every size up to the largest have to fit, in tiles of any length
         const int64_t few = std::min(total, kShortRows), mid = std::min(total, kMidRows);
         const int64_t tiles = std::max({(q.max_tokens + kTileLong - 1) / kTileLong * q.n, mid / kTileMid + q.n, few / kTileShort + q.n});
-        auto get = [&](auto** ptr, int64_t count) {
-            if (err == cudaSuccess) err = cudaMalloc((void**)ptr, (size_t)count * sizeof(**ptr));
-        };
-        for (int k = 0; k < 2; ++k) { get(&e->key[k], total); get(&e->pos[k], total); }
-        get(&e->hist, q.n * kDigits * sort_tiles);
-        get(&e->total, (int64_t)q.n * kDigits);
-        get(&e->part, tiles * 2 * e->pitch);
-        get(&e->chains, tiles + 2);
         e->chain_room = (uint32_t)tiles;
-    }
-    if (q.max_tokens > 0 && err == cudaSuccess) {
-        err = cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)(sizeof(OrderSmem) + 2 * sizeof(uint2) * kOrderMost));
+        int64_t bytes = 0;
+        auto place = [&](auto** ptr, int64_t count) { // the second time around, when the memory is there
+            if (e->memory) *ptr = reinterpret_cast<std::remove_reference_t<decltype(*ptr)>>(static_cast<char*>(e->memory) + bytes);
+            bytes += (count * (int64_t)sizeof(**ptr) + 255) / 256 * 256;
+        };
+        for (int round = 0; round < 2 && err == cudaSuccess; ++round) {
+            bytes = 0;
+            place(&e->key[0], total);
+            place(&e->pos[0], total);
+            place(&e->part, tiles * 2 * e->pitch);
+            place(&e->chains, tiles + 2);
+            if (sorts) {
+                place(&e->key[1], total);
+                place(&e->pos[1], total);
+                place(&e->hist, q.n * kDigits * ((q.max_tokens + kSortTile - 1) / kSortTile));
+                place(&e->total, (int64_t)q.n * kDigits);
+            }
+            if (round == 0 && err == cudaSuccess) err = cudaMalloc(&e->memory, (size_t)bytes);
+        }
+        if (err == cudaSuccess)
+            err = cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)(sizeof(OrderSmem) + 2 * sizeof(uint2) * kOrderMost));
         if (err == cudaSuccess) err = cudaFuncSetAttribute(order_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     }
     if (err != cudaSuccess) {
