@@ -186,11 +186,13 @@ __device__ __forceinline__ void lanes_alike(uint32_t (&alike)[N], const uint32_t
 // (131072 tokens of 16 bits: 27 us against 45 us; 8 x 2240: 12 us), and most SMs stay free for the
 // zeros.  What it takes is latency: per digit about 2 us of barriers and exchanged counts, and
 // 4 us for 8192 keys to be ranked and sent.
-constexpr int kOrderThreads = 1024;
-constexpr int kOrderWarps = kOrderThreads / 32;
-constexpr int kOrderDigitBits = 9;
-constexpr int kOrderDigits = 1 << kOrderDigitBits;
-constexpr int kOrderMost = 8192;            // keys of a block
+// Up to 4096 tokens of up to 16 bits a block of 512 threads does it alone: fewer warps have counts
+// to add up and meet at barriers (8 x 2240 rows of 650 floats added, all three launches: 34.5 -> 32.8 us;
+// 4 x 1000 of 200: 15.2 -> 14.1 us).
+constexpr int kOrderRounds = 8;             // keys of a thread, at most
+constexpr int kOrderThreads = 1024, kOrderThreadsFew = 512;
+constexpr int kOrderDigitBits = 9, kOrderDigitBitsFew = 8; // (a digit's counts are one thread's work)
+constexpr int kOrderMost = kOrderThreads * kOrderRounds, kOrderMostFew = kOrderThreadsFew * kOrderRounds; // keys of a block
 constexpr int kOrderFew = 2048;             // keys that are not worth a second block
 constexpr int kOrderCluster = 16;           // blocks of a cluster, at most
 
@@ -200,15 +202,18 @@ struct Order {
     int32_t index_bits;
     int32_t cluster_log, part_log;          // blocks of a cluster, keys of a block
     int32_t digit_bits, passes;
+    int32_t few;                            // one block of kOrderThreadsFew threads
     uint32_t *keys, *pos;                   // out: [n, count]
     uint32_t* chain_count;                  // set to 0 (see Sums)
 };
 
+template <int THREADS>
 struct OrderSmem {
-    uint16_t cnt[kOrderWarps][kOrderDigits];
-    uint32_t hist[kOrderDigits];            // read by the other blocks
-    uint32_t base[kOrderDigits];
-    uint32_t ws[kOrderWarps];
+    static constexpr int kWarps = THREADS / 32, kDigits = 1 << (THREADS == kOrderThreads ? kOrderDigitBits : kOrderDigitBitsFew);
+    uint16_t cnt[kWarps][kDigits];
+    uint32_t hist[kDigits];                 // read by the other blocks
+    uint32_t base[kDigits];
+    uint32_t ws[kWarps];
 };
 
 __device__ __forceinline__ uint32_t cluster_address(const void* p, uint32_t block) // of block's copy of a shared variable
@@ -230,11 +235,13 @@ __device__ __forceinline__ void store_cluster(uint32_t a, uint32_t x, uint32_t y
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-__global__ void __launch_bounds__(kOrderThreads, 1) order_kernel(EmbShape s, Order o)
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) order_kernel(EmbShape s, Order o)
 {
+    constexpr int kWarps = THREADS / 32;
     extern __shared__ __align__(16) unsigned char smem[];
-    OrderSmem& m = *reinterpret_cast<OrderSmem*>(smem);
-    uint2* buf = reinterpret_cast<uint2*>(smem + sizeof(OrderSmem)); // two buffers of (key, position)
+    OrderSmem<THREADS>& m = *reinterpret_cast<OrderSmem<THREADS>*>(smem);
+    uint2* buf = reinterpret_cast<uint2*>(smem + sizeof(OrderSmem<THREADS>)); // two buffers of (key, position)
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int32_t worker = blockIdx.x >> o.cluster_log;
     wait_for_previous_kernel();
@@ -244,8 +251,8 @@ __global__ void __launch_bounds__(kOrderThreads, 1) order_kernel(EmbShape s, Ord
     const uint32_t part = 1u << o.part_log;
     const uint32_t first = rank << o.part_log;
     const int have = (int)min((int64_t)part, max((int64_t)0, s.count - (int64_t)first));
-    const int rounds = part / kOrderThreads, slice = part / kOrderWarps;
-    constexpr int kRounds = kOrderMost / kOrderThreads;
+    const int rounds = part / THREADS, slice = part / kWarps;
+    constexpr int kRounds = kOrderRounds;
     uint32_t key[kRounds], pos[kRounds];
     uint16_t place[kRounds];
 #pragma unroll
@@ -295,20 +302,20 @@ __global__ void __launch_bounds__(kOrderThreads, 1) order_kernel(EmbShape s, Ord
             }
             if (lane == 31) m.ws[w] = incl;
             __syncthreads();
-            uint32_t v = m.ws[lane];
+            uint32_t v = lane < kWarps ? m.ws[lane] : 0u;
 #pragma unroll
             for (int q = 1; q < 32; q <<= 1) {
                 const uint32_t u = __shfl_up_sync(0xffffffffu, v, q);
                 if (lane >= q) v += u;
             }
-            const uint32_t before = __shfl_sync(0xffffffffu, v, (w + 31) & 31);
+            const uint32_t before = __shfl_sync(0xffffffffu, v, (w + 31) & 31); // up to the warp before
             __syncthreads();
             return incl - mine + (w ? before : 0u);
         };
         uint32_t own = 0;
         if (threadIdx.x < digits) {
 #pragma unroll
-            for (int k = 0; k < kOrderWarps; ++k) own += m.cnt[k][threadIdx.x];
+            for (int k = 0; k < kWarps; ++k) own += m.cnt[k][threadIdx.x];
             m.hist[threadIdx.x] = own;
         }
         if (blocks > 1) cluster_arrive();
@@ -316,7 +323,7 @@ __global__ void __launch_bounds__(kOrderThreads, 1) order_kernel(EmbShape s, Ord
         if (threadIdx.x < digits) {
             uint32_t at = start;
 #pragma unroll
-            for (int k = 0; k < kOrderWarps; ++k) {
+            for (int k = 0; k < kWarps; ++k) {
                 const uint32_t c = m.cnt[k][threadIdx.x];
                 m.cnt[k][threadIdx.x] = (uint16_t)at;
                 at += c;
@@ -353,7 +360,7 @@ __global__ void __launch_bounds__(kOrderThreads, 1) order_kernel(EmbShape s, Ord
         const bool last = pass + 1 == o.passes;
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
-            const int j = r * kOrderThreads + threadIdx.x;
+            const int j = r * THREADS + threadIdx.x;
             if (r >= rounds || j >= have) break;
             const uint2 kp = in[j];
             const uint32_t to = m.base[(kp.x >> shift) & (digits - 1)] + j;
@@ -969,27 +976,29 @@ int tile_of(int64_t rows) { return rows <= kShortRows ? kTileShort : rows <= kMi
 bool plan_order(const EmbShape& s, Order& o)
 {
     if (s.count > (int64_t)kOrderCluster * kOrderMost) return false;
-    // a block for every kOrderFew keys, while all workers' clusters run at once, or as many as their memory needs
-    o.cluster_log = 0;
-    while ((1 << o.cluster_log) < kOrderCluster && ((int64_t)kOrderFew << o.cluster_log) < s.count &&
-           (((int64_t)kOrderMost << o.cluster_log) < s.count || ((int64_t)s.n << (o.cluster_log + 1)) <= 148))
-        ++o.cluster_log;
-    o.part_log = 10;
-    while (((int64_t)1 << (o.part_log + o.cluster_log)) < s.count) ++o.part_log;
     int bits = 1;
     while ((s.vocab >> bits) != 0) ++bits; // keys go up to vocab
-    o.passes = (bits + kOrderDigitBits - 1) / kOrderDigitBits;
+    o.few = s.count <= kOrderMostFew && bits <= 2 * kOrderDigitBitsFew;
+    const int most = o.few ? kOrderDigitBitsFew : kOrderDigitBits;
+    o.passes = (bits + most - 1) / most;
     o.digit_bits = (bits + o.passes - 1) / o.passes;
+    // a block for every kOrderFew keys, while all workers' clusters run at once, or as many as their memory needs
+    o.cluster_log = 0;
+    while (!o.few && (1 << o.cluster_log) < kOrderCluster && ((int64_t)kOrderFew << o.cluster_log) < s.count &&
+           (((int64_t)kOrderMost << o.cluster_log) < s.count || ((int64_t)s.n << (o.cluster_log + 1)) <= 148))
+        ++o.cluster_log;
+    o.part_log = o.few ? 9 : 10; // a key for each thread
+    while (((int64_t)1 << (o.part_log + o.cluster_log)) < s.count) ++o.part_log;
     return true;
 }
 
-cudaError_t launch_order(const EmbShape& s, const Order& o, cudaStream_t st)
+template <int THREADS>
+cudaError_t launch_order_of(const EmbShape& s, const Order& o, cudaStream_t st)
 {
-    const size_t smem = sizeof(OrderSmem) + ((size_t)2 * sizeof(uint2) << o.part_log);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(s.n << o.cluster_log));
-    cfg.blockDim = dim3(kOrderThreads);
-    cfg.dynamicSmemBytes = smem;
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = sizeof(OrderSmem<THREADS>) + ((size_t)2 * sizeof(uint2) << o.part_log);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1000,7 +1009,23 @@ cudaError_t launch_order(const EmbShape& s, const Order& o, cudaStream_t st)
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, order_kernel, s, o);
+    return cudaLaunchKernelEx(&cfg, order_kernel<THREADS>, s, o);
+}
+cudaError_t launch_order(const EmbShape& s, const Order& o, cudaStream_t st)
+{
+    return o.few ? launch_order_of<kOrderThreadsFew>(s, o, st) : launch_order_of<kOrderThreads>(s, o, st);
+}
+
+// dynamic shared memory beyond the default, clusters of more than eight blocks
+cudaError_t allow_order()
+{
+    cudaError_t e = cudaFuncSetAttribute(order_kernel<kOrderThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         (int)(sizeof(OrderSmem<kOrderThreads>) + 2 * sizeof(uint2) * kOrderMost));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(order_kernel<kOrderThreads>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(order_kernel<kOrderThreadsFew>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)(sizeof(OrderSmem<kOrderThreadsFew>) + 2 * sizeof(uint2) * kOrderMostFew));
+    return e;
 }
 
 template <typename TD, int V, int C, int B>
@@ -1092,10 +1117,7 @@ int choco_embedding_init(choco_embedding** out, const choco_embedding_params* p)
             }
             if (round == 0 && err == cudaSuccess) err = cudaMalloc(&e->memory, (size_t)bytes);
         }
-        if (err == cudaSuccess)
-            err = cudaFuncSetAttribute(order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)(sizeof(OrderSmem) + 2 * sizeof(uint2) * kOrderMost));
-        if (err == cudaSuccess) err = cudaFuncSetAttribute(order_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (err == cudaSuccess) err = allow_order();
     }
     if (err != cudaSuccess) {
         cudaGetLastError();
