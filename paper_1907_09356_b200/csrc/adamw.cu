@@ -21,7 +21,12 @@ constexpr int kBlock = 256;                 // elements that share a scale; tens
 constexpr int kStepThreads = 128;            // short blocks: 256 threads took 5 % more, 64 no less
 constexpr int kStepWarps = kStepThreads / 32;
 constexpr int kChunkElems = kStepWarps * kBlock;
-// blocks on an SM: 64 registers a thread with 32-bit moments, 48 with codes, where more warps pay (552 us against 579)
+// Blocks of elements that a warp of the fast path has in flight.  With codes one is too few bytes to cover the
+// chain of reads before it (8 x 25.6 M elements: 548 us with one, 500 us with two, 660 us with three, which
+// no longer fit the registers); with 32-bit moments two are slower than one (2.09 ms against 2.01 ms).
+template <int BITS>
+constexpr int kBlocksAtOnce = BITS == 8 ? 2 : 1;
+// blocks on an SM: 64 registers a thread with 32-bit moments, 48 with codes, where more warps pay
 constexpr int kStepBlocks32 = 8, kStepBlocks8 = 10, kStepBlocksRest = 6;
 constexpr int kNormThreads = 128, kNormThreadsLong = 256; // 8 x 65 small tensors 6.1 us and 7.2 us, 16 x 28.95 M elements 262 us and 256 us
 constexpr int64_t kUnitLong = 16384, kUnitShort = 2048; // elements of a unit of the norms
@@ -412,17 +417,23 @@ __global__ void __launch_bounds__(kStepThreads, BITS == 8 ? kStepBlocks8 : kStep
 step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
             int64_t* skipped, State st, StepScalars sc, int32_t beside)
 {
+    constexpr int N = kBlocksAtOnce<BITS>;
     const Chunk ch = chunks[gridDim.x - 1 - blockIdx.x];
     const Tensor t = tensors[ch.tensor];
     if (!beside) wait_for_previous_kernel();
     allow_next_kernel();
-    const int64_t base = ch.begin + (int64_t)(threadIdx.x >> 5) * kBlock;
-    if (base + kBlock <= t.numel) {
-        Loaded<BITS, XT, GT> l;
-        load_block(l, t, st, base);
-        Factors f;
-        if (factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc)) finish_block(l, t, st, sc, f, base);
-        else if (ch.first && threadIdx.x == 0) skipped[t.group] += 1;
+    const int64_t base = ch.begin + (int64_t)(threadIdx.x >> 5) * kBlock, end = t.numel / kBlock * kBlock;
+    Loaded<BITS, XT, GT> l[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        if (base + k * kChunkElems < end) load_block(l[k], t, st, base + k * kChunkElems);
+    Factors f;
+    if (factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc)) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (base + k * kChunkElems < end) finish_block(l[k], t, st, sc, f, base + k * kChunkElems);
+    } else if (ch.first && threadIdx.x == 0) {
+        skipped[t.group] += 1;
     }
     if (beside) wait_for_previous_kernel();
 }
@@ -613,9 +624,10 @@ norm_kernel(const Tensor* __restrict__ tensors, const Unit* __restrict__ units, 
 
 } // namespace
 
-// Lists up to this many chunks take one launch for both kinds: 8 x 65 tensors of a ResNet-20, 11.9 us against 12.9;
-// 16 M elements, 68.1 against 68.8.  With codes the registers cost more: 4.4 M elements, 14.8 us against 15.0; 25 M, 83 against 72.
-constexpr int64_t kBothChunks32 = 32768, kBothChunks8 = 4096;
+// Lists of up to this many chunks take one launch for both kinds of blocks: 8 x 65 tensors of a ResNet-20, 11.9 us
+// against 12.9; 16 M elements, 68.1 against 68.8.  With codes the registers cost more: 4.4 M elements, 14.8 us
+// against 16.3; 16 M, 51 against 46.
+constexpr int64_t kTogether32 = 32768, kTogether8 = 8192;
 constexpr int kPairs = 9;               // of types: 3 x_dtype + g_dtype
 
 struct choco_adamw {
@@ -628,6 +640,8 @@ struct choco_adamw {
     int64_t elements;              // of m and v
     std::vector<int32_t> by_group;  // tensors with elements, group after group
     int64_t most_chunks, nunits, unit_elems;
+    bool together;                 // a short list: one launch for all blocks of a pair of types
+    int64_t whole_elems;           // of a chunk of whole aligned blocks
     int64_t begin[2 * kPairs + 1]; // in d_chunks, for every pair of types: other blocks, whole blocks of aligned tensors
     int64_t t;                     // step calls so far; a group has taken t - skipped[group] steps
     void* memory;                  // all that follows
@@ -746,6 +760,9 @@ int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Un
     }
     unit_begin.push_back((int64_t)units.size());
     o->nunits = (int64_t)units.size();
+    const bool eight = o->params.state_bits == 8;
+    o->together = o->most_chunks <= (eight ? kTogether8 : kTogether32);
+    o->whole_elems = kChunkElems * (o->together || !eight ? 1 : kBlocksAtOnce<8>);
     if (o->norm_only) o->most_chunks = 0; // no step
     return o->most_chunks > 0x7fffffff || o->nunits > 0x7fffffff ? CHOCO_ERR_TOO_LARGE : CHOCO_OK;
 }
@@ -763,7 +780,7 @@ std::vector<Chunk> cut(const choco_adamw* o, const std::vector<Tensor>& tensors,
             const Tensor& t = tensors[i];
             if (t.x_dtype * 3 + t.g_dtype != k / 2) continue;
             const int64_t whole = t.aligned ? t.numel / kBlock * kBlock : 0;
-            for (int64_t b = k % 2 ? 0 : whole; b < (k % 2 ? whole : t.numel); b += kChunkElems) {
+            for (int64_t b = k % 2 ? 0 : whole; b < (k % 2 ? whole : t.numel); b += k % 2 ? o->whole_elems : kChunkElems) {
                 chunks.push_back({i, !seen[t.group], b});
                 seen[t.group] = 1;
             }
@@ -909,8 +926,8 @@ int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* 
         beside = 1;
     };
     for (int32_t pair = 0; pair < kPairs; ++pair) {
-        const int64_t *b = opt->begin + 2 * pair, rest = b[1] - b[0], whole = b[2] - b[1];
-        if (rest > 0 && whole > 0 && rest + whole <= (eight ? kBothChunks8 : kBothChunks32)) {
+        const int64_t* b = opt->begin + 2 * pair;
+        if (opt->together && b[0] < b[1] && b[1] < b[2]) {
             launch(pair, kBoth, b[0], b[2]);
         } else {
             launch(pair, kRest, b[0], b[1]);
