@@ -1,8 +1,8 @@
 // AdamW over many tensors at once, with moments in 32 or in 8 bits, and the per-group gradient
 // norms that feed it (choco_adamw_* in choco.h).
 //
-// A list of tensors is cut into chunks of at most kChunkElems elements of one tensor; a table in
-// device memory says which tensor a chunk belongs to, so that one launch serves all tensors of all
+// A list of tensors is cut into chunks of kChunkElems elements of one tensor or fewer (twice as many
+// where a long list has 8-bit moments and the chunk is of whole aligned blocks); a table in device memory says which tensor a chunk belongs to, so that one launch serves all tensors of all
 // workers whatever their sizes.  Inside a chunk every warp owns blocks of kBlock = 256 elements, the
 // unit that shares a scale in 8 bits.
 #include <cmath>
