@@ -69,6 +69,7 @@ struct StepScalars {
     float rsqrt_bc2;        // 1 / sqrt(1 - beta2^t)
     float log_beta1, log_beta2; // natural logarithms
     int64_t t;
+    int64_t whole_elems;    // of a chunk of whole aligned blocks
 };
 
 inline double pow_int(double b, int64_t e)
@@ -412,6 +413,8 @@ step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ c
 // A resident grid that walks over the chunks, with the list read ahead, was slower (16 x 28.95 M
 // float32: 2.55 ms against 2.10 ms): short blocks started in order keep what is in flight together
 // in memory.
+// A chunk may be shorter than what the warps could take: in a short list it holds one block of
+// elements for each, and what follows belongs to the next chunk.
 template <int BITS, typename XT, typename GT>
 __global__ void __launch_bounds__(kStepThreads, BITS == 8 ? kStepBlocks8 : kStepBlocks32)
 step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
@@ -422,7 +425,8 @@ step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks
     const Tensor t = tensors[ch.tensor];
     if (!beside) wait_for_previous_kernel();
     allow_next_kernel();
-    const int64_t base = ch.begin + (int64_t)(threadIdx.x >> 5) * kBlock, end = t.numel / kBlock * kBlock;
+    const int64_t base = ch.begin + (int64_t)(threadIdx.x >> 5) * kBlock;
+    const int64_t end = min(t.numel / kBlock * kBlock, ch.begin + sc.whole_elems);
     Loaded<BITS, XT, GT> l[N];
 #pragma unroll
     for (int k = 0; k < N; ++k)
@@ -913,6 +917,7 @@ int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* 
     sc.log_beta1 = (float)std::log(p.beta1); sc.log_beta2 = (float)std::log(p.beta2);
     sc.step_size = (float)(lr / (1.0 - pow_int(p.beta1, sc.t)));
     sc.rsqrt_bc2 = (float)(1.0 / std::sqrt(1.0 - pow_int(p.beta2, sc.t)));
+    sc.whole_elems = opt->whole_elems;
     cudaStream_t st = (cudaStream_t)stream;
     const State state = {m, v, m_scale, v_scale};
     cudaError_t err = cudaSuccess;
