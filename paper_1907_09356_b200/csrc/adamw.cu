@@ -22,8 +22,8 @@ constexpr int kStepThreads = 128;            // short blocks: 256 threads took 5
 constexpr int kStepWarps = kStepThreads / 32;
 constexpr int kChunkElems = kStepWarps * kBlock;
 // Blocks of elements that a warp of the fast path has in flight.  With codes one is too few bytes to cover the
-// chain of reads before it (8 x 25.6 M elements: 548 us with one, 500 us with two, 660 us with three, which
-// no longer fit the registers); with 32-bit moments two are slower than one (2.09 ms against 2.01 ms).
+// chain of reads before it (8 x 25.6 M elements: 548 us with one, 509 us with two, 660 us with three; two
+// spill up to 44 bytes a thread at 48 registers, three far more); with 32-bit moments two are slower than one (2.09 ms against 2.01 ms).
 template <int BITS>
 constexpr int kBlocksAtOnce = BITS == 8 ? 2 : 1;
 // blocks on an SM: 64 registers a thread with 32-bit moments, 48 with codes, where more warps pay
@@ -386,7 +386,7 @@ __device__ __forceinline__ bool factors_of(Factors& f, const Tensor& t, float c,
 // one block of threads per chunk, one warp per block of elements
 template <int BITS, typename XT, typename GT>
 __global__ void __launch_bounds__(kStepThreads, kStepBlocksRest)
-step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
+step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* factor,
                  int64_t* skipped, State st, StepScalars sc, int32_t beside)
 {
     const Chunk ch = chunks[blockIdx.x];
@@ -417,7 +417,7 @@ step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ c
 // elements for each, and what follows belongs to the next chunk.
 template <int BITS, typename XT, typename GT>
 __global__ void __launch_bounds__(kStepThreads, BITS == 8 ? kStepBlocks8 : kStepBlocks32)
-step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
+step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* factor,
             int64_t* skipped, State st, StepScalars sc, int32_t beside)
 {
     constexpr int N = kBlocksAtOnce<BITS>;
@@ -446,7 +446,7 @@ step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks
 // this kernel's registers cost.
 template <int BITS, typename XT, typename GT>
 __global__ void __launch_bounds__(kStepThreads, kStepBlocksRest)
-step_both_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* __restrict__ factor,
+step_both_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* factor,
                  int64_t* skipped, State st, StepScalars sc, int32_t beside)
 {
     const Chunk ch = chunks[blockIdx.x];

@@ -51,6 +51,8 @@ __device__ __forceinline__ void store_from_float(void* p, int64_t i, int32_t dty
 
 // V consecutive elements as raw words, so that a batch of loads can be in flight before the first
 // is unpacked; V * sizeof(T) is 2, 4, 8, 16 or 32 bytes and the address a multiple of it (of 16 for 32).
+// Plain loads, not those of read-only memory: AdamW writes what it reads, and a kernel that was launched
+// early is there while the one before it still writes.
 template <typename T, int V>
 struct Raw {
     static constexpr int kBytes = V * (int)sizeof(T);
@@ -63,16 +65,16 @@ __device__ __forceinline__ void load_raw(Raw<T, V>& r, const T* p)
     if constexpr (b >= 16) {
 #pragma unroll
         for (int k = 0; k < b / 16; ++k) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4*>(p) + k);
+            const uint4 u = reinterpret_cast<const uint4*>(p)[k];
             r.w[4 * k] = u.x; r.w[4 * k + 1] = u.y; r.w[4 * k + 2] = u.z; r.w[4 * k + 3] = u.w;
         }
     } else if constexpr (b == 8) {
-        const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
         r.w[0] = u.x; r.w[1] = u.y;
     } else if constexpr (b == 4) {
-        r.w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
+        r.w[0] = *reinterpret_cast<const uint32_t*>(p);
     } else {
-        r.w[0] = __ldg(reinterpret_cast<const unsigned short*>(p));
+        r.w[0] = *reinterpret_cast<const unsigned short*>(p);
     }
 }
 template <typename T, int V>

@@ -65,8 +65,8 @@ __host__ __device__ constexpr int lookup_rows()
 
 template <typename TT, typename TO, int V, int N, bool NARROW>
 __global__ void __launch_bounds__(kEmbThreads)
-lookup_kernel(EmbShape s, const TT* __restrict__ table, const void* __restrict__ tokens, int32_t index_bits, int64_t tokens_ld,
-              TO* __restrict__ out, int64_t out_row, int64_t out_ld, uint32_t slabs, uint32_t narrow_log)
+lookup_kernel(EmbShape s, const TT* table, const void* tokens, int32_t index_bits, int64_t tokens_ld,
+              TO* out, int64_t out_row, int64_t out_ld, uint32_t slabs, uint32_t narrow_log)
 {
     constexpr int R = NARROW ? 1 : lookup_rows<TT, V, N>();
     const uint32_t lanes_log = NARROW ? narrow_log : 5; // lanes of a row

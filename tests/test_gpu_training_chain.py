@@ -1,0 +1,46 @@
+"""Lookup, gradient, norms and AdamW enqueued back to back, where every kernel may start while the one
+before it ends, against the same calls with a wait for the device after each."""
+import pytest
+import torch
+
+import paper_1907_09356_b200 as choco
+from test_gpu_embedding import BF16, DEV, F32, tokens_of
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab,dim,tail,count", [(300, 50, 1777, 600), (2000, 131, 40_001, 200)])
+def test_chained_calls_see_what_the_call_before_wrote(bits, dtype, vocab, dim, tail, count):
+    """Rows off 16-byte boundaries: memory sectors that two blocks of threads share are written by one
+    and read by the other in the next call."""
+    n, off = 3, [0, vocab * dim, vocab * dim + tail]
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    X0 = (torch.randn((n, off[2] + 1), generator=gen, device=DEV) * 0.1).to(dtype)
+    G0 = (torch.randn((n, off[2] + 1), generator=gen, device=DEV) * 0.01).to(F32)
+    tok = tokens_of(n, count, vocab, "zipf", 3)
+
+    def steps(wait):
+        X, G = X0.clone()[:, 1:], G0.clone()[:, 1:]
+        emb = choco.Embedding(n, vocab, dim, count, table_ld=off[2] + 1)
+        opt = choco.AdamW(X, G, off, 0.01, state_bits=bits)
+        rows = torch.zeros((n, count, dim), dtype=dtype, device=DEV)
+        norm, factor = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+        torch.cuda.synchronize()
+        for _ in range(25):
+            for call in (lambda: emb.forward(X, tok, rows), lambda: emb.backward(tok, rows, G, accumulate=True),
+                         lambda: opt.grad_norm(1.0, norm, factor), lambda: opt.step(1e-3, factor), lambda: opt.step(1e-3)):
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        result = [X.clone(), G.clone(), rows, norm, factor, opt.m, opt.v]
+        emb.close()
+        opt.close()
+        return result
+
+    want = steps(True)
+    for _ in range(3):
+        for a, b in zip(steps(False), want):
+            assert torch.equal(a, b)
