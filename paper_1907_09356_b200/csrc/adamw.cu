@@ -689,7 +689,10 @@ int allocate(choco_adamw* o, const std::vector<Chunk>& chunks, const std::vector
         o->memory = nullptr;
         return CHOCO_ERR_ALLOC;
     }
-    if (cudaMemcpy(o->memory, first.data(), first.size(), cudaMemcpyHostToDevice) != cudaSuccess) return CHOCO_ERR_CUDA;
+    // a copy from pageable memory may return before it has arrived, and a call on another stream would not wait for it
+    if (cudaMemcpy(o->memory, first.data(), first.size(), cudaMemcpyHostToDevice) != cudaSuccess ||
+        cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess)
+        return CHOCO_ERR_CUDA;
     char* const m = static_cast<char*>(o->memory);
     o->d_tensors = reinterpret_cast<Tensor*>(m + at[0]);
     o->d_chunks = reinterpret_cast<Chunk*>(m + at[1]);

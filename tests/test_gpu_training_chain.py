@@ -44,3 +44,34 @@ def test_chained_calls_see_what_the_call_before_wrote(bits, dtype, vocab, dim, t
     for _ in range(3):
         for a, b in zip(steps(False), want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_new_handle_on_another_stream(bits):
+    """The tables of a handle are on the device when its init returns: the first calls may be on any stream,
+    with nothing between that waits.  A thousand tensors make the copy a long one."""
+    n, sizes = 40, [700 + k for k in range(26)]
+    off = [0]
+    for s in sizes:
+        off.append(off[-1] + s)
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    X0, G = torch.randn((n, off[-1]), generator=gen, device=DEV), torch.randn((n, off[-1]), generator=gen, device=DEV) * 0.01
+    side = torch.cuda.Stream()
+    results = []
+    for k in range(12):
+        X = X0.clone()
+        norm, factor = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+        e = n * sum((s + 255) // 256 * 256 for s in sizes)
+        zeros = lambda count, t: torch.zeros(count, dtype=t, device=DEV)  # noqa: E731
+        states = (zeros(e, F32), zeros(e, F32)) if bits == 32 else (zeros(e, torch.int8), zeros(e, torch.uint8), zeros(e // 256, F32),
+                                                                    zeros(e // 256, F32))
+        torch.cuda.synchronize()
+        opt = choco.AdamW(X, G, off, 0.01, state_bits=bits, states=states)
+        opt.grad_norm(1.0, norm, factor, stream=side)
+        opt.step(1e-3, factor, stream=side)
+        side.synchronize()
+        results.append((X, norm, factor, *states))
+        opt.close()
+    for other in results[1:]:
+        for a, b in zip(results[0], other):
+            assert torch.equal(a, b)
