@@ -512,7 +512,12 @@ int choco_adamw_init(choco_adamw** out, int32_t n_tensors, const choco_adamw_ten
 int choco_adamw_destroy(choco_adamw* opt);
 /* *elements: length of m and v (a multiple of 256); offsets (may be NULL): n_tensors starts. */
 int choco_adamw_state_size(const choco_adamw* opt, int64_t* elements, int64_t* offsets);
-/* New gradient pointers for all tensors (HOST array).  Synchronises `stream`. */
+/*
+ * New gradient pointers for all tensors (HOST array).  Synchronises `stream`.  Graphs captured from
+ * choco_adamw_grad_norm and choco_adamw_step read the new gradients from then on; once a step has been
+ * captured, a gradient cannot move onto a 16-byte boundary or off one where that changes how its
+ * tensor is cut (CHOCO_ERR_UNSUPPORTED, nothing changed).
+ */
 int choco_adamw_set_grads(choco_adamw* opt, const void* const* g, void* stream);
 
 /*
@@ -531,6 +536,8 @@ int choco_adamw_grad_norm(choco_adamw* opt, float max_norm, float unscale, float
  * host synchronisation.  Infinite or NaN gradients that no factor keeps out leave the elements they
  * are in, and with 8-bit moments the blocks, without meaning.  After a step, X has changed outside the gossip step: call choco_invalidate
  * (or run with choco_set_carry(ctx, 0)) before the next choco_gossip_step.
+ * Under stream capture the call counts no step; every replay is a step of its own with the lr of the capture and
+ * the groups' own step numbers, which lie in device memory.  Replays and direct calls may alternate.
  */
 int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* v_scale, double lr,
                      const float* factor, void* stream);

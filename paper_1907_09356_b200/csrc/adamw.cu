@@ -26,8 +26,9 @@ constexpr int kChunkElems = kStepWarps * kBlock;
 // spill up to 44 bytes a thread at 48 registers, three far more); with 32-bit moments two are slower than one (2.09 ms against 2.01 ms).
 template <int BITS>
 constexpr int kBlocksAtOnce = BITS == 8 ? 2 : 1;
-// blocks on an SM: 64 registers a thread with 32-bit moments, 48 with codes, where more warps pay
-constexpr int kStepBlocks32 = 8, kStepBlocks8 = 10, kStepBlocksRest = 6;
+// blocks on an SM: 64 registers a thread with 32-bit moments, 48 with codes, where more warps pay; 72 for single accesses (8 x 65
+// small tensors: 12.1 us, 12.8 with six blocks)
+constexpr int kStepBlocks32 = 8, kStepBlocks8 = 10, kStepBlocksRest = 7;
 constexpr int kNormThreads = 128, kNormThreadsLong = 256; // 8 x 65 small tensors 6.1 us and 7.2 us, 16 x 28.95 M elements 262 us and 256 us
 constexpr int64_t kUnitLong = 16384, kUnitShort = 2048; // elements of a unit of the norms
 constexpr float kCodesM = 127.0f;           // codes k stand for s k^2, k up to 127 (m) and 255 (sqrt v)
@@ -61,6 +62,14 @@ struct Unit {
     int64_t begin;
 };
 
+// Steps of a handle, on the device: counts[0], those that the host has counted (calls that were no capture; written
+// by each), and for every group counts[1 + group], what it has taken fewer than those.  A captured step knows
+// neither when it is captured, so its replays take one off the group's count themselves.
+// Correction: what a captured step multiplies with, one per group.
+struct Correction {
+    float step_size, rsqrt_bc2;
+};
+
 struct StepScalars {
     float beta1, beta2, omb1, omb2, eps;
     float root_beta2, root_omb2; // sqrt(beta2), sqrt(1 - beta2)
@@ -70,9 +79,10 @@ struct StepScalars {
     float log_beta1, log_beta2; // natural logarithms
     int64_t t;
     int64_t whole_elems;    // of a chunk of whole aligned blocks
+    const Correction* corrections; // of a captured step, [groups]; else NULL
 };
 
-inline double pow_int(double b, int64_t e)
+__host__ __device__ inline double pow_int(double b, int64_t e)
 {
     double r = 1.0;
     for (; e > 0; e >>= 1, b *= b)
@@ -360,12 +370,16 @@ __device__ __forceinline__ void finish_block_any(LoadedAny<BITS, XT, GT>& l, con
 }
 
 // What this step multiplies with in one tensor; false: its group sits the step out.
+// (The group's factor and count come as values, so that both are asked for before either is looked at.)
 __device__ __forceinline__ bool factors_of(Factors& f, const Tensor& t, float c, int64_t skipped, const StepScalars& sc)
 {
     f.c = c;
     f.step_size = sc.step_size;
     f.rsqrt_bc2 = sc.rsqrt_bc2;
-    if (skipped != 0) { // this group has taken fewer steps than the others
+    if (sc.corrections) {
+        f.step_size = sc.corrections[t.group].step_size;
+        f.rsqrt_bc2 = sc.corrections[t.group].rsqrt_bc2;
+    } else if (skipped != 0) { // the group has taken another number of steps than the host has counted
         const float n = (float)(sc.t - skipped);
         f.step_size = __fdividef(sc.lr, -expm1f(n * sc.log_beta1));
         f.rsqrt_bc2 = rsqrtf(-expm1f(n * sc.log_beta2));
@@ -375,19 +389,45 @@ __device__ __forceinline__ bool factors_of(Factors& f, const Tensor& t, float c,
     return isfinite(c);
 }
 
+// Where the counts go, unless advance_kernel has seen to them.
+__device__ __forceinline__ void count_call(int64_t* counts, const StepScalars& sc, int32_t beside)
+{
+    if (!beside && !sc.corrections && blockIdx.x == 0 && threadIdx.x == 0) counts[0] = sc.t;
+}
+__device__ __forceinline__ void count_skip(int64_t* counts, const StepScalars& sc, const Chunk& ch, int32_t group)
+{
+    if (!sc.corrections && ch.first && threadIdx.x == 0) counts[1 + group] += 1;
+}
+
+// The launch before a captured step's others: every group's corrections, from the steps it has taken when this
+// runs, in float64 as the host forms them, and its new count.  Direct calls save this launch.
+__global__ void __launch_bounds__(128) advance_kernel(int64_t* counts, const float* factor, Correction* out, int32_t groups, double beta1,
+                                                      double beta2, double lr)
+{
+    wait_for_previous_kernel();
+    allow_next_kernel();
+    const int32_t k = blockIdx.x * 128 + threadIdx.x;
+    if (k >= groups) return;
+    if (factor && !isfinite(factor[k])) return; // sits the step out
+    const int64_t n = counts[0] - counts[1 + k] + 1;
+    out[k] = {(float)(lr / (1.0 - pow_int(beta1, n))), (float)(1.0 / sqrt(1.0 - pow_int(beta2, n)))};
+    counts[1 + k] -= 1;
+}
+
 // A step is, for each pair of types in the list, a launch of `step_rest_kernel` for the blocks that
 // need single accesses and one of `step_kernel` for whole blocks of aligned tensors; most lists need one
 // or two.  (In one kernel the first would set the registers of the others; a stack frame of 160
 // bytes alone cost 40 % of their speed.)  They touch different elements and run side by side: each
 // lets the next start as soon as all that came before the step has ended, and waits for the
 // one before it only at its end.
-// Nobody but the thread that finds `first` looks at the count of a group that sits a step out.
+// Nobody but the thread that finds `first` uses the count of a group that sits a step out, and no direct call
+// reads counts[0].
 
 // one block of threads per chunk, one warp per block of elements
 template <int BITS, typename XT, typename GT>
 __global__ void __launch_bounds__(kStepThreads, kStepBlocksRest)
 step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* factor,
-                 int64_t* skipped, State st, StepScalars sc, int32_t beside)
+                 int64_t* counts, State st, StepScalars sc, int32_t beside)
 {
     const Chunk ch = chunks[blockIdx.x];
     const Tensor t = tensors[ch.tensor];
@@ -399,9 +439,10 @@ step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ c
         LoadedAny<BITS, XT, GT> l;
         load_block_any(l, t, st, base, count);
         Factors f;
-        if (factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc)) finish_block_any(l, t, st, sc, f, base, count);
-        else if (ch.first && threadIdx.x == 0) skipped[t.group] += 1;
+        if (factors_of(f, t, factor ? factor[t.group] : 1.0f, counts[1 + t.group], sc)) finish_block_any(l, t, st, sc, f, base, count);
+        else count_skip(counts, sc, ch, t.group);
     }
+    count_call(counts, sc, beside);
     if (beside) wait_for_previous_kernel();
 }
 
@@ -418,7 +459,7 @@ step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ c
 template <int BITS, typename XT, typename GT>
 __global__ void __launch_bounds__(kStepThreads, BITS == 8 ? kStepBlocks8 : kStepBlocks32)
 step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* factor,
-            int64_t* skipped, State st, StepScalars sc, int32_t beside)
+            int64_t* counts, State st, StepScalars sc, int32_t beside)
 {
     constexpr int N = kBlocksAtOnce<BITS>;
     const Chunk ch = chunks[gridDim.x - 1 - blockIdx.x];
@@ -432,13 +473,14 @@ step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks
     for (int k = 0; k < N; ++k)
         if (base + k * kChunkElems < end) load_block(l[k], t, st, base + k * kChunkElems);
     Factors f;
-    if (factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc)) {
+    if (factors_of(f, t, factor ? factor[t.group] : 1.0f, counts[1 + t.group], sc)) {
 #pragma unroll
         for (int k = 0; k < N; ++k)
             if (base + k * kChunkElems < end) finish_block(l[k], t, st, sc, f, base + k * kChunkElems);
-    } else if (ch.first && threadIdx.x == 0) {
-        skipped[t.group] += 1;
+    } else {
+        count_skip(counts, sc, ch, t.group);
     }
+    count_call(counts, sc, beside);
     if (beside) wait_for_previous_kernel();
 }
 
@@ -447,7 +489,7 @@ step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks
 template <int BITS, typename XT, typename GT>
 __global__ void __launch_bounds__(kStepThreads, kStepBlocksRest)
 step_both_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* factor,
-                 int64_t* skipped, State st, StepScalars sc, int32_t beside)
+                 int64_t* counts, State st, StepScalars sc, int32_t beside)
 {
     const Chunk ch = chunks[blockIdx.x];
     const Tensor t = tensors[ch.tensor];
@@ -461,17 +503,18 @@ step_both_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ c
         if (base < whole) {
             Loaded<BITS, XT, GT> l;
             load_block(l, t, st, base);
-            go = factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc);
+            go = factors_of(f, t, factor ? factor[t.group] : 1.0f, counts[1 + t.group], sc);
             if (go) finish_block(l, t, st, sc, f, base);
         }
     } else if (base < t.numel) {
         const int count = (int)min((int64_t)kBlock, t.numel - base);
         LoadedAny<BITS, XT, GT> l;
         load_block_any(l, t, st, base, count);
-        go = factors_of(f, t, factor ? factor[t.group] : 1.0f, skipped[t.group], sc);
+        go = factors_of(f, t, factor ? factor[t.group] : 1.0f, counts[1 + t.group], sc);
         if (go) finish_block_any(l, t, st, sc, f, base, count);
     }
-    if (!go && ch.first && threadIdx.x == 0) skipped[t.group] += 1;
+    if (!go) count_skip(counts, sc, ch, t.group);
+    count_call(counts, sc, beside);
     if (beside) wait_for_previous_kernel();
 }
 
@@ -647,13 +690,15 @@ struct choco_adamw {
     bool together;                 // a short list: one launch for all blocks of a pair of types
     int64_t whole_elems;           // of a chunk of whole aligned blocks
     int64_t begin[2 * kPairs + 1]; // in d_chunks, for every pair of types: other blocks, whole blocks of aligned tensors
-    int64_t t;                     // step calls so far; a group has taken t - skipped[group] steps
+    int64_t t;                     // step calls so far that were no capture; a group has taken t - d_counts[1 + group] steps
+    bool captured;                 // a graph may hold launches over ranges of d_chunks
     void* memory;                  // all that follows
     Tensor* d_tensors;
     Chunk* d_chunks;               // room for most_chunks
     Unit* d_units;
     int64_t* d_unit_begin;         // [groups + 1]
-    int64_t* d_skipped;            // [groups]
+    int64_t* d_counts;             // [1 + groups]
+    Correction* d_corrections;     // [groups]
     double* d_partial;             // [nunits]
     uint32_t* d_done;              // [groups]
 };
@@ -672,7 +717,7 @@ int allocate(choco_adamw* o, const std::vector<Chunk>& chunks, const std::vector
 {
     const size_t groups = (size_t)o->params.groups;
     std::vector<char> first;
-    size_t at[7];
+    size_t at[8];
     auto place = [&](int k, const void* from, size_t bytes, size_t room) {
         at[k] = (first.size() + 255) / 256 * 256;
         first.resize(at[k] + (room > bytes ? room : bytes), 0);
@@ -682,10 +727,11 @@ int allocate(choco_adamw* o, const std::vector<Chunk>& chunks, const std::vector
     place(1, chunks.data(), sizeof(Chunk) * chunks.size(), sizeof(Chunk) * (size_t)o->most_chunks);
     place(2, units.data(), sizeof(Unit) * units.size(), 0);
     place(3, unit_begin.data(), sizeof(int64_t) * unit_begin.size(), 0);
-    place(4, nullptr, 0, sizeof(int64_t) * groups);
+    place(4, nullptr, 0, sizeof(int64_t) * (1 + groups));
     place(5, nullptr, 0, sizeof(uint32_t) * groups);
-    at[6] = (first.size() + 255) / 256 * 256;
-    if (cudaMalloc(&o->memory, at[6] + sizeof(double) * units.size()) != cudaSuccess) {
+    place(6, nullptr, 0, sizeof(Correction) * groups);
+    at[7] = (first.size() + 255) / 256 * 256;
+    if (cudaMalloc(&o->memory, at[7] + sizeof(double) * units.size()) != cudaSuccess) {
         o->memory = nullptr;
         return CHOCO_ERR_ALLOC;
     }
@@ -698,9 +744,10 @@ int allocate(choco_adamw* o, const std::vector<Chunk>& chunks, const std::vector
     o->d_chunks = reinterpret_cast<Chunk*>(m + at[1]);
     o->d_units = reinterpret_cast<Unit*>(m + at[2]);
     o->d_unit_begin = reinterpret_cast<int64_t*>(m + at[3]);
-    o->d_skipped = reinterpret_cast<int64_t*>(m + at[4]);
+    o->d_counts = reinterpret_cast<int64_t*>(m + at[4]);
     o->d_done = reinterpret_cast<uint32_t*>(m + at[5]);
-    o->d_partial = reinterpret_cast<double*>(m + at[6]);
+    o->d_corrections = reinterpret_cast<Correction*>(m + at[6]);
+    o->d_partial = reinterpret_cast<double*>(m + at[7]);
     return CHOCO_OK;
 }
 
@@ -870,6 +917,7 @@ int choco_adamw_set_grads(choco_adamw* opt, const void* const* g, void* stream)
             moved |= tensors[i].aligned != opt->tensors[i].aligned;
         }
         moved = moved && !opt->norm_only;
+        if (moved && opt->captured) return CHOCO_ERR_UNSUPPORTED; // a replay would find other chunks in the ranges it was captured with
         if (moved) chunks = cut(opt, tensors, begin);
         if (cudaStreamSynchronize(st) != cudaSuccess) return CHOCO_ERR_CUDA;
         // the tables on the device have to agree with each other and with the host's: if one copy fails, no call may use them
@@ -922,14 +970,23 @@ int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* 
     sc.rsqrt_bc2 = (float)(1.0 / std::sqrt(1.0 - pow_int(p.beta2, sc.t)));
     sc.whole_elems = opt->whole_elems;
     cudaStream_t st = (cudaStream_t)stream;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    cudaError_t err = cudaStreamIsCapturing(st, &capture);
+    if (status_of(err) != CHOCO_OK) return CHOCO_ERR_CUDA;
+    const bool capturing = capture != cudaStreamCaptureStatusNone;
+    sc.corrections = capturing ? opt->d_corrections : nullptr;
     const State state = {m, v, m_scale, v_scale};
-    cudaError_t err = cudaSuccess;
+    if (capturing) {
+        opt->captured = true;
+        err = launch_overlapped(advance_kernel, dim3((unsigned)((p.groups + 127) / 128)), dim3(128), 0, st, HotRange{}, opt->d_counts, factor,
+                                opt->d_corrections, p.groups, p.beta1, p.beta2, lr);
+    }
     int32_t beside = 0;
     auto launch = [&](int32_t pair, StepForm form, int64_t begin, int64_t end) {
         if (begin == end || err != cudaSuccess) return;
         const int32_t x = pair / 3, g = pair % 3;
         err = launch_overlapped(eight ? step_kernel_of<8>(x, g, form) : step_kernel_of<32>(x, g, form), dim3((unsigned)(end - begin)),
-                                dim3(kStepThreads), 0, st, HotRange{}, opt->d_tensors, opt->d_chunks + begin, factor, opt->d_skipped,
+                                dim3(kStepThreads), 0, st, HotRange{}, opt->d_tensors, opt->d_chunks + begin, factor, opt->d_counts,
                                 state, sc, beside);
         beside = 1;
     };
@@ -943,7 +1000,7 @@ int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* 
         }
     }
     if (status_of(err) != CHOCO_OK) return CHOCO_ERR_CUDA;
-    opt->t += 1;
+    if (!capturing) opt->t += 1;
     return CHOCO_OK;
 }
 
@@ -968,7 +1025,7 @@ int choco_adamw_get_steps(choco_adamw* opt, int64_t* steps, void* stream)
     if (!opt || !steps || !on_device(opt)) return CHOCO_ERR_INVALID_ARG;
     cudaStream_t st = (cudaStream_t)stream;
     const size_t bytes = sizeof(int64_t) * (size_t)opt->params.groups;
-    if (cudaMemcpyAsync(steps, opt->d_skipped, bytes, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+    if (cudaMemcpyAsync(steps, opt->d_counts + 1, bytes, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
         cudaStreamSynchronize(st) != cudaSuccess)
         return CHOCO_ERR_CUDA;
     for (int32_t k = 0; k < opt->params.groups; ++k) steps[k] = opt->t - steps[k];
@@ -985,10 +1042,10 @@ int choco_adamw_set_steps(choco_adamw* opt, const int64_t* steps, void* stream)
     }
     cudaStream_t st = (cudaStream_t)stream;
     try {
-        std::vector<int64_t> skipped(opt->params.groups);
-        for (int32_t k = 0; k < opt->params.groups; ++k) skipped[k] = most - steps[k];
-        if (cudaMemcpyAsync(opt->d_skipped, skipped.data(), sizeof(int64_t) * skipped.size(), cudaMemcpyHostToDevice, st) !=
-                cudaSuccess ||
+        std::vector<int64_t> counts(1 + (size_t)opt->params.groups);
+        counts[0] = most;
+        for (int32_t k = 0; k < opt->params.groups; ++k) counts[1 + k] = most - steps[k];
+        if (cudaMemcpyAsync(opt->d_counts, counts.data(), sizeof(int64_t) * counts.size(), cudaMemcpyHostToDevice, st) != cudaSuccess ||
             cudaStreamSynchronize(st) != cudaSuccess)
             return CHOCO_ERR_CUDA;
     } catch (const std::exception&) {
