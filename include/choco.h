@@ -485,7 +485,7 @@ typedef struct {
 } choco_adamw_tensor;
 typedef struct {
     double beta1, beta2;  /* in [0, 1)                                                           */
-    double eps;           /* > 0                                                                 */
+    double eps;           /* > 0 as a float32 (with 8-bit moments: >= 2^-126)                     */
     int32_t state_bits;   /* 32 or 8                                                             */
     int32_t groups;       /* >= 1                                                                */
 } choco_adamw_params;

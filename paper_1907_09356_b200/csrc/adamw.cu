@@ -5,6 +5,7 @@
 // where a long list has 8-bit moments and the chunk is of whole aligned blocks); a table in device memory says which tensor a chunk belongs to, so that one launch serves all tensors of all
 // workers whatever their sizes.  Inside a chunk every warp owns blocks of kBlock = 256 elements, the
 // unit that shares a scale in 8 bits.
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -96,13 +97,19 @@ __device__ __forceinline__ float warp_max(float v)
     return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
 }
 
-__device__ __forceinline__ float root_approx(float v) // within 2^-22 of sqrt(v)
+__device__ __forceinline__ float root_approx(float v) // within 2^-22 of sqrt(v); subnormal numbers are taken for 0
 {
     float r;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-__device__ __forceinline__ float reciprocal_approx(float v) // within 2^-22 of 1 / v
+__device__ __forceinline__ float root_approx_any(float v) // the same without that exception
+{
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float reciprocal_approx(float v) // within 2^-22 of 1 / v, v not subnormal
 {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
@@ -215,7 +222,7 @@ __device__ __forceinline__ void update8_codes(const StepScalars& sc, const Facto
     for (int e = 0; e < 8; ++e) {
         m[e] = __fmaf_rn(square_m(m[e]), sm1, g[e] * gm);
         const float r0 = square_v(v[e]) * sv2, q = g[e] * gv;
-        v[e] = root_approx(__fmaf_rn(r0, r0, q * q));
+        v[e] = root_approx_any(__fmaf_rn(r0, r0, q * q)); // gradients of 1e-19 have subnormal squares, and a root of 1e-20
         const float ratio = m[e] * reciprocal_approx(__fmaf_rn(v[e], f.rsqrt_bc2, sc.eps));
         x[e] = __fmaf_rn(-f.step_size, ratio, __fmaf_rn(-f.decay, x[e], x[e]));
         amax = fmaxf(amax, fabsf(m[e]));
@@ -856,6 +863,7 @@ int choco_adamw_init(choco_adamw** out, int32_t n_tensors, const choco_adamw_ten
     if (!(p->beta1 >= 0.0 && p->beta1 < 1.0) || !(p->beta2 >= 0.0 && p->beta2 < 1.0) || !((float)p->eps > 0.f) || !std::isfinite((float)p->eps))
         return CHOCO_ERR_INVALID_ARG;
     if (p->state_bits != 32 && p->state_bits != 8) return CHOCO_ERR_UNSUPPORTED;
+    if (p->state_bits == 8 && (float)p->eps < FLT_MIN) return CHOCO_ERR_INVALID_ARG; // the approximate quotient takes it for 0
     choco_adamw* o = new (std::nothrow) choco_adamw();
     if (!o) return CHOCO_ERR_ALLOC;
     o->params = *p;

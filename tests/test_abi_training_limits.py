@@ -1,0 +1,11 @@
+"""Limits that the init calls of the token tables and of AdamW state (no GPU needed)."""
+import pytest
+
+from test_abi_training_ops import _adamw, lib  # noqa: F401
+
+
+@pytest.mark.parametrize("eps", [1e-39, 1.1754942e-38, 1e-45])
+def test_eps_of_8_bit_moments_is_no_subnormal_number(lib, eps):  # noqa: F811
+    assert _adamw(lib, eps=eps, bits=8) == -1
+    assert _adamw(lib, eps=2.0 ** -126, bits=8) != -1            # (there may be no device to go on with)
+    assert _adamw(lib, eps=eps, bits=32) != -1

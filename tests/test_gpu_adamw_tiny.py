@@ -1,0 +1,49 @@
+"""AdamW where squares of gradients are subnormal numbers and eps is far below them."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1907_09356_b200 as choco
+from test_gpu_adamw import B1, B2, DEV, U
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-30, 2.0 ** -126])
+def test_gradients_with_subnormal_squares(bits, eps):
+    """First step from zeroed moments: m / sqrt(v) is the sign, whatever the size, so x moves by -lr sign.  v is
+    rounded to the subnormal grid, 2^-149 apart, twice; its root is off by half of that share of v, m and the
+    quotient by the roundings of test_gpu_adamw or the approximations' 2^-22 each (four of them)."""
+    d, lr = 1000, 1e-2
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    size = torch.logspace(-19, -17, d, dtype=torch.float64, device=DEV)
+    sign = torch.where(torch.rand(d, generator=gen, device=DEV) < 0.5, -1.0, 1.0)
+    G = (size * sign).float()[None]
+    X = torch.zeros((1, d), device=DEV)
+    opt = choco.AdamW(X, G, [0, d], eps=eps, beta1=B1, beta2=B2, state_bits=bits)
+    opt.step(lr)
+    v = (1 - B2) * G.double() ** 2
+    share = 0.5 * 2 * 2.0 ** -149 / v + 20 * U + (4 * 2.0 ** -22 if bits == 8 else 0.0)
+    assert bool(((X.double() / (-lr * sign.double()) - 1).abs() <= 1.01 * share).all())
+    for _ in range(3):
+        opt.step(lr)
+    assert bool(torch.isfinite(X).all()) and float(X.abs().max()) < 40 * lr   # nothing is divided by eps alone
+    opt.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_smallest_eps_divides_zeros(bits):
+    """m = v = 0 with the smallest eps allowed: 0 / eps is 0."""
+    eps = 2.0 ** -126 if bits == 8 else 1e-44
+    X = torch.ones((2, 700), device=DEV)
+    G = torch.zeros((2, 700), device=DEV)
+    G[1, ::3] = 1e-3
+    opt = choco.AdamW(X, G, np.array([0, 300, 700]), eps=eps, state_bits=bits)
+    for _ in range(3):
+        opt.step(1e-2)
+    assert bool((X[0] == 1).all()) and bool(torch.isfinite(X).all())
+    still = torch.ones(700, dtype=torch.bool, device=DEV)
+    still[::3] = False
+    assert bool((X[1][still] == 1).all()) and bool((X[1][~still] < 1).all())
+    opt.close()
