@@ -666,13 +666,14 @@ norm_kernel(const Tensor* __restrict__ tensors, const Unit* __restrict__ units, 
     if (threadIdx.x == 0) {
         o.done[u.group] = 0;
         const double nrm = (double)o.unscale * sqrt(acc);
-        o.norm[u.group] = (float)nrm;
+        const float rounded = (float)nrm; // infinite above float32's largest number too
+        o.norm[u.group] = rounded;
         double f = (double)o.unscale;
         if (o.max_norm > 0.f) {
             const double clip = (double)o.max_norm / (nrm + kNormEps);
             f *= clip < 1.0 ? clip : 1.0;
         }
-        o.factor[u.group] = isfinite(nrm) ? (float)f : __int_as_float(0x7fc00000);
+        o.factor[u.group] = isfinite(rounded) ? (float)f : __int_as_float(0x7fc00000);
     }
 }
 

@@ -1,4 +1,5 @@
-"""AdamW where squares of gradients are subnormal numbers and eps is far below them."""
+"""AdamW at the ends of the range: gradients with subnormal squares and an eps far below them, norms that float32
+cannot hold."""
 import numpy as np
 import pytest
 import torch
@@ -46,4 +47,30 @@ def test_the_smallest_eps_divides_zeros(bits):
     still = torch.ones(700, dtype=torch.bool, device=DEV)
     still[::3] = False
     assert bool((X[1][still] == 1).all()) and bool((X[1][~still] < 1).all())
+    opt.close()
+
+
+def test_a_norm_beyond_float32_is_infinite_and_its_factor_nan():
+    """Finite gradients whose norm only float64 can hold: the group sits the step out, as it does with infinite ones.
+    One whose norm is just below float32's largest number, 3.4028e38, keeps its factor; unscale counts."""
+    G = torch.zeros((4, 300), device=DEV)
+    G[0, :2] = 3e38                                              # norm 4.2e38
+    G[1, :2] = 2.4e38                                            # 3.394e38
+    G[2, :] = 3e38                                               # 5.2e39, times unscale 1.3e39 and 5.2e37
+    G[3, 7] = 1.0
+    X = torch.ones((4, 300), device=DEV)
+    opt = choco.AdamW(X, G, [0, 300])
+    norm, factor = torch.zeros(4, device=DEV), torch.zeros(4, device=DEV)
+    for unscale, over in ((1.0, [0, 2]), (0.25, [2]), (0.01, [])):
+        opt.grad_norm(1.0, norm, factor, unscale)
+        for k in range(4):
+            want = float(G[k].double().norm()) * unscale
+            if k in over:
+                assert float(norm[k]) == float("inf") and bool(torch.isnan(factor[k]))
+            else:
+                assert abs(float(norm[k]) - want) <= 2 * U * want and bool(torch.isfinite(factor[k]))
+        kept = X.clone()
+        opt.step(1e-3, factor)
+        for k in over:
+            assert torch.equal(X[k], kept[k])
     opt.close()
