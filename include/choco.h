@@ -439,7 +439,9 @@ int choco_embedding_destroy(choco_embedding* emb);
  *   tokens     DEVICE, int32 (index_bits = 32) or int64 (64), `count` >= 0 per worker (no limit
  *              but n count < 2^31), rows `tokens_ld` >= count elements apart, or 0: the same tokens
  *              for all workers.
- *   out        DEVICE; element (i, t, c) at i out_ld + t out_row + c; out_row >= dim.
+ *   out        DEVICE; element (i, t, c) at i out_ld + t out_row + c; out_row >= dim; no element belongs to two
+ *              (i, t): workers' blocks after one another or rows of all workers in turn, for instance
+ *              (CHOCO_ERR_INVALID_ARG where rows overlap).
  * Table, tokens and out do not overlap.
  */
 int choco_embedding_forward(choco_embedding* emb, const void* table, int32_t table_dtype, const void* tokens,
@@ -504,8 +506,8 @@ typedef struct {
  *                     divides by eps alone).  Codes and scales of zero are moments of zero: a
  *                     fresh run starts from zeroed arrays.
  * m and v (and the 8-bit codes) are 16-byte aligned, the scales 4-byte.
- * The list is copied; the tensors it points to have to stay where they are and not overlap (but for
- * gradients, which are only read).
+ * The list is copied; the tensors it points to have to stay where they are.  x and copy of a tensor overlap
+ * nothing else in the list (CHOCO_ERR_INVALID_ARG); gradients, which are only read, may overlap each other.
  */
 int choco_adamw_init(choco_adamw** out, int32_t n_tensors, const choco_adamw_tensor* tensors,
                      const choco_adamw_params* p);

@@ -5,6 +5,7 @@
 // where a long list has 8-bit moments and the chunk is of whole aligned blocks); a table in device memory says which tensor a chunk belongs to, so that one launch serves all tensors of all
 // workers whatever their sizes.  Inside a chunk every warp owns blocks of kBlock = 256 elements, the
 // unit that shares a scale in 8 bits.
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 #include <cstring>
@@ -685,12 +686,19 @@ norm_kernel(const Tensor* __restrict__ tensors, const Unit* __restrict__ units, 
 constexpr int64_t kTogether32 = 32768, kTogether8 = 8192;
 constexpr int kPairs = 9;               // of types: 3 x_dtype + g_dtype
 
+namespace {
+struct Range { // of addresses
+    uintptr_t begin, end;
+};
+} // namespace
+
 struct choco_adamw {
     choco_adamw_params params;
     int device;
     bool norm_only;                // no parameters: the list serves choco_adamw_grad_norm alone
     bool broken;                   // the tables on the device may be half written (a copy of new ones failed)
     std::vector<Tensor> tensors;   // as on the device
+    std::vector<Range> written;    // by a step, in order of their addresses
     std::vector<int64_t> offsets;
     int64_t elements;              // of m and v
     std::vector<int32_t> by_group;  // tensors with elements, group after group
@@ -774,6 +782,32 @@ void free_all(choco_adamw* o)
 
 bool all_aligned(const Tensor& t) { return aligned_to(t.x, 16) && aligned_to(t.g, 16) && aligned_to(t.copy, 16); }
 
+Range range_of(const void* p, int64_t numel, int32_t dtype)
+{
+    return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)(numel * dtype_size(dtype))};
+}
+// What a step writes, in order; false if two of these arrays share memory.  Throws std::bad_alloc.
+bool collect_written(choco_adamw* o)
+{
+    std::vector<Range>& w = o->written;
+    for (const Tensor& t : o->tensors) {
+        if (t.numel > 0 && t.x) w.push_back(range_of(t.x, t.numel, t.x_dtype));
+        if (t.numel > 0 && t.copy) w.push_back(range_of(t.copy, t.numel, t.copy_dtype));
+    }
+    std::sort(w.begin(), w.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+    for (size_t i = 1; i < w.size(); ++i)
+        if (w[i].begin < w[i - 1].end) return false;
+    return true;
+}
+bool is_written(const choco_adamw* o, const Tensor& t, const void* g)
+{
+    if (t.numel == 0) return false;
+    const Range r = range_of(g, t.numel, t.g_dtype);
+    // of the arrays that begin before r ends the last one reaches furthest
+    auto next = std::lower_bound(o->written.begin(), o->written.end(), r.end, [](const Range& a, uintptr_t e) { return a.begin < e; });
+    return next != o->written.begin() && (next - 1)->end > r.begin;
+}
+
 // Fills the host tables of `o`.  Throws std::bad_alloc.
 int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Unit>& units, std::vector<int64_t>& unit_begin)
 {
@@ -809,6 +843,11 @@ int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Un
         if (t.numel > 0) members[t.group].push_back(i);
     }
     o->elements = at;
+    if (!o->norm_only) {
+        if (!collect_written(o)) return CHOCO_ERR_INVALID_ARG;
+        for (const Tensor& t : o->tensors)
+            if (is_written(o, t, t.g)) return CHOCO_ERR_INVALID_ARG;
+    }
     // short units where the whole list has fewer than four long ones for each SM
     o->unit_elems = total >= kUnitLong * 4 * 148 ? kUnitLong : kUnitShort;
     for (int32_t k = 0; k < groups; ++k) {
@@ -910,6 +949,7 @@ int choco_adamw_set_grads(choco_adamw* opt, const void* const* g, void* stream)
     for (size_t i = 0; i < opt->tensors.size(); ++i) {
         if (opt->tensors[i].numel > 0 && !g[i]) return CHOCO_ERR_INVALID_ARG;
         if (!aligned_to(g[i], dtype_size(opt->tensors[i].g_dtype))) return CHOCO_ERR_MISALIGNED;
+        if (is_written(opt, opt->tensors[i], g[i])) return CHOCO_ERR_INVALID_ARG;
     }
     cudaStream_t st = (cudaStream_t)stream;
     auto send = [&](auto* to, const auto& from) {

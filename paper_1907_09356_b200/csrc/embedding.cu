@@ -969,6 +969,20 @@ int check_tokens(const choco_embedding* e, const void* tokens, int32_t bits, int
     return CHOCO_OK;
 }
 
+// Whether two of the rows [i, t], i < n, t < count, at i ld + t row, of `dim` elements each share one (ld, row >= 0).
+bool rows_overlap(int64_t n, int64_t count, int64_t dim, int64_t ld, int64_t row)
+{
+    using wide = __int128;
+    if (count > 1 && row < dim) return true;
+    if (n == 1 || ld >= (wide)(count - 1) * row + dim) return false;          // worker after worker
+    if (ld >= dim && row >= (wide)(n - 1) * ld + dim) return false;           // token after token
+    for (int64_t i = 1; i < n; ++i) { // row t of worker 0 and the rows of worker i on either side of it
+        const wide at = (wide)i * ld, t = at / row, over = at % row;
+        if ((t < count && over < dim) || (t + 1 < count && row - over < dim)) return true;
+    }
+    return false;
+}
+
 // (8 x 2240 rows of 650 added: 33.6 us in tiles of 16, 35.5 us of 32; 4 x 1000 rows of 200: 17.4 us of 8, 18.9 us of 16)
 int tile_of(int64_t rows) { return rows <= kShortRows ? kTileShort : rows <= kMidRows ? kTileMid : kTileLong; }
 
@@ -1143,6 +1157,7 @@ int choco_embedding_forward(choco_embedding* emb, const void* table, int32_t tab
     const int rc = check_tokens(emb, tokens, index_bits, count, tokens_ld);
     if (rc != CHOCO_OK) return rc;
     if (count > 0 && (!out || out_row < emb->p.dim || (emb->p.n > 1 && out_ld < 0))) return CHOCO_ERR_INVALID_ARG;
+    if (count > 0 && rows_overlap(emb->p.n, count, emb->p.dim, out_ld, out_row)) return CHOCO_ERR_INVALID_ARG;
     if (!aligned_to(table, dtype_size(table_dtype)) || !aligned_to(out, dtype_size(out_dtype))) return CHOCO_ERR_MISALIGNED;
     if (count == 0) return CHOCO_OK;
     const EmbShape s = shape_of(emb, count);
