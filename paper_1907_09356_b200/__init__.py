@@ -195,13 +195,12 @@ def _stream_of(stream, device: int) -> Optional[int]:
     return stream.cuda_stream or None
 
 
-def _on_one_device(what: str, *tensors) -> int:
-    """Index of the GPU that all of them are on."""
-    device = tensors[0].get_device()
+def _on_one_device(what: str, *tensors, of: int) -> int:
+    """`of`, the index of the handle's GPU, which all of them are on."""
     for t in tensors:
-        if t.get_device() != device or device < 0:
-            raise ChocoError(f"libchoco: {what} must be on one GPU", -1)
-    return device
+        if t.get_device() != of:
+            raise ChocoError(f"libchoco: {what} must be on one GPU, that of the handle ({of})", -1)
+    return of
 
 
 # --------------------------------------------------------------------------- C names
@@ -458,10 +457,9 @@ def _index_bits(t) -> int:
 
 def _token_rows(tokens, rows, n, dim) -> tuple:
     """(tokens per worker, stride of the tokens' rows, strides of `rows` from token to token and from
-    worker to worker) for tokens [n, T] and rows [n, T, dim] with unit stride inside their rows;
-    n and dim None: whatever they are."""
+    worker to worker) for tokens [n, T] and rows [n, T, dim] with unit stride inside their rows."""
     a, b = tokens.shape, rows.shape
-    if len(a) == 2 and len(b) == 3 and a[0] == b[0] == (n or a[0]) and a[1] == b[1] and b[2] == (dim or b[2]):
+    if len(a) == 2 and len(b) == 3 and a[0] == b[0] == n and a[1] == b[1] and b[2] == dim:
         count = a[1]
         ld, one = tokens.stride()
         worker, row, inside = rows.stride()
@@ -469,16 +467,49 @@ def _token_rows(tokens, rows, n, dim) -> tuple:
             return 0, ld, b[2], 0
         if (one == 1 or count == 1) and (inside == 1 or b[2] == 1):
             return count, ld, (row if count > 1 else max(b[2], row)), worker
-    raise ChocoError(f"libchoco: tokens must be [{n or 'n'}, T] and the rows [{n or 'n'}, T, {dim or 'dim'}], both contiguous inside "
+    raise ChocoError(f"libchoco: tokens must be [{n}, T] and the rows [{n}, T, {dim}], both contiguous inside "
                      f"their rows, not {list(a)} and {list(b)}", -1)
+
+
+class EmbeddingHandle(ctypes.c_void_p):
+    """What choco_embedding_init returns: the library's handle, with the device it belongs to and the layout of
+    the tables it serves."""
+
+    def describe(self, device: int, n: int, vocab: int, dim: int, table_row: int, table_ld: int) -> None:
+        self.device, self.n, self.vocab, self.dim = device, n, vocab, dim
+        self.table_row = table_row or dim
+        self.table_ld = table_ld or vocab * self.table_row
+        self.table_span = (vocab - 1) * self.table_row + dim      # elements from a table's first to its last
+
+
+def _check_table(emb, what: str, t) -> None:
+    """The arrays whose address alone goes to the library hold all n tables, where the handle says: rows of X or G
+    [n, >= span], tables [n, vocab, dim], one table [vocab, dim], or the elements in a row."""
+    shape, strides, n = t.shape, t.stride(), emb.n
+    k = len(shape)
+    if k == 2:
+        if shape[0] >= n and shape[1] >= emb.table_span and (strides[1] == 1 or shape[1] == 1) and (strides[0] == emb.table_ld or n == 1):
+            return
+        if n == 1 and shape[0] >= emb.vocab and shape[1] >= emb.dim and strides == (emb.table_row, 1):
+            return
+    elif k == 3:
+        if shape[0] >= n and shape[1] >= emb.vocab and shape[2] >= emb.dim and (strides[0] == emb.table_ld or n == 1) and (
+                strides[1] == emb.table_row or emb.vocab == 1) and (strides[2] == 1 or emb.dim == 1):
+            return
+    elif k == 1 and shape[0] >= (n - 1) * emb.table_ld + emb.table_span and strides[0] == 1:
+        return
+    raise ChocoError(f"libchoco: {what} of {list(shape)}, strides {list(strides)}, does not hold {n} tables of {emb.vocab} x {emb.dim} with rows "
+                     f"{emb.table_row} and tables {emb.table_ld} elements apart", -1)
 
 
 def choco_embedding_init(n: int, vocab: int, dim: int, max_tokens: int, table_row: int = 0, table_ld: int = 0,
                          scale: float = 1.0, padding: int = -1):
-    """Handle for the token tables of n workers (see choco.h); max_tokens = 0 serves lookups only."""
+    """Handle for the token tables of n workers (see choco.h) on the current device; max_tokens = 0 serves lookups only."""
+    import torch
     p = choco_embedding_params(n, scale, vocab, dim, table_row, table_ld, max_tokens, padding)
-    h = ctypes.c_void_p()
+    h = EmbeddingHandle()
     _check(load().choco_embedding_init(ctypes.byref(h), ctypes.byref(p)))
+    h.describe(torch.cuda.current_device(), n, vocab, dim, table_row, table_ld)
     return h
 
 
@@ -488,17 +519,23 @@ def choco_embedding_destroy(emb) -> None:
 
 def choco_embedding_forward(emb, table, tokens, out, stream=None, n=None, dim=None) -> None:
     """out[i, t] = scale * table_i[tokens[i, t]].  `table` is a tensor that starts at worker 0's first
-    row; tokens [n, T] int32 or int64; out [n, T, dim]."""
-    count, tokens_ld, row, ld = _token_rows(tokens, out, n, dim)
-    device = _on_one_device("table, tokens and out", out, tokens, table)
+    row; tokens [n, T] int32 or int64; out [n, T, dim].  n and dim, if given, are the handle's."""
+    if (n or emb.n) != emb.n or (dim or emb.dim) != emb.dim:
+        raise ChocoError(f"libchoco: the handle is for n = {emb.n}, dim = {emb.dim}", -1)
+    count, tokens_ld, row, ld = _token_rows(tokens, out, emb.n, emb.dim)
+    device = _on_one_device("table, tokens and out", out, tokens, table, of=emb.device)
+    _check_table(emb, "a table", table)
     _check(load().choco_embedding_forward(emb, table.data_ptr(), _dtype(table), tokens.data_ptr(), _index_bits(tokens), count,
                                           tokens_ld, out.data_ptr(), _dtype(out), row, ld, _stream_of(stream, device)))
 
 
 def choco_embedding_backward(emb, tokens, dout, grad, accumulate: bool = False, stream=None, n=None, dim=None) -> None:
     """grad_i[r] (+)= scale * sum of dout[i, t] over the t with tokens[i, t] = r, in the table's layout."""
-    count, tokens_ld, row, ld = _token_rows(tokens, dout, n, dim)
-    device = _on_one_device("tokens, dout and grad", grad, tokens, dout)
+    if (n or emb.n) != emb.n or (dim or emb.dim) != emb.dim:
+        raise ChocoError(f"libchoco: the handle is for n = {emb.n}, dim = {emb.dim}", -1)
+    count, tokens_ld, row, ld = _token_rows(tokens, dout, emb.n, emb.dim)
+    device = _on_one_device("tokens, dout and grad", grad, tokens, dout, of=emb.device)
+    _check_table(emb, "a grad", grad)
     _check(load().choco_embedding_backward(emb, tokens.data_ptr(), _index_bits(tokens), count, tokens_ld, dout.data_ptr(),
                                            _dtype(dout), row, ld, grad.data_ptr(), _dtype(grad), 1 if accumulate else 0,
                                            _stream_of(stream, device)))
@@ -536,7 +573,7 @@ def choco_adamw_set_grads(opt, pointers, stream=None) -> None:
 
 
 def choco_adamw_grad_norm(opt, max_norm: float, norm, factor, unscale: float = 1.0, stream=None) -> None:
-    device = _on_one_device("norm and factor", norm, factor)
+    device = _on_one_device("norm and factor", norm, factor, of=norm.get_device() if norm.is_cuda else 0)
     _check(load().choco_adamw_grad_norm(opt, max_norm, unscale, norm.data_ptr(), factor.data_ptr(), _stream_of(stream, device)))
 
 
@@ -650,10 +687,10 @@ class Embedding:
         self.handle = choco_embedding_init(n, vocab, dim, max_tokens, table_row, table_ld, scale, padding)
 
     def forward(self, table, tokens, out, stream=None):
-        choco_embedding_forward(self.handle, table, tokens, out, stream, self.n, self.dim)
+        choco_embedding_forward(self.handle, table, tokens, out, stream)
 
     def backward(self, tokens, dout, grad, accumulate: bool = False, stream=None):
-        choco_embedding_backward(self.handle, tokens, dout, grad, accumulate, stream, self.n, self.dim)
+        choco_embedding_backward(self.handle, tokens, dout, grad, accumulate, stream)
 
     def close(self):
         if getattr(self, "handle", None) is not None:
