@@ -541,14 +541,52 @@ def choco_embedding_backward(emb, tokens, dout, grad, accumulate: bool = False, 
                                            _stream_of(stream, device)))
 
 
+class AdamWHandle(ctypes.c_void_p):
+    """What choco_adamw_init returns: the library's handle, with the device it belongs to and the sizes of what its
+    calls take."""
+
+    def describe(self, device: int, n_tensors: int, groups: int, state_bits: int, elements: int) -> None:
+        self.device, self.n_tensors, self.groups, self.state_bits, self.elements = device, n_tensors, groups, state_bits, elements
+
+    def state_arrays(self) -> list:
+        """(type, length) of m, v and, with 8-bit moments, their scales."""
+        if self.state_bits == 32:
+            return [("float32", self.elements)] * 2
+        scales = ("float32", self.elements // ADAMW_BLOCK)
+        return [("int8", self.elements), ("uint8", self.elements), scales, scales]
+
+
+def _check_groups(opt, what: str, *tensors) -> None:
+    """Arrays of one float32 per group."""
+    for t in tensors:
+        if t.get_device() != opt.device or _dtype(t) != 0 or t.numel() < opt.groups or not t.is_contiguous():
+            raise ChocoError(f"libchoco: {what} must be contiguous float32 with one element for each of {opt.groups} groups, on GPU {opt.device}, "
+                             f"not {t.dtype} {list(t.shape)} on {t.device}", -1)
+
+
+def _check_states(opt, states, need: bool = True) -> None:
+    """Moments as the handle's calls take them: (m, v) or (m, v, m_scale, v_scale), all of them if `need`."""
+    want = opt.state_arrays()
+    got = [None if a is None else (str(a.dtype).rpartition(".")[2], a.numel()) for a in states]
+    good = len(got) >= len(want) and not any(got[len(want):])
+    for a, g, w in zip(states, got, want):
+        good = good and (g is None and (not need or opt.elements == 0) or g == w and a.is_contiguous() and a.get_device() == opt.device)
+    if not good:
+        raise ChocoError(f"libchoco: the moments must be contiguous arrays of {want} on GPU {opt.device}, not {got} on "
+                         f"{[str(a.device) for a in states if a is not None]}", -1)
+
+
 def choco_adamw_init(tensors, groups: int = 1, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                      state_bits: int = 32):
-    """tensors: numpy array of ADAMW_TENSOR records (see adamw_layer_tensors)."""
+    """tensors: numpy array of ADAMW_TENSOR records (see adamw_layer_tensors), on the current device."""
     import numpy as np
+    import torch
     t = np.ascontiguousarray(tensors, dtype=ADAMW_TENSOR)
     p = choco_adamw_params(beta1, beta2, eps, state_bits, groups)
-    h = ctypes.c_void_p()
+    h, e = AdamWHandle(), ctypes.c_int64()
     _check(load().choco_adamw_init(ctypes.byref(h), len(t), t.ctypes.data if len(t) else None, ctypes.byref(p)))
+    _check(load().choco_adamw_state_size(h, ctypes.byref(e), None))
+    h.describe(torch.cuda.current_device(), len(t), groups, state_bits, e.value)
     return h
 
 
@@ -559,6 +597,8 @@ def choco_adamw_destroy(opt) -> None:
 def choco_adamw_state_size(opt, n_tensors: int = 0):
     """(elements of the moments, first element of every tensor: an int64 array of n_tensors, all of the list)."""
     import numpy as np
+    if n_tensors not in (0, opt.n_tensors):
+        raise ChocoError(f"libchoco: the list has {opt.n_tensors} tensors, not {n_tensors}", -1)
     e = ctypes.c_int64()
     off = np.zeros(n_tensors, dtype=np.int64)
     _check(load().choco_adamw_state_size(opt, ctypes.byref(e), off.ctypes.data if n_tensors else None))
@@ -569,45 +609,62 @@ def choco_adamw_set_grads(opt, pointers, stream=None) -> None:
     """New gradient addresses, one per tensor of the list."""
     import numpy as np
     g = np.ascontiguousarray(pointers, dtype=np.uint64)
-    _check(load().choco_adamw_set_grads(opt, g.ctypes.data, _stream(stream)))
+    if g.shape != (opt.n_tensors,):
+        raise ChocoError(f"libchoco: one address for each of {opt.n_tensors} tensors", -1)
+    _check(load().choco_adamw_set_grads(opt, g.ctypes.data, _stream_of(stream, opt.device)))
 
 
 def choco_adamw_grad_norm(opt, max_norm: float, norm, factor, unscale: float = 1.0, stream=None) -> None:
-    device = _on_one_device("norm and factor", norm, factor, of=norm.get_device() if norm.is_cuda else 0)
-    _check(load().choco_adamw_grad_norm(opt, max_norm, unscale, norm.data_ptr(), factor.data_ptr(), _stream_of(stream, device)))
+    _check_groups(opt, "norm and factor", norm, factor)
+    _check(load().choco_adamw_grad_norm(opt, max_norm, unscale, norm.data_ptr(), factor.data_ptr(), _stream_of(stream, opt.device)))
 
 
 def choco_adamw_step(opt, m, v, m_scale, v_scale, lr: float, factor=None, stream=None) -> None:
-    for t in (m, v, m_scale, v_scale, factor):
-        if t is not None and not t.is_cuda:
-            raise ChocoError("libchoco: moments and factor must be on the GPU", -1)
-    _check(load().choco_adamw_step(opt, _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), lr, _ptr(factor), _stream(stream)))
+    _check_states(opt, (m, v, m_scale, v_scale))
+    _adamw_step(opt, m, v, m_scale, v_scale, lr, factor, stream)
+
+
+def _adamw_step(opt, m, v, m_scale, v_scale, lr, factor, stream) -> None:
+    """The step with moments that have been checked."""
+    if factor is not None:
+        _check_groups(opt, "factor", factor)
+    _check(load().choco_adamw_step(opt, _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), lr, _ptr(factor), _stream_of(stream, opt.device)))
 
 
 def choco_adamw_read_state(opt, m, v, m_scale, v_scale, m_out, v_out, stream=None) -> None:
     """The values of the moments; m_out and v_out (either may be None) have one type."""
+    _check_states(opt, (m, v, m_scale, v_scale), need=False)
+    _adamw_read_state(opt, m, v, m_scale, v_scale, m_out, v_out, stream)
+
+
+def _adamw_read_state(opt, m, v, m_scale, v_scale, m_out, v_out, stream) -> None:
+    """The same with moments that have been checked."""
     out = m_out if m_out is not None else v_out
     if m_out is not None and v_out is not None and m_out.dtype != v_out.dtype:
         raise ChocoError("libchoco: m_out and v_out have one type", -1)
-    for t in (m, v, m_scale, v_scale, m_out, v_out):
-        if t is not None and not t.is_cuda:
-            raise ChocoError("libchoco: moments and outputs must be on the GPU", -1)
+    for t in (m_out, v_out):
+        if t is not None and (t.get_device() != opt.device or t.numel() != opt.elements or not t.is_contiguous()):
+            raise ChocoError(f"libchoco: outputs must be contiguous with {opt.elements} elements on GPU {opt.device}", -1)
     _check(load().choco_adamw_read_state(opt, _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), _ptr(m_out), _ptr(v_out),
-                                         0 if out is None else _dtype(out), _stream(stream)))
+                                         0 if out is None else _dtype(out), _stream_of(stream, opt.device)))
 
 
 def choco_adamw_get_steps(opt, groups: int, stream=None):
     """Steps that every group has taken (int64 array)."""
     import numpy as np
+    if groups != opt.groups:
+        raise ChocoError(f"libchoco: the list has {opt.groups} groups, not {groups}", -1)
     steps = np.zeros(groups, dtype=np.int64)
-    _check(load().choco_adamw_get_steps(opt, steps.ctypes.data, _stream(stream)))
+    _check(load().choco_adamw_get_steps(opt, steps.ctypes.data, _stream_of(stream, opt.device)))
     return steps
 
 
 def choco_adamw_set_steps(opt, steps, stream=None) -> None:
     import numpy as np
     s = np.ascontiguousarray(steps, dtype=np.int64)
-    _check(load().choco_adamw_set_steps(opt, s.ctypes.data, _stream(stream)))
+    if s.shape != (opt.groups,):
+        raise ChocoError(f"libchoco: one step count for each of {opt.groups} groups", -1)
+    _check(load().choco_adamw_set_steps(opt, s.ctypes.data, _stream_of(stream, opt.device)))
 
 
 # --------------------------------------------------------------------------- convenience
@@ -627,6 +684,8 @@ def adamw_layer_tensors(X, G, layer_off, weight_decay=0.0, lr_scale=1.0, copy=No
     for name, a in (("x", X), ("g", G), ("copy", copy)):
         if a is None:
             continue
+        if a.get_device() != G.get_device():
+            raise ChocoError(f"libchoco: {name} is on {a.device} and G on {G.device}", -1)
         if not a.is_cuda or a.dim() != 2 or a.shape[0] != n or a.shape[1] < off[-1] or (a.shape[1] > 1 and a.stride(1) != 1):
             raise ChocoError(f"libchoco: {name} must be [{n}, >= {int(off[-1])}] on the GPU with contiguous rows", -1)
         t[name] = (a.data_ptr() + (rows * a.stride(0) + off[None, :-1]) * a.element_size()).astype(np.uint64)
@@ -712,7 +771,10 @@ class AdamW:
 
     def __init__(self, X, G, layer_off, weight_decay=0.0, lr_scale=1.0, copy=None, beta1: float = 0.9,
                  beta2: float = 0.999, eps: float = 1e-8, state_bits: int = 32, states=None, step: int = 0):
+        import torch
         tensors = adamw_layer_tensors(X, G, layer_off, weight_decay, lr_scale, copy)
+        if G.get_device() != torch.cuda.current_device():
+            raise ChocoError(f"libchoco: a handle belongs to the current device ({torch.cuda.current_device()}), and G is on {G.device}", -1)
         self.groups = G.shape[0]
         self._keep = (X, G, copy)      # the list holds their addresses
         self.handle = choco_adamw_init(tensors, self.groups, beta1, beta2, eps, state_bits)
@@ -720,45 +782,25 @@ class AdamW:
         self.elements, self.offsets = choco_adamw_state_size(self.handle, len(tensors))
         if X is not None:
             if states is None:
-                import torch
-                new = lambda count, dtype: torch.zeros(count, dtype=dtype, device=X.device)  # noqa: E731
-                if state_bits == 32:
-                    states = (new(self.elements, torch.float32), new(self.elements, torch.float32))
-                else:
-                    blocks = self.elements // ADAMW_BLOCK
-                    states = (new(self.elements, torch.int8), new(self.elements, torch.uint8),
-                              new(blocks, torch.float32), new(blocks, torch.float32))
-            self._check_states(states, state_bits)
+                states = [torch.zeros(count, dtype=getattr(torch, kind), device=X.device) for kind, count in self.handle.state_arrays()]
+            _check_states(self.handle, states)
             self.m, self.v, self.m_scale, self.v_scale = (tuple(states) + (None, None))[:4]
         if step:
             self.set_steps([step] * self.groups)
-
-    def _check_states(self, states, bits):
-        want = [("float32", self.elements)] * 2 if bits == 32 else [
-            ("int8", self.elements), ("uint8", self.elements), ("float32", self.elements // ADAMW_BLOCK),
-            ("float32", self.elements // ADAMW_BLOCK)]
-        got = [(str(a.dtype).rpartition(".")[2], a.numel()) for a in states]
-        if got != want or not all(a.is_contiguous() for a in states):
-            raise ChocoError(f"libchoco: the moments must be contiguous arrays of {want}, not {got}", -1)
 
     def grad_norm(self, max_norm: float, norm, factor, unscale: float = 1.0, stream=None):
         choco_adamw_grad_norm(self.handle, max_norm, norm, factor, unscale, stream)
 
     def step(self, lr: float, factor=None, stream=None):
-        choco_adamw_step(self.handle, self.m, self.v, self.m_scale, self.v_scale, lr, factor, stream)
+        _adamw_step(self.handle, self.m, self.v, self.m_scale, self.v_scale, lr, factor, stream)
 
     def read_state(self, m_out, v_out, stream=None):
-        for a in (m_out, v_out):
-            if a is not None and (a.numel() != self.elements or not a.is_contiguous()):
-                raise ChocoError(f"libchoco: outputs must be contiguous with {self.elements} elements", -1)
-        choco_adamw_read_state(self.handle, self.m, self.v, self.m_scale, self.v_scale, m_out, v_out, stream)
+        _adamw_read_state(self.handle, self.m, self.v, self.m_scale, self.v_scale, m_out, v_out, stream)
 
     def get_steps(self, stream=None):
         return choco_adamw_get_steps(self.handle, self.groups, stream)
 
     def set_steps(self, steps, stream=None):
-        if len(steps) != self.groups:
-            raise ChocoError(f"libchoco: one step count for each of {self.groups} groups", -1)
         choco_adamw_set_steps(self.handle, steps, stream)
 
     def close(self):

@@ -70,3 +70,90 @@ def test_handles_pass_as_pointers():
     word = ctypes.c_uint64(0x1234)
     libc.memcpy(ctypes.byref(h), ctypes.addressof(word), 8)      # as an init call writes it
     assert h.value == 0x1234
+
+
+def adamw(n_tensors=6, groups=3, bits=32, elements=1024):
+    h = choco.AdamWHandle()
+    h.describe(-1, n_tensors, groups, bits, elements)
+    return h
+
+
+@pytest.fixture
+def no_library(monkeypatch):
+    def no_call():
+        raise AssertionError("the library was called")
+    monkeypatch.setattr(choco, "load", no_call)
+
+
+def refused(call, match):
+    with pytest.raises(choco.ChocoError, match=match):
+        call()
+
+
+@pytest.mark.parametrize("bad", [torch.zeros(3, dtype=torch.float64), torch.zeros(3, dtype=torch.bfloat16), torch.zeros(2), torch.zeros(6)[::2]])
+def test_norms_and_factors_are_one_float_per_group(no_library, bad):
+    h, fine = adamw(), torch.zeros(3)
+    m = torch.zeros(1024)
+    message = "one element for each of 3 groups|are not supported"
+    refused(lambda: choco.choco_adamw_grad_norm(h, 1.0, bad, fine), message)
+    refused(lambda: choco.choco_adamw_grad_norm(h, 1.0, fine, bad), message)
+    refused(lambda: choco.choco_adamw_step(h, m, m.clone(), None, None, 1e-3, bad), message)
+    h.device = 1
+    refused(lambda: choco.choco_adamw_grad_norm(h, 1.0, fine, fine), message)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_moments_are_those_of_the_list(no_library, bits):
+    h, factor = adamw(bits=bits), torch.zeros(3)
+    make = lambda kinds: [torch.zeros(c, dtype=getattr(torch, k)) for k, c in kinds]  # noqa: E731
+    fine = make(h.state_arrays())
+    assert [a.numel() for a in fine] == ([1024, 1024] if bits == 32 else [1024, 1024, 4, 4])
+    padded = lambda a: (list(a) + [None, None])[:4]  # noqa: E731
+    wrong = []
+    for k in range(len(fine)):
+        wrong += [fine[:k] + [a] + fine[k + 1:] for a in (None, fine[k][:-1], fine[k].double(), torch.zeros(2 * len(fine[k]), dtype=fine[k].dtype)[::2])]
+    for states in wrong:
+        refused(lambda: choco.choco_adamw_step(h, *padded(states), 1e-3, factor), "the moments must be")
+        if all(a is not None for a in states):
+            refused(lambda: choco.choco_adamw_read_state(h, *padded(states), torch.zeros(1024), None), "the moments must be")
+    for out in (torch.zeros(1023), torch.zeros(2048)[::2]):
+        refused(lambda: choco.choco_adamw_read_state(h, *padded(fine), out, None), "outputs must be")
+    with pytest.raises(AssertionError):                          # all in place: it goes on, for one output alone too
+        choco.choco_adamw_step(h, *padded(fine), 1e-3, None)
+    only_m = [a if k % 2 == 0 else None for k, a in enumerate(padded(fine))]
+    with pytest.raises(AssertionError):
+        choco.choco_adamw_read_state(h, *only_m, torch.zeros(1024), None)
+    h.device = 1
+    refused(lambda: choco.choco_adamw_step(h, *padded(fine), 1e-3, None), "the moments must be")
+
+
+def test_host_arrays_have_an_element_for_each_tensor_or_group(no_library):
+    h = adamw()
+    refused(lambda: choco.choco_adamw_state_size(h, 5), "6 tensors")
+    refused(lambda: choco.choco_adamw_set_grads(h, [4096] * 5), "6 tensors")
+    refused(lambda: choco.choco_adamw_set_grads(h, [[4096] * 6]), "6 tensors")
+    refused(lambda: choco.choco_adamw_get_steps(h, 2), "3 groups")
+    refused(lambda: choco.choco_adamw_set_steps(h, [1, 2]), "3 groups")
+    refused(lambda: choco.choco_adamw_set_steps(h, 1), "3 groups")
+
+
+def test_rows_of_one_list_are_on_one_gpu():
+    class Elsewhere:                                             # a tensor of another GPU, as far as the checks look
+        is_cuda, shape, device = True, (2, 10), "cuda:1"
+
+        def get_device(self):
+            return 1
+
+        def dim(self):
+            return 2
+
+        def stride(self, k):
+            return (10, 1)[k]
+
+    class Here(Elsewhere):
+        device = "cuda:0"
+
+        def get_device(self):
+            return 0
+
+    refused(lambda: choco.adamw_layer_tensors(Elsewhere(), Here(), [0, 10]), "G on cuda:0")
