@@ -42,7 +42,7 @@ def train(workers=8, steps=200, bits=32, q="topk", vocab=512, dim=64, batch=16, 
     count = batch * (length - 1)
     scale = dim ** 0.5
     emb = choco.Embedding(workers, vocab, dim, count, table_ld=d, scale=scale)
-    opt = choco.AdamW(X, G, off, weight_decay=[0.01, 0.01, 0.0], state_bits=bits)
+    opt = choco.AdamW(X, G, off, weight_decay=[0.01, 0.01, 0.0], state_bits=bits, rounding="random" if bits == 8 else "nearest", seed=seed)
     kw = dict(k=max(1, d // 20)) if q in ("topk", "randk") else dict(s=16, bucket=512) if q == "qsgd" else {}
     gossip = choco.Choco(w, d, q, seed=seed, **kw)
     choco.choco_set_carry(gossip.ctx, False)                    # AdamW changes X between two gossip steps

@@ -512,6 +512,17 @@ typedef struct {
 int choco_adamw_init(choco_adamw** out, int32_t n_tensors, const choco_adamw_tensor* tensors,
                      const choco_adamw_params* p);
 int choco_adamw_destroy(choco_adamw* opt);
+/*
+ * How codes of 8-bit moments are rounded (CHOCO_ERR_UNSUPPORTED with 32 bits): random = 0, the start, to
+ * the nearest code, as above.  A nearest code stays where it is until its value has moved by half the distance to
+ * the next, 1/k of it for m and 2/k for v.  v falls by 1 - beta2 of itself a step at most, so with the usual beta2
+ * its codes hardly ever come down but with the largest v of their block: v ends up too large, by a quarter to a third
+ * under gradients of constant size, and by the square of the ratio where gradients of a part of a block become smaller.
+ * Runs of more than some hundred steps want random = 1: a value between two codes' goes to one or the other, the
+ * expected value of m and v being the value itself.  The 16 random bits of an element depend on its place in m and
+ * v, its group's step number and the seed alone: the same bits every time, and after choco_adamw_set_steps.
+ */
+int choco_adamw_set_rounding(choco_adamw* opt, int32_t random, uint64_t seed);
 /* *elements: length of m and v (a multiple of 256); offsets (may be NULL): n_tensors starts. */
 int choco_adamw_state_size(const choco_adamw* opt, int64_t* elements, int64_t* offsets);
 /*

@@ -31,7 +31,7 @@ EXPORTS = [
     "choco_layers_invalidate", "choco_layers_set_step", "choco_layers_set_nesterov", "choco_layers_set_graphs", "choco_layers_combined_steps",
     "choco_embedding_init", "choco_embedding_destroy", "choco_embedding_forward", "choco_embedding_backward",
     "choco_adamw_init", "choco_adamw_destroy", "choco_adamw_state_size", "choco_adamw_set_grads", "choco_adamw_grad_norm",
-    "choco_adamw_step", "choco_adamw_read_state", "choco_adamw_get_steps", "choco_adamw_set_steps",
+    "choco_adamw_set_rounding", "choco_adamw_step", "choco_adamw_read_state", "choco_adamw_get_steps", "choco_adamw_set_steps",
 ]
 
 DTYPES = {"float32": 0, "bfloat16": 1, "float16": 2}   # choco_dtype
@@ -141,6 +141,7 @@ def load() -> ctypes.CDLL:
         lib.choco_adamw_destroy.argtypes = [vp]
         lib.choco_adamw_state_size.argtypes = [vp, ctypes.POINTER(i64), vp]
         lib.choco_adamw_set_grads.argtypes = [vp, vp, vp]
+        lib.choco_adamw_set_rounding.argtypes = [vp, i32, u64]
         lib.choco_adamw_grad_norm.argtypes = [vp, f32, f32, vp, vp, vp]
         lib.choco_adamw_step.argtypes = [vp, vp, vp, vp, vp, f64, vp, vp]
         lib.choco_adamw_read_state.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp]
@@ -614,6 +615,11 @@ def choco_adamw_set_grads(opt, pointers, stream=None) -> None:
     _check(load().choco_adamw_set_grads(opt, g.ctypes.data, _stream_of(stream, opt.device)))
 
 
+def choco_adamw_set_rounding(opt, random: bool, seed: int = 0) -> None:
+    """8-bit codes to the nearest, or at random with the right expected value (see choco.h)."""
+    _check(load().choco_adamw_set_rounding(opt, 1 if random else 0, seed))
+
+
 def choco_adamw_grad_norm(opt, max_norm: float, norm, factor, unscale: float = 1.0, stream=None) -> None:
     _check_groups(opt, "norm and factor", norm, factor)
     _check(load().choco_adamw_grad_norm(opt, max_norm, unscale, norm.data_ptr(), factor.data_ptr(), _stream_of(stream, opt.device)))
@@ -767,17 +773,23 @@ class AdamW:
     """AdamW over the layers of all workers' rows: X and G are [n, ld] tensors, every worker a group.
     Owns the handle and (unless `states` hands them over) the moments: (m, v), or with 8-bit
     moments (m, v, m_scale, v_scale), flat arrays in the layout choco.h gives.  With X = None only
-    grad_norm can be called."""
+    grad_norm can be called.  rounding: of 8-bit moments, "nearest" or "random" (drawn from `seed`); long
+    runs want "random", see choco_adamw_set_rounding."""
 
     def __init__(self, X, G, layer_off, weight_decay=0.0, lr_scale=1.0, copy=None, beta1: float = 0.9,
-                 beta2: float = 0.999, eps: float = 1e-8, state_bits: int = 32, states=None, step: int = 0):
+                 beta2: float = 0.999, eps: float = 1e-8, state_bits: int = 32, states=None, step: int = 0,
+                 rounding: str = "nearest", seed: int = 0):
         import torch
+        if rounding not in ("nearest", "random"):
+            raise ChocoError(f"libchoco: rounding is nearest or random, not {rounding}", -1)
         tensors = adamw_layer_tensors(X, G, layer_off, weight_decay, lr_scale, copy)
         if G.get_device() != torch.cuda.current_device():
             raise ChocoError(f"libchoco: a handle belongs to the current device ({torch.cuda.current_device()}), and G is on {G.device}", -1)
         self.groups = G.shape[0]
         self._keep = (X, G, copy)      # the list holds their addresses
         self.handle = choco_adamw_init(tensors, self.groups, beta1, beta2, eps, state_bits)
+        if rounding == "random":
+            choco_adamw_set_rounding(self.handle, True, seed)
         self.m = self.v = self.m_scale = self.v_scale = None
         self.elements, self.offsets = choco_adamw_state_size(self.handle, len(tensors))
         if X is not None:

@@ -70,6 +70,7 @@ struct Unit {
 // Correction: what a captured step multiplies with, one per group.
 struct Correction {
     float step_size, rsqrt_bc2;
+    int64_t n;              // its steps, this one included
 };
 
 struct StepScalars {
@@ -82,6 +83,7 @@ struct StepScalars {
     int64_t t;
     int64_t whole_elems;    // of a chunk of whole aligned blocks
     const Correction* corrections; // of a captured step, [groups]; else NULL
+    uint64_t seed;          // of the random rounding
 };
 
 __host__ __device__ inline double pow_int(double b, int64_t e)
@@ -126,6 +128,9 @@ __device__ __forceinline__ uint32_t pack4(const float* k) // low bytes of four o
 }
 // 2^23 plus byte e of a word
 __device__ __forceinline__ float byte_bits(uint32_t w, int e) { return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 | e)); }
+
+// (h + 1/2) / 2^16 of 16 bits
+__device__ __forceinline__ float unit_of(uint32_t h) { return __fadd_rn(__uint_as_float(0x3F800000u | h << 7), -0x1.ffffp-1f); }
 
 // Codes as byte_bits leaves them (m's with 128 added) to k |k| and k^2: times the block's scale, m and sqrt(v).
 __device__ __forceinline__ float square_m(float bits)
@@ -186,6 +191,7 @@ __device__ __forceinline__ void store8(void* p, int64_t i, int32_t dtype, const 
 // What a step multiplies with, for one tensor of one group.
 struct Factors {
     float c, step_size, rsqrt_bc2, decay;
+    int64_t n;              // steps of the group, this one included
 };
 
 struct State {
@@ -214,8 +220,14 @@ __device__ __forceinline__ void update8(const StepScalars& sc, const Factors& f,
 // 507): products are fused, and roots and quotients are the approximate ones, whose 2^-22 is
 // nothing beside the per cent that a code rounds by.  Elements past the end of a tensor come as
 // zeros and stay zeros.
+// RANDOM: a value between two codes' goes to either one, to the upper with the probability that makes
+// the expected value (of m and of v, not of their roots) the value itself.  Nearest codes do not
+// move while a value moves by less than half the distance to the next (1/k of m, 2/k of v), and v falls
+// by no more than 1 - beta2 of itself a step.  `bits`: 16 random bits an element, whose bytes trade places for m.
+// The generator and the second rounding cost a third of the time (8 x 25.6 M elements: 505 -> 677 us).
+template <bool RANDOM>
 __device__ __forceinline__ void update8_codes(const StepScalars& sc, const Factors& f, float (&g)[8], float (&x)[8], float (&m)[8],
-                                              float (&v)[8], float& sm, float& sv)
+                                              float (&v)[8], float& sm, float& sv, const uint32_t (&bits)[4])
 {
     float amax = 0.f, rmax = 0.f;
     const float sm1 = sm * sc.beta1, sv2 = sv * sc.root_beta2, gm = f.c * sc.omb1, gv = f.c * sc.root_omb2;
@@ -236,10 +248,50 @@ __device__ __forceinline__ void update8_codes(const StepScalars& sc, const Facto
     const float to_m = kCodesM * rsqrtf(amax), to_v = kCodesV * rsqrtf(rmax);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        m[e] = __fmaf_rn(copysignf(root_approx(fabsf(m[e])), m[e]), to_m, kRound);
-        const float k = __fmaf_rn(root_approx(v[e]), to_v, kRound);
-        v[e] = v[e] > 0.f ? fmaxf(k, kRound + 1.0f) : k; // at least 1 where v > 0
+        if constexpr (RANDOM) {
+            const uint32_t h = __byte_perm(bits[e / 2], 0, e & 1 ? 0x4432 : 0x4410), swapped = __byte_perm(h, 0, 0x4401);
+            const float y = (fabsf(m[e]) * to_m) * to_m, w = (v[e] * to_v) * to_v;
+            const float k = truncf(root_approx(y)), up = (2.f * k + 1.f) * unit_of(swapped) < __fmaf_rn(-k, k, y) ? 1.f : 0.f;
+            m[e] = copysignf(fminf(k + up, kCodesM), m[e]) + kRound;
+            const float q = truncf(root_approx(w)), q2 = q * q, odd = 2.f * q + 1.f;
+            const float over = odd * unit_of(h) * __fmaf_rn(2.f, q2, odd) < __fmaf_rn(-q, q, w) * (w + q2) ? 1.f : 0.f;
+            const float code = fminf(q + over, kCodesV) + kRound;
+            v[e] = v[e] > 0.f ? fmaxf(code, kRound + 1.0f) : code;
+        } else {
+            m[e] = __fmaf_rn(copysignf(root_approx(fabsf(m[e])), m[e]), to_m, kRound);
+            const float k = __fmaf_rn(root_approx(v[e]), to_v, kRound);
+            v[e] = v[e] > 0.f ? fmaxf(k, kRound + 1.0f) : k; // at least 1 where v > 0
+        }
     }
+}
+
+// The random bits of a lane's 8 consecutive elements of a block of moments, in the halves of four words: they go by the place
+// in m and v, the group's step and the seed alone.
+__device__ __forceinline__ void random_bits(uint32_t (&bits)[4], const StepScalars& sc, const Factors& f, int64_t block_start)
+{
+    const uint64_t at = (uint64_t)block_start / 8 + (threadIdx.x & 31);
+    const uint4 r = philox4x32_10(make_uint4((uint32_t)at, (uint32_t)(at >> 32), (uint32_t)f.n, ((uint32_t)(f.n >> 32) << 8) | kStreamMoments),
+                                  make_uint2((uint32_t)sc.seed, (uint32_t)(sc.seed >> 32)));
+    bits[0] = r.x; bits[1] = r.y; bits[2] = r.z; bits[3] = r.w;
+}
+// The same bits where a lane has every 32nd element: element 32 j + lane is number lane % 8 of lane 4 j + lane / 8.
+__device__ __forceinline__ void spread_bits(uint32_t (&bits)[4])
+{
+    const uint32_t lane = threadIdx.x & 31, which = (lane & 7) >> 1;
+    uint32_t mine[4];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t other = __shfl_sync(0xffffffffu, bits[k], 4 * j + (lane >> 3));
+            if (which == k) w = other;
+        }
+        const uint32_t h = lane & 1 ? w >> 16 : w & 0xffffu;
+        mine[j / 2] = j & 1 ? mine[j / 2] | h << 16 : h;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) bits[k] = mine[k];
 }
 
 // What a lane needs of a whole block of an aligned tensor: 8 consecutive elements, moved in 128-bit
@@ -269,7 +321,7 @@ __device__ __forceinline__ void load_block(Loaded<BITS, XT, GT>& l, const Tensor
     }
 }
 
-template <int BITS, typename XT, typename GT>
+template <int BITS, bool RANDOM, typename XT, typename GT>
 __device__ __forceinline__ void finish_block(Loaded<BITS, XT, GT>& l, const Tensor& t, const State& st, const StepScalars& sc,
                                              const Factors& f, int64_t base)
 {
@@ -292,7 +344,9 @@ __device__ __forceinline__ void finish_block(Loaded<BITS, XT, GT>& l, const Tens
         store_vec<float, 8>(static_cast<float*>(st.m) + s, m);
         store_vec<float, 8>(static_cast<float*>(st.v) + s, v);
     } else {
-        update8_codes(sc, f, g, x, m, v, l.sm, l.sv);
+        uint32_t bits[4];
+        if constexpr (RANDOM) random_bits(bits, sc, f, t.state + base);
+        update8_codes<RANDOM>(sc, f, g, x, m, v, l.sm, l.sv, bits);
         *reinterpret_cast<uint2*>(static_cast<uint8_t*>(st.m) + s) = make_uint2(pack4(m), pack4(m + 4));
         *reinterpret_cast<uint2*>(static_cast<uint8_t*>(st.v) + s) = make_uint2(pack4(v), pack4(v + 4));
         if ((threadIdx.x & 31) == 0) {
@@ -340,7 +394,7 @@ __device__ __forceinline__ void load_block_any(LoadedAny<BITS, XT, GT>& l, const
         l.sv = st.v_scale[s0 / kBlock];
     }
 }
-template <int BITS, typename XT, typename GT>
+template <int BITS, bool RANDOM, typename XT, typename GT>
 __device__ __forceinline__ void finish_block_any(LoadedAny<BITS, XT, GT>& l, const Tensor& t, const State& st, const StepScalars& sc,
                                                  const Factors& f, int64_t base, int count)
 {
@@ -355,7 +409,12 @@ __device__ __forceinline__ void finish_block_any(LoadedAny<BITS, XT, GT>& l, con
     if constexpr (BITS == 32) {
         update8(sc, f, g, x, l.m, l.v);
     } else {
-        update8_codes(sc, f, g, x, l.m, l.v, l.sm, l.sv);
+        uint32_t bits[4];
+        if constexpr (RANDOM) {
+            random_bits(bits, sc, f, s0);
+            spread_bits(bits);
+        }
+        update8_codes<RANDOM>(sc, f, g, x, l.m, l.v, l.sm, l.sv, bits);
         if (lane == 0) {
             st.m_scale[s0 / kBlock] = l.sm;
             st.v_scale[s0 / kBlock] = l.sv;
@@ -384,11 +443,13 @@ __device__ __forceinline__ bool factors_of(Factors& f, const Tensor& t, float c,
     f.c = c;
     f.step_size = sc.step_size;
     f.rsqrt_bc2 = sc.rsqrt_bc2;
+    f.n = sc.t - skipped;
     if (sc.corrections) {
         f.step_size = sc.corrections[t.group].step_size;
         f.rsqrt_bc2 = sc.corrections[t.group].rsqrt_bc2;
+        f.n = sc.corrections[t.group].n;
     } else if (skipped != 0) { // the group has taken another number of steps than the host has counted
-        const float n = (float)(sc.t - skipped);
+        const float n = (float)f.n;
         f.step_size = __fdividef(sc.lr, -expm1f(n * sc.log_beta1));
         f.rsqrt_bc2 = rsqrtf(-expm1f(n * sc.log_beta2));
     }
@@ -418,7 +479,7 @@ __global__ void __launch_bounds__(128) advance_kernel(int64_t* counts, const flo
     if (k >= groups) return;
     if (factor && !isfinite(factor[k])) return; // sits the step out
     const int64_t n = counts[0] - counts[1 + k] + 1;
-    out[k] = {(float)(lr / (1.0 - pow_int(beta1, n))), (float)(1.0 / sqrt(1.0 - pow_int(beta2, n)))};
+    out[k] = {(float)(lr / (1.0 - pow_int(beta1, n))), (float)(1.0 / sqrt(1.0 - pow_int(beta2, n))), n};
     counts[1 + k] -= 1;
 }
 
@@ -432,7 +493,7 @@ __global__ void __launch_bounds__(128) advance_kernel(int64_t* counts, const flo
 // reads counts[0].
 
 // one block of threads per chunk, one warp per block of elements
-template <int BITS, typename XT, typename GT>
+template <int BITS, bool RANDOM, typename XT, typename GT>
 __global__ void __launch_bounds__(kStepThreads, kStepBlocksRest)
 step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* factor,
                  int64_t* counts, State st, StepScalars sc, int32_t beside)
@@ -447,7 +508,7 @@ step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ c
         LoadedAny<BITS, XT, GT> l;
         load_block_any(l, t, st, base, count);
         Factors f;
-        if (factors_of(f, t, factor ? factor[t.group] : 1.0f, counts[1 + t.group], sc)) finish_block_any(l, t, st, sc, f, base, count);
+        if (factors_of(f, t, factor ? factor[t.group] : 1.0f, counts[1 + t.group], sc)) finish_block_any<BITS, RANDOM>(l, t, st, sc, f, base, count);
         else count_skip(counts, sc, ch, t.group);
     }
     count_call(counts, sc, beside);
@@ -464,8 +525,8 @@ step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ c
 // in memory.
 // A chunk may be shorter than what the warps could take: in a short list it holds one block of
 // elements for each, and what follows belongs to the next chunk.
-template <int BITS, typename XT, typename GT>
-__global__ void __launch_bounds__(kStepThreads, BITS == 8 ? kStepBlocks8 : kStepBlocks32)
+template <int BITS, bool RANDOM, typename XT, typename GT>
+__global__ void __launch_bounds__(kStepThreads, BITS == 8 && !RANDOM ? kStepBlocks8 : kStepBlocks32)
 step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* factor,
             int64_t* counts, State st, StepScalars sc, int32_t beside)
 {
@@ -484,7 +545,7 @@ step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks
     if (factors_of(f, t, factor ? factor[t.group] : 1.0f, counts[1 + t.group], sc)) {
 #pragma unroll
         for (int k = 0; k < N; ++k)
-            if (base + k * kChunkElems < end) finish_block(l[k], t, st, sc, f, base + k * kChunkElems);
+            if (base + k * kChunkElems < end) finish_block<BITS, RANDOM>(l[k], t, st, sc, f, base + k * kChunkElems);
     } else {
         count_skip(counts, sc, ch, t.group);
     }
@@ -494,7 +555,7 @@ step_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks
 
 // Both kinds of chunks in one launch, for lists so short that a second launch takes longer than
 // this kernel's registers cost.
-template <int BITS, typename XT, typename GT>
+template <int BITS, bool RANDOM, typename XT, typename GT>
 __global__ void __launch_bounds__(kStepThreads, kStepBlocksRest)
 step_both_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ chunks, const float* factor,
                  int64_t* counts, State st, StepScalars sc, int32_t beside)
@@ -512,14 +573,14 @@ step_both_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ c
             Loaded<BITS, XT, GT> l;
             load_block(l, t, st, base);
             go = factors_of(f, t, factor ? factor[t.group] : 1.0f, counts[1 + t.group], sc);
-            if (go) finish_block(l, t, st, sc, f, base);
+            if (go) finish_block<BITS, RANDOM>(l, t, st, sc, f, base);
         }
     } else if (base < t.numel) {
         const int count = (int)min((int64_t)kBlock, t.numel - base);
         LoadedAny<BITS, XT, GT> l;
         load_block_any(l, t, st, base, count);
         go = factors_of(f, t, factor ? factor[t.group] : 1.0f, counts[1 + t.group], sc);
-        if (go) finish_block_any(l, t, st, sc, f, base, count);
+        if (go) finish_block_any<BITS, RANDOM>(l, t, st, sc, f, base, count);
     }
     if (!go) count_skip(counts, sc, ch, t.group);
     count_call(counts, sc, beside);
@@ -528,22 +589,26 @@ step_both_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ c
 
 using StepKernel = void (*)(const Tensor*, const Chunk*, const float*, int64_t*, State, StepScalars, int32_t);
 enum StepForm { kRest, kWhole, kBoth };
-template <int BITS, typename XT, typename GT>
+template <int BITS, bool RANDOM, typename XT, typename GT>
 StepKernel step_kernel_of(StepForm form)
 {
-    return form == kRest ? step_rest_kernel<BITS, XT, GT> : form == kWhole ? step_kernel<BITS, XT, GT> : step_both_kernel<BITS, XT, GT>;
+    return form == kRest    ? step_rest_kernel<BITS, RANDOM, XT, GT>
+           : form == kWhole ? step_kernel<BITS, RANDOM, XT, GT>
+                            : step_both_kernel<BITS, RANDOM, XT, GT>;
 }
-template <int BITS, typename XT>
+template <int BITS, bool RANDOM, typename XT>
 StepKernel step_kernel_of(int32_t g, StepForm form)
 {
-    return g == CHOCO_F32 ? step_kernel_of<BITS, XT, float>(form) : g == CHOCO_BF16 ? step_kernel_of<BITS, XT, __nv_bfloat16>(form)
-                                                                                    : step_kernel_of<BITS, XT, __half>(form);
+    return g == CHOCO_F32    ? step_kernel_of<BITS, RANDOM, XT, float>(form)
+           : g == CHOCO_BF16 ? step_kernel_of<BITS, RANDOM, XT, __nv_bfloat16>(form)
+                             : step_kernel_of<BITS, RANDOM, XT, __half>(form);
 }
-template <int BITS>
+template <int BITS, bool RANDOM>
 StepKernel step_kernel_of(int32_t x, int32_t g, StepForm form)
 {
-    return x == CHOCO_F32 ? step_kernel_of<BITS, float>(g, form) : x == CHOCO_BF16 ? step_kernel_of<BITS, __nv_bfloat16>(g, form)
-                                                                                  : step_kernel_of<BITS, __half>(g, form);
+    return x == CHOCO_F32    ? step_kernel_of<BITS, RANDOM, float>(g, form)
+           : x == CHOCO_BF16 ? step_kernel_of<BITS, RANDOM, __nv_bfloat16>(g, form)
+                             : step_kernel_of<BITS, RANDOM, __half>(g, form);
 }
 
 // 8 elements per thread; the moments are whole blocks.
@@ -707,6 +772,8 @@ struct choco_adamw {
     int64_t whole_elems;           // of a chunk of whole aligned blocks
     int64_t begin[2 * kPairs + 1]; // in d_chunks, for every pair of types: other blocks, whole blocks of aligned tensors
     int64_t t;                     // step calls so far that were no capture; a group has taken t - d_counts[1 + group] steps
+    bool random_codes;             // how 8-bit codes are rounded
+    uint64_t seed;
     bool captured;                 // a graph may hold launches over ranges of d_chunks
     void* memory;                  // all that follows
     Tensor* d_tensors;
@@ -982,6 +1049,15 @@ int choco_adamw_set_grads(choco_adamw* opt, const void* const* g, void* stream)
     return CHOCO_OK;
 }
 
+int choco_adamw_set_rounding(choco_adamw* opt, int32_t random, uint64_t seed)
+{
+    if (!opt || (random != 0 && random != 1)) return CHOCO_ERR_INVALID_ARG;
+    if (opt->params.state_bits != 8) return CHOCO_ERR_UNSUPPORTED;
+    opt->random_codes = random != 0;
+    opt->seed = seed;
+    return CHOCO_OK;
+}
+
 int choco_adamw_grad_norm(choco_adamw* opt, float max_norm, float unscale, float* norm, float* factor, void* stream)
 {
     if (!opt || !norm || !factor || !(max_norm >= 0.f) || !std::isfinite(max_norm) || !(unscale > 0.f) ||
@@ -1018,6 +1094,7 @@ int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* 
     sc.step_size = (float)(lr / (1.0 - pow_int(p.beta1, sc.t)));
     sc.rsqrt_bc2 = (float)(1.0 / std::sqrt(1.0 - pow_int(p.beta2, sc.t)));
     sc.whole_elems = opt->whole_elems;
+    sc.seed = opt->seed;
     cudaStream_t st = (cudaStream_t)stream;
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
     cudaError_t err = cudaStreamIsCapturing(st, &capture);
@@ -1034,7 +1111,10 @@ int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* 
     auto launch = [&](int32_t pair, StepForm form, int64_t begin, int64_t end) {
         if (begin == end || err != cudaSuccess) return;
         const int32_t x = pair / 3, g = pair % 3;
-        err = launch_overlapped(eight ? step_kernel_of<8>(x, g, form) : step_kernel_of<32>(x, g, form), dim3((unsigned)(end - begin)),
+        const StepKernel kernel = !eight              ? step_kernel_of<32, false>(x, g, form)
+                                  : opt->random_codes ? step_kernel_of<8, true>(x, g, form)
+                                                      : step_kernel_of<8, false>(x, g, form);
+        err = launch_overlapped(kernel, dim3((unsigned)(end - begin)),
                                 dim3(kStepThreads), 0, st, HotRange{}, opt->d_tensors, opt->d_chunks + begin, factor, opt->d_counts,
                                 state, sc, beside);
         beside = 1;

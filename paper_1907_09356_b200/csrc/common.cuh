@@ -27,6 +27,7 @@ constexpr int kTile = kTileThreads * kQuad * kTileIters; // 2048 coordinates
 
 constexpr uint32_t kStreamRandK = 0;     // generator stream of the random-k selection keys
 constexpr uint32_t kStreamDither = 1;    // generator stream of the QSGD dither
+constexpr uint32_t kStreamMoments = 2;   // generator stream of the rounding of AdamW's 8-bit moments
 
 // ---------------------------------------------------------------------------------------
 // Philox4x32-10 (Salmon et al., SC'11).  Counter = (coord / 4, worker, step low,
