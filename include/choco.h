@@ -399,8 +399,10 @@ int choco_profile_read(choco_ctx* ctx, int32_t* steps_recorded, double* update_m
  * The calls below serve all n workers at once on the arrays a run has anyway (rows of X and G),
  * or on separate tensors.  They follow the rules at the top: asynchronous on `stream`, calls on
  * one handle in stream order from one host thread at a time, nothing allocated after the init
- * call, nothing enqueued on error, same inputs give the same bits.  A handle belongs to the
- * device that was current at its init; a call with another device current returns
+ * call, nothing enqueued on error, same inputs give the same bits.  (CHOCO_ERR_CUDA from
+ * choco_embedding_backward or choco_adamw_step is the one exception: CUDA refused a launch, and launches
+ * of the call before that one may have gone out, so that what the call writes has no meaning.)  A handle
+ * belongs to the device that was current at its init; a call with another device current returns
  * CHOCO_ERR_INVALID_ARG.  Pointers are aligned to their elements (CHOCO_ERR_MISALIGNED).
  * ------------------------------------------------------------------------------------------ */
 

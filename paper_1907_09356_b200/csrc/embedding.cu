@@ -1048,7 +1048,6 @@ cudaError_t launch_sums(const EmbShape& s, Sums a, cudaStream_t st)
     a.slabs = (uint32_t)((s.dim + 32 * V * C - 1) / (32 * V * C));
     const uint64_t warps = (uint64_t)a.slabs * a.tiles * s.n;
     const uint64_t blocks = (warps + kSumThreads / 32 - 1) / (kSumThreads / 32);
-    if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
     return launch_overlapped(sum_tiles_kernel<TD, V, C, B>, dim3((unsigned)blocks), dim3(kSumThreads), 0, st, HotRange{}, s, a);
 }
 
@@ -1215,15 +1214,17 @@ int choco_embedding_backward(choco_embedding* emb, const void* tokens, int32_t i
                            vector_of(grad, grad_dtype, s.table_row, s.table_ld, s.dim, s.n, 8));
     cudaError_t err = cudaSuccess;
 
+    // every launch's size is known, and refused if it is too large, before the first goes out
+    const int32_t size = (int32_t)dtype_size(grad_dtype);
+    const int64_t per_row = (s.dim * size + kZeroSpan - 1) / kZeroSpan;
+    const int64_t zero_blocks = s.table_row == s.dim ? (s.vocab * s.dim * size + kZeroSpan - 1) / kZeroSpan : s.vocab * per_row;
+    // (no form of the sums has a warp take fewer than 64 columns)
+    const int64_t tiles = (count + tile_of(count * s.n) - 1) / tile_of(count * s.n);
+    if ((!accumulate && zero_blocks > 0x7fffffff) || (s.dim + 63) / 64 * tiles * s.n > 0x7fffffffLL * (kSumThreads / 32)) return CHOCO_ERR_TOO_LARGE;
     auto zero = [&](int32_t beside) {
         if (accumulate || err != cudaSuccess) return;
-        const int32_t size = (int32_t)dtype_size(grad_dtype);
-        const int64_t per_row = (s.dim * size + kZeroSpan - 1) / kZeroSpan;
-        const int64_t blocks = s.table_row == s.dim ? (s.vocab * s.dim * size + kZeroSpan - 1) / kZeroSpan : s.vocab * per_row;
-        if (blocks > 0x7fffffff) err = cudaErrorInvalidValue;
-        else
-            err = launch_overlapped(zero_kernel, dim3((unsigned)blocks, (unsigned)s.n), dim3(kEmbThreads), 0, st, HotRange{}, s,
-                                    static_cast<char*>(grad), size, (uint32_t)per_row, beside);
+        err = launch_overlapped(zero_kernel, dim3((unsigned)zero_blocks, (unsigned)s.n), dim3(kEmbThreads), 0, st, HotRange{}, s,
+                                static_cast<char*>(grad), size, (uint32_t)per_row, beside);
     };
     if (count <= kDirectTokens) {
         const bool apart = !accumulate && s.n * s.vocab * s.dim * dtype_size(grad_dtype) > kDirectZeroBytes;
