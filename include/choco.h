@@ -484,8 +484,8 @@ typedef struct {
     int64_t numel;        /* elements, >= 0                                                      */
     int32_t x_dtype, g_dtype, copy_dtype;
     int32_t group;        /* in [0, groups)                                                      */
-    double weight_decay;  /* >= 0                                                                */
-    double lr_scale;      /* factor on the learning rate of this tensor, >= 0                    */
+    double weight_decay;  /* >= 0, finite as a float32                                           */
+    double lr_scale;      /* factor on the learning rate of this tensor, >= 0, finite as a float32 */
 } choco_adamw_tensor;
 typedef struct {
     double beta1, beta2;  /* in [0, 1)                                                           */
@@ -545,7 +545,7 @@ int choco_adamw_set_grads(choco_adamw* opt, const void* const* g, void* stream);
 int choco_adamw_grad_norm(choco_adamw* opt, float max_norm, float unscale, float* norm, float* factor, void* stream);
 
 /*
- * choco_adamw_step -- one step of all tensors.  factor: DEVICE float [groups], the gradient
+ * choco_adamw_step -- one step of all tensors, lr >= 0 and finite as a float32.  factor: DEVICE float [groups], the gradient
  * factors c, or NULL for 1.  A group whose factor is infinite or NaN is left as it is, parameters,
  * moments, copy and step number, so that a step with overflowed gradients is skipped without a
  * host synchronisation.  Infinite or NaN gradients that no factor keeps out leave the elements they

@@ -886,7 +886,7 @@ int plan(choco_adamw* o, int32_t n, const choco_adamw_tensor* ts, std::vector<Un
         const choco_adamw_tensor& t = ts[i];
         if (t.numel < 0 || t.numel > (int64_t)1 << 38 || t.group < 0 || t.group >= groups) return CHOCO_ERR_INVALID_ARG;
         if (!dtype_ok(t.x_dtype) || !dtype_ok(t.g_dtype) || !dtype_ok(t.copy_dtype)) return CHOCO_ERR_INVALID_ARG;
-        if (!(t.weight_decay >= 0.0) || !(t.lr_scale >= 0.0) || !std::isfinite(t.weight_decay) || !std::isfinite(t.lr_scale))
+        if (!(t.weight_decay >= 0.0) || !(t.lr_scale >= 0.0) || !std::isfinite((float)t.weight_decay) || !std::isfinite((float)t.lr_scale))
             return CHOCO_ERR_INVALID_ARG;
         if (t.numel > 0 && !t.g) return CHOCO_ERR_INVALID_ARG;
         if (t.numel > 0 && !t.x) o->norm_only = true;
@@ -1075,7 +1075,7 @@ int choco_adamw_grad_norm(choco_adamw* opt, float max_norm, float unscale, float
 int choco_adamw_step(choco_adamw* opt, void* m, void* v, float* m_scale, float* v_scale, double lr, const float* factor,
                      void* stream)
 {
-    if (!opt || opt->norm_only || !(lr >= 0.0) || !std::isfinite(lr) || !on_device(opt)) return CHOCO_ERR_INVALID_ARG;
+    if (!opt || opt->norm_only || !(lr >= 0.0) || !std::isfinite((float)lr) || !on_device(opt)) return CHOCO_ERR_INVALID_ARG;
     const bool eight = opt->params.state_bits == 8;
     if (opt->elements > 0 && (!m || !v || (eight && (!m_scale || !v_scale)))) return CHOCO_ERR_INVALID_ARG;
     if (!aligned_to(m, 16) || !aligned_to(v, 16) || !aligned_to(m_scale, 4) || !aligned_to(v_scale, 4) || !aligned_to(factor, 4))

@@ -74,3 +74,14 @@ def test_a_norm_beyond_float32_is_infinite_and_its_factor_nan():
         for k in over:
             assert torch.equal(X[k], kept[k])
     opt.close()
+
+
+def test_a_learning_rate_that_float32_cannot_hold_is_refused():
+    X, G = torch.ones((1, 300), device=DEV), torch.ones((1, 300), device=DEV)
+    opt = choco.AdamW(X, G, [0, 300])
+    for lr in (1e39, 3.41e38, 1.7e308, -1.0, float("nan"), float("inf")):
+        with pytest.raises(choco.ChocoError) as e:
+            opt.step(lr)
+        assert e.value.code == -1
+    assert bool((X == 1).all()) and list(opt.get_steps()) == [0]
+    opt.close()
