@@ -232,8 +232,9 @@ __device__ __forceinline__ void store_cluster(uint32_t a, uint32_t x, uint32_t y
 {
     asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory");
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// (not the forms that a whole warp has to reach together: with fewer digits than lanes, warps come out of a branch)
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) order_kernel(EmbShape s, Order o)
