@@ -481,12 +481,15 @@ class EmbeddingHandle(ctypes.c_void_p):
         self.table_row = table_row or dim
         self.table_ld = table_ld or vocab * self.table_row
         self.table_span = (vocab - 1) * self.table_row + dim      # elements from a table's first to its last
+        self.row_strides = (self.table_ld, 1)
 
 
 def _check_table(emb, what: str, t) -> None:
     """The arrays whose address alone goes to the library hold all n tables, where the handle says: rows of X or G
     [n, >= span], tables [n, vocab, dim], one table [vocab, dim], or the elements in a row."""
     shape, strides, n = t.shape, t.stride(), emb.n
+    if strides == emb.row_strides and shape[0] >= n and shape[1] >= emb.table_span:
+        return                                                    # rows of X or G, as nearly all are
     k = len(shape)
     if k == 2:
         if shape[0] >= n and shape[1] >= emb.table_span and (strides[1] == 1 or shape[1] == 1) and (strides[0] == emb.table_ld or n == 1):
@@ -521,7 +524,7 @@ def choco_embedding_destroy(emb) -> None:
 def choco_embedding_forward(emb, table, tokens, out, stream=None, n=None, dim=None) -> None:
     """out[i, t] = scale * table_i[tokens[i, t]].  `table` is a tensor that starts at worker 0's first
     row; tokens [n, T] int32 or int64; out [n, T, dim].  n and dim, if given, are the handle's."""
-    if (n or emb.n) != emb.n or (dim or emb.dim) != emb.dim:
+    if (n or dim) and ((n or emb.n) != emb.n or (dim or emb.dim) != emb.dim):
         raise ChocoError(f"libchoco: the handle is for n = {emb.n}, dim = {emb.dim}", -1)
     count, tokens_ld, row, ld = _token_rows(tokens, out, emb.n, emb.dim)
     device = _on_one_device("table, tokens and out", out, tokens, table, of=emb.device)
@@ -532,7 +535,7 @@ def choco_embedding_forward(emb, table, tokens, out, stream=None, n=None, dim=No
 
 def choco_embedding_backward(emb, tokens, dout, grad, accumulate: bool = False, stream=None, n=None, dim=None) -> None:
     """grad_i[r] (+)= scale * sum of dout[i, t] over the t with tokens[i, t] = r, in the table's layout."""
-    if (n or emb.n) != emb.n or (dim or emb.dim) != emb.dim:
+    if (n or dim) and ((n or emb.n) != emb.n or (dim or emb.dim) != emb.dim):
         raise ChocoError(f"libchoco: the handle is for n = {emb.n}, dim = {emb.dim}", -1)
     count, tokens_ld, row, ld = _token_rows(tokens, dout, emb.n, emb.dim)
     device = _on_one_device("tokens, dout and grad", grad, tokens, dout, of=emb.device)
