@@ -457,7 +457,8 @@ int choco_embedding_forward(choco_embedding* emb, const void* table, int32_t tab
  * sum is added to what grad_i[r, :] holds instead (the gradient of an output layer that shares
  * the table, or of earlier micro-batches), and rows that no token names are neither read nor
  * written.  The tokens are sorted, rows summed in float32 in an order that depends on the tokens
- * and the sizes alone, and the result is rounded once.
+ * and the sizes alone, and the result is rounded once.  (With accumulate, float32 elements of named rows whose old
+ * value, sum or result is a subnormal number take it for 0.)
  * What dout holds at tokens outside [0, vocab) is not read into any sum.
  *   count      <= max_tokens (CHOCO_ERR_TOO_LARGE); 0 writes zeros (or nothing).
  *   dout       DEVICE; element (i, t, c) at i dout_ld + t dout_row + c; dout_row >= dim, or 0: one row
@@ -523,6 +524,7 @@ int choco_adamw_destroy(choco_adamw* opt);
  * Runs of more than some hundred steps want random = 1: a value between two codes' goes to one or the other, the
  * expected value of m and v being the value itself.  The 16 random bits of an element depend on its place in m and
  * v, its group's step number and the seed alone: the same bits every time, and after choco_adamw_set_steps.
+ * A graph keeps the rounding it was captured with.
  */
 int choco_adamw_set_rounding(choco_adamw* opt, int32_t random, uint64_t seed);
 /* *elements: length of m and v (a multiple of 256); offsets (may be NULL): n_tensors starts. */

@@ -2,7 +2,8 @@
 // norms that feed it (choco_adamw_* in choco.h).
 //
 // A list of tensors is cut into chunks of kChunkElems elements of one tensor or fewer (twice as many
-// where a long list has 8-bit moments and the chunk is of whole aligned blocks); a table in device memory says which tensor a chunk belongs to, so that one launch serves all tensors of all
+// where a long list has 8-bit moments and the chunk is of whole aligned blocks); a table in device
+// memory says which tensor a chunk belongs to, so that one launch serves all tensors of all
 // workers whatever their sizes.  Inside a chunk every warp owns blocks of kBlock = 256 elements, the
 // unit that shares a scale in 8 bits.
 #include <algorithm>
@@ -24,8 +25,9 @@ constexpr int kStepThreads = 128;            // short blocks: 256 threads took 5
 constexpr int kStepWarps = kStepThreads / 32;
 constexpr int kChunkElems = kStepWarps * kBlock;
 // Blocks of elements that a warp of the fast path has in flight.  With codes one is too few bytes to cover the
-// chain of reads before it (8 x 25.6 M elements: 548 us with one, 509 us with two, 660 us with three; two
-// spill up to 44 bytes a thread at 48 registers, three far more); with 32-bit moments two are slower than one (2.09 ms against 2.01 ms).
+// chain of reads before it (8 x 25.6 M elements: 552 us with one, 505 us with two, though they spill up to 60 bytes
+// of a thread's 48 registers, and 670 us with three, which spill 220); with 32-bit moments two, with 92 bytes
+// spilled, are slower than one (16 x 28.95 M: 2.32 ms against 2.06 ms).
 template <int BITS>
 constexpr int kBlocksAtOnce = BITS == 8 ? 2 : 1;
 // blocks on an SM: 64 registers a thread with 32-bit moments, 48 with codes, where more warps pay; 72 for single accesses (8 x 65
@@ -216,8 +218,8 @@ __device__ __forceinline__ void update8(const StepScalars& sc, const Factors& f,
 // A lane's 8 elements of a block with moments in 8 bits.  In: the codes as byte_bits leaves them and
 // the block's scales; out: x, the new codes as floats that hold them in their low bytes, and the new
 // scales.  Here instructions and registers, not bytes, would be the bound (with IEEE roots, quotients
-// and separate products 99 instructions an element: 828 us for 8 x 25.6 M elements whose bytes take
-// 507): products are fused, and roots and quotients are the approximate ones, whose 2^-22 is
+// and separate products 99 instructions an element: 828 us for 8 x 25.6 M elements whose bytes, at
+// the rate of a copy, take 507): products are fused, and roots and quotients are the approximate ones, whose 2^-22 is
 // nothing beside the per cent that a code rounds by.  Elements past the end of a tensor come as
 // zeros and stay zeros.
 // RANDOM: a value between two codes' goes to either one, to the upper with the probability that makes
@@ -520,8 +522,8 @@ step_rest_kernel(const Tensor* __restrict__ tensors, const Chunk* __restrict__ c
 // last is what the L2 cache still holds.  The list does not change between calls, so it is read
 // before the previous kernel has ended; a warp's operands are asked for before the group's factor
 // is known, since every latency in this chain is time in which nothing is in flight.
-// A resident grid that walks over the chunks, with the list read ahead, was slower (16 x 28.95 M
-// float32: 2.55 ms against 2.10 ms): short blocks started in order keep what is in flight together
+// A resident grid that walks over the chunks, with the list read ahead, was a fifth slower (16 x 28.95 M
+// float32: 2.55 ms, now 2.06 ms): short blocks started in order keep what is in flight together
 // in memory.
 // A chunk may be shorter than what the warps could take: in a short list it holds one block of
 // elements for each, and what follows belongs to the next chunk.
@@ -647,7 +649,8 @@ __global__ void __launch_bounds__(256) read_state_kernel(State st, void* m_out, 
 // Sums of squares in float64: squares of float32 values neither overflow nor vanish there.  A block
 // takes one unit (a run of one tensor's gradient); the last block of a group to finish adds up the
 // group's units in their order and forms its norm and factor.  What bounds it is the memory
-// (16 x 28.95 M float32: 255 us, 7.3 TB/s).
+// (16 x 28.95 M float32: 259 us, 7.2 TB/s; rows off 16-byte boundaries take single loads, 311 us for half
+// as many).
 template <int THREADS>
 __device__ __forceinline__ double sum_of_block(double acc, double* red) // thread 0 has the sum
 {
