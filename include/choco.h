@@ -568,6 +568,66 @@ int choco_adamw_read_state(choco_adamw* opt, const void* m, const void* v, const
 int choco_adamw_get_steps(choco_adamw* opt, int64_t* steps, void* stream);
 int choco_adamw_set_steps(choco_adamw* opt, const int64_t* steps, void* stream);
 
+/*
+ * Muon: a momentum step over matrices whose update is orthogonalised.  Per matrix, c the gradient factor of
+ * its group, |.| the Frobenius norm:
+ *     m = beta m + (1 - beta) c g ;   u = beta m + (1 - beta) c g  (nesterov = 1)  or  m
+ *     X = u / |u|  (0 where u = 0) ;  `steps` times:  X = (a I + b S + c4 S^2) X  with S = X X^T
+ *     x = x - (X lr lr_scale + x (lr lr_scale weight_decay))
+ * (a, b, c4 are a, b, c of choco_muon_params.)  The usual five steps with 3.4445, -4.7750, 2.0315 bring all singular
+ * values of X to between about 0.7 and 1.2.  Convolutions are matrices [c_out, c_in k k].
+ */
+typedef struct choco_muon choco_muon;
+typedef struct {
+    void* x;              /* parameters, updated in place; of choco_muon_orthogonalize the result  */
+    const void* g;        /* gradients, read-only                                                  */
+    void* copy;           /* second copy of the new parameters in another type, or NULL            */
+    int64_t rows, cols;   /* >= 0; min(rows, cols) <= 2^14, rows cols <= 2^30                       */
+    int64_t x_ld, g_ld, copy_ld; /* elements between rows, >= cols; 0 = cols                       */
+    int32_t x_dtype, g_dtype, copy_dtype;
+    int32_t group;        /* in [0, groups)                                                        */
+    double weight_decay;  /* >= 0, finite as a float32                                             */
+    double lr_scale;      /* factor on the learning rate of this matrix, >= 0, finite as a float32 */
+} choco_muon_matrix;
+typedef struct {
+    double beta;          /* in [0, 1)                                                             */
+    double a, b, c;       /* of the polynomial; it keeps values of [0, 1] below 1.9 in every step and  */
+                          /* |a + b s^2 + c s^4| below 15 there (CHOCO_ERR_INVALID_ARG)             */
+    int32_t nesterov;     /* 0 or 1                                                                */
+    int32_t steps;        /* 0 .. 64                                                               */
+    int32_t products;     /* 3: X, S and B carry 22 bits; 1: 11 bits, a third of the work; 0: 1 for  */
+                          /* matrices whose x is bfloat16, 3 for others                             */
+    int32_t groups;       /* >= 1                                                                  */
+} choco_muon_params;
+
+/*
+ * The momentum m is a caller-owned DEVICE float32 array over all matrices, row after row without gaps, in the order of the
+ * list, every matrix starting on a multiple of 256 elements (the gaps are neither read nor written): choco_muon_state_size
+ * elements in all, 16-byte aligned; zeros for a fresh run.  The list is copied; the arrays it points to have to stay where
+ * they are.  The addresses from the first element of an x or copy to its last (padding between rows included) overlap no
+ * other x, copy or g (CHOCO_ERR_INVALID_ARG); gradients may overlap each other.  init allocates the workspace: 4 to 8 bytes for each
+ * element of a matrix and of its m x m square, sides rounded up to 128, for as many matrices at a time as 2 GiB holds (or the largest).
+ */
+int choco_muon_init(choco_muon** out, int32_t n_matrices, const choco_muon_matrix* matrices, const choco_muon_params* p);
+int choco_muon_destroy(choco_muon* opt);
+/* *elements: length of m (a multiple of 256); offsets (may be NULL): n_matrices starts. */
+int choco_muon_state_size(const choco_muon* opt, int64_t* elements, int64_t* offsets);
+/* New gradient pointers for all matrices (HOST array), same row pitch.  Synchronises `stream`; captured graphs read the new ones. */
+int choco_muon_set_grads(choco_muon* opt, const void* const* g, void* stream);
+/*
+ * choco_muon_step -- one step of all matrices, lr >= 0 and finite as a float32.  factor: DEVICE float [groups] (for
+ * instance choco_adamw_grad_norm's), or NULL for 1.  A group whose factor is infinite or NaN is left as it is, parameters, momentum and copy.
+ * Infinite or NaN gradients that no factor keeps out leave their matrix without meaning.  The result does not
+ * depend on the other matrices of the list.  May be captured; a replay takes the captured lr.  X has then changed outside
+ * the gossip step: call choco_invalidate (or run with choco_set_carry(ctx, 0)) before the next choco_gossip_step.
+ */
+int choco_muon_step(choco_muon* opt, float* m, double lr, const float* factor, void* stream);
+/* x = the X above of u = g for every matrix of the list: no momentum, no decay, copy is not written. */
+int choco_muon_orthogonalize(choco_muon* opt, void* stream);
+/* Synchronises `stream`.  CHOCO_ERR_TIMEOUT if a bounded wait in a kernel of this handle ever ran out ("Device-side waits" above):
+ * the part of a matrix that it was to write was not written. */
+int choco_muon_status(choco_muon* opt, void* stream);
+
 const char* choco_strerror(int code);
 /* cudaError_t of the last failing CUDA call on this context (0 if none). */
 int choco_last_cuda_error(const choco_ctx* ctx);

@@ -32,6 +32,8 @@ EXPORTS = [
     "choco_embedding_init", "choco_embedding_destroy", "choco_embedding_forward", "choco_embedding_backward",
     "choco_adamw_init", "choco_adamw_destroy", "choco_adamw_state_size", "choco_adamw_set_grads", "choco_adamw_grad_norm",
     "choco_adamw_set_rounding", "choco_adamw_step", "choco_adamw_read_state", "choco_adamw_get_steps", "choco_adamw_set_steps",
+    "choco_muon_init", "choco_muon_destroy", "choco_muon_state_size", "choco_muon_set_grads", "choco_muon_step", "choco_muon_orthogonalize",
+    "choco_muon_status",
 ]
 
 DTYPES = {"float32": 0, "bfloat16": 1, "float16": 2}   # choco_dtype
@@ -71,10 +73,20 @@ class choco_adamw_params(ctypes.Structure):
                 ("state_bits", ctypes.c_int32), ("groups", ctypes.c_int32)]
 
 
+class choco_muon_params(ctypes.Structure):
+    _fields_ = [("beta", ctypes.c_double), ("a", ctypes.c_double), ("b", ctypes.c_double), ("c", ctypes.c_double), ("nesterov", ctypes.c_int32),
+                ("steps", ctypes.c_int32), ("products", ctypes.c_int32), ("groups", ctypes.c_int32)]
+
+
 # choco_adamw_tensor as a numpy record: a list of tensors is an array of these
 ADAMW_TENSOR = [("x", "<u8"), ("g", "<u8"), ("copy", "<u8"), ("numel", "<i8"), ("x_dtype", "<i4"), ("g_dtype", "<i4"),
                 ("copy_dtype", "<i4"), ("group", "<i4"), ("weight_decay", "<f8"), ("lr_scale", "<f8")]
 ADAMW_BLOCK = 256   # elements that share a scale; tensors start on multiples of it in the moments
+
+# choco_muon_matrix likewise
+MUON_MATRIX = [("x", "<u8"), ("g", "<u8"), ("copy", "<u8"), ("rows", "<i8"), ("cols", "<i8"), ("x_ld", "<i8"), ("g_ld", "<i8"), ("copy_ld", "<i8"),
+               ("x_dtype", "<i4"), ("g_dtype", "<i4"), ("copy_dtype", "<i4"), ("group", "<i4"), ("weight_decay", "<f8"), ("lr_scale", "<f8")]
+MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 _lib = None
 
@@ -147,6 +159,13 @@ def load() -> ctypes.CDLL:
         lib.choco_adamw_read_state.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp]
         lib.choco_adamw_get_steps.argtypes = [vp, vp, vp]
         lib.choco_adamw_set_steps.argtypes = [vp, vp, vp]
+        lib.choco_muon_init.argtypes = [ctypes.POINTER(vp), i32, vp, ctypes.POINTER(choco_muon_params)]
+        lib.choco_muon_destroy.argtypes = [vp]
+        lib.choco_muon_state_size.argtypes = [vp, ctypes.POINTER(i64), vp]
+        lib.choco_muon_set_grads.argtypes = [vp, vp, vp]
+        lib.choco_muon_step.argtypes = [vp, vp, f64, vp, vp]
+        lib.choco_muon_orthogonalize.argtypes = [vp, vp]
+        lib.choco_muon_status.argtypes = [vp, vp]
         for name in EXPORTS:
             if name not in ("choco_strerror",):
                 getattr(lib, name).restype = ctypes.c_int
@@ -676,6 +695,79 @@ def choco_adamw_set_steps(opt, steps, stream=None) -> None:
     _check(load().choco_adamw_set_steps(opt, s.ctypes.data, _stream_of(stream, opt.device)))
 
 
+class MuonHandle(ctypes.c_void_p):
+    """What choco_muon_init returns: the library's handle, with the device it belongs to and the sizes of what its
+    calls take."""
+
+    def describe(self, device: int, n_matrices: int, groups: int, elements: int) -> None:
+        self.device, self.n_matrices, self.groups, self.elements = device, n_matrices, groups, elements
+
+
+def _check_momentum(opt, m) -> None:
+    if m is None and opt.elements == 0:
+        return
+    if m is None or m.get_device() != opt.device or _dtype(m) != 0 or m.numel() != opt.elements or not m.is_contiguous():
+        raise ChocoError(f"libchoco: the momentum must be a contiguous float32 array of {opt.elements} elements on GPU {opt.device}, not "
+                         f"{None if m is None else (m.dtype, list(m.shape), str(m.device))}", -1)
+
+
+def choco_muon_init(matrices, groups: int = 1, beta: float = 0.95, nesterov: bool = True, steps: int = 5, coefficients=MUON_COEFFICIENTS,
+                    products: int = 0):
+    """matrices: numpy array of MUON_MATRIX records (see muon_layer_matrices), on the current device."""
+    import numpy as np
+    import torch
+    t = np.ascontiguousarray(matrices, dtype=MUON_MATRIX)
+    a, b, c = coefficients
+    p = choco_muon_params(beta, a, b, c, 1 if nesterov else 0, steps, products, groups)
+    h, e = MuonHandle(), ctypes.c_int64()
+    _check(load().choco_muon_init(ctypes.byref(h), len(t), t.ctypes.data if len(t) else None, ctypes.byref(p)))
+    _check(load().choco_muon_state_size(h, ctypes.byref(e), None))
+    h.describe(torch.cuda.current_device(), len(t), groups, e.value)
+    return h
+
+
+def choco_muon_destroy(opt) -> None:
+    _check(load().choco_muon_destroy(opt))
+
+
+def choco_muon_state_size(opt):
+    """(elements of the momentum, first element of every matrix: an int64 array)."""
+    import numpy as np
+    e, off = ctypes.c_int64(), np.zeros(opt.n_matrices, dtype=np.int64)
+    _check(load().choco_muon_state_size(opt, ctypes.byref(e), off.ctypes.data))
+    return e.value, off
+
+
+def choco_muon_set_grads(opt, pointers, stream=None) -> None:
+    """New gradient addresses, one per matrix of the list."""
+    import numpy as np
+    g = np.ascontiguousarray(pointers, dtype=np.uint64)
+    if g.shape != (opt.n_matrices,):
+        raise ChocoError(f"libchoco: one address for each of {opt.n_matrices} matrices", -1)
+    _check(load().choco_muon_set_grads(opt, g.ctypes.data, _stream_of(stream, opt.device)))
+
+
+def choco_muon_step(opt, m, lr: float, factor=None, stream=None) -> None:
+    _check_momentum(opt, m)
+    _muon_step(opt, m, lr, factor, stream)
+
+
+def _muon_step(opt, m, lr, factor, stream) -> None:
+    """The step with a momentum that has been checked."""
+    if factor is not None:
+        _check_groups(opt, "factor", factor)
+    _check(load().choco_muon_step(opt, _ptr(m), lr, _ptr(factor), _stream_of(stream, opt.device)))
+
+
+def choco_muon_orthogonalize(opt, stream=None) -> None:
+    _check(load().choco_muon_orthogonalize(opt, _stream_of(stream, opt.device)))
+
+
+def choco_muon_status(opt, stream=None) -> None:
+    """Waits for `stream`; raises if a bounded wait in a kernel ever ran out."""
+    _check(load().choco_muon_status(opt, _stream_of(stream, opt.device)))
+
+
 # --------------------------------------------------------------------------- convenience
 
 
@@ -704,6 +796,57 @@ def adamw_layer_tensors(X, G, layer_off, weight_decay=0.0, lr_scale=1.0, copy=No
     t["weight_decay"] = np.broadcast_to(np.asarray(weight_decay, dtype=np.float64), (layers,))[None]
     t["lr_scale"] = np.broadcast_to(np.asarray(lr_scale, dtype=np.float64), (layers,))[None]
     return t.reshape(-1)
+
+
+def muon_layer_matrices(X, G, layer_off, shapes, weight_decay=0.0, lr_scale=None, copy=None):
+    """The list of matrices (worker by worker, layer by layer, group = worker) for rows of X and G [n, >= layer_off[-1]] cut at
+    layer_off.  shapes: (rows, cols) of a layer, with as many elements as the layer has, or None for one that is no
+    matrix (a bias, a table) and left out.  weight_decay and lr_scale are numbers or one per layer; without
+    lr_scale a matrix has sqrt(max(1, rows / cols))."""
+    import numpy as np
+    off = np.asarray(layer_off, dtype=np.int64)
+    n, layers = G.shape[0], len(off) - 1
+    if layers < 1 or off[0] != 0 or np.any(np.diff(off) < 0) or len(shapes) != layers:
+        raise ChocoError("libchoco: layer_off must start at 0 and not decrease, with a shape (or None) for each layer", -1)
+    which = [k for k in range(layers) if shapes[k] is not None]
+    dims = np.array([shapes[k] for k in which], dtype=np.int64).reshape(-1, 2)
+    if not which or np.any(dims < 0) or np.any(dims[:, 0] * dims[:, 1] != np.diff(off)[which]):
+        raise ChocoError("libchoco: the shapes must be those of the layers' elements, one matrix at least", -1)
+    t = np.zeros((n, len(which)), dtype=MUON_MATRIX)
+    rows = np.arange(n, dtype=np.int64)[:, None]
+    for name, a in (("x", X), ("g", G), ("copy", copy)):
+        if a is None:
+            continue
+        if a.get_device() != G.get_device():
+            raise ChocoError(f"libchoco: {name} is on {a.device} and G on {G.device}", -1)
+        if not a.is_cuda or a.dim() != 2 or a.shape[0] != n or a.shape[1] < off[-1] or (a.shape[1] > 1 and a.stride(1) != 1):
+            raise ChocoError(f"libchoco: {name} must be [{n}, >= {int(off[-1])}] on the GPU with contiguous rows", -1)
+        t[name] = (a.data_ptr() + (rows * a.stride(0) + off[which][None]) * a.element_size()).astype(np.uint64)
+        t[name + "_dtype"] = _dtype(a)
+    t["rows"], t["cols"] = dims[None, :, 0], dims[None, :, 1]
+    t["group"] = rows
+    if lr_scale is None:
+        t["lr_scale"] = np.sqrt(np.maximum(1.0, dims[:, 0] / np.maximum(dims[:, 1], 1)))[None]
+    else:
+        t["lr_scale"] = np.broadcast_to(np.asarray(lr_scale, dtype=np.float64), (layers,))[which][None]
+    t["weight_decay"] = np.broadcast_to(np.asarray(weight_decay, dtype=np.float64), (layers,))[which][None]
+    return t.reshape(-1)
+
+
+def _matrix_records(name, tensors):
+    """Addresses, types, sizes and row pitches of 2-D tensors, or of the matrices of 3-D ones."""
+    import numpy as np
+    parts = []
+    for a in tensors:
+        if not a.is_cuda or a.dim() not in (2, 3) or (a.shape[-1] > 1 and a.stride(-1) != 1) or a.device != tensors[0].device:
+            raise ChocoError(f"libchoco: {name} are matrices, or stacks of them, with contiguous rows on one GPU", -1)
+        count, step = (1, 0) if a.dim() == 2 else (a.shape[0], a.stride(0))
+        t = np.zeros(count, dtype=[("at", "<u8"), ("kind", "<i4"), ("rows", "<i8"), ("cols", "<i8"), ("ld", "<i8")])
+        t["at"] = (a.data_ptr() + np.arange(count, dtype=np.int64) * step * a.element_size()).astype(np.uint64)
+        t["kind"], t["rows"], t["cols"] = _dtype(a), a.shape[-2], a.shape[-1]
+        t["ld"] = a.stride(-2) if a.shape[-2] > 1 else a.shape[-1]
+        parts.append(t)
+    return np.concatenate(parts)
 
 
 @dataclasses.dataclass
@@ -821,6 +964,83 @@ class AdamW:
     def close(self):
         if getattr(self, "handle", None) is not None:
             choco_adamw_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Orthogonalizer:
+    """outputs[k] = the orthogonalised inputs[k] (see choco.h): lists of matrices, or of stacks [count, rows, cols] of them.
+    The arrays have to stay where they are; outputs may not overlap."""
+
+    def __init__(self, inputs, outputs, steps: int = 5, coefficients=MUON_COEFFICIENTS, products: int = 0):
+        import numpy as np
+        import torch
+        inputs, outputs = list(inputs), list(outputs)
+        if not inputs or [tuple(a.shape) for a in inputs] != [tuple(a.shape) for a in outputs]:
+            raise ChocoError("libchoco: inputs and outputs have the same shapes, one matrix at least", -1)
+        a, b = _matrix_records("inputs", inputs), _matrix_records("outputs", outputs)
+        if inputs[0].device != outputs[0].device or inputs[0].get_device() != torch.cuda.current_device():
+            raise ChocoError(f"libchoco: a handle belongs to the current device ({torch.cuda.current_device()}), and the matrices are on "
+                             f"{inputs[0].device} and {outputs[0].device}", -1)
+        if len(a) == 0:
+            raise ChocoError("libchoco: one matrix at least", -1)
+        t = np.zeros(len(a), dtype=MUON_MATRIX)
+        t["g"], t["g_dtype"], t["g_ld"] = a["at"], a["kind"], a["ld"]
+        t["x"], t["x_dtype"], t["x_ld"] = b["at"], b["kind"], b["ld"]
+        t["rows"], t["cols"] = a["rows"], a["cols"]
+        self._keep = (inputs, outputs)
+        self.handle = choco_muon_init(t, steps=steps, coefficients=coefficients, products=products)
+
+    def apply(self, stream=None):
+        choco_muon_orthogonalize(self.handle, stream)
+
+    def status(self, stream=None):
+        choco_muon_status(self.handle, stream)
+
+    def close(self):
+        if getattr(self, "handle", None) is not None:
+            choco_muon_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Muon:
+    """Muon over the matrices among the layers of all workers' rows: X and G are [n, ld] tensors, every worker a
+    group; shapes names the matrices (see muon_layer_matrices), other layers are left alone.  Owns the handle and (unless
+    `states` hands it over) the momentum, a flat array in the layout choco.h gives."""
+
+    def __init__(self, X, G, layer_off, shapes, weight_decay=0.0, lr_scale=None, copy=None, beta: float = 0.95, nesterov: bool = True,
+                 steps: int = 5, coefficients=MUON_COEFFICIENTS, products: int = 0, states=None):
+        import torch
+        matrices = muon_layer_matrices(X, G, layer_off, shapes, weight_decay, lr_scale, copy)
+        if G.get_device() != torch.cuda.current_device():
+            raise ChocoError(f"libchoco: a handle belongs to the current device ({torch.cuda.current_device()}), and G is on {G.device}", -1)
+        self.groups = G.shape[0]
+        self._keep = (X, G, copy)      # the list holds their addresses
+        self.handle = choco_muon_init(matrices, self.groups, beta, nesterov, steps, coefficients, products)
+        self.elements, self.offsets = choco_muon_state_size(self.handle)
+        self.m = torch.zeros(self.elements, dtype=torch.float32, device=X.device) if states is None else states
+        _check_momentum(self.handle, self.m)
+
+    def step(self, lr: float, factor=None, stream=None):
+        _muon_step(self.handle, self.m, lr, factor, stream)
+
+    def status(self, stream=None):
+        choco_muon_status(self.handle, stream)
+
+    def close(self):
+        if getattr(self, "handle", None) is not None:
+            choco_muon_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

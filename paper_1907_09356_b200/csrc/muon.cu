@@ -1,0 +1,1046 @@
+// Muon: a momentum step whose update is orthogonalised matrix by matrix.
+//
+// With U the averaged gradient of a matrix, X_0 = U / |U| (Frobenius) and m its smaller side,
+//     S = X X^T,   B = a I + b S + c S^2,   X <- B X          (`steps` times)
+// takes every singular value s to s (a + b s^2 + c s^4): an odd polynomial that drives them towards one.  The
+// work is three chains of products per step: S (m x m, symmetric), S^2 (likewise) and B X (m x k).
+//
+// Numbers.  The products run on the tensor cores, float16 factors and float32 sums.  X, S and B are scaled
+// by powers of two into the middle of float16's range (X by 2^ex with 2^ex ~ sqrt(m k), so that its elements start
+// near 1; S and B by 2^es ~ m, so that their diagonals do) and kept as a float16 value and, with three products, the
+// float16 value of what that leaves: hi hi + hi lo + lo hi carries 22 bits.  One product carries 11 and is what 16-bit
+// results take: over five steps its roundings come to 0.0012 .. 0.0017 of the result (2-norm), as much as rounding the
+// result to bfloat16 (0.0017); with three they come to 4e-7.
+//
+// Layout.  X, S and B lie in the workspace as tiles of 128 rows x 64 halves, in the very bytes that the tensor
+// cores read from shared memory (tensor.cuh), high part and low part behind one another.  A tile is one contiguous
+// copy in either direction and needs no descriptor.  The side of a matrix with fewer elements is the row side (tall ones
+// are turned on the way in and out), padding is zero and stays zero.  S and B are symmetric: only tiles on or below the
+// diagonal are computed, stored and read; a product that needs one above it reads the stored one turned.
+#include <math.h>
+#include <cstring>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "common.cuh"
+#include "dtypes.cuh"
+#include "tensor.cuh"
+
+namespace choco {
+namespace {
+
+constexpr int kSide = 128;                         // rows of a tile, columns of a product's part
+constexpr int kHalves = 64;                        // columns of a tile
+constexpr uint32_t kTileBytes = kSide * kHalves * 2;
+constexpr uint32_t kPieceBytes = kTileBytes / 2;   // half of its rows
+constexpr int kBlock = 256;                        // matrices start on multiples of this in the momentum
+constexpr int kUnit = 4096;                        // elements of one block of the momentum kernel
+constexpr int kUnitThreads = 256;
+constexpr int kTileThreads2 = 256;                 // of the kernels that cut matrices into tiles and put them together
+
+struct Matrix {
+    void* x;
+    const void* g;
+    void* copy;
+    int64_t x_ld, g_ld, copy_ld;
+    int64_t state;          // first element in m
+    int64_t at[2];          // tiles of X and of its successor, in bytes of the workspace
+    int64_t s_at, b_at;     // of S and B
+    int32_t rows, cols;
+    int32_t m, k;           // rows and columns of X: the smaller side and the larger
+    int32_t mt, nb;         // tiles of X: rows of tiles, tiles in a row (an even number)
+    int32_t ex, es;         // powers of two that X, and S and B, are scaled by
+    int32_t group;
+    float weight_decay, lr_scale;
+    int32_t unit0, units;   // blocks of the momentum kernel
+    int8_t x_dtype, g_dtype, copy_dtype;
+    bool tall;              // rows > cols
+    bool whole;             // rows of g behind one another, and its elements in aligned fours
+};
+struct Unit {
+    int32_t matrix;
+    int32_t part;           // of its units
+};
+struct Part {               // of a product: kSide CG rows from kSide CG i, and as many columns from kSide CG j
+    int32_t matrix;
+    int16_t i, j;
+};
+struct Block {              // a tile of X
+    int32_t matrix;
+    int16_t row, col;
+};
+struct Scale {              // of a matrix in this step: X_0 = (U first) second; both 0 where it is left alone or zero
+    float first, second;
+};
+
+__device__ __forceinline__ float averaged(float m, float g, float beta, float omb) { return m * beta + g * omb; }
+
+// ---------------------------------------------------------------------------------------- momentum and norms
+struct MomentArgs {
+    const Matrix* mats;
+    const Unit* units;
+    float* m;               // null: no momentum, U = g
+    const float* factor;    // null: 1
+    double* partial;        // per unit
+    uint32_t* done;         // per matrix, 0 between calls
+    Scale* scale;           // per matrix
+    float beta, omb;
+    int32_t nesterov;
+};
+
+// m = beta m + (1 - beta) c g, and the sum of squares of U by unit.  The last unit of a matrix to finish adds its
+// units up in their order and forms the scale, in float64: squares of small gradients leave float32's range.
+template <typename GT>
+__device__ double moment_unit(const MomentArgs& a, const Matrix& t, int64_t begin, int64_t end, float c)
+{
+    double sum = 0.0;
+    float* m = a.m ? a.m + t.state : nullptr;
+    const GT* g = static_cast<const GT*>(t.g);
+    if (t.whole) {
+        const int64_t quads = end / 4 * 4;
+        for (int64_t e = begin + 4 * (int64_t)threadIdx.x; e < quads; e += 4 * kUnitThreads) {
+            Raw<GT, 4> raw;
+            load_raw(raw, g + e);
+            float u[4];
+            if (m) {
+                const float4 old = *reinterpret_cast<const float4*>(m + e);
+                float v[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float gq = raw_get(raw, q) * c;
+                    v[q] = averaged(v[q], gq, a.beta, a.omb);
+                    u[q] = a.nesterov ? averaged(v[q], gq, a.beta, a.omb) : v[q];
+                }
+                *reinterpret_cast<float4*>(m + e) = make_float4(v[0], v[1], v[2], v[3]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) u[q] = raw_get(raw, q) * c;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum = fma((double)u[q], (double)u[q], sum);
+        }
+        begin = quads > begin ? quads : begin;
+    }
+    for (int64_t e = begin + threadIdx.x; e < end; e += kUnitThreads) {
+        const int64_t row = (uint32_t)e / (uint32_t)t.cols, col = (uint32_t)e % (uint32_t)t.cols;
+        const float ge = to_float(g[row * t.g_ld + col]) * c;
+        float u = ge;
+        if (m) {
+            const float v = averaged(m[e], ge, a.beta, a.omb);
+            m[e] = v;
+            u = a.nesterov ? averaged(v, ge, a.beta, a.omb) : v;
+        }
+        sum = fma((double)u, (double)u, sum);
+    }
+    return sum;
+}
+
+__device__ __forceinline__ double block_sum(double v, double* ws) // 256 threads; the sum is thread 0's
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double s = 0.0;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < kUnitThreads / 32; ++w) s += ws[w];
+    __syncthreads();
+    return s;
+}
+
+__global__ void __launch_bounds__(kUnitThreads) moment_kernel(MomentArgs a)
+{
+    __shared__ double ws[kUnitThreads / 32];
+    __shared__ bool last;
+    const Unit un = a.units[blockIdx.x];
+    const Matrix& t = a.mats[un.matrix];
+    allow_next_kernel();
+    wait_for_previous_kernel();
+    const float c = a.factor ? a.factor[t.group] : 1.f;
+    const bool skip = !isfinite(c);
+    double sum = 0.0;
+    if (!skip) {
+        const int64_t begin = (int64_t)un.part * kUnit, all = (int64_t)t.rows * t.cols;
+        const int64_t end = begin + kUnit < all ? begin + kUnit : all;
+        if (t.g_dtype == CHOCO_F32) sum = moment_unit<float>(a, t, begin, end, c);
+        else if (t.g_dtype == CHOCO_BF16) sum = moment_unit<__nv_bfloat16>(a, t, begin, end, c);
+        else sum = moment_unit<__half>(a, t, begin, end, c);
+    }
+    sum = block_sum(sum, ws);
+    if (threadIdx.x == 0) {
+        a.partial[t.unit0 + un.part] = sum;
+        __threadfence();
+        last = atomicAdd(a.done + un.matrix, 1u) == (uint32_t)t.units - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    sum = 0.0;
+    for (int i = threadIdx.x; i < t.units; i += kUnitThreads) sum += __ldcg(a.partial + t.unit0 + i);
+    sum = block_sum(sum, ws);
+    if (threadIdx.x == 0) {
+        a.done[un.matrix] = 0;
+        Scale s = {0.f, 0.f};
+        if (!skip && sum != 0.0) {
+            const double f = ldexp(1.0, t.ex) / sqrt(sum);   // from 1e-44 to 1e49: in two factors where float32 ends
+            const double pre = f > 1e30 ? 0x1p100 : f < 1e-30 ? 0x1p-100 : 1.0;
+            s.first = (float)pre;
+            s.second = (float)(f / pre);
+        }
+        a.scale[un.matrix] = s;
+    }
+}
+
+// ---------------------------------------------------------------------------------------- matrices <-> tiles
+struct TileArgs {
+    const Matrix* mats;
+    const Block* blocks;
+    uint8_t* work;
+    const Scale* scale;
+    float* m;
+    const float* factor;
+    float beta, omb, lr;
+    int32_t nesterov;
+    int32_t planes;
+    int32_t which;          // of the two X
+    int32_t update;         // x -= lr .. O (a step), or x = O
+};
+
+__device__ __forceinline__ uint32_t piece_at(int row, int piece) { return (uint32_t)(row * 128 + ((piece ^ (row & 7)) << 4)); }
+
+__device__ __forceinline__ uint32_t two_halves(float a, float b)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// eight values as float16, and what that leaves as float16
+__device__ __forceinline__ void split8(const float* v, uint4& hi, uint4& lo, bool want_lo)
+{
+    uint32_t h[4], l[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        h[q] = two_halves(v[2 * q], v[2 * q + 1]);
+        if (want_lo) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[q]));
+            l[q] = two_halves(v[2 * q] - f.x, v[2 * q + 1] - f.y);
+        }
+    }
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+__device__ __forceinline__ void join8(uint4 hi, uint4 lo, float* v, bool has_lo)
+{
+    const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[q]));
+        if (has_lo) {
+            const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&l[q]));
+            f.x += r.x;
+            f.y += r.y;
+        }
+        v[2 * q] = f.x;
+        v[2 * q + 1] = f.y;
+    }
+}
+
+// U of one element of the matrix
+__device__ __forceinline__ float update_of(const TileArgs& a, const Matrix& t, int row, int col, float c)
+{
+    const float g = bits_to_float(load_bits(t.g, (int64_t)row * t.g_ld + col, t.g_dtype), t.g_dtype) * c;
+    if (!a.m) return g;
+    const float m = a.m[t.state + (int64_t)row * t.cols + col];
+    return a.nesterov ? averaged(m, g, a.beta, a.omb) : m;
+}
+
+// A tile of X_0: 128 rows x 64 columns of U, turned where the matrix is tall.
+__global__ void __launch_bounds__(kTileThreads2) cut_kernel(TileArgs a)
+{
+    __shared__ float turn[kHalves][kSide + 1];
+    const Block bl = a.blocks[blockIdx.x];
+    const Matrix& t = a.mats[bl.matrix];
+    const int row0 = bl.row * kSide, col0 = bl.col * kHalves;
+    allow_next_kernel();
+    wait_for_previous_kernel();
+    const Scale sc = a.scale[bl.matrix];
+    const bool live = sc.second != 0.f;     // (true for NaN)
+    const float c = a.factor ? a.factor[t.group] : 1.f;
+    if (t.tall) {
+        if (live)
+            for (int e = threadIdx.x; e < kSide * kHalves; e += kTileThreads2) {
+                const int r = e % kSide, q = e / kSide;
+                turn[q][r] = row0 + r < t.m && col0 + q < t.k ? update_of(a, t, col0 + q, row0 + r, c) : 0.f;
+            }
+        __syncthreads();
+    }
+    uint8_t* to = a.work + t.at[0] + ((int64_t)bl.row * t.nb + bl.col) * a.planes * kTileBytes;
+    const int piece = threadIdx.x & 7;
+    for (int r = threadIdx.x >> 3; r < kSide; r += kTileThreads2 / 8) {
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int col = col0 + piece * 8 + q;
+            float u = 0.f;
+            if (live) u = t.tall ? turn[piece * 8 + q][r] : row0 + r < t.m && col < t.k ? update_of(a, t, row0 + r, col, c) : 0.f;
+            v[q] = u * sc.first * sc.second;
+        }
+        uint4 hi, lo;
+        split8(v, hi, lo, a.planes == 2);
+        *reinterpret_cast<uint4*>(to + piece_at(r, piece)) = hi;
+        if (a.planes == 2) *reinterpret_cast<uint4*>(to + kTileBytes + piece_at(r, piece)) = lo;
+    }
+}
+
+__device__ __forceinline__ void apply_one(const TileArgs& a, const Matrix& t, int row, int col, float o)
+{
+    if (!a.update) {
+        store_from_float(t.x, (int64_t)row * t.x_ld + col, t.x_dtype, o);
+        return;
+    }
+    const int64_t at = (int64_t)row * t.x_ld + col;
+    const float x = bits_to_float(load_bits(t.x, at, t.x_dtype), t.x_dtype), lr = a.lr * t.lr_scale;
+    const float next = x - (o * lr + x * (a.lr * t.weight_decay * t.lr_scale));
+    store_from_float(t.x, at, t.x_dtype, next);
+    if (t.copy) store_from_float(t.copy, (int64_t)row * t.copy_ld + col, t.copy_dtype, next);
+}
+
+// The last X of a matrix, tile by tile, to where it goes.
+__global__ void __launch_bounds__(kTileThreads2) apply_kernel(TileArgs a)
+{
+    __shared__ float turn[kHalves][kSide + 1];
+    const Block bl = a.blocks[blockIdx.x];
+    const Matrix& t = a.mats[bl.matrix];
+    const int row0 = bl.row * kSide, col0 = bl.col * kHalves;
+    allow_next_kernel();
+    wait_for_previous_kernel();
+    if (a.factor && !isfinite(a.factor[t.group])) return;
+    const uint8_t* from = a.work + t.at[a.which] + ((int64_t)bl.row * t.nb + bl.col) * a.planes * kTileBytes;
+    const float unscale = exp2f((float)-t.ex);
+    const int piece = threadIdx.x & 7;
+    for (int r = threadIdx.x >> 3; r < kSide; r += kTileThreads2 / 8) {
+        const uint4 hi = *reinterpret_cast<const uint4*>(from + piece_at(r, piece));
+        const uint4 lo = a.planes == 2 ? *reinterpret_cast<const uint4*>(from + kTileBytes + piece_at(r, piece)) : make_uint4(0, 0, 0, 0);
+        float v[8];
+        join8(hi, lo, v, a.planes == 2);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) turn[piece * 8 + q][r] = v[q] * unscale;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < kSide * kHalves; e += kTileThreads2) {
+        const int r = t.tall ? e % kSide : e / kHalves, q = t.tall ? e / kSide : e % kHalves;
+        if (row0 + r < t.m && col0 + q < t.k) apply_one(a, t, t.tall ? col0 + q : row0 + r, t.tall ? row0 + r : col0 + q, turn[q][r]);
+    }
+}
+
+// ---------------------------------------------------------------------------------------- products
+enum Kind { kGram, kSquare, kNext };    // S = X X^T;  B = a I + b S + c S^2;  X' = B X
+
+struct ProductArgs {
+    const Matrix* mats;
+    const Part* parts;
+    uint8_t* work;
+    uint32_t* errors;
+    float a, b, c;
+    int32_t which;          // of the two X: the one that is read
+};
+
+template <int P, int CG>
+struct Plan {
+    static constexpr int kPlanes = P == 3 ? 2 : 1;
+    static constexpr uint32_t kOperand = kPlanes * kTileBytes;
+    static constexpr uint32_t kStage = 2 * kOperand;             // of both factors, 64 of K
+    static constexpr int kStages = P == 3 ? 3 : CG == 2 ? 6 : 3; // one product and one CTA: two blocks of threads to an SM
+    // The tensor cores cut sums to float32 towards zero, a bias of half a unit in the last place for every 16 of K.  With three
+    // products the sums therefore leave tensor memory after every 64 of K and are added up in registers, to the nearest.
+    static constexpr int kChunk = P == 3 ? 1 : 1 << 20;          // steps of 64 of K between two of these
+    static constexpr int kSums = P == 3 ? 2 : 1;                 // sets of sums in tensor memory
+    static constexpr uint32_t kColumns = kSide * CG;             // of one set: the part's columns
+    static constexpr int kWarps = 4 * CG;                        // that take the sums; two more feed the tensor cores
+    static constexpr int kThreads = CG == 2 ? 384 : 192;         // (three whole warpgroups where registers move between them)
+    static constexpr int kBlocks = P == 1 && CG == 1 ? 2 : 1;    // to an SM
+    static constexpr uint32_t kOut = 2 * kOperand;               // bytes of 128 x 128 results
+    static constexpr uint32_t kShared = kStages * kStage + 1024;
+    static_assert(CG * kOut <= kStages * kStage, "results are put together where the factors were");
+};
+
+template <int THREADS>
+__device__ __forceinline__ void block_part_sync() // of the threads that take the sums, which come first in a block
+{
+    asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+}
+
+// Copies of one factor for 64 of K into shared memory.  Rows [128 i, 128 i + 128) of X (along its rows) ...
+template <int PL>
+__device__ __forceinline__ void fetch_along(uint8_t* to, const uint8_t* x, int64_t tile, uint64_t* bar)
+{
+    bulk_load(to, x + tile * PL * kTileBytes, PL * kTileBytes, bar);
+}
+// ... or 128 columns, of tiles `tile` and `tile + 1`, their upper or lower 64 rows
+template <int PL>
+__device__ __forceinline__ void fetch_turned(uint8_t* to, const uint8_t* x, int64_t tile, int lower, uint64_t* bar)
+{
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+        for (int p = 0; p < PL; ++p)
+            bulk_load(to + p * kTileBytes + cb * kPieceBytes, x + ((tile + cb) * PL + p) * kTileBytes + lower * kPieceBytes, kPieceBytes, bar);
+}
+
+template <int KIND, int P, int CG>
+__global__ void __launch_bounds__(Plan<P, CG>::kThreads, Plan<P, CG>::kBlocks) __cluster_dims__(CG, 1, 1) product_kernel(ProductArgs a)
+{
+    using L = Plan<P, CG>;
+    constexpr int PL = L::kPlanes, ST = L::kStages;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t full[ST], empty[ST], peer[ST], sums[2], taken[2], third;
+    __shared__ uint32_t tmem_at;
+    __shared__ volatile uint32_t failed;
+    uint8_t* stage = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const Part part = a.parts[blockIdx.x / CG];
+    const Matrix& t = a.mats[part.matrix];
+    const int it = part.i * CG + rank, jt = part.j * CG + rank;  // this CTA's rows of tiles of the two factors
+    const int mt = t.mt, nb = t.nb;
+    const int columns = KIND == kNext ? nb / 2 : mt;             // of tiles of 128 columns
+    const bool has_a = it < mt, has_b = jt < columns;
+    const bool same = KIND == kGram && part.i == part.j;         // both factors are the same rows
+    const int nk = KIND == kGram ? (t.k + kHalves - 1) / kHalves : (t.m + kHalves - 1) / kHalves;
+    if (tid == 0) {
+        for (int s = 0; s < ST; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+            mbar_init(&peer[s], 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&sums[s], 1);
+            mbar_init(&taken[s], L::kWarps * CG);
+        }
+        mbar_init(&third, 1);
+        failed = 0;
+    }
+    if (warp == 0) tmem_alloc<CG>(&tmem_at, L::kSums * L::kColumns);
+    tmem_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync();
+    tmem_fence_after();
+    const uint32_t acc = tmem_at;
+    allow_next_kernel();
+    wait_for_previous_kernel();
+
+    const uint8_t* x = a.work + t.at[a.which];
+    const uint8_t* s_in = a.work + t.s_at;
+    const uint8_t* first = KIND == kGram ? x : KIND == kSquare ? s_in : a.work + t.b_at;
+    // (128 sums a thread want more registers than 384 threads can have: 168 each at launch become 224 and 40)
+    const uint32_t from = acc + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * kSide;
+    if (warp < L::kWarps) {                                      // the sums: a thread has 128 columns of a row
+        if constexpr (P == 3 && CG == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        float v[P == 3 ? kSide : 1];
+#pragma unroll
+        for (int e = 0; e < (P == 3 ? kSide : 1); ++e) v[e] = 0.f;
+        const int chunks = (nk + L::kChunk - 1) / L::kChunk;
+        for (int ch = 0; ch < chunks; ++ch) {
+            if (!mbar_wait(&sums[ch & 1], (ch >> 1) & 1)) {
+                failed = 1;
+                break;
+            }
+            tmem_fence_after();
+            if constexpr (P == 3) {
+#pragma unroll
+                for (int q = 0; q < kSide / 32; ++q) {
+                    uint32_t r[32];
+                    tmem_load32(from + (ch & 1) * L::kColumns + q * 32, r);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[q * 32 + e] += __uint_as_float(r[e]);
+                }
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_at(&taken[ch & 1], 0);
+            }
+        }
+        // results go out as tiles; S at the same place comes in first where B needs it
+        block_part_sync<L::kWarps * 32>();
+        auto there = [&](int h) { return has_a && part.j * CG + h < columns; };
+        const int64_t out_tile = KIND == kNext ? (int64_t)it * nb + 2 * part.j * CG : ((int64_t)it * mt + part.j * CG) * 2;
+        if (KIND == kSquare && !failed) {
+            if (tid == 0) {
+                mbar_expect_tx(&third, (there(0) ? L::kOut : 0) + (CG == 2 && there(1) ? L::kOut : 0));
+                for (int h = 0; h < CG; ++h)
+                    if (there(h)) bulk_load(stage + h * L::kOut, s_in + (out_tile + 2 * h) * PL * kTileBytes, L::kOut, &third);
+            }
+            if (!mbar_wait(&third, 0)) failed = 1;
+        }
+        if (!failed) {
+            const float up = exp2f((float)t.es), down = exp2f((float)-t.es), gram = exp2f((float)(t.es - 2 * t.ex));
+            const int r = tid & 127, h = warp >> 2;
+            uint8_t* out = stage + h * L::kOut;
+            const bool diagonal = it == part.j * CG + h;
+#pragma unroll
+            for (int q32 = 0; q32 < kSide / 32; ++q32) {
+                float w[32];
+                if constexpr (P == 3) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) w[e] = v[q32 * 32 + e];
+                } else {
+                    uint32_t bits[32];
+                    tmem_load32(from + q32 * 32, bits);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) w[e] = __uint_as_float(bits[e]);
+                }
+#pragma unroll
+                for (int p8 = 0; p8 < 4; ++p8) {
+                    const int p = q32 * 4 + p8;
+                    uint4* hi = reinterpret_cast<uint4*>(out + (p >> 3) * PL * kTileBytes + piece_at(r, p & 7));
+                    uint4* lo = reinterpret_cast<uint4*>(out + ((p >> 3) * PL + PL - 1) * kTileBytes + piece_at(r, p & 7));
+                    float f[8];
+                    if constexpr (KIND == kSquare) {
+                        float s[8];
+                        join8(*hi, *lo, s, PL == 2);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            f[q] = fmaf(a.b, s[q], a.c * down * w[p8 * 8 + q]);
+                            if (diagonal && r == p * 8 + q) f[q] += a.a * up;
+                        }
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) f[q] = w[p8 * 8 + q] * (KIND == kGram ? gram : down);
+                    }
+                    uint4 h4, l4;
+                    split8(f, h4, l4, PL == 2);
+                    *hi = h4;
+                    if (PL == 2) *lo = l4;
+                }
+            }
+            fence_async();
+        }
+        block_part_sync<L::kWarps * 32>();
+        if (tid == 0 && !failed) {
+            uint8_t* to = KIND == kGram ? a.work + t.s_at : KIND == kSquare ? a.work + t.b_at : a.work + t.at[a.which ^ 1];
+            for (int h = 0; h < CG; ++h)
+                if (there(h)) bulk_store(to + (out_tile + 2 * h) * PL * kTileBytes, stage + h * L::kOut, L::kOut);
+            bulk_stores_done();
+        }
+    } else {
+        if constexpr (P == 3 && CG == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == L::kWarps) {                                     // the copies
+            if (lane == 0) {
+                fence_async();
+                int kb = 0;
+                for (; kb < nk; ++kb) {
+                    const int s = kb % ST;
+                    if (kb >= ST && !mbar_wait(&empty[s], (kb / ST - 1) & 1)) {
+                        failed = 1;
+                        break;
+                    }
+                    uint8_t* to_a = stage + s * L::kStage;
+                    uint8_t* to_b = to_a + L::kOperand;
+                    const int ct = kb >> 1;
+                    const bool load_b = has_b && !same;
+                    mbar_expect_tx(&full[s], (has_a ? L::kOperand : 0) + (load_b ? L::kOperand : 0));
+                    if (has_a) {
+                        if (KIND == kGram) fetch_along<PL>(to_a, x, (int64_t)it * nb + kb, &full[s]);
+                        else if (ct / CG <= part.i) fetch_along<PL>(to_a, first, ((int64_t)it * mt + ct) * 2 + (kb & 1), &full[s]);
+                        else fetch_turned<PL>(to_a, first, ((int64_t)ct * mt + it) * 2, kb & 1, &full[s]);
+                    }
+                    if (load_b) {
+                        if (KIND == kGram) fetch_along<PL>(to_b, x, (int64_t)jt * nb + kb, &full[s]);
+                        else if (KIND == kNext) fetch_turned<PL>(to_b, x, (int64_t)ct * nb + 2 * jt, kb & 1, &full[s]);
+                        else if (ct / CG <= part.j) fetch_along<PL>(to_b, first, ((int64_t)jt * mt + ct) * 2 + (kb & 1), &full[s]);
+                        else fetch_turned<PL>(to_b, first, ((int64_t)ct * mt + jt) * 2, kb & 1, &full[s]);
+                    }
+                }
+                if (failed)                                          // copies under way are sat out
+                    for (int q = kb > ST ? kb - ST : 0; q < kb; ++q) mbar_wait(&full[q % ST], (q / ST) & 1);
+            }
+        } else if (warp == L::kWarps + 1) {                          // the products
+            if (lane == 0 && rank == 0) {
+                bool ok = true;
+                for (int kb = 0; kb < nk; ++kb) {
+                    const int s = kb % ST, ch = kb / L::kChunk;
+                    const bool begins = kb % L::kChunk == 0;
+                    if (begins && ch >= 2) ok = mbar_wait_cluster(&taken[ch & 1], (ch / 2 - 1) & 1);
+                    ok = ok && mbar_wait(&full[s], (kb / ST) & 1);
+                    if (CG == 2) ok = ok && mbar_wait_cluster(&peer[s], (kb / ST) & 1);
+                    if (!ok) {
+                        failed = 1;
+                        break;
+                    }
+                    tmem_fence_after();
+                    const int ct = kb >> 1;
+                    const bool turn_a = KIND != kGram && ct / CG > part.i;
+                    const bool turn_b = KIND == kNext || (KIND == kSquare && ct / CG > part.j);
+                    const uint32_t at_a = smem_u32(stage) + s * L::kStage, at_b = same ? at_a : at_a + L::kOperand;
+                    const uint32_t shape = product_shape(kSide * CG, kSide * CG) | (turn_a ? kTurnA : 0) | (turn_b ? kTurnB : 0);
+                    const uint64_t da = turn_a ? operand_turned(at_a, kPieceBytes) : operand_along(at_a);
+                    const uint64_t db = turn_b ? operand_turned(at_b, kPieceBytes) : operand_along(at_b);
+                    const uint64_t na = turn_a ? kNextTurned : kNextAlong, nbk = turn_b ? kNextTurned : kNextAlong;
+                    const uint32_t to = acc + (ch & 1) * (L::kSums == 2 ? L::kColumns : 0);
+                    constexpr uint64_t low = kTileBytes >> 4;
+                    if constexpr (P == 3)                            // the small products first, while the sums are small
+#pragma unroll
+                        for (int q = 0; q < kHalves / 16; ++q) {
+                            product<CG>(to, da + q * na, db + q * nbk + low, shape, !begins || q > 0);
+                            product<CG>(to, da + q * na + low, db + q * nbk, shape, true);
+                        }
+#pragma unroll
+                    for (int q = 0; q < kHalves / 16; ++q) product<CG>(to, da + q * na, db + q * nbk, shape, P == 3 || !begins || q > 0);
+                    products_done<CG>(&empty[s]);
+                    if (kb + 1 == nk || (kb + 1) % L::kChunk == 0) products_done<CG>(&sums[ch & 1]);
+                }
+            } else if (lane == 0) {                                  // the other CTA of a pair tells the first what has come
+                for (int kb = 0; kb < nk; ++kb) {
+                    const int s = kb % ST;
+                    if (!mbar_wait(&full[s], (kb / ST) & 1)) {
+                        failed = 1;
+                        break;
+                    }
+                    fence_async();
+                    mbar_arrive_at(&peer[s], 0);
+                }
+            }
+        }
+    }
+    __syncwarp();
+    tmem_fence_before();
+    __syncthreads();
+    if (tid == 0 && failed) atomicAdd(a.errors, 1u);
+    if (CG == 2) cluster_sync();
+    if (warp == 0) tmem_free<CG>(acc, L::kSums * L::kColumns);
+}
+
+using ProductKernel = void (*)(ProductArgs);
+template <int P, int CG>
+ProductKernel product_of(int kind)
+{
+    return kind == kGram ? product_kernel<kGram, P, CG> : kind == kSquare ? product_kernel<kSquare, P, CG> : product_kernel<kNext, P, CG>;
+}
+
+// matrices of a wave that take the same kernels: one product or three, one CTA to a part or two
+struct Class {
+    int64_t symmetric, symmetric_end;   // parts of S and B
+    int64_t next, next_end;             // parts of X'
+};
+struct Wave {
+    int64_t blocks[2], blocks_end[2];   // tiles of X, of matrices with one product and with three
+    Class classes[2][2];                // [three products][pairs]
+};
+
+constexpr int64_t kWaveBytes = (int64_t)2 << 30; // workspace that matrices are taken together up to
+constexpr int64_t kMostElements = (int64_t)1 << 30;
+constexpr int32_t kMostSide = 1 << 14;           // of the smaller side: S is m x m
+
+struct Range { // of addresses
+    uintptr_t begin, end;
+};
+
+} // namespace
+} // namespace choco
+
+using namespace choco;
+
+struct choco_muon {
+    choco_muon_params params;
+    int device;
+    bool broken;                   // the table on the device may be half written
+    std::vector<Matrix> mats;      // as on the device
+    std::vector<Range> written;
+    std::vector<int64_t> offsets;
+    std::vector<Wave> waves;
+    int64_t elements;
+    int64_t nunits;
+    void* memory;
+    Matrix* d_mats;
+    Unit* d_units;
+    Part* d_parts;
+    Block* d_blocks;
+    double* d_partial;
+    uint32_t* d_done;
+    uint32_t* d_errors;
+    Scale* d_scale;
+    uint8_t* d_work;
+};
+
+namespace {
+
+bool on_device(const choco_muon* o)
+{
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == o->device;
+}
+int status_of(cudaError_t e)
+{
+    if (e == cudaSuccess) return CHOCO_OK;
+    cudaGetLastError();
+    return CHOCO_ERR_CUDA;
+}
+void free_all(choco_muon* o)
+{
+    cudaFree(o->memory);
+    delete o;
+}
+
+Range range_of(const void* p, int64_t rows, int64_t cols, int64_t ld, int32_t dtype)
+{
+    return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)(((rows - 1) * ld + cols) * dtype_size(dtype))};
+}
+
+// Largest singular value that the polynomial makes of one in [0, most], and the largest |a + b s^2 + c s^4| on the way.
+void reach(const choco_muon_params& p, double most, double* value, double* slope)
+{
+    *value = *slope = 0.0;
+    for (int i = 0; i <= 4096; ++i) {
+        const double s = most * i / 4096, q = std::fabs(p.a + s * s * (p.b + s * s * p.c));
+        *slope = std::max(*slope, q);
+        *value = std::max(*value, s * q);
+    }
+}
+bool polynomial_ok(const choco_muon_params& p)
+{
+    if (!std::isfinite(p.a) || !std::isfinite(p.b) || !std::isfinite(p.c)) return false;
+    double most = 1.0;
+    for (int k = 0; k < p.steps; ++k) {
+        double value, slope;
+        reach(p, most, &value, &slope);
+        if (!(value <= 1.9) || !(slope <= 15.0)) return false; // S and B stay inside float16 at their scales
+        most = std::max(1.0, value);
+    }
+    return true;
+}
+
+template <typename T>
+int64_t carve(int64_t& at, int64_t count)
+{
+    at = (at + 255) / 256 * 256;
+    const int64_t here = at;
+    at += (int64_t)sizeof(T) * count;
+    return here;
+}
+
+// Fills the host tables.  Throws std::bad_alloc.
+int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit>& units, std::vector<Part>& parts, std::vector<Block>& blocks,
+         int64_t* work)
+{
+    int64_t at = 0;
+    std::vector<int32_t> kinds; // of every matrix: 1 = three products
+    for (int32_t i = 0; i < n; ++i) {
+        const choco_muon_matrix& q = ms[i];
+        if (q.rows < 0 || q.cols < 0 || q.x_ld < 0 || q.g_ld < 0 || q.copy_ld < 0) return CHOCO_ERR_INVALID_ARG;
+        if (q.group < 0 || q.group >= o->params.groups || !dtype_ok(q.x_dtype) || !dtype_ok(q.g_dtype) || !dtype_ok(q.copy_dtype))
+            return CHOCO_ERR_INVALID_ARG;
+        if (!(q.weight_decay >= 0.0) || !(q.lr_scale >= 0.0) || !std::isfinite((float)q.weight_decay) || !std::isfinite((float)q.lr_scale))
+            return CHOCO_ERR_INVALID_ARG;
+        const bool some = q.rows > 0 && q.cols > 0;
+        if (some && (!q.x || !q.g)) return CHOCO_ERR_INVALID_ARG;
+        if ((q.x_ld && q.x_ld < q.cols) || (q.g_ld && q.g_ld < q.cols) || (q.copy_ld && q.copy_ld < q.cols)) return CHOCO_ERR_INVALID_ARG;
+        if (!aligned_to(q.x, dtype_size(q.x_dtype)) || !aligned_to(q.g, dtype_size(q.g_dtype)) || !aligned_to(q.copy, dtype_size(q.copy_dtype)))
+            return CHOCO_ERR_MISALIGNED;
+        if (some && (std::min(q.rows, q.cols) > kMostSide || std::max(q.rows, q.cols) > kMostElements / std::min(q.rows, q.cols) ||
+                     std::max({q.x_ld, q.g_ld, q.copy_ld}) > (int64_t)1 << 38))
+            return CHOCO_ERR_TOO_LARGE;
+        Matrix t = {};
+        t.x = q.x; t.g = q.g; t.copy = q.copy;
+        t.rows = some ? (int32_t)q.rows : 0; t.cols = some ? (int32_t)q.cols : 0;
+        t.x_ld = q.x_ld ? q.x_ld : q.cols; t.g_ld = q.g_ld ? q.g_ld : q.cols; t.copy_ld = q.copy_ld ? q.copy_ld : q.cols;
+        t.state = at;
+        t.tall = t.rows > t.cols;
+        t.m = std::min(t.rows, t.cols); t.k = std::max(t.rows, t.cols);
+        t.mt = (t.m + kSide - 1) / kSide;
+        t.nb = (t.k + kSide - 1) / kSide * 2;
+        if (some) {
+            t.ex = std::min(14, (int)std::floor(std::log2(std::sqrt((double)t.m * t.k))));
+            t.es = std::min(12, (int)std::ceil(std::log2((double)t.m)));
+        }
+        t.group = q.group;
+        t.weight_decay = (float)q.weight_decay; t.lr_scale = (float)q.lr_scale;
+        t.x_dtype = (int8_t)q.x_dtype; t.g_dtype = (int8_t)q.g_dtype; t.copy_dtype = (int8_t)q.copy_dtype;
+        t.whole = (t.g_ld == t.cols || t.rows == 1) && aligned_to(q.g, 4 * dtype_size(q.g_dtype));
+        t.unit0 = (int32_t)units.size();
+        const int64_t count = (int64_t)t.rows * t.cols;
+        t.units = (int32_t)((count + kUnit - 1) / kUnit);
+        for (int32_t u = 0; u < t.units; ++u) units.push_back({i, u});
+        if (units.size() > 0x7fffffff) return CHOCO_ERR_TOO_LARGE;
+        o->mats.push_back(t);
+        o->offsets.push_back(at);
+        kinds.push_back(o->params.products == 3 || (o->params.products == 0 && (q.x_dtype != CHOCO_BF16)));
+        at += (count + kBlock - 1) / kBlock * kBlock;
+        if (at > (int64_t)1 << 38) return CHOCO_ERR_TOO_LARGE;
+        if (some) {
+            o->written.push_back(range_of(q.x, t.rows, t.cols, t.x_ld, q.x_dtype));
+            if (q.copy) o->written.push_back(range_of(q.copy, t.rows, t.cols, t.copy_ld, q.copy_dtype));
+        }
+    }
+    o->elements = at;
+    o->nunits = (int64_t)units.size();
+    // waves: matrices in order, as many as the workspace holds together
+    *work = 0;
+    for (int32_t i = 0; i < n;) {
+        int64_t bytes = 0;
+        int32_t end = i;
+        for (; end < n; ++end) {
+            Matrix& t = o->mats[end];
+            const int64_t planes = kinds[end] ? 2 : 1, xb = (int64_t)t.mt * t.nb * planes * kTileBytes, sb = (int64_t)t.mt * t.mt * 2 * planes * kTileBytes;
+            if (bytes > 0 && bytes + 2 * (xb + sb) > kWaveBytes) break;
+            t.at[0] = bytes; t.at[1] = bytes + xb;
+            t.s_at = bytes + 2 * xb; t.b_at = t.s_at + sb;
+            bytes += 2 * (xb + sb);
+        }
+        *work = std::max(*work, bytes);
+        Wave w = {};
+        for (int three = 0; three < 2; ++three) {
+            w.blocks[three] = (int64_t)blocks.size();
+            for (int32_t q = i; q < end; ++q)
+                if (kinds[q] == three)
+                    for (int32_t r = 0; r < o->mats[q].mt; ++r)
+                        for (int32_t c = 0; c < o->mats[q].nb; ++c) blocks.push_back({q, (int16_t)r, (int16_t)c});
+            w.blocks_end[three] = (int64_t)blocks.size();
+            for (int pairs = 0; pairs < 2; ++pairs) {
+                Class& cl = w.classes[three][pairs];
+                const int cg = pairs + 1;
+                std::vector<int32_t> these;
+                for (int32_t q = i; q < end; ++q)
+                    if (kinds[q] == three && o->mats[q].mt > 0 && (o->mats[q].mt > 1) == (pairs == 1)) these.push_back(q);
+                // the longest first: a launch ends with short ones
+                std::sort(these.begin(), these.end(), [&](int32_t x, int32_t y) {
+                    return o->mats[x].k != o->mats[y].k ? o->mats[x].k > o->mats[y].k : x < y;
+                });
+                cl.symmetric = (int64_t)parts.size();
+                for (int32_t q : these)
+                    for (int32_t r = 0; r < (o->mats[q].mt + cg - 1) / cg; ++r)
+                        for (int32_t c = 0; c <= r; ++c) parts.push_back({q, (int16_t)r, (int16_t)c});
+                cl.symmetric_end = cl.next = (int64_t)parts.size();
+                std::sort(these.begin(), these.end(), [&](int32_t x, int32_t y) {
+                    return o->mats[x].m != o->mats[y].m ? o->mats[x].m > o->mats[y].m : x < y;
+                });
+                for (int32_t q : these)
+                    for (int32_t c = 0; c < (o->mats[q].nb / 2 + cg - 1) / cg; ++c)
+                        for (int32_t r = 0; r < (o->mats[q].mt + cg - 1) / cg; ++r) parts.push_back({q, (int16_t)r, (int16_t)c});
+                cl.next_end = (int64_t)parts.size();
+            }
+        }
+        o->waves.push_back(w);
+        i = end;
+    }
+    return blocks.size() > 0x7fffffff || parts.size() > 0x3fffffff ? CHOCO_ERR_TOO_LARGE : CHOCO_OK;
+}
+
+// Whether arrays that a step writes share memory, with each other or with gradients.
+bool overlap(choco_muon* o)
+{
+    std::vector<Range>& w = o->written;
+    std::sort(w.begin(), w.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+    for (size_t i = 1; i < w.size(); ++i)
+        if (w[i].begin < w[i - 1].end) return true;
+    return false;
+}
+bool is_written(const choco_muon* o, const Matrix& t, const void* g)
+{
+    if (t.rows == 0) return false;
+    const Range r = range_of(g, t.rows, t.cols, t.g_ld, t.g_dtype);
+    auto next = std::lower_bound(o->written.begin(), o->written.end(), r.end, [](const Range& a, uintptr_t e) { return a.begin < e; });
+    return next != o->written.begin() && (next - 1)->end > r.begin;
+}
+
+template <int P, int CG>
+cudaError_t allow_shared()
+{
+    cudaError_t e = cudaSuccess;
+    for (int kind = 0; kind < 3 && e == cudaSuccess; ++kind)
+        e = cudaFuncSetAttribute((const void*)product_of<P, CG>(kind), cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<P, CG>::kShared);
+    return e;
+}
+
+int allocate(choco_muon* o, const std::vector<Unit>& units, const std::vector<Part>& parts, const std::vector<Block>& blocks, int64_t work)
+{
+    int64_t at = 0;
+    const int64_t n = (int64_t)o->mats.size();
+    const int64_t mats = carve<Matrix>(at, n), un = carve<Unit>(at, (int64_t)units.size()), pa = carve<Part>(at, (int64_t)parts.size()),
+                  bl = carve<Block>(at, (int64_t)blocks.size()), pt = carve<double>(at, o->nunits), done = carve<uint32_t>(at, n),
+                  err = carve<uint32_t>(at, 1), sc = carve<Scale>(at, n);
+    at = (at + 1023) / 1024 * 1024;
+    const int64_t wk = at;
+    at += work;
+    if (cudaMalloc(&o->memory, (size_t)at) != cudaSuccess) return CHOCO_ERR_ALLOC;
+    uint8_t* base = static_cast<uint8_t*>(o->memory);
+    o->d_mats = reinterpret_cast<Matrix*>(base + mats);
+    o->d_units = reinterpret_cast<Unit*>(base + un);
+    o->d_parts = reinterpret_cast<Part*>(base + pa);
+    o->d_blocks = reinterpret_cast<Block*>(base + bl);
+    o->d_partial = reinterpret_cast<double*>(base + pt);
+    o->d_done = reinterpret_cast<uint32_t*>(base + done);
+    o->d_errors = reinterpret_cast<uint32_t*>(base + err);
+    o->d_scale = reinterpret_cast<Scale*>(base + sc);
+    o->d_work = base + wk;
+    cudaStream_t st;
+    if (cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking) != cudaSuccess) return CHOCO_ERR_CUDA;
+    auto send = [&](void* to, const auto& from) {
+        return from.empty() || cudaMemcpyAsync(to, from.data(), sizeof(from[0]) * from.size(), cudaMemcpyHostToDevice, st) == cudaSuccess;
+    };
+    bool ok = cudaMemsetAsync(o->d_done, 0, (size_t)(sc - done), st) == cudaSuccess; // counts and errors
+    ok = ok && send(o->d_mats, o->mats) && send(o->d_units, units) && send(o->d_parts, parts) && send(o->d_blocks, blocks);
+    ok = cudaStreamSynchronize(st) == cudaSuccess && ok;
+    cudaStreamDestroy(st);
+    if (!ok) return CHOCO_ERR_CUDA;
+    return allow_shared<1, 1>() == cudaSuccess && allow_shared<1, 2>() == cudaSuccess && allow_shared<3, 1>() == cudaSuccess &&
+                   allow_shared<3, 2>() == cudaSuccess
+               ? CHOCO_OK
+               : CHOCO_ERR_CUDA;
+}
+
+cudaError_t launch_products(const choco_muon* o, const Wave& w, int kind, int which, cudaStream_t st)
+{
+    const choco_muon_params& p = o->params;
+    cudaError_t e = cudaSuccess;
+    for (int three = 0; three < 2; ++three)
+        for (int pairs = 0; pairs < 2; ++pairs) {
+            const Class& cl = w.classes[three][pairs];
+            const int64_t begin = kind == kNext ? cl.next : cl.symmetric, end = kind == kNext ? cl.next_end : cl.symmetric_end;
+            if (begin == end || e != cudaSuccess) continue;
+            const ProductArgs a = {o->d_mats, o->d_parts + begin, o->d_work, o->d_errors, (float)p.a, (float)p.b, (float)p.c, which};
+            const ProductKernel kernel = three ? (pairs ? product_of<3, 2>(kind) : product_of<3, 1>(kind))
+                                               : (pairs ? product_of<1, 2>(kind) : product_of<1, 1>(kind));
+            const int threads = pairs ? Plan<3, 2>::kThreads : Plan<3, 1>::kThreads;
+            const size_t smem = three ? (pairs ? Plan<3, 2>::kShared : Plan<3, 1>::kShared) : (pairs ? Plan<1, 2>::kShared : Plan<1, 1>::kShared);
+            e = launch_overlapped(kernel, dim3((unsigned)((end - begin) * (pairs + 1))), dim3(threads), smem, st, HotRange{}, a);
+        }
+    return e;
+}
+
+int run(choco_muon* o, float* m, double lr, const float* factor, bool update, cudaStream_t st)
+{
+    const choco_muon_params& p = o->params;
+    if (o->nunits == 0) return CHOCO_OK;
+    const MomentArgs ma = {o->d_mats, o->d_units, m, factor, o->d_partial, o->d_done, o->d_scale, (float)p.beta, (float)(1.0 - p.beta), p.nesterov};
+    cudaError_t e = launch_overlapped(moment_kernel, dim3((unsigned)o->nunits), dim3(kUnitThreads), 0, st, HotRange{}, ma);
+    for (const Wave& w : o->waves) {
+        TileArgs ta = {o->d_mats, nullptr, o->d_work, o->d_scale, m, factor, (float)p.beta, (float)(1.0 - p.beta), (float)lr, p.nesterov, 0, 0, update};
+        auto tiles = [&](void (*kernel)(TileArgs)) {
+            for (int three = 0; three < 2; ++three) {
+                if (w.blocks[three] == w.blocks_end[three] || e != cudaSuccess) continue;
+                ta.blocks = o->d_blocks + w.blocks[three];
+                ta.planes = three + 1;
+                e = launch_overlapped(kernel, dim3((unsigned)(w.blocks_end[three] - w.blocks[three])), dim3(kTileThreads2), 0, st, HotRange{}, ta);
+            }
+        };
+        tiles(cut_kernel);
+        for (int k = 0; k < p.steps; ++k)
+            for (int kind : {kGram, kSquare, kNext})
+                if (e == cudaSuccess) e = launch_products(o, w, kind, k & 1, st);
+        ta.which = p.steps & 1;
+        tiles(apply_kernel);
+    }
+    return status_of(e);
+}
+
+} // namespace
+
+extern "C" {
+
+int choco_muon_init(choco_muon** out, int32_t n_matrices, const choco_muon_matrix* matrices, const choco_muon_params* p)
+{
+    if (!out) return CHOCO_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (n_matrices < 1 || !matrices || !p || p->groups < 1) return CHOCO_ERR_INVALID_ARG;
+    if (!(p->beta >= 0.0 && p->beta < 1.0) || (p->nesterov != 0 && p->nesterov != 1) || p->steps < 0 || p->steps > 64) return CHOCO_ERR_INVALID_ARG;
+    if (p->products != 0 && p->products != 1 && p->products != 3) return CHOCO_ERR_UNSUPPORTED;
+    if (!polynomial_ok(*p)) return CHOCO_ERR_INVALID_ARG;
+    choco_muon* o = new (std::nothrow) choco_muon();
+    if (!o) return CHOCO_ERR_ALLOC;
+    o->params = *p;
+    int rc = CHOCO_OK;
+    try {
+        std::vector<Unit> units;
+        std::vector<Part> parts;
+        std::vector<Block> blocks;
+        int64_t work = 0;
+        rc = plan(o, n_matrices, matrices, units, parts, blocks, &work);
+        if (rc == CHOCO_OK && overlap(o)) rc = CHOCO_ERR_INVALID_ARG;
+        for (const Matrix& t : o->mats)
+            if (rc == CHOCO_OK && is_written(o, t, t.g)) rc = CHOCO_ERR_INVALID_ARG;
+        if (rc == CHOCO_OK && cudaGetDevice(&o->device) != cudaSuccess) rc = CHOCO_ERR_CUDA;
+        if (rc == CHOCO_OK) rc = allocate(o, units, parts, blocks, work);
+    } catch (const std::exception&) {
+        rc = CHOCO_ERR_ALLOC;
+    }
+    if (rc != CHOCO_OK) {
+        cudaGetLastError();
+        free_all(o);
+        return rc;
+    }
+    *out = o;
+    return CHOCO_OK;
+}
+
+int choco_muon_destroy(choco_muon* opt)
+{
+    if (!opt) return CHOCO_ERR_INVALID_ARG;
+    free_all(opt); // cudaFree waits for what still uses the memory
+    return CHOCO_OK;
+}
+
+int choco_muon_state_size(const choco_muon* opt, int64_t* elements, int64_t* offsets)
+{
+    if (!opt || !elements) return CHOCO_ERR_INVALID_ARG;
+    *elements = opt->elements;
+    if (offsets) std::memcpy(offsets, opt->offsets.data(), sizeof(int64_t) * opt->offsets.size());
+    return CHOCO_OK;
+}
+
+int choco_muon_set_grads(choco_muon* opt, const void* const* g, void* stream)
+{
+    if (!opt || !g || !on_device(opt)) return CHOCO_ERR_INVALID_ARG;
+    for (size_t i = 0; i < opt->mats.size(); ++i) {
+        const Matrix& t = opt->mats[i];
+        if (t.rows > 0 && !g[i]) return CHOCO_ERR_INVALID_ARG;
+        if (!aligned_to(g[i], dtype_size(t.g_dtype))) return CHOCO_ERR_MISALIGNED;
+        if (is_written(opt, t, g[i])) return CHOCO_ERR_INVALID_ARG;
+    }
+    cudaStream_t st = (cudaStream_t)stream;
+    try {
+        std::vector<Matrix> mats = opt->mats;
+        for (size_t i = 0; i < mats.size(); ++i) {
+            mats[i].g = g[i];
+            mats[i].whole = (mats[i].g_ld == mats[i].cols || mats[i].rows == 1) && aligned_to(g[i], 4 * dtype_size(mats[i].g_dtype));
+        }
+        if (cudaStreamSynchronize(st) != cudaSuccess) return CHOCO_ERR_CUDA;
+        opt->broken = true; // until the table on the device is whole
+        if (cudaMemcpyAsync(opt->d_mats, mats.data(), sizeof(Matrix) * mats.size(), cudaMemcpyHostToDevice, st) != cudaSuccess ||
+            cudaStreamSynchronize(st) != cudaSuccess)
+            return CHOCO_ERR_CUDA;
+        opt->mats.swap(mats);
+        opt->broken = false;
+    } catch (const std::exception&) {
+        return CHOCO_ERR_ALLOC;
+    }
+    return CHOCO_OK;
+}
+
+int choco_muon_step(choco_muon* opt, float* m, double lr, const float* factor, void* stream)
+{
+    if (!opt || !(lr >= 0.0) || !std::isfinite((float)lr) || !on_device(opt)) return CHOCO_ERR_INVALID_ARG;
+    if (opt->elements > 0 && !m) return CHOCO_ERR_INVALID_ARG;
+    if (!aligned_to(m, 16) || !aligned_to(factor, 4)) return CHOCO_ERR_MISALIGNED;
+    if (opt->broken) return CHOCO_ERR_CUDA;
+    return run(opt, m, lr, factor, true, (cudaStream_t)stream);
+}
+
+int choco_muon_orthogonalize(choco_muon* opt, void* stream)
+{
+    if (!opt || !on_device(opt)) return CHOCO_ERR_INVALID_ARG;
+    if (opt->broken) return CHOCO_ERR_CUDA;
+    return run(opt, nullptr, 0.0, nullptr, false, (cudaStream_t)stream);
+}
+
+int choco_muon_status(choco_muon* opt, void* stream)
+{
+    if (!opt || !on_device(opt)) return CHOCO_ERR_INVALID_ARG;
+    uint32_t errors = 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (cudaMemcpyAsync(&errors, opt->d_errors, sizeof(errors), cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
+        return CHOCO_ERR_CUDA;
+    return errors ? CHOCO_ERR_TIMEOUT : CHOCO_OK;
+}
+
+} // extern "C"
