@@ -628,6 +628,61 @@ int choco_muon_orthogonalize(choco_muon* opt, void* stream);
  * the part of a matrix that it was to write was not written. */
 int choco_muon_status(choco_muon* opt, void* stream);
 
+/*
+ * Group norm with an activation, channels last, for n workers with parameters of their own (a scale and a shift for
+ * each channel, layers of a row of X; their gradients go to rows of G).  For worker i, image b and group k of
+ * channels / groups neighbouring channels, over its channels and all pixels:
+ *     xhat = (x - mean) rstd ;   rstd = 1 / sqrt(variance + eps) ;   z = weight xhat + bias ;   y = act(z)
+ */
+typedef struct choco_group_norm choco_group_norm;
+typedef enum {
+    CHOCO_ACT_NONE = 0,
+    CHOCO_ACT_RELU = 1,
+    CHOCO_ACT_SILU = 2,   /* z / (1 + exp(-z))                                                     */
+    CHOCO_ACT_GELU = 3    /* z (1 + erf(z / sqrt(2))) / 2                                          */
+} choco_activation;
+typedef struct {
+    int32_t n;            /* workers, 1 .. 65535                                                   */
+    int32_t groups;       /* divides channels; at most 4096 channels to a group                    */
+    int64_t channels;     /* 1 .. 2^20                                                             */
+    int64_t max_images;   /* most images of one worker in a call for gradients of the parameters   */
+    double eps;           /* >= 0, finite as a float32                                             */
+    int32_t activation;   /* choco_activation                                                      */
+    int32_t unused;
+} choco_group_norm_params;
+/* An array of pixels: element (i, b, p, c) at i worker + b image + p pixel + c, strides >= 0 in elements. */
+typedef struct {
+    void* data;           /* DEVICE                                                                */
+    int64_t worker, image, pixel;
+    int32_t dtype;        /* choco_dtype                                                           */
+    int32_t unused;
+} choco_pixels;
+
+/* Allocates 8 n max_images channels bytes for sums of channels (max_images = 0: forward, and dx, only). */
+int choco_group_norm_init(choco_group_norm** out, const choco_group_norm_params* p);
+int choco_group_norm_destroy(choco_group_norm* gn);
+/*
+ * choco_group_norm_forward -- y from x, in float32 (the statistics' last step in float64), rounded once to y's type.
+ *   images, pixels   of a worker, of an image; 0: nothing is done.
+ *   y                no element belongs to two places; y is x itself (address, strides and type alike), or another set of channels
+ *                    of the same wider array, or shares no addresses with it (CHOCO_ERR_INVALID_ARG).
+ *   weight, bias     worker i's at i param_ld, [channels], of type param_dtype; NULL: 1 and 0.  param_ld = 0: the same for all workers.
+ *   mean, rstd       DEVICE float [n, images, groups], what choco_group_norm_backward wants; either may be NULL.
+ */
+int choco_group_norm_forward(choco_group_norm* gn, int64_t images, int64_t pixels, const choco_pixels* x, const choco_pixels* y, const void* weight,
+                             const void* bias, int64_t param_ld, int32_t param_dtype, float* mean, float* rstd, void* stream);
+/*
+ * choco_group_norm_backward -- with dz = dy act'(z):
+ *     dx = rstd (weight dz - mean over the group of weight dz - xhat (mean over the group of weight dz xhat))
+ *     dweight = sum over images and pixels of dz xhat ;   dbias = sum of dz       (added to what is there with accumulate = 1)
+ * mean and rstd are those of the forward call (and stand for themselves: relu's slope is 1 exactly where z of these numbers is above
+ * 0).  Sums in a fixed order.  dx: NULL or of x's type, with the rules for y, against x and dy.  dweight, dbias: worker i's at i grad_ld,
+ * [channels], of type grad_dtype, either may be NULL; images <= max_images where there is one.  They share no memory with the other arrays.
+ */
+int choco_group_norm_backward(choco_group_norm* gn, int64_t images, int64_t pixels, const choco_pixels* x, const choco_pixels* dy, const choco_pixels* dx,
+                              const void* weight, const void* bias, int64_t param_ld, int32_t param_dtype, const float* mean, const float* rstd,
+                              void* dweight, void* dbias, int64_t grad_ld, int32_t grad_dtype, int32_t accumulate, void* stream);
+
 const char* choco_strerror(int code);
 /* cudaError_t of the last failing CUDA call on this context (0 if none). */
 int choco_last_cuda_error(const choco_ctx* ctx);

@@ -34,6 +34,7 @@ EXPORTS = [
     "choco_adamw_set_rounding", "choco_adamw_step", "choco_adamw_read_state", "choco_adamw_get_steps", "choco_adamw_set_steps",
     "choco_muon_init", "choco_muon_destroy", "choco_muon_state_size", "choco_muon_set_grads", "choco_muon_step", "choco_muon_orthogonalize",
     "choco_muon_status",
+    "choco_group_norm_init", "choco_group_norm_destroy", "choco_group_norm_forward", "choco_group_norm_backward",
 ]
 
 DTYPES = {"float32": 0, "bfloat16": 1, "float16": 2}   # choco_dtype
@@ -87,6 +88,19 @@ ADAMW_BLOCK = 256   # elements that share a scale; tensors start on multiples of
 MUON_MATRIX = [("x", "<u8"), ("g", "<u8"), ("copy", "<u8"), ("rows", "<i8"), ("cols", "<i8"), ("x_ld", "<i8"), ("g_ld", "<i8"), ("copy_ld", "<i8"),
                ("x_dtype", "<i4"), ("g_dtype", "<i4"), ("copy_dtype", "<i4"), ("group", "<i4"), ("weight_decay", "<f8"), ("lr_scale", "<f8")]
 MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}   # choco_activation
+
+
+class choco_group_norm_params(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("groups", ctypes.c_int32), ("channels", ctypes.c_int64), ("max_images", ctypes.c_int64),
+                ("eps", ctypes.c_double), ("activation", ctypes.c_int32), ("unused", ctypes.c_int32)]
+
+
+class choco_pixels(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("worker", ctypes.c_int64), ("image", ctypes.c_int64), ("pixel", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("unused", ctypes.c_int32)]
+
 
 _lib = None
 
@@ -166,6 +180,11 @@ def load() -> ctypes.CDLL:
         lib.choco_muon_step.argtypes = [vp, vp, f64, vp, vp]
         lib.choco_muon_orthogonalize.argtypes = [vp, vp]
         lib.choco_muon_status.argtypes = [vp, vp]
+        px = ctypes.POINTER(choco_pixels)
+        lib.choco_group_norm_init.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(choco_group_norm_params)]
+        lib.choco_group_norm_destroy.argtypes = [vp]
+        lib.choco_group_norm_forward.argtypes = [vp, i64, i64, px, px, vp, vp, i64, i32, vp, vp, vp]
+        lib.choco_group_norm_backward.argtypes = [vp, i64, i64, px, px, px, vp, vp, i64, i32, vp, vp, vp, vp, i64, i32, i32, vp]
         for name in EXPORTS:
             if name not in ("choco_strerror",):
                 getattr(lib, name).restype = ctypes.c_int
@@ -768,6 +787,106 @@ def choco_muon_status(opt, stream=None) -> None:
     _check(load().choco_muon_status(opt, _stream_of(stream, opt.device)))
 
 
+class GroupNormHandle(ctypes.c_void_p):
+    """What choco_group_norm_init returns: the library's handle, with the device it belongs to and its sizes."""
+
+    def describe(self, device: int, n: int, channels: int, groups: int) -> None:
+        self.device, self.n, self.channels, self.groups = device, n, channels, groups
+
+
+def _pixels_of(gn, what: str, t):
+    """(choco_pixels, images, pixels) of an array [n, images, ..., channels]: what lies between images and channels are pixels, which
+    have one stride."""
+    shape, strides = t.shape, t.stride()
+    if t.get_device() != gn.device:
+        raise ChocoError(f"libchoco: {what} must be on the handle's GPU ({gn.device}), not {t.device}", -1)
+    if len(shape) < 3 or shape[0] != gn.n or shape[-1] != gn.channels or (strides[-1] != 1 and shape[-1] > 1):
+        raise ChocoError(f"libchoco: {what} must be [{gn.n}, images, pixels, {gn.channels}] with neighbouring channels, not {list(shape)}, "
+                         f"strides {list(strides)}", -1)
+    pixels, step = 1, 0
+    for k in range(len(shape) - 2, 1, -1):
+        if shape[k] == 1:
+            continue
+        if pixels == 1:
+            step = strides[k]
+        elif strides[k] != pixels * step and pixels > 0 and shape[k] > 0:
+            raise ChocoError(f"libchoco: the pixels of {what} must have one stride, not {list(strides)} for {list(shape)}", -1)
+        pixels *= shape[k]
+    return choco_pixels(t.data_ptr(), strides[0], strides[1], step, _dtype(t), 0), shape[1], pixels
+
+
+def _channels_of(gn, what: str, *tensors):
+    """(stride from worker to worker, type) of arrays [n, channels] with neighbouring channels; None is left out."""
+    found = None
+    for t in tensors:
+        if t is None:
+            continue
+        if t.get_device() != gn.device or t.dim() != 2 or t.shape[0] != gn.n or t.shape[1] != gn.channels or (t.stride(1) != 1 and gn.channels > 1):
+            raise ChocoError(f"libchoco: {what} must be [{gn.n}, {gn.channels}] with neighbouring channels on GPU {gn.device}, not {list(t.shape)}, "
+                             f"strides {list(t.stride())} on {t.device}", -1)
+        this = (t.stride(0), _dtype(t))
+        if found is not None and this != found and (gn.n > 1 or this[1] != found[1]):
+            raise ChocoError(f"libchoco: {what} have one type and one stride from worker to worker", -1)
+        found = found or this
+    return found or (gn.channels, 0)
+
+
+def _check_stats(gn, images: int, *tensors) -> None:
+    for t in tensors:
+        if t is not None and (t.get_device() != gn.device or _dtype(t) != 0 or tuple(t.shape) != (gn.n, images, gn.groups) or not t.is_contiguous()):
+            raise ChocoError(f"libchoco: mean and rstd must be contiguous float32 [{gn.n}, {images}, {gn.groups}] on GPU {gn.device}, not {t.dtype} "
+                             f"{list(t.shape)} on {t.device}", -1)
+
+
+def choco_group_norm_init(n: int, channels: int, groups: int, max_images: int = 0, eps: float = 1e-5, activation: str = "none"):
+    """Handle for the norms of n workers (see choco.h) on the current device; max_images = 0: no gradients of parameters."""
+    import torch
+    if activation not in ACTIVATIONS:
+        raise ChocoError(f"libchoco: activations are {', '.join(ACTIVATIONS)}, not {activation}", -1)
+    p = choco_group_norm_params(n, groups, channels, max_images, eps, ACTIVATIONS[activation], 0)
+    h = GroupNormHandle()
+    _check(load().choco_group_norm_init(ctypes.byref(h), ctypes.byref(p)))
+    h.describe(torch.cuda.current_device(), n, channels, groups)
+    return h
+
+
+def choco_group_norm_destroy(gn) -> None:
+    _check(load().choco_group_norm_destroy(gn))
+
+
+def choco_group_norm_forward(gn, x, weight, bias, y, mean=None, rstd=None, stream=None) -> None:
+    """y = act(weight xhat + bias).  x and y [n, images, pixels, channels] (or with more axes of pixels); weight and bias [n, channels],
+    or None; mean and rstd [n, images, groups] receive the statistics."""
+    ax, images, pixels = _pixels_of(gn, "x", x)
+    ay, *same = _pixels_of(gn, "y", y)
+    if same != [images, pixels]:
+        raise ChocoError(f"libchoco: y must have the shape of x, {list(x.shape)}, not {list(y.shape)}", -1)
+    ld, kind = _channels_of(gn, "weight and bias", weight, bias)
+    _check_stats(gn, images, mean, rstd)
+    _check(load().choco_group_norm_forward(gn, images, pixels, ctypes.byref(ax), ctypes.byref(ay), _ptr(weight), _ptr(bias), ld, kind, _ptr(mean),
+                                           _ptr(rstd), _stream_of(stream, gn.device)))
+
+
+def choco_group_norm_backward(gn, x, dy, weight, bias, mean, rstd, dx, dweight, dbias, accumulate: bool = False, stream=None) -> None:
+    """The gradients of that; dx, dweight and dbias may be None."""
+    ax, images, pixels = _pixels_of(gn, "x", x)
+    ay, *same = _pixels_of(gn, "dy", dy)
+    ad = None
+    if dx is not None:
+        ad, *other = _pixels_of(gn, "dx", dx)
+        same += other
+    if any(s != (images, pixels)[k % 2] for k, s in enumerate(same)):
+        raise ChocoError(f"libchoco: dy and dx must have the shape of x, {list(x.shape)}", -1)
+    ld, kind = _channels_of(gn, "weight and bias", weight, bias)
+    gld, gkind = _channels_of(gn, "dweight and dbias", dweight, dbias)
+    if mean is None or rstd is None:
+        raise ChocoError("libchoco: mean and rstd of the forward call are needed", -1)
+    _check_stats(gn, images, mean, rstd)
+    _check(load().choco_group_norm_backward(gn, images, pixels, ctypes.byref(ax), ctypes.byref(ay), None if ad is None else ctypes.byref(ad),
+                                            _ptr(weight), _ptr(bias), ld, kind, _ptr(mean), _ptr(rstd), _ptr(dweight), _ptr(dbias), gld, gkind,
+                                            1 if accumulate else 0, _stream_of(stream, gn.device)))
+
+
 # --------------------------------------------------------------------------- convenience
 
 
@@ -1041,6 +1160,31 @@ class Muon:
     def close(self):
         if getattr(self, "handle", None) is not None:
             choco_muon_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class GroupNorm:
+    """Owns a choco_group_norm handle; see choco_group_norm_init."""
+
+    def __init__(self, n: int, channels: int, groups: int, max_images: int = 0, eps: float = 1e-5, activation: str = "none"):
+        self.n, self.channels, self.groups = n, channels, groups
+        self.handle = choco_group_norm_init(n, channels, groups, max_images, eps, activation)
+
+    def forward(self, x, weight, bias, y, mean=None, rstd=None, stream=None):
+        choco_group_norm_forward(self.handle, x, weight, bias, y, mean, rstd, stream)
+
+    def backward(self, x, dy, weight, bias, mean, rstd, dx, dweight, dbias, accumulate: bool = False, stream=None):
+        choco_group_norm_backward(self.handle, x, dy, weight, bias, mean, rstd, dx, dweight, dbias, accumulate, stream)
+
+    def close(self):
+        if getattr(self, "handle", None) is not None:
+            choco_group_norm_destroy(self.handle)
             self.handle = None
 
     def __del__(self):
