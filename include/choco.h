@@ -592,7 +592,7 @@ typedef struct {
 typedef struct {
     double beta;          /* in [0, 1)                                                             */
     double a, b, c;       /* of the polynomial; it keeps values of [0, 1] below 1.9 in every step and  */
-                          /* |a + b s^2 + c s^4| below 15 there (CHOCO_ERR_INVALID_ARG)             */
+                          /* |a + b s^2 + c s^4|, |b + c s^2| below 15 (CHOCO_ERR_INVALID_ARG)       */
     int32_t nesterov;     /* 0 or 1                                                                */
     int32_t steps;        /* 0 .. 64                                                               */
     int32_t products;     /* 3: X, S and B carry 22 bits; 1: 11 bits, a third of the work; 0: 1 for  */

@@ -139,9 +139,10 @@ __device__ __forceinline__ void add_up(const Share<VEC>& sh, const NormArgs& a, 
         row = (int)threadIdx.x >> 5;
         writes = (int)(threadIdx.x & 31) < sh.columns;
     }
-    if (writes)
+    if (writes) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) red[row * width + sh.column * VEC + e] = make_float2(s1[e], s2[e]);
+    }
     __syncthreads();
     for (int c = threadIdx.x; c < width; c += kNormThreads) {
         float2 v = red[c];
@@ -296,12 +297,13 @@ __global__ void __launch_bounds__(kNormThreads) forward_kernel(NormArgs a)
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j)
                     if (i0 + j < sh.steps && sh.pixel(i0 + j) < sh.end) load_raw(r[j], x + sh.pixel(i0 + j) * a.x.pixel + c0);
-                if (i0 == 0)
+                if (i0 == 0) {
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
                         p[e] = raw_get(first, e);
                         if (sh.lane == 0) l.first[c0 + e] = p[e];
                     }
+                }
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j) {
                     if (i0 + j >= sh.steps || sh.pixel(i0 + j) >= sh.end) continue;

@@ -1,13 +1,13 @@
 // Muon: a momentum step whose update is orthogonalised matrix by matrix.
 //
 // With U the averaged gradient of a matrix, X_0 = U / |U| (Frobenius) and m its smaller side,
-//     S = X X^T,   B = a I + b S + c S^2,   X <- B X          (`steps` times)
+//     S = X X^T,   T = b I + c S,   B = a I + S T,   X <- B X          (`steps` times)
 // takes every singular value s to s (a + b s^2 + c s^4): an odd polynomial that drives them towards one.  The
-// work is three chains of products per step: S (m x m, symmetric), S^2 (likewise) and B X (m x k).
+// work is three products per step: X X^T (m x m, symmetric), S T (likewise) and B X (m x k).
 //
 // Numbers.  The products run on the tensor cores, float16 factors and float32 sums.  X, S and B are scaled
 // by powers of two into the middle of float16's range (X by 2^ex with 2^ex ~ sqrt(m k), so that its elements start
-// near 1; S and B by 2^es ~ m, so that their diagonals do) and kept as a float16 value and, with three products, the
+// near 1; S, T and B by 2^es ~ m, so that their diagonals do) and kept as a float16 value and, with three products, the
 // float16 value of what that leaves: hi hi + hi lo + lo hi carries 22 bits.  One product carries 11 and is what 16-bit
 // results take: over five steps its roundings come to 0.0012 .. 0.0017 of the result (2-norm), as much as rounding the
 // result to bfloat16 (0.0017); with three they come to 4e-7.
@@ -48,7 +48,7 @@ struct Matrix {
     int64_t x_ld, g_ld, copy_ld;
     int64_t state;          // first element in m
     int64_t at[2];          // tiles of X and of its successor, in bytes of the workspace
-    int64_t s_at, b_at;     // of S and B
+    int64_t s_at, t_at, b_at; // of S, T and B
     int32_t rows, cols;
     int32_t m, k;           // rows and columns of X: the smaller side and the larger
     int32_t mt, nb;         // tiles of X: rows of tiles, tiles in a row (an even number)
@@ -204,7 +204,7 @@ struct TileArgs {
     const float* factor;
     float beta, omb, lr;
     int32_t nesterov;
-    int32_t planes;
+    int32_t planes;         // parts of the tiles that are read (X_0 has two)
     int32_t which;          // of the two X
     int32_t update;         // x -= lr .. O (a step), or x = O
 };
@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kTileThreads2) cut_kernel(TileArgs a)
             }
         __syncthreads();
     }
-    uint8_t* to = a.work + t.at[0] + ((int64_t)bl.row * t.nb + bl.col) * a.planes * kTileBytes;
+    uint8_t* to = a.work + t.at[0] + ((int64_t)bl.row * t.nb + bl.col) * 2 * kTileBytes;
     const int piece = threadIdx.x & 7;
     for (int r = threadIdx.x >> 3; r < kSide; r += kTileThreads2 / 8) {
         float v[8];
@@ -288,9 +288,9 @@ __global__ void __launch_bounds__(kTileThreads2) cut_kernel(TileArgs a)
             v[q] = u * sc.first * sc.second;
         }
         uint4 hi, lo;
-        split8(v, hi, lo, a.planes == 2);
+        split8(v, hi, lo, true);
         *reinterpret_cast<uint4*>(to + piece_at(r, piece)) = hi;
-        if (a.planes == 2) *reinterpret_cast<uint4*>(to + kTileBytes + piece_at(r, piece)) = lo;
+        *reinterpret_cast<uint4*>(to + kTileBytes + piece_at(r, piece)) = lo;
     }
 }
 
@@ -336,93 +336,145 @@ __global__ void __launch_bounds__(kTileThreads2) apply_kernel(TileArgs a)
 }
 
 // ---------------------------------------------------------------------------------------- products
-enum Kind { kGram, kSquare, kNext };    // S = X X^T;  B = a I + b S + c S^2;  X' = B X
+enum Kind { kGram, kSquare, kNext };    // S = X X^T and T = b I + c S;  B = a I + S T;  X' = B X
 
 struct ProductArgs {
     const Matrix* mats;
     const Part* parts;
     uint8_t* work;
     uint32_t* errors;
+    int32_t count;          // of the parts
     float a, b, c;
     int32_t which;          // of the two X: the one that is read
+    int32_t planes;         // parts of its tiles in the workspace (S, T and B and the next X have as many as take part in products)
 };
 
-template <int P, int CG>
+// PA, PB: parts of the first and of the second factor.  1, 1: one product; 2, 2: three (low by low is left out); 1, 2: two, for
+// the first B X with one: the roundings of X_0 are the ones that all steps magnify.
+template <int PA, int PB, int CG>
 struct Plan {
-    static constexpr int kPlanes = P == 3 ? 2 : 1;
-    static constexpr uint32_t kOperand = kPlanes * kTileBytes;
-    static constexpr uint32_t kStage = 2 * kOperand;             // of both factors, 64 of K
-    static constexpr int kStages = P == 3 ? 3 : CG == 2 ? 6 : 3; // one product and one CTA: two blocks of threads to an SM
-    // The tensor cores cut sums to float32 towards zero, a bias of half a unit in the last place for every 16 of K.  With three
-    // products the sums therefore leave tensor memory after every 64 of K and are added up in registers, to the nearest.
-    static constexpr int kChunk = P == 3 ? 1 : 1 << 20;          // steps of 64 of K between two of these
-    static constexpr int kSums = P == 3 ? 2 : 1;                 // sets of sums in tensor memory
-    static constexpr uint32_t kColumns = kSide * CG;             // of one set: the part's columns
+    static constexpr uint32_t kFirst = PA * kTileBytes, kSecond = PB * kTileBytes;
+    static constexpr uint32_t kStage = kFirst + kSecond;         // of both factors, 64 of K
+    static constexpr int kStages = PA == 2 ? 3 : CG == 1 ? 3 : PB == 2 ? 4 : 6; // (one CTA, not three products: two blocks of threads to an SM)
+    static constexpr bool kLeave = PA == 2;
+    static constexpr uint32_t kColumns = kSide * CG;             // of tensor memory: the part's columns, twice
     static constexpr int kWarps = 4 * CG;                        // that take the sums; two more feed the tensor cores
     static constexpr int kThreads = CG == 2 ? 384 : 192;         // (three whole warpgroups where registers move between them)
-    static constexpr int kBlocks = P == 1 && CG == 1 ? 2 : 1;    // to an SM
-    static constexpr uint32_t kOut = 2 * kOperand;               // bytes of 128 x 128 results
-    static constexpr uint32_t kShared = kStages * kStage + 1024;
-    static_assert(CG * kOut <= kStages * kStage, "results are put together where the factors were");
+    static constexpr int kBlocks = PB == 1 && CG == 1 ? 2 : 1;   // to an SM
+    static constexpr uint32_t kSend = kSide / 4 * 128;           // bytes of a warp's rows of a tile
+    static constexpr uint32_t kShared = kStages * kStage + kWarps * kSend;
 };
-
-template <int THREADS>
-__device__ __forceinline__ void block_part_sync() // of the threads that take the sums, which come first in a block
-{
-    asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
-}
+// The tensor cores cut sums to float32 towards zero, a bias of half a unit in the last place for every 16 of K.  With three
+// products the sums therefore leave tensor memory now and then and are added up in registers, to the nearest (error after five
+// steps on 650 x 2600, against 2.8e-6 of plain float32 products: 5e-5 where they stay, 5.6e-6, 3.2e-6 and 1.8e-6 where they leave after 256, 128
+// and 64 of K).  Leaving takes tensor memory from the products, 260 cycles each time.  Longer sums leave less often, as the error of plain products grows
+// with their length too.
+__host__ __device__ constexpr int steps_to_leave(int nk) { return nk >= 64 ? 4 : nk >= 16 ? 2 : 1; }
 
 // Copies of one factor for 64 of K into shared memory.  Rows [128 i, 128 i + 128) of X (along its rows) ...
 template <int PL>
-__device__ __forceinline__ void fetch_along(uint8_t* to, const uint8_t* x, int64_t tile, uint64_t* bar)
+__device__ __forceinline__ void fetch_along(uint8_t* to, const uint8_t* x, int64_t tile, int planes, uint64_t* bar)
 {
-    bulk_load(to, x + tile * PL * kTileBytes, PL * kTileBytes, bar);
+    bulk_load(to, x + tile * planes * kTileBytes, PL * kTileBytes, bar);
 }
 // ... or 128 columns, of tiles `tile` and `tile + 1`, their upper or lower 64 rows
 template <int PL>
-__device__ __forceinline__ void fetch_turned(uint8_t* to, const uint8_t* x, int64_t tile, int lower, uint64_t* bar)
+__device__ __forceinline__ void fetch_turned(uint8_t* to, const uint8_t* x, int64_t tile, int planes, int lower, uint64_t* bar)
 {
 #pragma unroll
     for (int cb = 0; cb < 2; ++cb)
 #pragma unroll
         for (int p = 0; p < PL; ++p)
-            bulk_load(to + p * kTileBytes + cb * kPieceBytes, x + ((tile + cb) * PL + p) * kTileBytes + lower * kPieceBytes, kPieceBytes, bar);
+            bulk_load(to + p * kTileBytes + cb * kPieceBytes, x + ((tile + cb) * planes + p) * kTileBytes + lower * kPieceBytes, kPieceBytes, bar);
 }
 
-template <int KIND, int P, int CG>
-__global__ void __launch_bounds__(Plan<P, CG>::kThreads, Plan<P, CG>::kBlocks) __cluster_dims__(CG, 1, 1) product_kernel(ProductArgs a)
+template <int N>
+__device__ __forceinline__ void add_at(float (&w)[N], int column, float x)
 {
-    using L = Plan<P, CG>;
-    constexpr int PL = L::kPlanes, ST = L::kStages;
-    extern __shared__ uint8_t raw[];
-    __shared__ uint64_t full[ST], empty[ST], peer[ST], sums[2], taken[2], third;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (e == column) w[e] += x;
+}
+// A warp's 32 rows of a tile (64 columns a lane, one row each): through 4 KiB of shared memory, high part and low part
+// one after the other.  Straight from registers the rows, 128 bytes apart, cost 8000 cycles for 128 x 128 results.
+template <int PL>
+__device__ __forceinline__ void send_tile(const float (&w)[kHalves], uint8_t* mine, uint8_t* to, int lane)
+{
+#pragma unroll
+    for (int p = 0; p < PL; ++p) {
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+#pragma unroll
+        for (int piece = 0; piece < 8; ++piece) {
+            uint4 hi, lo;
+            split8(w + piece * 8, hi, lo, p == 1);
+            *reinterpret_cast<uint4*>(mine + piece_at(lane, piece)) = p ? lo : hi;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            bulk_store(to + p * kTileBytes, mine, kSide / 4 * 128);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    }
+}
+
+// What the roles of a block know about a part.
+template <int KIND, int CG, bool LEAVE>
+struct Job {
+    Part part;
+    const Matrix* t;
+    int it, jt;              // this CTA's rows of tiles of the two factors
+    int mt, nb, nk, leave;   // nk: steps of 64 of K, `leave`: after how many sums leave tensor memory
+    int columns;             // of tiles of 128 columns of the result
+    bool has_a, has_b, same; // same: both factors are the same rows
+
+    __device__ Job(const ProductArgs& a, int index, uint32_t rank)
+    {
+        part = a.parts[index];
+        t = a.mats + part.matrix;
+        it = part.i * CG + rank;
+        jt = part.j * CG + rank;
+        mt = t->mt;
+        nb = t->nb;
+        columns = KIND == kNext ? nb / 2 : mt;
+        has_a = it < mt;
+        has_b = jt < columns;
+        same = KIND == kGram && part.i == part.j;
+        nk = ((KIND == kGram ? t->k : t->m) + kHalves - 1) / kHalves;
+        leave = LEAVE ? steps_to_leave(nk) : nk;
+    }
+    // a tile above the diagonal's parts is stored turned
+    __device__ bool turns_a(int kb) const { return KIND != kGram && (kb >> 1) / CG > part.i; }
+    __device__ bool turns_b(int kb) const { return KIND == kNext || (KIND == kSquare && (kb >> 1) / CG > part.j); }
+};
+
+// One block (a pair of them) to an SM works on one part after another.  A warp copies factors in, a warp issues products, the
+// others take the sums out while the products of the next part are under way: tensor memory holds two sets of sums.
+template <int KIND, int PA, int PB, int CG>
+__global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::kBlocks) __cluster_dims__(CG, 1, 1) product_kernel(ProductArgs a)
+{
+    using L = Plan<PA, PB, CG>;
+    constexpr int PL = PA, ST = L::kStages;                      // PL: parts of the results
+    extern __shared__ __align__(1024) uint8_t stage[];           // (all other shared memory lies behind it)
+    __shared__ uint64_t full[ST], empty[ST], sums[2], taken[2];
     __shared__ uint32_t tmem_at;
     __shared__ volatile uint32_t failed;
-    uint8_t* stage = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
-    const Part part = a.parts[blockIdx.x / CG];
-    const Matrix& t = a.mats[part.matrix];
-    const int it = part.i * CG + rank, jt = part.j * CG + rank;  // this CTA's rows of tiles of the two factors
-    const int mt = t.mt, nb = t.nb;
-    const int columns = KIND == kNext ? nb / 2 : mt;             // of tiles of 128 columns
-    const bool has_a = it < mt, has_b = jt < columns;
-    const bool same = KIND == kGram && part.i == part.j;         // both factors are the same rows
-    const int nk = KIND == kGram ? (t.k + kHalves - 1) / kHalves : (t.m + kHalves - 1) / kHalves;
+    const int begin = blockIdx.x / CG, step = gridDim.x / CG;
     if (tid == 0) {
         for (int s = 0; s < ST; ++s) {
-            mbar_init(&full[s], 1);
+            mbar_init(&full[s], CG == 2 && rank == 0 ? 2 : 1);   // the first CTA of a pair hears of the other one's copies too
             mbar_init(&empty[s], 1);
-            mbar_init(&peer[s], 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&sums[s], 1);
             mbar_init(&taken[s], L::kWarps * CG);
         }
-        mbar_init(&third, 1);
         failed = 0;
     }
-    if (warp == 0) tmem_alloc<CG>(&tmem_at, L::kSums * L::kColumns);
+    if (warp == 0) tmem_alloc<CG>(&tmem_at, 2 * L::kColumns);
     tmem_fence_before();
     __syncthreads();
     if (CG == 2) cluster_sync();
@@ -431,176 +483,173 @@ __global__ void __launch_bounds__(Plan<P, CG>::kThreads, Plan<P, CG>::kBlocks) _
     allow_next_kernel();
     wait_for_previous_kernel();
 
-    const uint8_t* x = a.work + t.at[a.which];
-    const uint8_t* s_in = a.work + t.s_at;
-    const uint8_t* first = KIND == kGram ? x : KIND == kSquare ? s_in : a.work + t.b_at;
     // (128 sums a thread want more registers than 384 threads can have: 168 each at launch become 224 and 40)
-    const uint32_t from = acc + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * kSide;
     if (warp < L::kWarps) {                                      // the sums: a thread has 128 columns of a row
-        if constexpr (P == 3 && CG == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-        float v[P == 3 ? kSide : 1];
-#pragma unroll
-        for (int e = 0; e < (P == 3 ? kSide : 1); ++e) v[e] = 0.f;
-        const int chunks = (nk + L::kChunk - 1) / L::kChunk;
-        for (int ch = 0; ch < chunks; ++ch) {
-            if (!mbar_wait(&sums[ch & 1], (ch >> 1) & 1)) {
-                failed = 1;
-                break;
-            }
+        if constexpr (L::kLeave && CG == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        const uint32_t from = acc + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * kSide;
+        const int r = tid & 127, h = warp >> 2;
+        uint8_t* mine = stage + ST * L::kStage + warp * L::kSend;
+        const uint32_t rows = (warp & 3) * L::kSend;             // of a tile, in bytes
+        bool ok = true;
+        auto wait_sums = [&](uint32_t ch) {
+            ok = mbar_wait(&sums[ch & 1], (ch >> 1) & 1);
             tmem_fence_after();
-            if constexpr (P == 3) {
+            return ok;
+        };
+        auto leave_sums = [&](uint32_t ch) {
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_at(&taken[ch & 1], 0);
+        };
+        uint32_t ch = 0;                                         // sets of sums so far
+        for (int index = begin; index < a.count && ok; index += step) {
+            const Job<KIND, CG, L::kLeave> job(a, index, rank);
+            const Matrix& t = *job.t;
+            float v[L::kLeave ? kSide : 1];
 #pragma unroll
-                for (int q = 0; q < kSide / 32; ++q) {
-                    uint32_t r[32];
-                    tmem_load32(from + (ch & 1) * L::kColumns + q * 32, r);
+            for (int e = 0; e < (L::kLeave ? kSide : 1); ++e) v[e] = 0.f;
+            if constexpr (L::kLeave) {
+                for (int kb = 0; kb < job.nk; kb += job.leave, ++ch) {
+                    if (!wait_sums(ch)) break;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) v[q * 32 + e] += __uint_as_float(r[e]);
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t bits[64];
+                        tmem_load64(from + (ch & 1) * L::kColumns + q * 64, bits);
+                        if (q == 1) leave_sums(ch);
+#pragma unroll
+                        for (int e = 0; e < 64; ++e) v[q * 64 + e] += __uint_as_float(bits[e]);
+                    }
                 }
-                tmem_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_at(&taken[ch & 1], 0);
+            } else {
+                wait_sums(ch);
             }
-        }
-        // results go out as tiles; S at the same place comes in first where B needs it
-        block_part_sync<L::kWarps * 32>();
-        auto there = [&](int h) { return has_a && part.j * CG + h < columns; };
-        const int64_t out_tile = KIND == kNext ? (int64_t)it * nb + 2 * part.j * CG : ((int64_t)it * mt + part.j * CG) * 2;
-        if (KIND == kSquare && !failed) {
-            if (tid == 0) {
-                mbar_expect_tx(&third, (there(0) ? L::kOut : 0) + (CG == 2 && there(1) ? L::kOut : 0));
-                for (int h = 0; h < CG; ++h)
-                    if (there(h)) bulk_load(stage + h * L::kOut, s_in + (out_tile + 2 * h) * PL * kTileBytes, L::kOut, &third);
-            }
-            if (!mbar_wait(&third, 0)) failed = 1;
-        }
-        if (!failed) {
-            const float up = exp2f((float)t.es), down = exp2f((float)-t.es), gram = exp2f((float)(t.es - 2 * t.ex));
-            const int r = tid & 127, h = warp >> 2;
-            uint8_t* out = stage + h * L::kOut;
-            const bool diagonal = it == part.j * CG + h;
+            if (!ok) break;
+            const int tile = job.part.j * CG + h;                // of 128 columns
+            const bool there = job.has_a && tile < job.columns;
+            const int own = job.it == tile ? r : -1;             // this thread's column on the diagonal
+            const int64_t at = (KIND == kNext ? (int64_t)job.it * job.nb + 2 * tile : ((int64_t)job.it * job.mt + tile) * 2) * PL * kTileBytes;
+            const float up = exp2f((float)t.es), scale = KIND == kGram ? exp2f((float)(t.es - 2 * t.ex)) : exp2f((float)-t.es);
 #pragma unroll
-            for (int q32 = 0; q32 < kSide / 32; ++q32) {
-                float w[32];
-                if constexpr (P == 3) {
+            for (int cb = 0; cb < 2; ++cb) {
+                float w[kHalves];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) w[e] = v[q32 * 32 + e];
-                } else {
+                for (int q = 0; q < 2; ++q) {
                     uint32_t bits[32];
-                    tmem_load32(from + q32 * 32, bits);
+                    if constexpr (!L::kLeave) tmem_load32(from + (ch & 1) * L::kColumns + cb * kHalves + q * 32, bits);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) w[e] = __uint_as_float(bits[e]);
+                    for (int e = 0; e < 32; ++e) w[q * 32 + e] = (L::kLeave ? v[L::kLeave ? cb * kHalves + q * 32 + e : 0] : __uint_as_float(bits[e])) * scale;
                 }
+                if (!L::kLeave && cb == 1) leave_sums(ch);
+                if (!there) continue;
+                const int column = own - cb * kHalves;           // in this tile
+                if (KIND == kSquare) add_at(w, column, a.a * up);
+                send_tile<PL>(w, mine, a.work + (KIND == kGram ? t.s_at : KIND == kSquare ? t.b_at : t.at[a.which ^ 1]) + at + cb * PL * kTileBytes + rows, lane);
+                if (KIND == kGram) {
 #pragma unroll
-                for (int p8 = 0; p8 < 4; ++p8) {
-                    const int p = q32 * 4 + p8;
-                    uint4* hi = reinterpret_cast<uint4*>(out + (p >> 3) * PL * kTileBytes + piece_at(r, p & 7));
-                    uint4* lo = reinterpret_cast<uint4*>(out + ((p >> 3) * PL + PL - 1) * kTileBytes + piece_at(r, p & 7));
-                    float f[8];
-                    if constexpr (KIND == kSquare) {
-                        float s[8];
-                        join8(*hi, *lo, s, PL == 2);
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) {
-                            f[q] = fmaf(a.b, s[q], a.c * down * w[p8 * 8 + q]);
-                            if (diagonal && r == p * 8 + q) f[q] += a.a * up;
-                        }
-                    } else {
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) f[q] = w[p8 * 8 + q] * (KIND == kGram ? gram : down);
-                    }
-                    uint4 h4, l4;
-                    split8(f, h4, l4, PL == 2);
-                    *hi = h4;
-                    if (PL == 2) *lo = l4;
+                    for (int e = 0; e < kHalves; ++e) w[e] *= a.c;
+                    add_at(w, column, a.b * up);
+                    send_tile<PL>(w, mine, a.work + t.t_at + at + cb * PL * kTileBytes + rows, lane);
                 }
             }
-            fence_async();
+            if (!L::kLeave) ++ch;
         }
-        block_part_sync<L::kWarps * 32>();
-        if (tid == 0 && !failed) {
-            uint8_t* to = KIND == kGram ? a.work + t.s_at : KIND == kSquare ? a.work + t.b_at : a.work + t.at[a.which ^ 1];
-            for (int h = 0; h < CG; ++h)
-                if (there(h)) bulk_store(to + (out_tile + 2 * h) * PL * kTileBytes, stage + h * L::kOut, L::kOut);
-            bulk_stores_done();
-        }
+        if (!ok) failed = 1;
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else {
-        if constexpr (P == 3 && CG == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (warp == L::kWarps) {                                     // the copies
-            if (lane == 0) {
-                fence_async();
-                int kb = 0;
-                for (; kb < nk; ++kb) {
-                    const int s = kb % ST;
-                    if (kb >= ST && !mbar_wait(&empty[s], (kb / ST - 1) & 1)) {
-                        failed = 1;
-                        break;
-                    }
+        if constexpr (L::kLeave && CG == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == L::kWarps && lane == 0) {                    // the copies
+            fence_async();
+            uint32_t n = 0;                                      // steps of 64 of K so far
+            bool ok = true;
+            for (int index = begin; index < a.count && ok; index += step) {
+                const Job<KIND, CG, L::kLeave> job(a, index, rank);
+                const uint8_t* x = a.work + job.t->at[a.which];
+                const uint8_t* first = KIND == kGram ? x : a.work + (KIND == kSquare ? job.t->s_at : job.t->b_at);
+                const bool load_b = job.has_b && !job.same;
+                const uint32_t bytes = (job.has_a ? L::kFirst : 0) + (load_b ? L::kSecond : 0);
+                for (int kb = 0; kb < job.nk; ++kb, ++n) {
+                    const uint32_t s = n % ST;
+                    if (n >= ST) ok = mbar_wait(&empty[s], (n / ST - 1) & 1);
+                    if (!ok) break;
                     uint8_t* to_a = stage + s * L::kStage;
-                    uint8_t* to_b = to_a + L::kOperand;
+                    uint8_t* to_b = to_a + L::kFirst;
                     const int ct = kb >> 1;
-                    const bool load_b = has_b && !same;
-                    mbar_expect_tx(&full[s], (has_a ? L::kOperand : 0) + (load_b ? L::kOperand : 0));
-                    if (has_a) {
-                        if (KIND == kGram) fetch_along<PL>(to_a, x, (int64_t)it * nb + kb, &full[s]);
-                        else if (ct / CG <= part.i) fetch_along<PL>(to_a, first, ((int64_t)it * mt + ct) * 2 + (kb & 1), &full[s]);
-                        else fetch_turned<PL>(to_a, first, ((int64_t)ct * mt + it) * 2, kb & 1, &full[s]);
+                    mbar_expect_tx(&full[s], bytes);
+                    if (job.has_a) {
+                        if (KIND == kGram) fetch_along<PA>(to_a, x, (int64_t)job.it * job.nb + kb, a.planes, &full[s]);
+                        else if (!job.turns_a(kb)) fetch_along<PA>(to_a, first, ((int64_t)job.it * job.mt + ct) * 2 + (kb & 1), PL, &full[s]);
+                        else fetch_turned<PA>(to_a, first, ((int64_t)ct * job.mt + job.it) * 2, PL, kb & 1, &full[s]);
                     }
                     if (load_b) {
-                        if (KIND == kGram) fetch_along<PL>(to_b, x, (int64_t)jt * nb + kb, &full[s]);
-                        else if (KIND == kNext) fetch_turned<PL>(to_b, x, (int64_t)ct * nb + 2 * jt, kb & 1, &full[s]);
-                        else if (ct / CG <= part.j) fetch_along<PL>(to_b, first, ((int64_t)jt * mt + ct) * 2 + (kb & 1), &full[s]);
-                        else fetch_turned<PL>(to_b, first, ((int64_t)ct * mt + jt) * 2, kb & 1, &full[s]);
+                        if (KIND == kGram) fetch_along<PB>(to_b, x, (int64_t)job.jt * job.nb + kb, a.planes, &full[s]);
+                        else if (KIND == kNext) fetch_turned<PB>(to_b, x, (int64_t)ct * job.nb + 2 * job.jt, a.planes, kb & 1, &full[s]);
+                        else if (!job.turns_b(kb)) fetch_along<PB>(to_b, a.work + job.t->t_at, ((int64_t)job.jt * job.mt + ct) * 2 + (kb & 1), PL, &full[s]);
+                        else fetch_turned<PB>(to_b, a.work + job.t->t_at, ((int64_t)ct * job.mt + job.jt) * 2, PL, kb & 1, &full[s]);
                     }
                 }
-                if (failed)                                          // copies under way are sat out
-                    for (int q = kb > ST ? kb - ST : 0; q < kb; ++q) mbar_wait(&full[q % ST], (q / ST) & 1);
             }
-        } else if (warp == L::kWarps + 1) {                          // the products
-            if (lane == 0 && rank == 0) {
-                bool ok = true;
-                for (int kb = 0; kb < nk; ++kb) {
-                    const int s = kb % ST, ch = kb / L::kChunk;
-                    const bool begins = kb % L::kChunk == 0;
-                    if (begins && ch >= 2) ok = mbar_wait_cluster(&taken[ch & 1], (ch / 2 - 1) & 1);
-                    ok = ok && mbar_wait(&full[s], (kb / ST) & 1);
-                    if (CG == 2) ok = ok && mbar_wait_cluster(&peer[s], (kb / ST) & 1);
-                    if (!ok) {
-                        failed = 1;
-                        break;
+            if (!ok) {                                           // copies under way are sat out
+                failed = 1;
+                for (uint32_t q = n > ST ? n - ST : 0; q < n; ++q) mbar_wait(&full[q % ST], (q / ST) & 1);
+            }
+        } else if (warp == L::kWarps + 1 && lane == 0) {         // the products
+            uint32_t n = 0, ch = 0;
+            bool ok = true, ready = false;                       // ready: the next step's factors (and room for its sums) are known to be there
+            for (int index = begin; index < a.count && ok; index += step) {
+                const Job<KIND, CG, L::kLeave> job(a, index, rank);
+                for (int kb = 0; kb < job.nk; ++kb, ++n) {
+                    const uint32_t s = n % ST;
+                    if (CG == 2 && rank == 1) {                  // the other CTA of a pair tells the first what has come
+                        ok = mbar_wait(&full[s], (n / ST) & 1);
+                        if (!ok) break;
+                        mbar_arrive_at(&full[s], 0);
+                        continue;
+                    }
+                    const bool begins = kb % job.leave == 0, ends = kb + 1 == job.nk || (kb + 1) % job.leave == 0;
+                    if (!ready) {
+                        if (begins && ch >= 2) ok = mbar_wait(&taken[ch & 1], (ch / 2 - 1) & 1);
+                        ok = ok && mbar_wait(&full[s], (n / ST) & 1);
+                        if (!ok) break;
                     }
                     tmem_fence_after();
-                    const int ct = kb >> 1;
-                    const bool turn_a = KIND != kGram && ct / CG > part.i;
-                    const bool turn_b = KIND == kNext || (KIND == kSquare && ct / CG > part.j);
-                    const uint32_t at_a = smem_u32(stage) + s * L::kStage, at_b = same ? at_a : at_a + L::kOperand;
+                    const bool turn_a = job.turns_a(kb), turn_b = job.turns_b(kb);
+                    const uint32_t at_a = smem_u32(stage) + s * L::kStage, at_b = job.same ? at_a : at_a + L::kFirst;
                     const uint32_t shape = product_shape(kSide * CG, kSide * CG) | (turn_a ? kTurnA : 0) | (turn_b ? kTurnB : 0);
                     const uint64_t da = turn_a ? operand_turned(at_a, kPieceBytes) : operand_along(at_a);
                     const uint64_t db = turn_b ? operand_turned(at_b, kPieceBytes) : operand_along(at_b);
-                    const uint64_t na = turn_a ? kNextTurned : kNextAlong, nbk = turn_b ? kNextTurned : kNextAlong;
-                    const uint32_t to = acc + (ch & 1) * (L::kSums == 2 ? L::kColumns : 0);
+                    const uint64_t na = turn_a ? kNextTurned : kNextAlong, nb = turn_b ? kNextTurned : kNextAlong;
+                    const uint32_t to = acc + (ch & 1) * L::kColumns;
                     constexpr uint64_t low = kTileBytes >> 4;
-                    if constexpr (P == 3)                            // the small products first, while the sums are small
+                    // Half of the products, a look at the barriers of the next step while the tensor cores work on them (300 cycles
+                    // that would lie between two steps), and the other half.  The small products come first, while the sums are small.
+                    auto high = [&](int q) { product<CG>(to, da + q * na, db + q * nb, shape, PB == 2 || !begins || q > 0); };
+                    if constexpr (PB == 2) {
 #pragma unroll
                         for (int q = 0; q < kHalves / 16; ++q) {
-                            product<CG>(to, da + q * na, db + q * nbk + low, shape, !begins || q > 0);
-                            product<CG>(to, da + q * na + low, db + q * nbk, shape, true);
+                            product<CG>(to, da + q * na, db + q * nb + low, shape, !begins || q > 0);
+                            if constexpr (PA == 2) product<CG>(to, da + q * na + low, db + q * nb, shape, true);
                         }
-#pragma unroll
-                    for (int q = 0; q < kHalves / 16; ++q) product<CG>(to, da + q * na, db + q * nbk, shape, P == 3 || !begins || q > 0);
-                    products_done<CG>(&empty[s]);
-                    if (kb + 1 == nk || (kb + 1) % L::kChunk == 0) products_done<CG>(&sums[ch & 1]);
-                }
-            } else if (lane == 0) {                                  // the other CTA of a pair tells the first what has come
-                for (int kb = 0; kb < nk; ++kb) {
-                    const int s = kb % ST;
-                    if (!mbar_wait(&full[s], (kb / ST) & 1)) {
-                        failed = 1;
-                        break;
+                    } else {
+                        high(0);
+                        high(1);
                     }
-                    fence_async();
-                    mbar_arrive_at(&peer[s], 0);
+                    const uint32_t next = n + 1, then = ch + 1;
+                    ready = (kb + 1 < job.nk || index + step < a.count) && mbar_test(&full[next % ST], (next / ST) & 1) &&
+                            (!ends || then < 2 || mbar_test(&taken[then & 1], (then / 2 - 1) & 1));
+                    if constexpr (PB == 2) {
+                        high(0);
+                        high(1);
+                    }
+                    high(2);
+                    high(3);
+                    products_done<CG>(&empty[s]);
+                    if (ends) {
+                        products_done<CG>(&sums[ch & 1]);
+                        ++ch;
+                    }
                 }
             }
+            if (!ok) failed = 1;
         }
     }
     __syncwarp();
@@ -608,14 +657,38 @@ __global__ void __launch_bounds__(Plan<P, CG>::kThreads, Plan<P, CG>::kBlocks) _
     __syncthreads();
     if (tid == 0 && failed) atomicAdd(a.errors, 1u);
     if (CG == 2) cluster_sync();
-    if (warp == 0) tmem_free<CG>(acc, L::kSums * L::kColumns);
+    if (warp == 0) tmem_free<CG>(acc, 2 * L::kColumns);
 }
 
 using ProductKernel = void (*)(ProductArgs);
-template <int P, int CG>
-ProductKernel product_of(int kind)
+struct Launch {
+    ProductKernel kernel;
+    int threads, shared, blocks;    // blocks: to an SM
+};
+template <int KIND, int PA, int PB, int CG>
+Launch launch_of()
 {
-    return kind == kGram ? product_kernel<kGram, P, CG> : kind == kSquare ? product_kernel<kSquare, P, CG> : product_kernel<kNext, P, CG>;
+    using L = Plan<PA, PB, CG>;
+    return {product_kernel<KIND, PA, PB, CG>, L::kThreads, (int)L::kShared, L::kBlocks};
+}
+// `first`: the product reads X_0, which has two parts in any case
+template <int CG>
+Launch launch_of(int kind, bool three, bool first)
+{
+    if (three) return kind == kGram ? launch_of<kGram, 2, 2, CG>() : kind == kSquare ? launch_of<kSquare, 2, 2, CG>() : launch_of<kNext, 2, 2, CG>();
+    if (kind == kNext) return first ? launch_of<kNext, 1, 2, CG>() : launch_of<kNext, 1, 1, CG>();
+    return kind == kGram ? launch_of<kGram, 1, 1, CG>() : launch_of<kSquare, 1, 1, CG>();
+}
+template <int CG>
+cudaError_t allow_shared()
+{
+    cudaError_t e = cudaSuccess;
+    for (int kind = 0; kind < 3; ++kind)
+        for (int mode = 0; mode < 3 && e == cudaSuccess; ++mode) {
+            const Launch l = launch_of<CG>(kind, mode == 0, mode == 1);
+            e = cudaFuncSetAttribute((const void*)l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, l.shared);
+        }
+    return e;
 }
 
 // matrices of a wave that take the same kernels: one product or three, one CTA to a part or two
@@ -643,7 +716,7 @@ using namespace choco;
 
 struct choco_muon {
     choco_muon_params params;
-    int device;
+    int device, sms;
     bool broken;                   // the table on the device may be half written
     std::vector<Matrix> mats;      // as on the device
     std::vector<Range> written;
@@ -687,13 +760,13 @@ Range range_of(const void* p, int64_t rows, int64_t cols, int64_t ld, int32_t dt
     return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)(((rows - 1) * ld + cols) * dtype_size(dtype))};
 }
 
-// Largest singular value that the polynomial makes of one in [0, most], and the largest |a + b s^2 + c s^4| on the way.
+// Largest singular value that the polynomial makes of one in [0, most], and the largest |a + b s^2 + c s^4| and |b + c s^2| on the way.
 void reach(const choco_muon_params& p, double most, double* value, double* slope)
 {
     *value = *slope = 0.0;
     for (int i = 0; i <= 4096; ++i) {
-        const double s = most * i / 4096, q = std::fabs(p.a + s * s * (p.b + s * s * p.c));
-        *slope = std::max(*slope, q);
+        const double s = most * i / 4096, inner = p.b + s * s * p.c, q = std::fabs(p.a + s * s * inner);
+        *slope = std::max({*slope, q, std::fabs(inner)});
         *value = std::max(*value, s * q);
     }
 }
@@ -704,7 +777,7 @@ bool polynomial_ok(const choco_muon_params& p)
     for (int k = 0; k < p.steps; ++k) {
         double value, slope;
         reach(p, most, &value, &slope);
-        if (!(value <= 1.9) || !(slope <= 15.0)) return false; // S and B stay inside float16 at their scales
+        if (!(value <= 1.9) || !(slope <= 15.0)) return false; // S, T and B stay inside float16 at their scales
         most = std::max(1.0, value);
     }
     return true;
@@ -764,7 +837,7 @@ int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit
         if (units.size() > 0x7fffffff) return CHOCO_ERR_TOO_LARGE;
         o->mats.push_back(t);
         o->offsets.push_back(at);
-        kinds.push_back(o->params.products == 3 || (o->params.products == 0 && (q.x_dtype != CHOCO_BF16)));
+        kinds.push_back(o->params.products == 3 || (o->params.products == 0 && (q.x_dtype != CHOCO_BF16 || t.m <= kSide)));
         at += (count + kBlock - 1) / kBlock * kBlock;
         if (at > (int64_t)1 << 38) return CHOCO_ERR_TOO_LARGE;
         if (some) {
@@ -781,11 +854,11 @@ int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit
         int32_t end = i;
         for (; end < n; ++end) {
             Matrix& t = o->mats[end];
-            const int64_t planes = kinds[end] ? 2 : 1, xb = (int64_t)t.mt * t.nb * planes * kTileBytes, sb = (int64_t)t.mt * t.mt * 2 * planes * kTileBytes;
-            if (bytes > 0 && bytes + 2 * (xb + sb) > kWaveBytes) break;
-            t.at[0] = bytes; t.at[1] = bytes + xb;
-            t.s_at = bytes + 2 * xb; t.b_at = t.s_at + sb;
-            bytes += 2 * (xb + sb);
+            const int64_t planes = kinds[end] ? 2 : 1, x0 = (int64_t)t.mt * t.nb * 2 * kTileBytes, xb = x0 / 2 * planes, sb = (int64_t)t.mt * t.mt * 2 * planes * kTileBytes;
+            if (bytes > 0 && bytes + x0 + xb + 3 * sb > kWaveBytes) break;
+            t.at[0] = bytes; t.at[1] = bytes + x0;
+            t.s_at = bytes + x0 + xb; t.t_at = t.s_at + sb; t.b_at = t.t_at + sb;
+            bytes += x0 + xb + 3 * sb;
         }
         *work = std::max(*work, bytes);
         Wave w = {};
@@ -843,15 +916,6 @@ bool is_written(const choco_muon* o, const Matrix& t, const void* g)
     return next != o->written.begin() && (next - 1)->end > r.begin;
 }
 
-template <int P, int CG>
-cudaError_t allow_shared()
-{
-    cudaError_t e = cudaSuccess;
-    for (int kind = 0; kind < 3 && e == cudaSuccess; ++kind)
-        e = cudaFuncSetAttribute((const void*)product_of<P, CG>(kind), cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<P, CG>::kShared);
-    return e;
-}
-
 int allocate(choco_muon* o, const std::vector<Unit>& units, const std::vector<Part>& parts, const std::vector<Block>& blocks, int64_t work)
 {
     int64_t at = 0;
@@ -883,13 +947,10 @@ int allocate(choco_muon* o, const std::vector<Unit>& units, const std::vector<Pa
     ok = cudaStreamSynchronize(st) == cudaSuccess && ok;
     cudaStreamDestroy(st);
     if (!ok) return CHOCO_ERR_CUDA;
-    return allow_shared<1, 1>() == cudaSuccess && allow_shared<1, 2>() == cudaSuccess && allow_shared<3, 1>() == cudaSuccess &&
-                   allow_shared<3, 2>() == cudaSuccess
-               ? CHOCO_OK
-               : CHOCO_ERR_CUDA;
+    return allow_shared<1>() == cudaSuccess && allow_shared<2>() == cudaSuccess ? CHOCO_OK : CHOCO_ERR_CUDA;
 }
 
-cudaError_t launch_products(const choco_muon* o, const Wave& w, int kind, int which, cudaStream_t st)
+cudaError_t launch_products(const choco_muon* o, const Wave& w, int kind, int step, cudaStream_t st)
 {
     const choco_muon_params& p = o->params;
     cudaError_t e = cudaSuccess;
@@ -898,12 +959,11 @@ cudaError_t launch_products(const choco_muon* o, const Wave& w, int kind, int wh
             const Class& cl = w.classes[three][pairs];
             const int64_t begin = kind == kNext ? cl.next : cl.symmetric, end = kind == kNext ? cl.next_end : cl.symmetric_end;
             if (begin == end || e != cudaSuccess) continue;
-            const ProductArgs a = {o->d_mats, o->d_parts + begin, o->d_work, o->d_errors, (float)p.a, (float)p.b, (float)p.c, which};
-            const ProductKernel kernel = three ? (pairs ? product_of<3, 2>(kind) : product_of<3, 1>(kind))
-                                               : (pairs ? product_of<1, 2>(kind) : product_of<1, 1>(kind));
-            const int threads = pairs ? Plan<3, 2>::kThreads : Plan<3, 1>::kThreads;
-            const size_t smem = three ? (pairs ? Plan<3, 2>::kShared : Plan<3, 1>::kShared) : (pairs ? Plan<1, 2>::kShared : Plan<1, 1>::kShared);
-            e = launch_overlapped(kernel, dim3((unsigned)((end - begin) * (pairs + 1))), dim3(threads), smem, st, HotRange{}, a);
+            const ProductArgs a = {o->d_mats, o->d_parts + begin, o->d_work, o->d_errors, (int32_t)(end - begin), (float)p.a, (float)p.b, (float)p.c,
+                                   step & 1, three || step == 0 ? 2 : 1};
+            const Launch l = pairs ? launch_of<2>(kind, three, step == 0) : launch_of<1>(kind, three, step == 0);
+            const int64_t most = (int64_t)o->sms * l.blocks / (pairs + 1);
+            e = launch_overlapped(l.kernel, dim3((unsigned)(std::min(end - begin, most) * (pairs + 1))), dim3(l.threads), l.shared, st, HotRange{}, a);
         }
     return e;
 }
@@ -920,14 +980,14 @@ int run(choco_muon* o, float* m, double lr, const float* factor, bool update, cu
             for (int three = 0; three < 2; ++three) {
                 if (w.blocks[three] == w.blocks_end[three] || e != cudaSuccess) continue;
                 ta.blocks = o->d_blocks + w.blocks[three];
-                ta.planes = three + 1;
+                ta.planes = three || p.steps == 0 ? 2 : 1;
                 e = launch_overlapped(kernel, dim3((unsigned)(w.blocks_end[three] - w.blocks[three])), dim3(kTileThreads2), 0, st, HotRange{}, ta);
             }
         };
         tiles(cut_kernel);
         for (int k = 0; k < p.steps; ++k)
             for (int kind : {kGram, kSquare, kNext})
-                if (e == cudaSuccess) e = launch_products(o, w, kind, k & 1, st);
+                if (e == cudaSuccess) e = launch_products(o, w, kind, k, st);
         ta.which = p.steps & 1;
         tiles(apply_kernel);
     }
@@ -959,7 +1019,9 @@ int choco_muon_init(choco_muon** out, int32_t n_matrices, const choco_muon_matri
         if (rc == CHOCO_OK && overlap(o)) rc = CHOCO_ERR_INVALID_ARG;
         for (const Matrix& t : o->mats)
             if (rc == CHOCO_OK && is_written(o, t, t.g)) rc = CHOCO_ERR_INVALID_ARG;
-        if (rc == CHOCO_OK && cudaGetDevice(&o->device) != cudaSuccess) rc = CHOCO_ERR_CUDA;
+        if (rc == CHOCO_OK && (cudaGetDevice(&o->device) != cudaSuccess ||
+                               cudaDeviceGetAttribute(&o->sms, cudaDevAttrMultiProcessorCount, o->device) != cudaSuccess))
+            rc = CHOCO_ERR_CUDA;
         if (rc == CHOCO_OK) rc = allocate(o, units, parts, blocks, work);
     } catch (const std::exception&) {
         rc = CHOCO_ERR_ALLOC;
