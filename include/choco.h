@@ -643,7 +643,7 @@ typedef enum {
 } choco_activation;
 typedef struct {
     int32_t n;            /* workers, 1 .. 65535                                                   */
-    int32_t groups;       /* divides channels; at most 4096 channels to a group                    */
+    int32_t groups;       /* divides channels; at most 2048 channels to a group                    */
     int64_t channels;     /* 1 .. 2^20                                                             */
     int64_t max_images;   /* most images of one worker in a call for gradients of the parameters   */
     double eps;           /* >= 0, finite as a float32                                             */

@@ -788,18 +788,29 @@ def choco_muon_status(opt, stream=None) -> None:
 
 
 class GroupNormHandle(ctypes.c_void_p):
-    """What choco_group_norm_init returns: the library's handle, with the device it belongs to and its sizes."""
+    """What choco_group_norm_init returns: the library's handle, with the device it belongs to, its sizes, and the layouts of arrays that
+    its calls have found to be in order."""
 
     def describe(self, device: int, n: int, channels: int, groups: int) -> None:
         self.device, self.n, self.channels, self.groups = device, n, channels, groups
+        self.layouts: dict = {}
 
 
 def _pixels_of(gn, what: str, t):
     """(choco_pixels, images, pixels) of an array [n, images, ..., channels]: what lies between images and channels are pixels, which
     have one stride."""
-    shape, strides = t.shape, t.stride()
+    key = (what, t.shape, t.stride(), t.dtype)
+    found = gn.layouts.get(key)
+    if found is None:
+        found = gn.layouts[key] = _pixel_layout(gn, what, t)
     if t.get_device() != gn.device:
         raise ChocoError(f"libchoco: {what} must be on the handle's GPU ({gn.device}), not {t.device}", -1)
+    found[0].data = t.data_ptr()
+    return found
+
+
+def _pixel_layout(gn, what: str, t):
+    shape, strides = t.shape, t.stride()
     if len(shape) < 3 or shape[0] != gn.n or shape[-1] != gn.channels or (strides[-1] != 1 and shape[-1] > 1):
         raise ChocoError(f"libchoco: {what} must be [{gn.n}, images, pixels, {gn.channels}] with neighbouring channels, not {list(shape)}, "
                          f"strides {list(strides)}", -1)
@@ -812,19 +823,24 @@ def _pixels_of(gn, what: str, t):
         elif strides[k] != pixels * step and pixels > 0 and shape[k] > 0:
             raise ChocoError(f"libchoco: the pixels of {what} must have one stride, not {list(strides)} for {list(shape)}", -1)
         pixels *= shape[k]
-    return choco_pixels(t.data_ptr(), strides[0], strides[1], step, _dtype(t), 0), shape[1], pixels
+    return choco_pixels(None, strides[0], strides[1], step, _dtype(t), 0), shape[1], pixels
 
 
-def _channels_of(gn, what: str, *tensors):
+def _channels_of(gn, what: str, first, second):
     """(stride from worker to worker, type) of arrays [n, channels] with neighbouring channels; None is left out."""
     found = None
-    for t in tensors:
+    for t in (first, second):
         if t is None:
             continue
-        if t.get_device() != gn.device or t.dim() != 2 or t.shape[0] != gn.n or t.shape[1] != gn.channels or (t.stride(1) != 1 and gn.channels > 1):
-            raise ChocoError(f"libchoco: {what} must be [{gn.n}, {gn.channels}] with neighbouring channels on GPU {gn.device}, not {list(t.shape)}, "
-                             f"strides {list(t.stride())} on {t.device}", -1)
-        this = (t.stride(0), _dtype(t))
+        key = (what, t.shape, t.stride(), t.dtype)
+        this = gn.layouts.get(key)
+        if this is None:
+            if t.dim() != 2 or t.shape[0] != gn.n or t.shape[1] != gn.channels or (t.stride(1) != 1 and gn.channels > 1):
+                raise ChocoError(f"libchoco: {what} must be [{gn.n}, {gn.channels}] with neighbouring channels, not {list(t.shape)}, "
+                                 f"strides {list(t.stride())}", -1)
+            this = gn.layouts[key] = (t.stride(0), _dtype(t))
+        if t.get_device() != gn.device:
+            raise ChocoError(f"libchoco: {what} must be on GPU {gn.device}, not on {t.device}", -1)
         if found is not None and this != found and (gn.n > 1 or this[1] != found[1]):
             raise ChocoError(f"libchoco: {what} have one type and one stride from worker to worker", -1)
         found = found or this
@@ -833,7 +849,7 @@ def _channels_of(gn, what: str, *tensors):
 
 def _check_stats(gn, images: int, *tensors) -> None:
     for t in tensors:
-        if t is not None and (t.get_device() != gn.device or _dtype(t) != 0 or tuple(t.shape) != (gn.n, images, gn.groups) or not t.is_contiguous()):
+        if t is not None and (t.get_device() != gn.device or _dtype(t) != 0 or t.shape != (gn.n, images, gn.groups) or not t.is_contiguous()):
             raise ChocoError(f"libchoco: mean and rstd must be contiguous float32 [{gn.n}, {images}, {gn.groups}] on GPU {gn.device}, not {t.dtype} "
                              f"{list(t.shape)} on {t.device}", -1)
 
@@ -863,8 +879,8 @@ def choco_group_norm_forward(gn, x, weight, bias, y, mean=None, rstd=None, strea
         raise ChocoError(f"libchoco: y must have the shape of x, {list(x.shape)}, not {list(y.shape)}", -1)
     ld, kind = _channels_of(gn, "weight and bias", weight, bias)
     _check_stats(gn, images, mean, rstd)
-    _check(load().choco_group_norm_forward(gn, images, pixels, ctypes.byref(ax), ctypes.byref(ay), _ptr(weight), _ptr(bias), ld, kind, _ptr(mean),
-                                           _ptr(rstd), _stream_of(stream, gn.device)))
+    _check(load().choco_group_norm_forward(gn, images, pixels, ax, ay, _ptr(weight), _ptr(bias), ld, kind, _ptr(mean), _ptr(rstd),
+                                           _stream_of(stream, gn.device)))
 
 
 def choco_group_norm_backward(gn, x, dy, weight, bias, mean, rstd, dx, dweight, dbias, accumulate: bool = False, stream=None) -> None:
@@ -882,8 +898,7 @@ def choco_group_norm_backward(gn, x, dy, weight, bias, mean, rstd, dx, dweight, 
     if mean is None or rstd is None:
         raise ChocoError("libchoco: mean and rstd of the forward call are needed", -1)
     _check_stats(gn, images, mean, rstd)
-    _check(load().choco_group_norm_backward(gn, images, pixels, ctypes.byref(ax), ctypes.byref(ay), None if ad is None else ctypes.byref(ad),
-                                            _ptr(weight), _ptr(bias), ld, kind, _ptr(mean), _ptr(rstd), _ptr(dweight), _ptr(dbias), gld, gkind,
+    _check(load().choco_group_norm_backward(gn, images, pixels, ax, ay, ad, _ptr(weight), _ptr(bias), ld, kind, _ptr(mean), _ptr(rstd), _ptr(dweight), _ptr(dbias), gld, gkind,
                                             1 if accumulate else 0, _stream_of(stream, gn.device)))
 
 

@@ -24,10 +24,12 @@ namespace {
 
 enum Activation { kNone, kRelu, kSilu, kGelu };
 
-constexpr int kNormThreads = 256;
+constexpr int kNormThreads = 128;
 constexpr int kNormWarps = kNormThreads / 32;
-constexpr int kAtOnce = 4;              // pixels whose loads a thread has under way
-constexpr int64_t kMostSlice = 4096;    // channels of a slice, and of a group: their sums are in shared memory
+constexpr int kNormBlocks = 4;          // to an SM, by registers
+constexpr int kAtOnce = 4;              // pixels whose loads a thread has under way where it keeps no more
+constexpr int kWaits = 2;               // groups in which a thread's copies to shared memory are waited for
+constexpr int64_t kMostSlice = 2048;    // channels of a slice, and of a group: their sums are in shared memory
 
 struct Pixels {                         // element (i, b, p, c) at i worker + b image + p pixel + c
     void* data;
@@ -46,22 +48,76 @@ struct NormArgs {
     int32_t images, channels, per_group, groups;
     int32_t slice, slices;              // channels of a slice, slices of an image
     int32_t cluster;
+    int32_t share;                      // pixels of a block
+    int32_t rounds, lanes, steps;       // see Share
+    uint32_t per_column;                // 2^16 / columns, rounded up
     int32_t kept;                       // pixels of a thread whose values it keeps
     int32_t param_dtype, activation;
     double eps;
+    double inverse;                     // of the values of a group of an image
 };
 
-__device__ __forceinline__ float2 load_peer(const float2* p, uint32_t rank) // of another block of the cluster
+__device__ __forceinline__ void store_peer(float2* p, uint32_t rank, float2 v) // where p is in another block of the cluster
 {
-    float2 v;
-    asm volatile("{\n\t.reg .b32 r;\n\tmapa.shared::cluster.u32 r, %2, %3;\n\tld.shared::cluster.v2.f32 {%0, %1}, [r];\n\t}"
-                 : "=f"(v.x), "=f"(v.y)
-                 : "r"(smem_u32(p)), "r"(rank)
+    asm volatile("{\n\t.reg .b32 r;\n\tmapa.shared::cluster.u32 r, %0, %1;\n\tst.shared::cluster.v2.f32 [r], {%2, %3};\n\t}" ::"r"(smem_u32(p)), "r"(rank),
+                 "f"(v.x), "f"(v.y)
                  : "memory");
-    return v;
+}
+__device__ __forceinline__ int cluster_at() // of the clusters along the grid's first axis
+{
+    int c;
+    asm volatile("mov.u32 %0, %%clusterid.x;" : "=r"(c));
+    return c;
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+
+// Two neighbouring channels at a time, in the register pairs that sm_100's float32 instructions for two take (as structs of two
+// floats the moves between them cost what the instructions save).
+using Pair = uint64_t;
+__device__ __forceinline__ Pair shuffled(Pair a, int o) { return __shfl_xor_sync(0xffffffffu, a, o); }
+__device__ __forceinline__ Pair pair_of(float x, float y)
+{
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x), "f"(y));
+    return p;
+}
+__device__ __forceinline__ float2 floats_of(Pair p)
+{
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
+    return f;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b)
+{
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
+{
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+
+// Values of a pixel: pairs of channels (of VEC = 1 the second one is nothing)
+template <typename T, int VEC>
+__device__ __forceinline__ Pair raw_pair(const Raw<T, VEC>& r, int p)
+{
+    if constexpr (std::is_same_v<T, __nv_bfloat16> && VEC > 1)
+        return pair_of(__uint_as_float(r.w[p] << 16), __uint_as_float(r.w[p] & 0xffff0000u));
+    else
+        return pair_of(raw_get(r, 2 * p), VEC > 1 ? raw_get(r, VEC > 1 ? 2 * p + 1 : 0) : 0.f);
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_pairs(T* to, const Pair* f)
+{
+    float v[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = e & 1 ? floats_of(f[e / 2]).y : floats_of(f[e / 2]).x;
+    store_vec<T, VEC>(to, v);
+}
 
 // 16-bit results carry 8 or 11 bits: the fast exponential and quotient (2 units in the last place of float32 and 2^-21 |z|) do for them
 template <bool FAST>
@@ -72,10 +128,17 @@ __device__ __forceinline__ float sigmoid(float z)
 template <int ACT, bool FAST>
 __device__ __forceinline__ float act_of(float z)
 {
-    if constexpr (ACT == kRelu) return z < 0.f ? 0.f : z; // NaN stays one
-    else if constexpr (ACT == kSilu) return z * sigmoid<FAST>(z);
-    else if constexpr (ACT == kGelu) return z * (0.5f * (1.f + erff(z * 0.70710678f)));
-    else return z;
+    if constexpr (ACT == kRelu) {
+        float y;
+        asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(z));
+        return y;
+    } else if constexpr (ACT == kSilu) {
+        return z * sigmoid<FAST>(z);
+    } else if constexpr (ACT == kGelu) {
+        return z * (0.5f * (1.f + erff(z * 0.70710678f)));
+    } else {
+        return z;
+    }
 }
 template <int ACT, bool FAST>
 __device__ __forceinline__ float slope_of(float z) // relu is decided elsewhere
@@ -99,392 +162,572 @@ struct Share {
     int rounds;
     int lanes;                          // threads that share a column
     int lane, column;                   // (of a round)
-    int64_t begin, end;                 // pixels of the block
-    int steps;                          // pixels of a thread, at most
+    int64_t first;                      // pixel of the block's and the lane's first step
+    int steps, mine;                    // pixels of a thread at most, and of this one
     bool folds;                         // columns of a warp repeat: lanes are added up by shuffles first
     int rows;                           // partial sums of a column in shared memory
 
     __device__ Share(const NormArgs& a, uint32_t rank)
     {
         columns = a.slice / VEC;
-        rounds = (columns + kNormThreads - 1) / kNormThreads;
-        lanes = rounds > 1 ? 1 : kNormThreads / columns;
-        lane = rounds > 1 ? 0 : (int)threadIdx.x / columns;
-        column = rounds > 1 ? (int)threadIdx.x : (int)threadIdx.x % columns;
-        begin = a.pixels * rank / a.cluster;
-        end = a.pixels * (rank + 1) / a.cluster;
-        steps = (int)((end - begin + lanes - 1) / lanes);
+        rounds = a.rounds;
+        lanes = a.lanes;
+        lane = rounds > 1 ? 0 : (int)(threadIdx.x * a.per_column >> 16);
+        column = rounds > 1 ? (int)threadIdx.x : (int)threadIdx.x - lane * columns;
+        const int64_t begin = (int64_t)a.share * rank, left = a.pixels - begin;
+        const int count = (int)max((int64_t)0, min((int64_t)a.share, left)) - lane;
+        first = begin + lane;
+        steps = a.steps;
+        mine = count > 0 ? min(steps, (int)(((uint32_t)count + lanes - 1) / (uint32_t)lanes)) : 0;
         folds = columns < 32 && (columns & (columns - 1)) == 0;
         rows = folds ? kNormWarps : lanes;
     }
     __device__ bool active(int round) const { return lane < lanes && round * kNormThreads + column < columns; }
     __device__ int channel(int round) const { return (round * kNormThreads + column) * VEC; }
-    __device__ int64_t pixel(int step) const { return begin + lane + (int64_t)step * lanes; }
+    __device__ int kept(int most, int round) const { return max(0, min(most - round * steps, mine)); } // of this thread's pixels
 };
 
-// Adds up a round's sums of channels over the block; `part` receives them.
+__device__ __forceinline__ float2 plus(float2 a, float2 b) { return make_float2(a.x + b.x, a.y + b.y); }
+
+// Adds up a round's sums of channels over the block and hands them to all blocks of the cluster, which keep the sums of each in `parts`.
 template <int VEC>
-__device__ __forceinline__ void add_up(const Share<VEC>& sh, const NormArgs& a, int round, float* s1, float* s2, float2* red, float2* part)
+__device__ __forceinline__ void add_up(const Share<VEC>& sh, const NormArgs& a, int round, Pair* s1, Pair* s2, float2* red, float2* parts, uint32_t rank)
 {
+    constexpr int NP = (VEC + 1) / 2;
     const int first = round * kNormThreads * VEC, width = (sh.rounds > 1 ? min(kNormThreads, sh.columns - round * kNormThreads) : sh.columns) * VEC;
     int row = sh.lane;
     bool writes = sh.active(round);
     if (sh.folds) {
-        for (int o = sh.columns; o < 32; o <<= 1)
+        for (int o = sh.columns; o < 32; o <<= 1) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                s1[e] += __shfl_xor_sync(0xffffffffu, s1[e], o);
-                s2[e] += __shfl_xor_sync(0xffffffffu, s2[e], o);
+            for (int p = 0; p < NP; ++p) {
+                s1[p] = add2(s1[p], shuffled(s1[p], o));
+                s2[p] = add2(s2[p], shuffled(s2[p], o));
             }
+        }
         row = (int)threadIdx.x >> 5;
         writes = (int)(threadIdx.x & 31) < sh.columns;
     }
     if (writes) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) red[row * width + sh.column * VEC + e] = make_float2(s1[e], s2[e]);
+        for (int e = 0; e < VEC; ++e)
+            red[row * width + sh.column * VEC + e] = e & 1 ? make_float2(floats_of(s1[e / 2]).y, floats_of(s2[e / 2]).y)
+                                                           : make_float2(floats_of(s1[e / 2]).x, floats_of(s2[e / 2]).x);
     }
     __syncthreads();
     for (int c = threadIdx.x; c < width; c += kNormThreads) {
         float2 v = red[c];
-        for (int r = 1; r < sh.rows; ++r) {
-            const float2 w = red[r * width + c];
-            v.x += w.x;
-            v.y += w.y;
+        for (int r = 1; r < sh.rows; ++r) v = plus(v, red[r * width + c]);
+        for (int k = 0; k < a.cluster; ++k) {
+            if (a.cluster > 1) store_peer(parts + rank * a.slice + first + c, k, v);
+            else parts[first + c] = v;
         }
-        part[first + c] = v;
     }
     __syncthreads();
 }
 
-// Sums of channels over the cluster, in the order of its blocks.  Ends with an arrival at the cluster's barrier that the
-// caller waits for before it leaves: until then others read `part`.
-__device__ __forceinline__ void exchange(const NormArgs& a, const float2* part, float2* total)
+// Sums of channels over the cluster, in the order of its blocks.
+__device__ __forceinline__ void exchange(const NormArgs& a, const float2* parts, float2* total)
 {
     if (a.cluster > 1) {
         cluster_arrive();
         cluster_wait();
     }
     for (int c = threadIdx.x; c < a.slice; c += kNormThreads) {
-        float2 v = part[c];
-        if (a.cluster > 1) {
-            v = make_float2(0.f, 0.f);
-            for (int k = 0; k < a.cluster; ++k) {
-                const float2 w = load_peer(part + c, k);
-                v.x += w.x;
-                v.y += w.y;
-            }
-        }
+        float2 v = parts[c];
+        for (int k = 1; k < a.cluster; ++k) v = plus(v, parts[k * a.slice + c]);
         total[c] = v;
     }
-    if (a.cluster > 1) cluster_arrive();
     __syncthreads();
 }
 
-__device__ __forceinline__ double warp_add(double v)
+// Shared memory of a block: four numbers for each channel of the slice, their sums (of each block and of all), partial sums of
+// threads, and the values that are kept.
+struct Layout {
+    float4* channel;
+    float2 *parts, *total, *red;
+    uint8_t* kept;
+};
+// partial sums of threads: rows of the slice's channels (Share)
+__host__ __device__ constexpr int partial_sums(int vec, int slice)
 {
+    const int columns = slice / vec;
+    if (columns >= kNormThreads) return kNormThreads * vec;
+    const bool folds = columns < 32 && (columns & (columns - 1)) == 0;
+    return (folds ? kNormWarps : kNormThreads / columns) * slice;
+}
+__host__ __device__ constexpr size_t fixed_bytes(int vec, int slice, int cluster)
+{
+    return ((size_t)((3 + cluster) * slice + partial_sums(vec, slice)) * sizeof(float2) + 15) & ~(size_t)15;
+}
+template <int VEC>
+__device__ __forceinline__ Layout layout_of(uint8_t* raw, const NormArgs& a)
+{
+    Layout l;
+    l.channel = reinterpret_cast<float4*>(raw);
+    l.total = reinterpret_cast<float2*>(l.channel + a.slice);
+    l.parts = l.total + a.slice;
+    l.red = l.parts + a.cluster * a.slice;
+    l.kept = raw + fixed_bytes(VEC, a.slice, a.cluster);
+    return l;
+}
+
+// For every channel of the slice what its group says: number(channel, group, first channel to add, step to the next, sum over those
+// who add together) and then use(channel, the two numbers).  Small groups are added up by each of their channels, others by a warp.
+template <typename Number, typename Use>
+__device__ __forceinline__ void each_channel(const NormArgs& a, const Layout& l, Number number, Use use)
+{
+    if (a.per_group <= 8) {
+        for (int c = threadIdx.x; c < a.slice; c += kNormThreads) use(c, number(c, c / a.per_group, 0, 1, [](auto v) { return v; }));
+    } else {
+        for (int g = threadIdx.x >> 5; g < a.slice / a.per_group; g += kNormWarps) {
+            const int lane = threadIdx.x & 31;
+            const float2 v = number(g * a.per_group + lane, g, lane, 32, [](auto t) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+                for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+                return t;
+            });
+            for (int c = g * a.per_group + lane; c < (g + 1) * a.per_group; c += 32) use(c, v);
+        }
+    }
+    __syncthreads();
 }
 __device__ __forceinline__ float param(const void* p, int64_t at, int32_t dtype, float other)
 {
     return p ? bits_to_float(load_bits(p, at, dtype), dtype) : other;
 }
 
-// Shared memory of a block: sums of the slice's channels (own and all), two numbers for each of its groups, partial sums of
-// threads, a number for each channel, and the values that are kept.
-struct Layout {
-    float2 *part, *total, *group, *red;
-    float* first;
-    uint8_t* kept;
-};
-__host__ __device__ constexpr size_t fixed_bytes(int vec, int slice, int per_group)
-{
-    return ((size_t)(2 * slice + slice / per_group + kNormThreads * vec) * sizeof(float2) + (size_t)slice * sizeof(float) + 15) & ~(size_t)15;
-}
-template <int VEC>
-__device__ __forceinline__ Layout layout_of(uint8_t* raw, const NormArgs& a)
-{
-    Layout l;
-    l.part = reinterpret_cast<float2*>(raw);
-    l.total = l.part + a.slice;
-    l.group = l.total + a.slice;
-    l.red = l.group + a.slice / a.per_group;
-    l.first = reinterpret_cast<float*>(l.red + kNormThreads * VEC);
-    l.kept = raw + fixed_bytes(VEC, a.slice, a.per_group);
-    return l;
-}
-
+// One access of a thread from memory to its slot (an address in shared memory): copied past the registers, so that a thread
+// has many under way (a copy has 4 bytes at least).  Copies are committed and waited for in groups.
 template <typename T, int VEC>
-__device__ __forceinline__ void keep(uint8_t* kept, int slot, const Raw<T, VEC>& r)
+constexpr uint32_t kSlot = kNormThreads * Raw<T, VEC>::kBytes; // from one of a thread's slots to its next
+template <typename T, int VEC>
+__device__ __forceinline__ uint32_t slot_of(const uint8_t* kept, int slot)
+{
+    return smem_u32(kept) + slot * kSlot<T, VEC> + threadIdx.x * Raw<T, VEC>::kBytes;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void keep(uint32_t slot, const T* from)
 {
     constexpr int b = Raw<T, VEC>::kBytes;
-    uint8_t* p = kept + ((size_t)slot * kNormThreads + threadIdx.x) * b;
-    if constexpr (b == 16) *reinterpret_cast<uint4*>(p) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
-    else if constexpr (b == 8) *reinterpret_cast<uint2*>(p) = make_uint2(r.w[0], r.w[1]);
-    else if constexpr (b == 4) *reinterpret_cast<uint32_t*>(p) = r.w[0];
-    else *reinterpret_cast<unsigned short*>(p) = (unsigned short)r.w[0];
+    if constexpr (b == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot), "l"(from) : "memory");
+    else if constexpr (b >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(slot), "l"(from), "n"(b) : "memory");
+    else asm volatile("st.shared.u16 [%0], %1;" ::"r"(slot), "h"(*reinterpret_cast<const unsigned short*>(from)) : "memory");
+}
+__device__ __forceinline__ void keep_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void keep_wait(int group) // of kWaits that were committed
+{
+    if (group == 0) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+__device__ __forceinline__ int group_begin(int kept, int group) { return group == 0 ? 0 : group == 1 ? kept >> 1 : kept; }
+// All copies of a thread for a round, from pixel to pixel of its column
+template <typename T, int VEC>
+__device__ __forceinline__ void ask(uint32_t slot, const T* from, int64_t step, int begin, int end)
+{
+    from += begin * step;
+    slot += begin * kSlot<T, VEC>;
+#pragma unroll 4
+    for (int i = begin; i < end; ++i) {
+        keep<T, VEC>(slot, from);
+        slot += kSlot<T, VEC>;
+        from += step;
+    }
 }
 template <typename T, int VEC>
-__device__ __forceinline__ void kept_raw(Raw<T, VEC>& r, const uint8_t* kept, int slot)
+__device__ __forceinline__ void keep_raw(const Raw<T, VEC>& r, uint32_t slot) // VEC elements of 4 bytes or more
 {
-    load_raw(r, reinterpret_cast<const T*>(kept + ((size_t)slot * kNormThreads + threadIdx.x) * Raw<T, VEC>::kBytes));
+    constexpr int b = Raw<T, VEC>::kBytes;
+    if constexpr (b == 16) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(slot), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]) : "memory");
+    else asm volatile("st.shared.b32 [%0], %1;" ::"r"(slot), "r"(r.w[0]) : "memory");
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void kept_raw(Raw<T, VEC>& r, uint32_t slot)
+{
+    constexpr int b = Raw<T, VEC>::kBytes;
+    if constexpr (b == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "r"(slot) : "memory");
+    else if constexpr (b == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r.w[0]), "=r"(r.w[1]) : "r"(slot) : "memory");
+    else if constexpr (b == 4) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r.w[0]) : "r"(slot) : "memory");
+    else {
+        unsigned short h;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(slot) : "memory");
+        r.w[0] = h;
+    }
 }
 
 // ---------------------------------------------------------------------------------------- forward
 template <typename XT, typename YT, int VEC, int ACT>
-__device__ __forceinline__ void finish_forward(const NormArgs& a, const Share<VEC>& sh, const Layout& l, const XT* x, YT* y, int worker, int slice0)
+__device__ __forceinline__ void finish_forward(const NormArgs& a, const Share<VEC>& sh, const Layout& l, const XT* x, YT* y)
 {
+    constexpr int NP = (VEC + 1) / 2;
     for (int round = 0; round < sh.rounds; ++round) {
         if (!sh.active(round)) continue;
         const int c0 = sh.channel(round);
-        float m[VEC], scale[VEC], shift[VEC];
+        Pair m[NP], scale[NP], shift[NP]; // -mean, weight rstd, bias
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float2 st = l.group[(c0 + e) / a.per_group];
-            const int64_t at = (int64_t)worker * a.param_ld + slice0 + c0 + e;
-            m[e] = st.x;
-            scale[e] = st.y * param(a.weight, at, a.param_dtype, 1.f);
-            shift[e] = param(a.bias, at, a.param_dtype, 0.f);
+        for (int p = 0; p < NP; ++p) {
+            const float4 u = l.channel[c0 + 2 * p], v = VEC > 1 ? l.channel[c0 + 2 * p + 1] : u;
+            m[p] = pair_of(u.x, v.x);
+            scale[p] = pair_of(u.y, v.y);
+            shift[p] = pair_of(u.z, v.z);
         }
-        for (int i0 = 0; i0 < sh.steps; i0 += kAtOnce) {
-            Raw<XT, VEC> r[kAtOnce];
+        auto take = [&](const Raw<XT, VEC>& r, YT* to) {
+            Pair f[NP];
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                const int slot = round * sh.steps + i0 + j;
-                if (i0 + j < sh.steps && sh.pixel(i0 + j) < sh.end) {
-                    if (slot < a.kept) kept_raw(r[j], l.kept, slot);
-                    else load_raw(r[j], x + sh.pixel(i0 + j) * a.x.pixel + c0);
+            for (int p = 0; p < NP; ++p) {
+                f[p] = fma2(add2(raw_pair(r, p), m[p]), scale[p], shift[p]);
+                if constexpr (ACT != kNone) {
+                    const float2 z = floats_of(f[p]);
+                    f[p] = pair_of(act_of<ACT, sizeof(YT) == 2>(z.x), act_of<ACT, sizeof(YT) == 2>(z.y));
                 }
             }
+            store_pairs<YT, VEC>(to, f);
+        };
+        const int kept = sh.kept(a.kept, round);
+        const XT* from = x + sh.first * a.x.pixel + c0;
+        YT* to = y + sh.first * a.y.pixel + c0;
+        const int64_t from_step = sh.lanes * a.x.pixel, to_step = sh.lanes * a.y.pixel;
+        uint32_t slot = slot_of<XT, VEC>(l.kept, round * sh.steps);
+#pragma unroll 4
+        for (int i = 0; i < kept; ++i) {
+            Raw<XT, VEC> r;
+            kept_raw(r, slot);
+            take(r, to);
+            to += to_step;
+            slot += kSlot<XT, VEC>;
+        }
+        for (int i0 = kept; i0 < sh.mine; i0 += kAtOnce) {
+            Raw<XT, VEC> r[kAtOnce];
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                if (i0 + j >= sh.steps || sh.pixel(i0 + j) >= sh.end) continue;
-                float f[VEC];
+            for (int j = 0; j < kAtOnce; ++j)
+                if (i0 + j < sh.mine) load_raw(r[j], from + (i0 + j) * from_step);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) f[e] = act_of<ACT, sizeof(YT) == 2>(fmaf(raw_get(r[j], e) - m[e], scale[e], shift[e]));
-                store_vec<YT, VEC>(y + sh.pixel(i0 + j) * a.y.pixel + c0, f);
-            }
+            for (int j = 0; j < kAtOnce; ++j)
+                if (i0 + j < sh.mine) {
+                    take(r[j], to);
+                    to += to_step;
+                }
         }
     }
 }
 
 template <typename XT, typename YT, int VEC>
-__global__ void __launch_bounds__(kNormThreads) forward_kernel(NormArgs a)
+__global__ void __launch_bounds__(kNormThreads, kNormBlocks) forward_kernel(NormArgs a)
 {
+    constexpr int NP = (VEC + 1) / 2;
     extern __shared__ __align__(16) uint8_t raw[];
-    const uint32_t rank = blockIdx.x % (uint32_t)a.cluster, item = blockIdx.x / (uint32_t)a.cluster;
-    const int row = (int)(item / (uint32_t)a.slices), slice0 = (int)(item % (uint32_t)a.slices) * a.slice;
-    const int worker = row / a.images, image = row % a.images;
+    const uint32_t rank = cluster_rank();
+    const uint32_t item = cluster_at();                          // slices of an image run side by side: they share memory's rows
+    const int row = item / (uint32_t)a.slices, slice0 = item % (uint32_t)a.slices * a.slice, worker = row / (uint32_t)a.images, image = row % (uint32_t)a.images;
+    if (a.cluster > 1) cluster_arrive();
     const Share<VEC> sh(a, rank);
     const Layout l = layout_of<VEC>(raw, a);
     const XT* x = static_cast<const XT*>(a.x.data) + worker * a.x.worker + image * a.x.image + slice0;
     YT* y = static_cast<YT*>(a.y.data) + worker * a.y.worker + image * a.y.image + slice0;
     allow_next_kernel();
     wait_for_previous_kernel();
+    if (a.cluster > 1) cluster_wait();                           // all blocks are there: they write to each other
+    auto ask_round = [&](int round) {
+        const int kept = sh.active(round) ? sh.kept(a.kept, round) : 0;
+        const XT* from = x + sh.first * a.x.pixel + sh.channel(round);
+        for (int g = 0; g < kWaits; ++g) {
+            ask<XT, VEC>(slot_of<XT, VEC>(l.kept, round * sh.steps), from, sh.lanes * a.x.pixel, group_begin(kept, g), group_begin(kept, g + 1));
+            keep_commit();
+        }
+    };
     // Sums of x - p and (x - p)^2 with p the channel's value at the image's first pixel: float32 loses nothing where
     // the mean is far from zero
     for (int round = 0; round < sh.rounds; ++round) {
-        float s1[VEC], s2[VEC], p[VEC];
+        ask_round(round);
+        if (round == 0)
+            for (int c = threadIdx.x; c < a.slice; c += kNormThreads) {
+                const int64_t at = (int64_t)worker * a.param_ld + slice0 + c;
+                l.channel[c].y = param(a.weight, at, a.param_dtype, 1.f);
+                l.channel[c].z = param(a.bias, at, a.param_dtype, 0.f);
+            }
+        Pair s1[NP], s2[NP], pivot[NP];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) s1[e] = s2[e] = 0.f;
+        for (int p = 0; p < NP; ++p) s1[p] = s2[p] = pair_of(0.f, 0.f);
         if (sh.active(round)) {
-            const int c0 = sh.channel(round);
+            const int c0 = sh.channel(round), kept = sh.kept(a.kept, round);
+            const XT* from = x + sh.first * a.x.pixel + c0;
+            const int64_t from_step = sh.lanes * a.x.pixel;
             Raw<XT, VEC> first;
             load_raw(first, x + c0);
-            for (int i0 = 0; i0 < sh.steps; i0 += kAtOnce) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const float2 v = floats_of(raw_pair(first, p));
+                pivot[p] = pair_of(-v.x, -v.y);
+                if (sh.lane == 0) {
+                    l.channel[c0 + 2 * p].w = v.x;
+                    if (VEC > 1) l.channel[c0 + 2 * p + 1].w = v.y;
+                }
+            }
+            auto take = [&](const Raw<XT, VEC>& r) {
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const Pair d = add2(raw_pair(r, p), pivot[p]);
+                    s1[p] = add2(s1[p], d);
+                    s2[p] = fma2(d, d, s2[p]);
+                }
+            };
+            uint32_t slot = slot_of<XT, VEC>(l.kept, round * sh.steps);
+#pragma unroll 1
+            for (int g = 0; g < kWaits; ++g) {
+                keep_wait(g);
+                const int end = group_begin(kept, g + 1);
+#pragma unroll 4
+                for (int i = group_begin(kept, g); i < end; ++i) {
+                    Raw<XT, VEC> r;
+                    kept_raw(r, slot);
+                    take(r);
+                    slot += kSlot<XT, VEC>;
+                }
+            }
+            for (int i0 = kept; i0 < sh.mine; i0 += kAtOnce) {
                 Raw<XT, VEC> r[kAtOnce];
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j)
-                    if (i0 + j < sh.steps && sh.pixel(i0 + j) < sh.end) load_raw(r[j], x + sh.pixel(i0 + j) * a.x.pixel + c0);
-                if (i0 == 0) {
+                    if (i0 + j < sh.mine) load_raw(r[j], from + (i0 + j) * from_step);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        p[e] = raw_get(first, e);
-                        if (sh.lane == 0) l.first[c0 + e] = p[e];
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) {
-                    if (i0 + j >= sh.steps || sh.pixel(i0 + j) >= sh.end) continue;
-                    const int slot = round * sh.steps + i0 + j;
-                    if (slot < a.kept) keep(l.kept, slot, r[j]);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float d = raw_get(r[j], e) - p[e];
-                        s1[e] += d;
-                        s2[e] = fmaf(d, d, s2[e]);
-                    }
-                }
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (i0 + j < sh.mine) take(r[j]);
             }
         }
-        add_up(sh, a, round, s1, s2, l.red, l.part);
+        add_up(sh, a, round, s1, s2, l.red, l.parts, cluster_rank());
     }
-    exchange(a, l.part, l.total);
-    // groups: a warp each; the sums of x and x^2 in float64, which bears the difference of the two
-    const double count = (double)a.pixels, inverse = 1.0 / (count * a.per_group);
-    for (int g = threadIdx.x >> 5; g < a.slice / a.per_group; g += kNormWarps) {
+    exchange(a, l.parts, l.total);
+    // the sums of x and x^2 of a group in float64, which bears the difference of the two
+    const double count = (double)a.pixels;
+    each_channel(a, l, [&](int c, int g, int from, int step, auto sum) {
         double t1 = 0.0, t2 = 0.0;
-        for (int c = threadIdx.x & 31; c < a.per_group; c += 32) {
-            const float2 v = l.total[g * a.per_group + c];
-            const double p = (double)l.first[g * a.per_group + c];
-            t1 += fma(count, p, (double)v.x);
-            t2 += (double)v.y + p * fma(count, p, 2.0 * (double)v.x);
+        for (int k = g * a.per_group + from; k < (g + 1) * a.per_group; k += step) {
+            const float2 v = l.total[k];
+            const double p = (double)l.channel[k].w, s = (double)v.x, n = count * p;
+            t1 += n + s;
+            t2 = fma(p, n + 2.0 * s, t2) + (double)v.y;
         }
-        t1 = warp_add(t1) * inverse;
-        t2 = warp_add(t2) * inverse;
-        const double var = t2 - t1 * t1;
-        const float2 st = make_float2((float)t1, (float)(1.0 / sqrt((var > 0.0 || var != var ? var : 0.0) + a.eps)));
-        if ((threadIdx.x & 31) == 0) {
-            l.group[g] = st;
+        t1 = sum(t1) * a.inverse;
+        t2 = sum(t2) * a.inverse;
+        const double var = fma(-t1, t1, t2);
+        const float2 st = make_float2((float)t1, 1.f / sqrtf((float)((var > 0.0 || var != var ? var : 0.0) + a.eps)));
+        if (rank == 0 && c == g * a.per_group) {
             const int64_t at = (int64_t)row * a.groups + slice0 / a.per_group + g;
-            if (rank == 0 && a.mean) a.mean[at] = st.x;
-            if (rank == 0 && a.rstd) a.rstd[at] = st.y;
+            if (a.mean) a.mean[at] = st.x;
+            if (a.rstd) a.rstd[at] = st.y;
         }
-    }
-    __syncthreads();
+        return st;
+    }, [&](int c, float2 st) {
+        l.channel[c].x = -st.x;
+        l.channel[c].y *= st.y;
+    });
     switch (a.activation) {
-    case kRelu: finish_forward<XT, YT, VEC, kRelu>(a, sh, l, x, y, worker, slice0); break;
-    case kSilu: finish_forward<XT, YT, VEC, kSilu>(a, sh, l, x, y, worker, slice0); break;
-    case kGelu: finish_forward<XT, YT, VEC, kGelu>(a, sh, l, x, y, worker, slice0); break;
-    default: finish_forward<XT, YT, VEC, kNone>(a, sh, l, x, y, worker, slice0); break;
-    }
-    if (a.cluster > 1) {
-        __syncwarp();
-        cluster_wait();
+    case kRelu: finish_forward<XT, YT, VEC, kRelu>(a, sh, l, x, y); break;
+    case kSilu: finish_forward<XT, YT, VEC, kSilu>(a, sh, l, x, y); break;
+    case kGelu: finish_forward<XT, YT, VEC, kGelu>(a, sh, l, x, y); break;
+    default: finish_forward<XT, YT, VEC, kNone>(a, sh, l, x, y); break;
     }
 }
 
 // ---------------------------------------------------------------------------------------- backward
-// Of a channel, in the registers of the threads that have it.  relu's slope is 1 where x is past `border` on the side that the sign of
-// the scale says: the border is formed in float64 and rounded so that float32 values compare with it as with the exact
-// one, which no z near 0 in float32 does.
-struct Channel {
-    float mean, scale, shift;           // z = (x - mean) scale + shift
-    float border;
-    uint32_t flip;                      // sign bit where x has to be below
-};
-__device__ __forceinline__ Channel channel_of(const NormArgs& a, float2 st, int64_t at)
+// What the first pass wants of a channel: -mean, weight rstd, bias or (relu) a border, rstd with the sign that goes with it.  relu's slope
+// is 1 where x is past the border on the side that the sign of weight rstd says, x ^ sign > border.  The border is formed in float64
+// and rounded down, so that values of float32 compare with it as with the number itself, which no z near 0 in float32 does.
+__device__ __forceinline__ float4 channel_of(const NormArgs& a, float2 st, int64_t at)
 {
     const float w = param(a.weight, at, a.param_dtype, 1.f), b = param(a.bias, at, a.param_dtype, 0.f);
-    Channel ch;
-    ch.mean = st.x;
-    ch.scale = st.y * w;
-    ch.shift = b;
-    ch.border = __int_as_float(0x7f800000);
-    ch.flip = 0;
-    if (a.activation == kRelu) {
-        const double slope = (double)st.y * (double)w;
-        if (slope == 0.0) {
-            if (b > 0.f) ch.border = __int_as_float(0xff800000);
-        } else {
-            // x > edge, or -x > -edge
-            double edge = (double)st.x - (double)b / slope;
-            if (slope < 0.0) {
-                edge = -edge;
-                ch.flip = 0x80000000u;
+    if (a.activation != kRelu) return make_float4(-st.x, st.y * w, b, st.y);
+    const double slope = (double)st.y * (double)w;
+    double edge = (double)st.x - (double)b / slope;
+    float border = __double2float_rd(slope < 0.0 ? -edge : edge);
+    if (slope == 0.0) border = __int_as_float(b > 0.f ? 0xff800000 : 0x7f800000); // all or none
+    return make_float4(-st.x, st.y * w, border, slope < 0.0 ? -st.y : st.y);
+}
+
+// dz of a thread's channels at a pixel
+template <typename XT, typename YT, int VEC, int ACT>
+struct Slopes {
+    static constexpr int NP = (VEC + 1) / 2;
+    [[maybe_unused]] static constexpr bool kFast = sizeof(XT) == 2 && sizeof(YT) == 2;
+    static constexpr bool kPacked = ACT == kRelu && sizeof(XT) == 2 && std::is_same_v<XT, YT> && VEC > 1;
+    Pair mean[NP], scale[NP], shift[NP];
+    uint32_t border[kPacked ? NP : 1], sign[kPacked ? NP : 2 * NP];
+
+    __device__ void load(const float4* channel)
+    {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const float4 u = channel[2 * p], v = VEC > 1 ? channel[2 * p + 1] : u;
+            mean[p] = pair_of(u.x, v.x);
+            scale[p] = pair_of(u.y, v.y);
+            shift[p] = pair_of(u.z, v.z);
+            if constexpr (kPacked) {
+                // past a border of float32 is past the next lower one of the 16-bit type, for its values
+                XT lo, hi;
+                if constexpr (std::is_same_v<XT, __half>) { lo = __float2half_rd(u.z); hi = __float2half_rd(v.z); }
+                else { lo = __float2bfloat16_rd(u.z); hi = __float2bfloat16_rd(v.z); }
+                border[p] = (uint32_t) * reinterpret_cast<unsigned short*>(&lo) | (uint32_t) * reinterpret_cast<unsigned short*>(&hi) << 16;
+                sign[p] = (__float_as_uint(u.w) >> 16 & 0x8000u) | (__float_as_uint(v.w) & 0x80000000u);
+            } else {
+                sign[2 * p] = __float_as_uint(u.w) & 0x80000000u;
+                sign[2 * p + 1] = __float_as_uint(v.w) & 0x80000000u;
             }
-            ch.border = __double2float_rd(edge);
         }
     }
-    return ch;
-}
-template <int ACT, bool FAST>
-__device__ __forceinline__ float dz_of(const Channel& ch, float x, float dy)
+    // relu, 16 bits: dy where the slope is 1, in its own type
+    __device__ __forceinline__ void mask(const Raw<XT, VEC>& rx, Raw<YT, VEC>& ry) const
+    {
+        if constexpr (kPacked) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const uint32_t turned = rx.w[p] ^ sign[p];
+                uint32_t past;
+                if constexpr (std::is_same_v<XT, __half>)
+                    past = __hgt2_mask(*reinterpret_cast<const __half2*>(&turned), *reinterpret_cast<const __half2*>(&border[p]));
+                else past = __hgt2_mask(*reinterpret_cast<const __nv_bfloat162*>(&turned), *reinterpret_cast<const __nv_bfloat162*>(&border[p]));
+                ry.w[p] &= past;
+            }
+        }
+    }
+    __device__ __forceinline__ Pair dz(const Raw<XT, VEC>& rx, const Raw<YT, VEC>& ry, int p, Pair x) const
+    {
+        if constexpr (kPacked) {
+            return raw_pair(ry, p);                              // (masked before)
+        } else if constexpr (ACT == kRelu) {
+            const float2 dy = floats_of(raw_pair(ry, p)), v = floats_of(x), edge = floats_of(shift[p]);
+            return pair_of(__uint_as_float(__float_as_uint(v.x) ^ sign[2 * p]) > edge.x ? dy.x : 0.f,
+                           __uint_as_float(__float_as_uint(v.y) ^ sign[2 * p + 1]) > edge.y ? dy.y : 0.f);
+        } else if constexpr (ACT == kNone) {
+            return raw_pair(ry, p);
+        } else {
+            const float2 z = floats_of(fma2(add2(x, mean[p]), scale[p], shift[p])), dy = floats_of(raw_pair(ry, p));
+            return pair_of(dy.x * slope_of<ACT, kFast>(z.x), dy.y * slope_of<ACT, kFast>(z.y));
+        }
+    }
+};
+
+template <typename XT, typename YT, int VEC>
+__device__ __forceinline__ void ask_both(const NormArgs& a, const Share<VEC>& sh, const Layout& l, const XT* x, const YT* dy, int round)
 {
-    if constexpr (ACT == kRelu) return __uint_as_float(__float_as_uint(x) ^ ch.flip) > ch.border ? dy : 0.f;
-    else if constexpr (ACT == kNone) return dy;
-    else return dy * slope_of<ACT, FAST>(fmaf(x - ch.mean, ch.scale, ch.shift));
+    const int kept = sh.active(round) ? sh.kept(a.kept, round) : 0;
+    const uint32_t slot_x = slot_of<XT, VEC>(l.kept, round * sh.steps);
+    const uint32_t slot_y = slot_of<YT, VEC>(l.kept + (size_t)a.kept * kSlot<XT, VEC>, round * sh.steps);
+    const XT* from_x = x + sh.first * a.x.pixel + sh.channel(round);
+    const YT* from_y = dy + sh.first * a.y.pixel + sh.channel(round);
+    for (int g = 0; g < kWaits; ++g) {
+        ask<XT, VEC>(slot_x, from_x, sh.lanes * a.x.pixel, group_begin(kept, g), group_begin(kept, g + 1));
+        ask<YT, VEC>(slot_y, from_y, sh.lanes * a.y.pixel, group_begin(kept, g), group_begin(kept, g + 1));
+        keep_commit();
+    }
 }
 
 // Both passes over a block's share: sums of dz and dz (x - mean) by channel, or dx.
 template <typename XT, typename YT, int VEC, int ACT, bool FINISH>
-__device__ __forceinline__ void backward_pass(const NormArgs& a, const Share<VEC>& sh, const Layout& l, const XT* x, const YT* dy, XT* dx,
-                                              int row, int worker, int slice0)
+__device__ __forceinline__ void backward_pass(const NormArgs& a, const Share<VEC>& sh, const Layout& l, const XT* x, const YT* dy, XT* dx)
 {
-    constexpr bool kFast = sizeof(XT) == 2 && sizeof(YT) == 2;
-    uint8_t* kept_dy = l.kept + (size_t)a.kept * kNormThreads * Raw<XT, VEC>::kBytes;
+    constexpr int NP = (VEC + 1) / 2;
+    constexpr bool kFolds = sizeof(XT) == 2;
+    const uint8_t* kept_dy = l.kept + (size_t)a.kept * kSlot<XT, VEC>;
     for (int round = 0; round < sh.rounds; ++round) {
-        float s1[VEC], s2[VEC];
+        if (!FINISH && round > 0) ask_both<XT, YT, VEC>(a, sh, l, x, dy, round); // (the first round's are under way)
+        Pair s1[NP], s2[NP];    // (of the second pass: what is added to weight rstd dz, -k1 - (x - mean) k2)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) s1[e] = s2[e] = 0.f;
+        for (int p = 0; p < NP; ++p) s1[p] = s2[p] = pair_of(0.f, 0.f);
         if (sh.active(round)) {
-            const int c0 = sh.channel(round);
-            Channel ch[VEC];
-            float k1[VEC], k2[VEC];
+            const int c0 = sh.channel(round), kept = sh.kept(a.kept, round), slot0 = round * sh.steps;
+            const XT* from_x = x + sh.first * a.x.pixel + c0;
+            const YT* from_y = dy + sh.first * a.y.pixel + c0;
+            const int64_t step_x = sh.lanes * a.x.pixel, step_y = sh.lanes * a.y.pixel, step_to = sh.lanes * a.dx.pixel;
+            XT* to = FINISH ? dx + sh.first * a.dx.pixel + c0 : nullptr;
+            Slopes<XT, YT, VEC, ACT> sl;
+            sl.load(l.channel + c0);
+            if (FINISH) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const int g = (c0 + e) / a.per_group;
-                const int64_t at = (int64_t)row * a.groups + slice0 / a.per_group + g;
-                const float2 st = make_float2(a.mean[at], a.rstd[at]);
-                ch[e] = channel_of(a, st, (int64_t)worker * a.param_ld + slice0 + c0 + e);
-                if (FINISH) {
-                    k1[e] = l.group[g].x;
-                    k2[e] = l.group[g].y;
+                for (int p = 0; p < NP; ++p) {
+                    const float2 u = l.parts[c0 + 2 * p], v = VEC > 1 ? l.parts[c0 + 2 * p + 1] : u;
+                    s1[p] = pair_of(u.x, v.x);
+                    s2[p] = pair_of(u.y, v.y);
+                    // values of 16 bits lose nothing where x - mean is multiplied out: x k2 + (mean k2 + k1)
+                    if constexpr (kFolds) s1[p] = fma2(sl.mean[p], s2[p], s1[p]);
                 }
             }
-            for (int i0 = 0; i0 < sh.steps; i0 += kAtOnce) {
+            auto take = [&](const Raw<XT, VEC>& rx, const Raw<YT, VEC>& ry) {
+                Pair f[NP];
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const Pair xp = raw_pair(rx, p), dz = sl.dz(rx, ry, p, xp);
+                    if (FINISH) {
+                        f[p] = fma2(dz, sl.scale[p], fma2(kFolds ? xp : add2(xp, sl.mean[p]), s2[p], s1[p]));
+                    } else {
+                        s1[p] = add2(s1[p], dz);
+                        s2[p] = fma2(dz, add2(xp, sl.mean[p]), s2[p]);
+                    }
+                }
+                if (FINISH) {
+                    store_pairs<XT, VEC>(to, f);
+                    to += step_to;
+                }
+            };
+            uint32_t slot_x = slot_of<XT, VEC>(l.kept, slot0), slot_y = slot_of<YT, VEC>(kept_dy, slot0);
+#pragma unroll 1
+            for (int g = 0; g < kWaits; ++g) {
+                if (!FINISH) keep_wait(g);
+                const int end = group_begin(kept, g + 1);
+#pragma unroll 2
+                for (int i = group_begin(kept, g); i < end; ++i) {
+                    Raw<XT, VEC> rx;
+                    Raw<YT, VEC> ry;
+                    kept_raw(rx, slot_x);
+                    kept_raw(ry, slot_y);
+                    if constexpr (!FINISH && Slopes<XT, YT, VEC, ACT>::kPacked) {
+                        sl.mask(rx, ry);
+                        keep_raw(ry, slot_y);                    // for the second pass
+                    }
+                    take(rx, ry);
+                    slot_x += kSlot<XT, VEC>;
+                    slot_y += kSlot<YT, VEC>;
+                }
+            }
+            for (int i0 = kept; i0 < sh.mine; i0 += kAtOnce) {
                 Raw<XT, VEC> rx[kAtOnce];
                 Raw<YT, VEC> ry[kAtOnce];
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) {
-                    const int slot = round * sh.steps + i0 + j;
-                    if (i0 + j < sh.steps && sh.pixel(i0 + j) < sh.end) {
-                        if (FINISH && slot < a.kept) {
-                            kept_raw(rx[j], l.kept, slot);
-                            kept_raw(ry[j], kept_dy, slot);
-                        } else {
-                            load_raw(rx[j], x + sh.pixel(i0 + j) * a.x.pixel + c0);
-                            load_raw(ry[j], dy + sh.pixel(i0 + j) * a.y.pixel + c0);
-                        }
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (i0 + j < sh.mine) {
+                        load_raw(rx[j], from_x + (i0 + j) * step_x);
+                        load_raw(ry[j], from_y + (i0 + j) * step_y);
                     }
-                }
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) {
-                    if (i0 + j >= sh.steps || sh.pixel(i0 + j) >= sh.end) continue;
-                    const int slot = round * sh.steps + i0 + j;
-                    if (!FINISH && slot < a.kept) {
-                        keep(l.kept, slot, rx[j]);
-                        keep(kept_dy, slot, ry[j]);
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (i0 + j < sh.mine) {
+                        sl.mask(rx[j], ry[j]);
+                        take(rx[j], ry[j]);
                     }
-                    float f[VEC];
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float xe = raw_get(rx[j], e), dz = dz_of<ACT, kFast>(ch[e], xe, raw_get(ry[j], e)), d = xe - ch[e].mean;
-                        if (FINISH) {
-                            f[e] = fmaf(dz, ch[e].scale, -fmaf(d, k2[e], k1[e]));
-                        } else {
-                            s1[e] += dz;
-                            s2[e] = fmaf(dz, d, s2[e]);
-                        }
-                    }
-                    if (FINISH) store_vec<XT, VEC>(dx + sh.pixel(i0 + j) * a.dx.pixel + c0, f);
-                }
             }
         }
-        if (!FINISH) add_up(sh, a, round, s1, s2, l.red, l.part);
+        if (!FINISH) add_up(sh, a, round, s1, s2, l.red, l.parts, cluster_rank());
     }
 }
 
 template <typename XT, typename YT, int VEC, bool FINISH>
-__device__ __forceinline__ void backward_pass_act(const NormArgs& a, const Share<VEC>& sh, const Layout& l, const XT* x, const YT* dy, XT* dx,
-                                                  int row, int worker, int slice0)
+__device__ __forceinline__ void backward_pass_act(const NormArgs& a, const Share<VEC>& sh, const Layout& l, const XT* x, const YT* dy, XT* dx)
 {
     switch (a.activation) {
-    case kRelu: backward_pass<XT, YT, VEC, kRelu, FINISH>(a, sh, l, x, dy, dx, row, worker, slice0); break;
-    case kSilu: backward_pass<XT, YT, VEC, kSilu, FINISH>(a, sh, l, x, dy, dx, row, worker, slice0); break;
-    case kGelu: backward_pass<XT, YT, VEC, kGelu, FINISH>(a, sh, l, x, dy, dx, row, worker, slice0); break;
-    default: backward_pass<XT, YT, VEC, kNone, FINISH>(a, sh, l, x, dy, dx, row, worker, slice0); break;
+    case kRelu: backward_pass<XT, YT, VEC, kRelu, FINISH>(a, sh, l, x, dy, dx); break;
+    case kSilu: backward_pass<XT, YT, VEC, kSilu, FINISH>(a, sh, l, x, dy, dx); break;
+    case kGelu: backward_pass<XT, YT, VEC, kGelu, FINISH>(a, sh, l, x, dy, dx); break;
+    default: backward_pass<XT, YT, VEC, kNone, FINISH>(a, sh, l, x, dy, dx); break;
     }
 }
 
 template <typename XT, typename YT, int VEC>
-__global__ void __launch_bounds__(kNormThreads) backward_kernel(NormArgs a)
+__global__ void __launch_bounds__(kNormThreads, kNormBlocks) backward_kernel(NormArgs a)
 {
     extern __shared__ __align__(16) uint8_t raw[];
-    const uint32_t rank = blockIdx.x % (uint32_t)a.cluster, item = blockIdx.x / (uint32_t)a.cluster;
-    const int row = (int)(item / (uint32_t)a.slices), slice0 = (int)(item % (uint32_t)a.slices) * a.slice;
-    const int worker = row / a.images, image = row % a.images;
+    const uint32_t rank = cluster_rank();
+    const uint32_t item = cluster_at();                          // slices of an image run side by side: they share memory's rows
+    const int row = item / (uint32_t)a.slices, slice0 = item % (uint32_t)a.slices * a.slice, worker = row / (uint32_t)a.images, image = row % (uint32_t)a.images;
+    if (a.cluster > 1) cluster_arrive();
     const Share<VEC> sh(a, rank);
     const Layout l = layout_of<VEC>(raw, a);
     const XT* x = static_cast<const XT*>(a.x.data) + worker * a.x.worker + image * a.x.image + slice0;
@@ -492,39 +735,41 @@ __global__ void __launch_bounds__(kNormThreads) backward_kernel(NormArgs a)
     XT* dx = a.dx.data ? static_cast<XT*>(a.dx.data) + worker * a.dx.worker + image * a.dx.image + slice0 : nullptr;
     allow_next_kernel();
     wait_for_previous_kernel();
-    backward_pass_act<XT, YT, VEC, false>(a, sh, l, x, dy, dx, row, worker, slice0);
-    exchange(a, l.part, l.total);
-    if (rank == 0 && a.sums)
-        for (int c = threadIdx.x; c < a.slice; c += kNormThreads) {
-            const float r = a.rstd[(int64_t)row * a.groups + (slice0 + c) / a.per_group];
-            a.sums[(int64_t)row * a.channels + slice0 + c] = make_float2(l.total[c].x, l.total[c].y * r);
-        }
-    if (dx) {
-        // dx = scale dz - (k1 + (x - mean) k2):  k1 = rstd mean(w dz), k2 = rstd^3 mean(w dz (x - mean))
-        const double inverse = 1.0 / ((double)a.pixels * a.per_group);
-        for (int g = threadIdx.x >> 5; g < a.slice / a.per_group; g += kNormWarps) {
-            double t1 = 0.0, t2 = 0.0;
-            for (int c = threadIdx.x & 31; c < a.per_group; c += 32) {
-                const float2 v = l.total[g * a.per_group + c];
-                const double w = (double)param(a.weight, (int64_t)worker * a.param_ld + slice0 + g * a.per_group + c, a.param_dtype, 1.f);
-                t1 += w * (double)v.x;
-                t2 += w * (double)v.y;
-            }
-            const double r = (double)a.rstd[(int64_t)row * a.groups + slice0 / a.per_group + g];
-            t1 = warp_add(t1) * inverse * r;
-            t2 = warp_add(t2) * inverse * r * r * r;
-            if ((threadIdx.x & 31) == 0) l.group[g] = make_float2((float)t1, (float)t2);
-        }
-        __syncthreads();
-        backward_pass_act<XT, YT, VEC, true>(a, sh, l, x, dy, dx, row, worker, slice0);
+    if (a.cluster > 1) cluster_wait();                           // all blocks are there: they write to each other
+    ask_both<XT, YT, VEC>(a, sh, l, x, dy, 0);
+    const int64_t stats = (int64_t)row * a.groups + slice0 / a.per_group;
+    for (int c = threadIdx.x; c < a.slice; c += kNormThreads) {
+        const int g = c / a.per_group;
+        l.channel[c] = channel_of(a, make_float2(a.mean[stats + g], a.rstd[stats + g]), (int64_t)worker * a.param_ld + slice0 + c);
     }
-    if (a.cluster > 1) {
-        __syncwarp();
-        cluster_wait();
+    __syncthreads();
+    backward_pass_act<XT, YT, VEC, false>(a, sh, l, x, dy, dx);
+    exchange(a, l.parts, l.total);
+    if (rank == 0 && a.sums)
+        for (int c = threadIdx.x; c < a.slice; c += kNormThreads)
+            a.sums[(int64_t)row * a.channels + slice0 + c] = make_float2(l.total[c].x, l.total[c].y * fabsf(l.channel[c].w));
+    if (dx) {
+        // dx = weight rstd dz - k1 - (x - mean) k2:  k1 = mean(weight rstd dz), k2 = rstd^2 mean(weight rstd dz (x - mean))
+        const float inverse = (float)a.inverse;
+        each_channel(a, l, [&](int c, int g, int from, int step, auto sum) {
+            float t1 = 0.f, t2 = 0.f;
+            for (int k = g * a.per_group + from; k < (g + 1) * a.per_group; k += step) {
+                const float2 v = l.total[k];
+                const float scale = l.channel[k].y;
+                t1 = fmaf(scale, v.x, t1);
+                t2 = fmaf(scale, v.y, t2);
+            }
+            return make_float2(-sum(t1) * inverse, -sum(t2) * inverse);
+        }, [&](int c, float2 k) {
+            const float r = l.channel[c].w;
+            l.parts[c] = make_float2(k.x, k.y * r * r);  // (the blocks' sums are done with)
+        });
+        backward_pass_act<XT, YT, VEC, true>(a, sh, l, x, dy, dx);
     }
 }
 
 // dw and db: sums over a worker's images, in float64.  A block has 32 channels of a worker, its warps every eighth image.
+constexpr int kGradThreads = 256;
 struct GradArgs {
     const float2* sums;
     void* dweight;
@@ -533,9 +778,9 @@ struct GradArgs {
     int32_t images, channels, blocks;   // blocks to a worker
     int32_t grad_dtype, accumulate;
 };
-__global__ void __launch_bounds__(kNormThreads) grad_kernel(GradArgs a)
+__global__ void __launch_bounds__(kGradThreads) grad_kernel(GradArgs a)
 {
-    __shared__ double2 part[kNormWarps][32];
+    __shared__ double2 part[kGradThreads / 32][32];
     const int worker = blockIdx.x / (uint32_t)a.blocks, c = (int)(blockIdx.x % (uint32_t)a.blocks) * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
     allow_next_kernel();
     wait_for_previous_kernel();
@@ -543,7 +788,7 @@ __global__ void __launch_bounds__(kNormThreads) grad_kernel(GradArgs a)
     if (c < a.channels) {
         const float2* s = a.sums + (int64_t)worker * a.images * a.channels + c;
 #pragma unroll 4
-        for (int b = warp; b < a.images; b += kNormWarps) {
+        for (int b = warp; b < a.images; b += kGradThreads / 32) {
             const float2 w = s[(int64_t)b * a.channels];
             v.x += (double)w.x;
             v.y += (double)w.y;
@@ -555,7 +800,7 @@ __global__ void __launch_bounds__(kNormThreads) grad_kernel(GradArgs a)
     void* out = warp ? a.dweight : a.dbias; // one warp to each
     if (!out) return;
     double t = 0.0;
-    for (int k = 0; k < kNormWarps; ++k) t += warp ? part[k][threadIdx.x & 31].y : part[k][threadIdx.x & 31].x;
+    for (int k = 0; k < kGradThreads / 32; ++k) t += warp ? part[k][threadIdx.x & 31].y : part[k][threadIdx.x & 31].x;
     const int64_t at = (int64_t)worker * a.grad_ld + c;
     if (a.accumulate) t += (double)bits_to_float(load_bits(out, at, a.grad_dtype), a.grad_dtype);
     store_from_float(out, at, a.grad_dtype, (float)t);
@@ -588,6 +833,11 @@ NormKernel kernel_of(bool backward, int32_t x, int32_t y, int vec)
 }
 
 constexpr int kMostShared = 227 * 1024;
+// Kept bytes of a block, at most where a cluster can be larger: three and four blocks to an SM, so that some read while others add up or
+// write.  (us, forward 2 x 64 images of 112 x 112 x 64 bf16 / 8 x 128 of 32 x 32 x 16 f32: 50 KiB 116 / 37.7, 72 KiB 116 / 30.5, 100 KiB with 256 threads
+// 112 / 33.4; backward 2 x 64 of 56 x 56 x 256 bf16 / 4 x 32 of 7 x 7 x 2048 f16: 34 KiB 205 / 66, 50 KiB 190 / 60, 72 KiB 197 / 62.)  And at least
+// where few images ask for more blocks.
+constexpr int64_t kShareForward = 72 * 1024, kShareBackward = 50 * 1024, kLeast = 32 * 1024;
 constexpr int64_t kMostSize = (int64_t)1 << 40; // elements that strides may span
 
 } // namespace
@@ -669,44 +919,46 @@ int64_t gcd(int64_t a, int64_t b) { return b ? gcd(b, a % b) : a; }
 
 // How a call is cut: channels of a slice, blocks of a cluster, pixels that a thread keeps.
 struct Cut {
-    int vec, slice, cluster, kept;
+    int vec, slice, cluster, share, rounds, lanes, steps, kept;
     size_t shared;
 };
 // A slice is a whole number of groups and of accesses.
-Cut cut_of(const choco_group_norm_params& p, int64_t images, int64_t pixels, int vec, int64_t bytes /* kept of an element */)
+Cut cut_of(const choco_group_norm_params& p, int64_t images, int64_t pixels, int vec, int64_t es /* bytes of an element of x */, int64_t bytes /* kept of one */, int64_t most)
 {
     const int64_t per = p.channels / p.groups, unit = per / gcd(per, vec) * vec, rows = p.n * images;
     Cut best = {};
     best.vec = vec;
-    // long rows of pixels first, halved while more than eight blocks of 96 KiB would be needed and rows stay at 64 bytes
-    int64_t count = p.channels / unit; // units of a slice: a divisor of this
-    auto fits = [&](int64_t c) { return c * unit <= kMostSlice && c * unit * bytes * pixels <= (int64_t)8 * 96 * 1024; };
+    // The widest slice whose image one block keeps within `most`; if none is, rows of 64 bytes at least and a cluster.
+    const int64_t count = p.channels / unit; // slices are whole parts of it
+    auto part_below = [&](int64_t u) {       // the next smaller part
+        for (--u; u > 1 && count % u;) --u;
+        return u;
+    };
     int64_t units = count;
-    while (units > 1 && !fits(units)) {
-        int64_t next = units - 1;
-        while (count % next) --next;
-        if (units * unit <= kMostSlice && next * unit * bytes < 64) break;
-        units = next;
-    }
+    while (units > 1 && (units * unit > kMostSlice || (units * unit * bytes * pixels > most && part_below(units) * unit * es >= 64))) units = part_below(units);
     best.slice = (int)(units * unit);
     const int64_t slices = p.channels / best.slice, total = best.slice * bytes * pixels;
-    // blocks: enough for 96 KiB each, and for all SMs where there are few rows (but no share below 16 KiB)
+    // blocks: enough for `most` each, and for all SMs where there are few rows (but no share below kLeast)
     int cluster = 1;
-    while (cluster < 8 && (total > (int64_t)cluster * 96 * 1024 || (rows * slices * cluster < 296 && total > (int64_t)cluster * 32 * 1024))) cluster *= 2;
+    while (cluster < 8 && (total > cluster * most || (rows * slices * cluster < 296 && total > cluster * kLeast))) cluster *= 2;
     if (cluster > pixels) cluster = (int)pixels;
     best.cluster = cluster;
-    const int columns = best.slice / vec, rounds = (columns + kNormThreads - 1) / kNormThreads, lanes = rounds > 1 ? 1 : kNormThreads / columns;
-    const int64_t share = (pixels + cluster - 1) / cluster, steps = rounds * ((share + lanes - 1) / lanes);
-    const size_t fixed = fixed_bytes(vec, best.slice, (int)per), each = (size_t)kNormThreads * vec * bytes;
+    const int columns = best.slice / vec;
+    best.rounds = (columns + kNormThreads - 1) / kNormThreads;
+    best.lanes = best.rounds > 1 ? 1 : kNormThreads / columns;
+    best.share = (int)((pixels + cluster - 1) / cluster);
+    best.steps = (best.share + best.lanes - 1) / best.lanes;
+    const int64_t steps = (int64_t)best.rounds * best.steps;
+    const size_t fixed = fixed_bytes(vec, best.slice, cluster), each = (size_t)kNormThreads * vec * bytes;
     best.kept = (int)std::min<int64_t>(steps, ((int64_t)kMostShared - (int64_t)fixed) / (int64_t)each);
     best.shared = fixed + each * best.kept;
     return best;
 }
 
-cudaError_t launch_clusters(NormKernel kernel, int64_t blocks, int cluster, size_t shared, cudaStream_t st, const NormArgs& a)
+cudaError_t launch_clusters(NormKernel kernel, dim3 grid, int cluster, size_t shared, cudaStream_t st, const NormArgs& a)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(kNormThreads);
     cfg.dynamicSmemBytes = shared;
     cfg.stream = st;
@@ -748,6 +1000,7 @@ int fill(const choco_group_norm* gn, int64_t images, int64_t pixels, const void*
     a.images = (int32_t)images; a.channels = (int32_t)p.channels; a.groups = p.groups; a.per_group = (int32_t)(p.channels / p.groups);
     a.activation = p.activation;
     a.eps = p.eps;
+    a.inverse = 1.0 / ((double)pixels * a.per_group);
     return CHOCO_OK;
 }
 
@@ -755,19 +1008,25 @@ int launch(choco_group_norm* gn, NormArgs& a, bool backward, const choco_pixels&
 {
     const choco_group_norm_params& p = gn->params;
     const int vec = widest(p, a.images, a.pixels, x, y, dx);
-    const Cut c = cut_of(p, a.images, a.pixels, vec, dtype_size(x.dtype) + (backward ? dtype_size(y.dtype) : 0));
+    const Cut c = cut_of(p, a.images, a.pixels, vec, dtype_size(x.dtype), dtype_size(x.dtype) + (backward ? dtype_size(y.dtype) : 0),
+                         backward ? kShareBackward : kShareForward);
     a.slice = c.slice;
     a.slices = a.channels / c.slice;
     a.cluster = c.cluster;
+    a.share = c.share;
     a.kept = c.kept;
-    const int64_t blocks = (int64_t)p.n * a.images * a.slices * c.cluster;
-    if (blocks > 0x7fffffff) return CHOCO_ERR_TOO_LARGE;
+    a.rounds = c.rounds; a.lanes = c.lanes; a.steps = c.steps;
+    a.per_column = (65536u * vec + c.slice - 1) / c.slice;
+    const int64_t along = (int64_t)p.n * a.images * a.slices * c.cluster;
+    if (along > 0x7fffffff) return CHOCO_ERR_TOO_LARGE;
     const NormKernel kernel = kernel_of(backward, x.dtype, y.dtype, vec);
     if (gn->allowed[backward] != kernel) {
-        if (status_of(cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared)) != CHOCO_OK) return CHOCO_ERR_CUDA;
+        if (status_of(cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared)) != CHOCO_OK ||
+            status_of(cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100)) != CHOCO_OK)
+            return CHOCO_ERR_CUDA;
         gn->allowed[backward] = kernel;
     }
-    return status_of(launch_clusters(kernel, blocks, c.cluster, c.shared, st, a));
+    return status_of(launch_clusters(kernel, dim3((unsigned)along), c.cluster, c.shared, st, a));
 }
 
 } // namespace
@@ -856,7 +1115,7 @@ int choco_group_norm_backward(choco_group_norm* gn, int64_t images, int64_t pixe
     }
     if (!grads || (!some && accumulate)) return CHOCO_OK;
     const GradArgs g = {gn->sums, dweight, dbias, grad_ld, some ? (int32_t)images : 0, (int32_t)p.channels, (int32_t)((p.channels + 31) / 32), grad_dtype, accumulate};
-    return status_of(launch_overlapped(grad_kernel, dim3((unsigned)(g.blocks * p.n)), dim3(kNormThreads), 0, (cudaStream_t)stream, HotRange{}, g));
+    return status_of(launch_overlapped(grad_kernel, dim3((unsigned)(g.blocks * p.n)), dim3(kGradThreads), 0, (cudaStream_t)stream, HotRange{}, g));
 }
 
 } // extern "C"
