@@ -573,7 +573,7 @@ int choco_adamw_set_steps(choco_adamw* opt, const int64_t* steps, void* stream);
  * its group, |.| the Frobenius norm:
  *     m = beta m + (1 - beta) c g ;   u = beta m + (1 - beta) c g  (nesterov = 1)  or  m
  *     X = u / |u|  (0 where u = 0) ;  `steps` times:  X = (a I + b S + c4 S^2) X  with S = X X^T
- *     x = x - (X lr lr_scale + x (lr lr_scale weight_decay))
+ *     x = x - (X lr lr_scale + x (lr weight_decay))
  * (a, b, c4 are a, b, c of choco_muon_params.)  The usual five steps with 3.4445, -4.7750, 2.0315 bring all singular
  * values of X to between about 0.7 and 1.2.  Convolutions are matrices [c_out, c_in k k].
  */
@@ -587,7 +587,7 @@ typedef struct {
     int32_t x_dtype, g_dtype, copy_dtype;
     int32_t group;        /* in [0, groups)                                                        */
     double weight_decay;  /* >= 0, finite as a float32                                             */
-    double lr_scale;      /* factor on the learning rate of this matrix, >= 0, finite as a float32 */
+    double lr_scale;      /* factor on X's part of the step, >= 0, finite as a float32           */
 } choco_muon_matrix;
 typedef struct {
     double beta;          /* in [0, 1)                                                             */

@@ -802,6 +802,8 @@ def _pixels_of(gn, what: str, t):
     key = (what, t.shape, t.stride(), t.dtype)
     found = gn.layouts.get(key)
     if found is None:
+        if len(gn.layouts) > 1000:       # batches of ever new shapes
+            gn.layouts.clear()
         found = gn.layouts[key] = _pixel_layout(gn, what, t)
     if t.get_device() != gn.device:
         raise ChocoError(f"libchoco: {what} must be on the handle's GPU ({gn.device}), not {t.device}", -1)

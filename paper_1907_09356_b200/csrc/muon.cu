@@ -39,6 +39,7 @@ constexpr uint32_t kPieceBytes = kTileBytes / 2;   // half of its rows
 constexpr int kBlock = 256;                        // matrices start on multiples of this in the momentum
 constexpr int kUnit = 4096;                        // elements of one block of the momentum kernel
 constexpr int kUnitThreads = 256;
+constexpr int kMostSplits = 4;                     // of a part of X X^T along K
 constexpr int kTileThreads2 = 256;                 // of the kernels that cut matrices into tiles and put them together
 
 struct Matrix {
@@ -55,7 +56,7 @@ struct Matrix {
     int32_t ex, es;         // powers of two that X, and S and B, are scaled by
     int32_t group;
     float weight_decay, lr_scale;
-    int32_t unit0, units;   // blocks of the momentum kernel
+    int32_t unit0, units;   // blocks of the momentum kernel (small matrices: none)
     int8_t x_dtype, g_dtype, copy_dtype;
     bool tall;              // rows > cols
     bool whole;             // rows of g behind one another, and its elements in aligned fours
@@ -66,11 +67,14 @@ struct Unit {
 };
 struct Part {               // of a product: kSide CG rows from kSide CG i, and as many columns from kSide CG j
     int32_t matrix;
-    int16_t i, j;
+    int32_t i, j;
+    int32_t begin, steps;   // of K, in steps of 64; a part of X X^T may be split along K
+    int32_t split, splits;  // which of how many
+    int32_t slot;           // where the sums of all its splits lie, and their counter
 };
 struct Block {              // a tile of X
     int32_t matrix;
-    int16_t row, col;
+    int32_t row, col;
 };
 struct Scale {              // of a matrix in this step: X_0 = (U first) second; both 0 where it is left alone or zero
     float first, second;
@@ -93,7 +97,7 @@ struct MomentArgs {
 
 // m = beta m + (1 - beta) c g, and the sum of squares of U by unit.  The last unit of a matrix to finish adds its
 // units up in their order and forms the scale, in float64: squares of small gradients leave float32's range.
-template <typename GT>
+template <int THREADS, typename GT>
 __device__ double moment_unit(const MomentArgs& a, const Matrix& t, int64_t begin, int64_t end, float c)
 {
     double sum = 0.0;
@@ -101,7 +105,8 @@ __device__ double moment_unit(const MomentArgs& a, const Matrix& t, int64_t begi
     const GT* g = static_cast<const GT*>(t.g);
     if (t.whole) {
         const int64_t quads = end / 4 * 4;
-        for (int64_t e = begin + 4 * (int64_t)threadIdx.x; e < quads; e += 4 * kUnitThreads) {
+#pragma unroll 4
+        for (int64_t e = begin + 4 * (int64_t)threadIdx.x; e < quads; e += 4 * THREADS) {
             Raw<GT, 4> raw;
             load_raw(raw, g + e);
             float u[4];
@@ -124,7 +129,7 @@ __device__ double moment_unit(const MomentArgs& a, const Matrix& t, int64_t begi
         }
         begin = quads > begin ? quads : begin;
     }
-    for (int64_t e = begin + threadIdx.x; e < end; e += kUnitThreads) {
+    for (int64_t e = begin + threadIdx.x; e < end; e += THREADS) {
         const int64_t row = (uint32_t)e / (uint32_t)t.cols, col = (uint32_t)e % (uint32_t)t.cols;
         const float ge = to_float(g[row * t.g_ld + col]) * c;
         float u = ge;
@@ -138,7 +143,28 @@ __device__ double moment_unit(const MomentArgs& a, const Matrix& t, int64_t begi
     return sum;
 }
 
-__device__ __forceinline__ double block_sum(double v, double* ws) // 256 threads; the sum is thread 0's
+template <int THREADS>
+__device__ __forceinline__ double moment_unit(const MomentArgs& a, const Matrix& t, int64_t begin, int64_t end, float c)
+{
+    if (t.g_dtype == CHOCO_F32) return moment_unit<THREADS, float>(a, t, begin, end, c);
+    if (t.g_dtype == CHOCO_BF16) return moment_unit<THREADS, __nv_bfloat16>(a, t, begin, end, c);
+    return moment_unit<THREADS, __half>(a, t, begin, end, c);
+}
+// X_0's scale from the sum of squares
+__device__ __forceinline__ Scale scale_of(double sum, int ex)
+{
+    Scale s = {0.f, 0.f};
+    if (sum != 0.0) {
+        const double f = ldexp(1.0, ex) / sqrt(sum);     // from 1e-44 to 1e49: in two factors where float32 ends
+        const double pre = f > 1e30 ? 0x1p100 : f < 1e-30 ? 0x1p-100 : 1.0;
+        s.first = (float)pre;
+        s.second = (float)(f / pre);
+    }
+    return s;
+}
+
+template <int THREADS>
+__device__ __forceinline__ double block_sum(double v, double* ws) // the sum is thread 0's
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -146,7 +172,7 @@ __device__ __forceinline__ double block_sum(double v, double* ws) // 256 threads
     __syncthreads();
     double s = 0.0;
     if (threadIdx.x == 0)
-        for (int w = 0; w < kUnitThreads / 32; ++w) s += ws[w];
+        for (int w = 0; w < THREADS / 32; ++w) s += ws[w];
     __syncthreads();
     return s;
 }
@@ -165,11 +191,9 @@ __global__ void __launch_bounds__(kUnitThreads) moment_kernel(MomentArgs a)
     if (!skip) {
         const int64_t begin = (int64_t)un.part * kUnit, all = (int64_t)t.rows * t.cols;
         const int64_t end = begin + kUnit < all ? begin + kUnit : all;
-        if (t.g_dtype == CHOCO_F32) sum = moment_unit<float>(a, t, begin, end, c);
-        else if (t.g_dtype == CHOCO_BF16) sum = moment_unit<__nv_bfloat16>(a, t, begin, end, c);
-        else sum = moment_unit<__half>(a, t, begin, end, c);
+        sum = moment_unit<kUnitThreads>(a, t, begin, end, c);
     }
-    sum = block_sum(sum, ws);
+    sum = block_sum<kUnitThreads>(sum, ws);
     if (threadIdx.x == 0) {
         a.partial[t.unit0 + un.part] = sum;
         __threadfence();
@@ -180,17 +204,10 @@ __global__ void __launch_bounds__(kUnitThreads) moment_kernel(MomentArgs a)
     __threadfence();
     sum = 0.0;
     for (int i = threadIdx.x; i < t.units; i += kUnitThreads) sum += __ldcg(a.partial + t.unit0 + i);
-    sum = block_sum(sum, ws);
+    sum = block_sum<kUnitThreads>(sum, ws);
     if (threadIdx.x == 0) {
         a.done[un.matrix] = 0;
-        Scale s = {0.f, 0.f};
-        if (!skip && sum != 0.0) {
-            const double f = ldexp(1.0, t.ex) / sqrt(sum);   // from 1e-44 to 1e49: in two factors where float32 ends
-            const double pre = f > 1e30 ? 0x1p100 : f < 1e-30 ? 0x1p-100 : 1.0;
-            s.first = (float)pre;
-            s.second = (float)(f / pre);
-        }
-        a.scale[un.matrix] = s;
+        a.scale[un.matrix] = scale_of(skip ? 0.0 : sum, t.ex);
     }
 }
 
@@ -247,13 +264,68 @@ __device__ __forceinline__ void join8(uint4 hi, uint4 lo, float* v, bool has_lo)
     }
 }
 
-// U of one element of the matrix
-__device__ __forceinline__ float update_of(const TileArgs& a, const Matrix& t, int row, int col, float c)
+// Eight neighbouring elements, of which the first `valid` are there (others: 0): one or two accesses of 16 bytes where the address allows
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int valid, float* v)
 {
-    const float g = bits_to_float(load_bits(t.g, (int64_t)row * t.g_ld + col, t.g_dtype), t.g_dtype) * c;
-    if (!a.m) return g;
-    const float m = a.m[t.state + (int64_t)row * t.cols + col];
-    return a.nesterov ? averaged(m, g, a.beta, a.omb) : m;
+    if (valid >= 8 && ((uintptr_t)p & 15) == 0) {
+        Raw<T, 8> r;
+        load_raw(r, p);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = raw_get(r, q);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = q < valid ? to_float(p[q]) : 0.f;
+    }
+}
+__device__ __forceinline__ void load8(const void* p, int64_t at, int32_t dtype, int valid, float* v)
+{
+    if (dtype == CHOCO_F32) load8(static_cast<const float*>(p) + at, valid, v);
+    else if (dtype == CHOCO_BF16) load8(static_cast<const __nv_bfloat16*>(p) + at, valid, v);
+    else load8(static_cast<const __half*>(p) + at, valid, v);
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int valid, const float* v)
+{
+    if (valid >= 8 && ((uintptr_t)p & 15) == 0) {
+        store_vec<T, 8>(p, v);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (q < valid) p[q] = from_float<T>(v[q]);
+    }
+}
+__device__ __forceinline__ void store8(void* p, int64_t at, int32_t dtype, int valid, const float* v)
+{
+    if (dtype == CHOCO_F32) store8(static_cast<float*>(p) + at, valid, v);
+    else if (dtype == CHOCO_BF16) store8(static_cast<__nv_bfloat16*>(p) + at, valid, v);
+    else store8(static_cast<__half*>(p) + at, valid, v);
+}
+// U from (row, col) on
+__device__ __forceinline__ void update8(const TileArgs& a, const Matrix& t, int row, int col, int valid, float c, float* u)
+{
+    load8(t.g, (int64_t)row * t.g_ld + col, t.g_dtype, valid, u);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) u[q] *= c;
+    if (!a.m) return;
+    float m[8];
+    load8(a.m + t.state + (int64_t)row * t.cols + col, valid, m);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) u[q] = a.nesterov ? averaged(m[q], u[q], a.beta, a.omb) : m[q];
+}
+// x (and its copy) from (row, col) on
+__device__ __forceinline__ void apply8(const TileArgs& a, const Matrix& t, int row, int col, int valid, float* o)
+{
+    const int64_t at = (int64_t)row * t.x_ld + col;
+    if (a.update) {
+        float x[8];
+        load8(t.x, at, t.x_dtype, valid, x);
+        const float lr = a.lr * t.lr_scale, decay = a.lr * t.weight_decay;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) o[q] = x[q] - (o[q] * lr + x[q] * decay);
+        if (t.copy) store8(t.copy, (int64_t)row * t.copy_ld + col, t.copy_dtype, valid, o);
+    }
+    store8(t.x, at, t.x_dtype, valid, o);
 }
 
 // A tile of X_0: 128 rows x 64 columns of U, turned where the matrix is tall.
@@ -268,43 +340,35 @@ __global__ void __launch_bounds__(kTileThreads2) cut_kernel(TileArgs a)
     const Scale sc = a.scale[bl.matrix];
     const bool live = sc.second != 0.f;     // (true for NaN)
     const float c = a.factor ? a.factor[t.group] : 1.f;
-    if (t.tall) {
-        if (live)
-            for (int e = threadIdx.x; e < kSide * kHalves; e += kTileThreads2) {
-                const int r = e % kSide, q = e / kSide;
-                turn[q][r] = row0 + r < t.m && col0 + q < t.k ? update_of(a, t, col0 + q, row0 + r, c) : 0.f;
-            }
+    if (t.tall && live) {
+#pragma unroll 2
+        for (int e = threadIdx.x; e < kHalves * kSide / 8; e += kTileThreads2) {
+            const int q = e / (kSide / 8), r = e % (kSide / 8) * 8;
+            float u[8] = {};
+            if (col0 + q < t.k && row0 + r < t.m) update8(a, t, col0 + q, row0 + r, t.m - row0 - r, c, u);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) turn[q][r + k] = u[k];
+        }
         __syncthreads();
     }
     uint8_t* to = a.work + t.at[0] + ((int64_t)bl.row * t.nb + bl.col) * 2 * kTileBytes;
-    const int piece = threadIdx.x & 7;
+    const int piece = threadIdx.x & 7, col = col0 + piece * 8;
+#pragma unroll 2
     for (int r = threadIdx.x >> 3; r < kSide; r += kTileThreads2 / 8) {
-        float v[8];
+        float v[8] = {};
+        if (live && t.tall) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const int col = col0 + piece * 8 + q;
-            float u = 0.f;
-            if (live) u = t.tall ? turn[piece * 8 + q][r] : row0 + r < t.m && col < t.k ? update_of(a, t, row0 + r, col, c) : 0.f;
-            v[q] = u * sc.first * sc.second;
+            for (int q = 0; q < 8; ++q) v[q] = turn[piece * 8 + q][r];
+        } else if (live && row0 + r < t.m && col < t.k) {
+            update8(a, t, row0 + r, col, t.k - col, c, v);
         }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = v[q] * sc.first * sc.second;
         uint4 hi, lo;
         split8(v, hi, lo, true);
         *reinterpret_cast<uint4*>(to + piece_at(r, piece)) = hi;
         *reinterpret_cast<uint4*>(to + kTileBytes + piece_at(r, piece)) = lo;
     }
-}
-
-__device__ __forceinline__ void apply_one(const TileArgs& a, const Matrix& t, int row, int col, float o)
-{
-    if (!a.update) {
-        store_from_float(t.x, (int64_t)row * t.x_ld + col, t.x_dtype, o);
-        return;
-    }
-    const int64_t at = (int64_t)row * t.x_ld + col;
-    const float x = bits_to_float(load_bits(t.x, at, t.x_dtype), t.x_dtype), lr = a.lr * t.lr_scale;
-    const float next = x - (o * lr + x * (a.lr * t.weight_decay * t.lr_scale));
-    store_from_float(t.x, at, t.x_dtype, next);
-    if (t.copy) store_from_float(t.copy, (int64_t)row * t.copy_ld + col, t.copy_dtype, next);
 }
 
 // The last X of a matrix, tile by tile, to where it goes.
@@ -319,19 +383,30 @@ __global__ void __launch_bounds__(kTileThreads2) apply_kernel(TileArgs a)
     if (a.factor && !isfinite(a.factor[t.group])) return;
     const uint8_t* from = a.work + t.at[a.which] + ((int64_t)bl.row * t.nb + bl.col) * a.planes * kTileBytes;
     const float unscale = exp2f((float)-t.ex);
-    const int piece = threadIdx.x & 7;
+    const int piece = threadIdx.x & 7, col = col0 + piece * 8;
+#pragma unroll 2
     for (int r = threadIdx.x >> 3; r < kSide; r += kTileThreads2 / 8) {
         const uint4 hi = *reinterpret_cast<const uint4*>(from + piece_at(r, piece));
         const uint4 lo = a.planes == 2 ? *reinterpret_cast<const uint4*>(from + kTileBytes + piece_at(r, piece)) : make_uint4(0, 0, 0, 0);
         float v[8];
         join8(hi, lo, v, a.planes == 2);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) turn[piece * 8 + q][r] = v[q] * unscale;
+        for (int q = 0; q < 8; ++q) {
+            v[q] *= unscale;
+            if (t.tall) turn[piece * 8 + q][r] = v[q];
+        }
+        if (!t.tall && row0 + r < t.m && col < t.k) apply8(a, t, row0 + r, col, t.k - col, v);
     }
+    if (!t.tall) return;
     __syncthreads();
-    for (int e = threadIdx.x; e < kSide * kHalves; e += kTileThreads2) {
-        const int r = t.tall ? e % kSide : e / kHalves, q = t.tall ? e / kSide : e % kHalves;
-        if (row0 + r < t.m && col0 + q < t.k) apply_one(a, t, t.tall ? col0 + q : row0 + r, t.tall ? row0 + r : col0 + q, turn[q][r]);
+#pragma unroll 2
+    for (int e = threadIdx.x; e < kHalves * kSide / 8; e += kTileThreads2) {
+        const int q = e / (kSide / 8), r = e % (kSide / 8) * 8;
+        if (col0 + q >= t.k || row0 + r >= t.m) continue;
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = turn[q][r + k];
+        apply8(a, t, col0 + q, row0 + r, t.m - row0 - r, v);
     }
 }
 
@@ -346,6 +421,8 @@ struct ProductArgs {
     int32_t count;          // of the parts
     float a, b, c;
     int32_t which;          // of the two X: the one that is read
+    float* partial;         // sums of split parts, 128 x 128 each
+    uint32_t* arrived;      // how many splits are there, 0 between launches
     int32_t planes;         // parts of its tiles in the workspace (S, T and B and the next X have as many as take part in products)
 };
 
@@ -388,6 +465,11 @@ __device__ __forceinline__ void fetch_turned(uint8_t* to, const uint8_t* x, int6
             bulk_load(to + p * kTileBytes + cb * kPieceBytes, x + ((tile + cb) * planes + p) * kTileBytes + lower * kPieceBytes, kPieceBytes, bar);
 }
 
+template <int THREADS>
+__device__ __forceinline__ void warps_sync(int barrier) // of four warps of a block
+{
+    asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(THREADS) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void add_at(float (&w)[N], int column, float x)
 {
@@ -441,7 +523,7 @@ struct Job {
         has_a = it < mt;
         has_b = jt < columns;
         same = KIND == kGram && part.i == part.j;
-        nk = ((KIND == kGram ? t->k : t->m) + kHalves - 1) / kHalves;
+        nk = part.steps;
         leave = LEAVE ? steps_to_leave(nk) : nk;
     }
     // a tile above the diagonal's parts is stored turned
@@ -460,6 +542,7 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
     __shared__ uint64_t full[ST], empty[ST], sums[2], taken[2];
     __shared__ uint32_t tmem_at;
     __shared__ volatile uint32_t failed;
+    __shared__ volatile bool last[2];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     const int begin = blockIdx.x / CG, step = gridDim.x / CG;
@@ -527,19 +610,63 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
             const int tile = job.part.j * CG + h;                // of 128 columns
             const bool there = job.has_a && tile < job.columns;
             const int own = job.it == tile ? r : -1;             // this thread's column on the diagonal
+            const int splits = KIND == kGram ? job.part.splits : 1;
+            float* partial = nullptr;                            // of this CTA's tile: split after split, column after column
+            if (KIND == kGram && splits > 1) {
+                const int64_t place = ((int64_t)job.part.slot * CG + rank) * CG + h;
+                partial = a.partial + place * kMostSplits * (kSide * kSide) + r;
+                float* here = partial + job.part.split * (kSide * kSide);
+#pragma unroll
+                for (int q32 = 0; q32 < kSide / 32; ++q32) {
+                    uint32_t bits[32];
+                    if constexpr (!L::kLeave) tmem_load32(from + (ch & 1) * L::kColumns + q32 * 32, bits);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        __stcg(here + (q32 * 32 + e) * kSide, L::kLeave ? v[L::kLeave ? q32 * 32 + e : 0] : __uint_as_float(bits[e]));
+                }
+                if (!L::kLeave) leave_sums(ch);
+                // the last split to arrive adds them all up in their order
+                __threadfence();
+                warps_sync<128>(1 + h);
+                if (r == 0) last[h] = atomicAdd(a.arrived + place, 1u) == (uint32_t)splits - 1;
+                warps_sync<128>(1 + h);
+                const bool mine_to_do = last[h];
+                warps_sync<128>(1 + h);                          // (read before the next part writes it)
+                if (!mine_to_do) {
+                    if (!L::kLeave) ++ch;
+                    continue;
+                }
+                __threadfence();
+                if (r == 0) a.arrived[place] = 0;
+            }
             const int64_t at = (KIND == kNext ? (int64_t)job.it * job.nb + 2 * tile : ((int64_t)job.it * job.mt + tile) * 2) * PL * kTileBytes;
             const float up = exp2f((float)t.es), scale = KIND == kGram ? exp2f((float)(t.es - 2 * t.ex)) : exp2f((float)-t.es);
 #pragma unroll
             for (int cb = 0; cb < 2; ++cb) {
                 float w[kHalves];
+                if (KIND == kGram && splits > 1) {
+#pragma unroll
+                    for (int e = 0; e < kHalves; ++e) w[e] = 0.f;
+                    for (int k = 0; k < splits; ++k) {           // (all loads of a split under way together)
+                        const float* sum = partial + k * (kSide * kSide) + cb * kHalves * kSide;
+                        float u[kHalves];
+#pragma unroll
+                        for (int e = 0; e < kHalves; ++e) u[e] = __ldcg(sum + e * kSide);
+#pragma unroll
+                        for (int e = 0; e < kHalves; ++e) w[e] += u[e];
+                    }
+#pragma unroll
+                    for (int e = 0; e < kHalves; ++e) w[e] *= scale;
+                }
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
+                    if (KIND == kGram && splits > 1) break;
                     uint32_t bits[32];
                     if constexpr (!L::kLeave) tmem_load32(from + (ch & 1) * L::kColumns + cb * kHalves + q * 32, bits);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) w[q * 32 + e] = (L::kLeave ? v[L::kLeave ? cb * kHalves + q * 32 + e : 0] : __uint_as_float(bits[e])) * scale;
                 }
-                if (!L::kLeave && cb == 1) leave_sums(ch);
+                if (!L::kLeave && cb == 1 && splits == 1) leave_sums(ch);
                 if (!there) continue;
                 const int column = own - cb * kHalves;           // in this tile
                 if (KIND == kSquare) add_at(w, column, a.a * up);
@@ -557,7 +684,7 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else {
         if constexpr (L::kLeave && CG == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (warp == L::kWarps && lane == 0) {                    // the copies
+        if (warp == L::kWarps) {                                 // the copies
             fence_async();
             uint32_t n = 0;                                      // steps of 64 of K so far
             bool ok = true;
@@ -574,27 +701,30 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
                     uint8_t* to_a = stage + s * L::kStage;
                     uint8_t* to_b = to_a + L::kFirst;
                     const int ct = kb >> 1;
-                    mbar_expect_tx(&full[s], bytes);
-                    if (job.has_a) {
-                        if (KIND == kGram) fetch_along<PA>(to_a, x, (int64_t)job.it * job.nb + kb, a.planes, &full[s]);
-                        else if (!job.turns_a(kb)) fetch_along<PA>(to_a, first, ((int64_t)job.it * job.mt + ct) * 2 + (kb & 1), PL, &full[s]);
-                        else fetch_turned<PA>(to_a, first, ((int64_t)ct * job.mt + job.it) * 2, PL, kb & 1, &full[s]);
+                    if (elect_one()) {
+                        mbar_expect_tx(&full[s], bytes);
+                        if (job.has_a) {
+                            if (KIND == kGram) fetch_along<PA>(to_a, x, (int64_t)job.it * job.nb + job.part.begin + kb, a.planes, &full[s]);
+                            else if (!job.turns_a(kb)) fetch_along<PA>(to_a, first, ((int64_t)job.it * job.mt + ct) * 2 + (kb & 1), PL, &full[s]);
+                            else fetch_turned<PA>(to_a, first, ((int64_t)ct * job.mt + job.it) * 2, PL, kb & 1, &full[s]);
+                        }
+                        if (load_b) {
+                            if (KIND == kGram) fetch_along<PB>(to_b, x, (int64_t)job.jt * job.nb + job.part.begin + kb, a.planes, &full[s]);
+                            else if (KIND == kNext) fetch_turned<PB>(to_b, x, (int64_t)ct * job.nb + 2 * job.jt, a.planes, kb & 1, &full[s]);
+                            else if (!job.turns_b(kb)) fetch_along<PB>(to_b, a.work + job.t->t_at, ((int64_t)job.jt * job.mt + ct) * 2 + (kb & 1), PL, &full[s]);
+                            else fetch_turned<PB>(to_b, a.work + job.t->t_at, ((int64_t)ct * job.mt + job.jt) * 2, PL, kb & 1, &full[s]);
+                        }
                     }
-                    if (load_b) {
-                        if (KIND == kGram) fetch_along<PB>(to_b, x, (int64_t)job.jt * job.nb + kb, a.planes, &full[s]);
-                        else if (KIND == kNext) fetch_turned<PB>(to_b, x, (int64_t)ct * job.nb + 2 * job.jt, a.planes, kb & 1, &full[s]);
-                        else if (!job.turns_b(kb)) fetch_along<PB>(to_b, a.work + job.t->t_at, ((int64_t)job.jt * job.mt + ct) * 2 + (kb & 1), PL, &full[s]);
-                        else fetch_turned<PB>(to_b, a.work + job.t->t_at, ((int64_t)ct * job.mt + job.jt) * 2, PL, kb & 1, &full[s]);
-                    }
+                    __syncwarp();
                 }
             }
             if (!ok) {                                           // copies under way are sat out
                 failed = 1;
                 for (uint32_t q = n > ST ? n - ST : 0; q < n; ++q) mbar_wait(&full[q % ST], (q / ST) & 1);
             }
-        } else if (warp == L::kWarps + 1 && lane == 0) {         // the products
+        } else if (warp == L::kWarps + 1) {                      // the products
             uint32_t n = 0, ch = 0;
-            bool ok = true, ready = false;                       // ready: the next step's factors (and room for its sums) are known to be there
+            bool ok = true;
             for (int index = begin; index < a.count && ok; index += step) {
                 const Job<KIND, CG, L::kLeave> job(a, index, rank);
                 for (int kb = 0; kb < job.nk; ++kb, ++n) {
@@ -602,15 +732,14 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
                     if (CG == 2 && rank == 1) {                  // the other CTA of a pair tells the first what has come
                         ok = mbar_wait(&full[s], (n / ST) & 1);
                         if (!ok) break;
-                        mbar_arrive_at(&full[s], 0);
+                        if (elect_one()) mbar_arrive_at(&full[s], 0);
+                        __syncwarp();
                         continue;
                     }
                     const bool begins = kb % job.leave == 0, ends = kb + 1 == job.nk || (kb + 1) % job.leave == 0;
-                    if (!ready) {
-                        if (begins && ch >= 2) ok = mbar_wait(&taken[ch & 1], (ch / 2 - 1) & 1);
-                        ok = ok && mbar_wait(&full[s], (n / ST) & 1);
-                        if (!ok) break;
-                    }
+                    if (begins && ch >= 2) ok = mbar_wait(&taken[ch & 1], (ch / 2 - 1) & 1);
+                    ok = ok && mbar_wait(&full[s], (n / ST) & 1);
+                    if (!ok) break;
                     tmem_fence_after();
                     const bool turn_a = job.turns_a(kb), turn_b = job.turns_b(kb);
                     const uint32_t at_a = smem_u32(stage) + s * L::kStage, at_b = job.same ? at_a : at_a + L::kFirst;
@@ -620,33 +749,24 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
                     const uint64_t na = turn_a ? kNextTurned : kNextAlong, nb = turn_b ? kNextTurned : kNextAlong;
                     const uint32_t to = acc + (ch & 1) * L::kColumns;
                     constexpr uint64_t low = kTileBytes >> 4;
-                    // Half of the products, a look at the barriers of the next step while the tensor cores work on them (300 cycles
-                    // that would lie between two steps), and the other half.  The small products come first, while the sums are small.
                     auto high = [&](int q) { product<CG>(to, da + q * na, db + q * nb, shape, PB == 2 || !begins || q > 0); };
-                    if constexpr (PB == 2) {
+                    if (elect_one()) {
+                        if constexpr (PB == 2) {                 // the small products come first, while the sums are small
 #pragma unroll
-                        for (int q = 0; q < kHalves / 16; ++q) {
-                            product<CG>(to, da + q * na, db + q * nb + low, shape, !begins || q > 0);
-                            if constexpr (PA == 2) product<CG>(to, da + q * na + low, db + q * nb, shape, true);
+                            for (int q = 0; q < kHalves / 16; ++q) {
+                                product<CG>(to, da + q * na, db + q * nb + low, shape, !begins || q > 0);
+                                if constexpr (PA == 2) product<CG>(to, da + q * na + low, db + q * nb, shape, true);
+                            }
                         }
-                    } else {
                         high(0);
                         high(1);
+                        high(2);
+                        high(3);
+                        products_done<CG>(&empty[s]);
+                        if (ends) products_done<CG>(&sums[ch & 1]);
                     }
-                    const uint32_t next = n + 1, then = ch + 1;
-                    ready = (kb + 1 < job.nk || index + step < a.count) && mbar_test(&full[next % ST], (next / ST) & 1) &&
-                            (!ends || then < 2 || mbar_test(&taken[then & 1], (then / 2 - 1) & 1));
-                    if constexpr (PB == 2) {
-                        high(0);
-                        high(1);
-                    }
-                    high(2);
-                    high(3);
-                    products_done<CG>(&empty[s]);
-                    if (ends) {
-                        products_done<CG>(&sums[ch & 1]);
-                        ++ch;
-                    }
+                    __syncwarp();
+                    if (ends) ++ch;
                 }
             }
             if (!ok) failed = 1;
@@ -658,6 +778,246 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
     if (tid == 0 && failed) atomicAdd(a.errors, 1u);
     if (CG == 2) cluster_sync();
     if (warp == 0) tmem_free<CG>(acc, 2 * L::kColumns);
+}
+
+// ---------------------------------------------------------------------------------------- small matrices
+// A matrix that fits a block's shared memory takes one launch for the whole step: momentum, norm, all products and the new
+// parameters, with X, S, T and B where the tensor cores read them.  (64 x 576, 18 launches: 187 us; this: TIME_SMALL us.)  Rows of tiles are cut
+// to the smaller side, a multiple of 16; the first factor of a product always has 128 rows and reads on into what lies behind, which
+// makes rows of sums that nobody looks at.
+constexpr int kSmallThreads = 512;
+constexpr int kSmallShared = 227 * 1024 - 1024;
+constexpr uint32_t kTmemColumns = 512;
+
+struct SmallLayout {
+    int rows, blocks, square;   // of tiles: rows; tiles of X; tiles of S in a row
+    uint32_t tile;              // bytes of one part of a tile
+    uint32_t s_at, t_at, bytes;
+    __host__ __device__ SmallLayout(int m, int k)
+    {
+        rows = (m + 15) / 16 * 16;
+        blocks = (k + kHalves - 1) / kHalves;
+        square = (rows + kHalves - 1) / kHalves;
+        tile = rows * 128;
+        s_at = blocks * 2 * tile;
+        t_at = s_at + square * 2 * tile;
+        bytes = t_at + square * 2 * tile + kTileBytes;
+    }
+};
+__host__ __device__ inline bool is_small(int m, int k) // (only tiles that can fit are multiplied out)
+{
+    return m > 0 && m <= kSide && k <= 1 << 14 && SmallLayout(m, k).bytes <= (uint32_t)kSmallShared;
+}
+
+struct SmallArgs {
+    MomentArgs moment;
+    TileArgs tile;
+    const int32_t* list;
+    uint32_t* errors;
+    float a, b, c;
+    int32_t steps;
+};
+
+__global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
+{
+    extern __shared__ __align__(1024) uint8_t stage[];
+    __shared__ double ws[kSmallThreads / 32];
+    __shared__ uint64_t done;
+    __shared__ uint32_t tmem_at;
+    __shared__ Scale scale;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const Matrix& t = a.moment.mats[a.list[blockIdx.x]];
+    const SmallLayout l(t.m, t.k);
+    if (tid == 0) mbar_init(&done, 1);
+    if (warp == 0) tmem_alloc<1>(&tmem_at, kTmemColumns);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t acc = tmem_at;
+    allow_next_kernel();
+    wait_for_previous_kernel();
+    const float c = a.moment.factor ? a.moment.factor[t.group] : 1.f;
+    const bool skip = !isfinite(c);
+    bool ok = true;
+    if (!skip) {
+        const double sum = block_sum<kSmallThreads>(moment_unit<kSmallThreads>(a.moment, t, 0, (int64_t)t.rows * t.cols, c), ws);
+        if (tid == 0) scale = scale_of(sum, t.ex);
+        __syncthreads();                                         // (and the momentum is written)
+        const Scale sc = scale;
+        const bool live = sc.second != 0.f;
+        auto x_tile = [&](int block, int part) { return stage + (block * 2 + part) * l.tile; };
+        auto put = [&](uint8_t* tile, int row, int piece, const float* v) {
+            uint4 hi, lo;
+            split8(v, hi, lo, true);
+            *reinterpret_cast<uint4*>(tile + piece_at(row, piece)) = hi;
+            *reinterpret_cast<uint4*>(tile + l.tile + piece_at(row, piece)) = lo;
+        };
+        if (!t.tall) {
+#pragma unroll 2
+            for (int e = tid; e < l.rows * l.blocks * 8; e += kSmallThreads) {
+                const int row = e / (l.blocks * 8), piece = e % (l.blocks * 8);
+                float v[8] = {};
+                if (live && row < t.m && piece * 8 < t.k) update8(a.tile, t, row, piece * 8, t.k - piece * 8, c, v);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] = v[q] * sc.first * sc.second;
+                put(x_tile(piece >> 3, 0), row, piece & 7, v);
+            }
+        } else {
+#pragma unroll 2
+            for (int e = tid; e < l.blocks * kHalves * (l.rows / 8); e += kSmallThreads) {
+                const int col = e % (l.blocks * kHalves), row = e / (l.blocks * kHalves) * 8;
+                float v[8] = {};
+                if (live && row < t.m && col < t.k) update8(a.tile, t, col, row, t.m - row, c, v);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const float u = v[q] * sc.first * sc.second;
+                    const __half hi = __float2half_rn(u);
+                    uint8_t* at = x_tile(col >> 6, 0) + piece_at(row + q, (col & 63) >> 3) + (col & 7) * 2;
+                    *reinterpret_cast<__half*>(at) = hi;
+                    *reinterpret_cast<__half*>(at + l.tile) = __float2half_rn(u - __half2float(hi));
+                }
+            }
+        }
+        uint32_t phase = 0;
+        auto begin_products = [&]() { // what was written is there for the tensor cores
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            tmem_fence_before();
+            __syncthreads();
+            tmem_fence_after();
+        };
+        auto wait_products = [&]() {
+            ok = __syncthreads_and(mbar_wait(&done, phase));
+            phase ^= 1;
+            tmem_fence_after();
+            return ok;
+        };
+        // Three products of 16 of K from `begin` to `end`, the small ones of all of them first, while the sums are small
+        auto products = [&](uint32_t to, uint32_t shape, int begin, int end, auto first, auto second) {
+            const uint64_t low = l.tile >> 4;
+            for (int q = begin; q < end; ++q) {
+                const uint64_t f = first(q), g = second(q);
+                product<1>(to, f, g + low, shape, q > begin);
+                product<1>(to, f + low, g, shape, true);
+            }
+            for (int q = begin; q < end; ++q) product<1>(to, first(q), second(q), shape, true);
+        };
+        const uint32_t base = smem_u32(stage), shape = product_shape(kSide, l.rows);
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const int row = (warp & 3) * 32 + lane, share = warp >> 2;  // a warp has 32 rows and every fourth unit of their columns
+        const bool rows_here = (warp & 3) * 32 < l.rows;
+        const float up = exp2f((float)t.es), down = exp2f((float)-t.es), gram = exp2f((float)(t.es - 2 * t.ex));
+        // sums of X X^T in several parts, added up in registers (see steps_to_leave)
+        const int parts = min(min((int)kTmemColumns / l.rows, 16), l.blocks), each = (l.blocks + parts - 1) / parts, used = (l.blocks + each - 1) / each;
+        for (int step = 0; step < a.steps && ok; ++step) {
+            begin_products();
+            if (warp == 0 && elect_one()) {
+                auto x = [&](int q) { return operand_along(base + (q >> 2) * 2 * l.tile + (q & 3) * 32); };
+                for (int p = 0; p < used; ++p)
+                    products(acc + p * l.rows, shape, p * each * (kHalves / 16), min((p + 1) * each, l.blocks) * (kHalves / 16), x, x);
+                products_done<1>(&done);
+            }
+            if (!wait_products()) break;
+            if (rows_here)
+                for (int piece = share; piece < l.rows / 8; piece += 4) {
+                    float f[8] = {};
+                    for (int p = 0; p < used; ++p) {
+                        uint32_t r[8];
+                        tmem_load8(acc + lanes + p * l.rows + piece * 8, r);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) f[q] += __uint_as_float(r[q]);
+                    }
+                    if (row < l.rows) {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) f[q] *= gram;
+                        put(stage + l.s_at + (piece >> 3) * 2 * l.tile, row, piece & 7, f);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) f[q] = f[q] * a.c + (row == piece * 8 + q ? a.b * up : 0.f);
+                        put(stage + l.t_at + (piece >> 3) * 2 * l.tile, row, piece & 7, f);
+                    }
+                }
+            begin_products();
+            if (warp == 0 && elect_one()) {
+                auto at = [&](uint32_t from) { return [=](int q) { return operand_along(from + (q >> 2) * 2 * l.tile + (q & 3) * 32); }; };
+                products(acc, shape, 0, l.rows / 16, at(base + l.s_at), at(base + l.t_at));
+                products_done<1>(&done);
+            }
+            if (!wait_products()) break;
+            if (rows_here)                                       // B takes the place of S
+                for (int piece = share; piece < l.rows / 8; piece += 4) {
+                    uint32_t r[8];
+                    tmem_load8(acc + lanes + piece * 8, r);
+                    if (row < l.rows) {
+                        float f[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) f[q] = __uint_as_float(r[q]) * down + (row == piece * 8 + q ? a.a * up : 0.f);
+                        put(stage + l.s_at + (piece >> 3) * 2 * l.tile, row, piece & 7, f);
+                    }
+                }
+            begin_products();
+            // B X, 256 columns at a time, two of these under way; the new columns take the place of the old ones
+            auto next = [&](int first) {
+                const int count = min(4, l.blocks - first);
+                const uint32_t wide = product_shape(kSide, count * kHalves) | kTurnB;
+                products(acc + (first & 4) * kHalves, wide, 0, l.rows / 16,
+                         [&](int q) { return operand_along(base + l.s_at + (q >> 2) * 2 * l.tile + (q & 3) * 32); },
+                         [&](int q) { return operand_turned(base + first * 2 * l.tile + q * 2048, 2 * l.tile); });
+                products_done<1>(&done);
+            };
+            if (warp == 0 && elect_one()) next(0);
+            for (int first = 0; first < l.blocks && ok; first += 4) {
+                if (!wait_products()) break;
+                if (warp == 0 && first + 4 < l.blocks && elect_one()) next(first + 4);
+                __syncwarp();
+                const int units = min(4, l.blocks - first) * 2;
+                if (rows_here)
+                    for (int u = share; u < units; u += 4) {
+                        uint32_t r[32];
+                        tmem_load32(acc + (first & 4) * kHalves + lanes + u * 32, r);
+                        if (row < l.rows) {
+#pragma unroll
+                            for (int p = 0; p < 4; ++p) {
+                                float f[8];
+#pragma unroll
+                                for (int q = 0; q < 8; ++q) f[q] = __uint_as_float(r[p * 8 + q]) * down;
+                                put(x_tile(first + (u >> 1), 0), row, (u & 1) * 4 + p, f);
+                            }
+                        }
+                    }
+                tmem_fence_before();                             // (read before the products after the next ones write there)
+            }
+        }
+        __syncthreads();
+        const float unscale = exp2f((float)-t.ex);
+        if (!ok) {
+            if (tid == 0) atomicAdd(a.errors, 1u);
+        } else if (!t.tall) {
+            for (int e = tid; e < t.m * l.blocks * 8; e += kSmallThreads) {
+                const int r = e / (l.blocks * 8), piece = e % (l.blocks * 8);
+                if (piece * 8 >= t.k) continue;
+                const uint8_t* at = x_tile(piece >> 3, 0) + piece_at(r, piece & 7);
+                float v[8];
+                join8(*reinterpret_cast<const uint4*>(at), *reinterpret_cast<const uint4*>(at + l.tile), v, true);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] *= unscale;
+                apply8(a.tile, t, r, piece * 8, t.k - piece * 8, v);
+            }
+        } else {
+            for (int e = tid; e < l.blocks * kHalves * (l.rows / 8); e += kSmallThreads) {
+                const int col = e % (l.blocks * kHalves), r = e / (l.blocks * kHalves) * 8;
+                if (col >= t.k || r >= t.m) continue;
+                float v[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const uint8_t* at = x_tile(col >> 6, 0) + piece_at(r + q, (col & 63) >> 3) + (col & 7) * 2;
+                    v[q] = (__half2float(*reinterpret_cast<const __half*>(at)) + __half2float(*reinterpret_cast<const __half*>(at + l.tile))) * unscale;
+                }
+                apply8(a.tile, t, col, r, t.m - r, v);
+            }
+        }
+    }
+    tmem_fence_before();
+    __syncthreads();
+    if (warp == 0) tmem_free<1>(acc, kTmemColumns);
 }
 
 using ProductKernel = void (*)(ProductArgs);
@@ -693,7 +1053,7 @@ cudaError_t allow_shared()
 
 // matrices of a wave that take the same kernels: one product or three, one CTA to a part or two
 struct Class {
-    int64_t symmetric, symmetric_end;   // parts of S and B
+    int64_t symmetric, gram_end, symmetric_end; // parts of S, of B
     int64_t next, next_end;             // parts of X'
 };
 struct Wave {
@@ -722,8 +1082,14 @@ struct choco_muon {
     std::vector<Range> written;
     std::vector<int64_t> offsets;
     std::vector<Wave> waves;
+    std::vector<int32_t> small;    // matrices that one block of threads takes through the whole step
+    int64_t small_shared;
     int64_t elements;
     int64_t nunits;
+    int32_t* d_small;
+    int64_t split_tiles;           // 128 x 128 results that splits are added up for, of one launch
+    float* d_split;
+    uint32_t* d_arrived;
     void* memory;
     Matrix* d_mats;
     Unit* d_units;
@@ -797,7 +1163,7 @@ int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit
          int64_t* work)
 {
     int64_t at = 0;
-    std::vector<int32_t> kinds; // of every matrix: 1 = three products
+    std::vector<int32_t> kinds; // of every matrix: 1 = three products, -1: in no wave
     for (int32_t i = 0; i < n; ++i) {
         const choco_muon_matrix& q = ms[i];
         if (q.rows < 0 || q.cols < 0 || q.x_ld < 0 || q.g_ld < 0 || q.copy_ld < 0) return CHOCO_ERR_INVALID_ARG;
@@ -832,12 +1198,17 @@ int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit
         t.whole = (t.g_ld == t.cols || t.rows == 1) && aligned_to(q.g, 4 * dtype_size(q.g_dtype));
         t.unit0 = (int32_t)units.size();
         const int64_t count = (int64_t)t.rows * t.cols;
-        t.units = (int32_t)((count + kUnit - 1) / kUnit);
+        const bool small = is_small(t.m, t.k);
+        if (small) {
+            o->small.push_back(i);
+            o->small_shared = std::max(o->small_shared, (int64_t)SmallLayout(t.m, t.k).bytes);
+        }
+        t.units = small ? 0 : (int32_t)((count + kUnit - 1) / kUnit);
         for (int32_t u = 0; u < t.units; ++u) units.push_back({i, u});
         if (units.size() > 0x7fffffff) return CHOCO_ERR_TOO_LARGE;
         o->mats.push_back(t);
         o->offsets.push_back(at);
-        kinds.push_back(o->params.products == 3 || (o->params.products == 0 && (q.x_dtype != CHOCO_BF16 || t.m <= kSide)));
+        kinds.push_back(small || !some ? -1 : o->params.products == 3 || (o->params.products == 0 && (q.x_dtype != CHOCO_BF16 || t.m <= kSide)));
         at += (count + kBlock - 1) / kBlock * kBlock;
         if (at > (int64_t)1 << 38) return CHOCO_ERR_TOO_LARGE;
         if (some) {
@@ -847,6 +1218,11 @@ int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit
     }
     o->elements = at;
     o->nunits = (int64_t)units.size();
+    // the longest first, so that the launch ends with short ones
+    std::sort(o->small.begin(), o->small.end(), [&](int32_t x, int32_t y) {
+        const uint32_t p = SmallLayout(o->mats[x].m, o->mats[x].k).bytes, q = SmallLayout(o->mats[y].m, o->mats[y].k).bytes;
+        return p != q ? p > q : x < y;
+    });
     // waves: matrices in order, as many as the workspace holds together
     *work = 0;
     for (int32_t i = 0; i < n;) {
@@ -854,6 +1230,7 @@ int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit
         int32_t end = i;
         for (; end < n; ++end) {
             Matrix& t = o->mats[end];
+            if (kinds[end] < 0) continue;
             const int64_t planes = kinds[end] ? 2 : 1, x0 = (int64_t)t.mt * t.nb * 2 * kTileBytes, xb = x0 / 2 * planes, sb = (int64_t)t.mt * t.mt * 2 * planes * kTileBytes;
             if (bytes > 0 && bytes + x0 + xb + 3 * sb > kWaveBytes) break;
             t.at[0] = bytes; t.at[1] = bytes + x0;
@@ -861,13 +1238,14 @@ int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit
             bytes += x0 + xb + 3 * sb;
         }
         *work = std::max(*work, bytes);
+        if (bytes == 0) break;   // (nothing but small ones was left)
         Wave w = {};
         for (int three = 0; three < 2; ++three) {
             w.blocks[three] = (int64_t)blocks.size();
             for (int32_t q = i; q < end; ++q)
                 if (kinds[q] == three)
                     for (int32_t r = 0; r < o->mats[q].mt; ++r)
-                        for (int32_t c = 0; c < o->mats[q].nb; ++c) blocks.push_back({q, (int16_t)r, (int16_t)c});
+                        for (int32_t c = 0; c < o->mats[q].nb; ++c) blocks.push_back({q, r, c});
             w.blocks_end[three] = (int64_t)blocks.size();
             for (int pairs = 0; pairs < 2; ++pairs) {
                 Class& cl = w.classes[three][pairs];
@@ -880,16 +1258,41 @@ int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit
                     return o->mats[x].k != o->mats[y].k ? o->mats[x].k > o->mats[y].k : x < y;
                 });
                 cl.symmetric = (int64_t)parts.size();
-                for (int32_t q : these)
-                    for (int32_t r = 0; r < (o->mats[q].mt + cg - 1) / cg; ++r)
-                        for (int32_t c = 0; c <= r; ++c) parts.push_back({q, (int16_t)r, (int16_t)c});
+                auto symmetric = [&](auto add) {
+                    for (int32_t q : these)
+                        for (int32_t r = 0; r < (o->mats[q].mt + cg - 1) / cg; ++r)
+                            for (int32_t c = 0; c <= r; ++c) add(o->mats[q], Part{q, r, c, 0, 0, 0, 1, 0});
+                };
+                auto steps_of = [](int32_t k) { return (k + kHalves - 1) / kHalves; };
+                // X X^T: where the parts are too few for all SMs, long ones are split along K, into pieces of eight steps at least
+                int64_t few = 0;
+                symmetric([&](const Matrix&, const Part&) { ++few; });
+                const int64_t room = std::max<int64_t>(1, o->sms / cg / std::max<int64_t>(few, 1));
+                int32_t slots = 0;
+                symmetric([&](const Matrix& t, Part p) {
+                    const int32_t steps = steps_of(t.k);
+                    p.splits = (int32_t)std::max<int64_t>(1, std::min({room, (int64_t)kMostSplits, (int64_t)steps / 8}));
+                    if (p.splits > 1) p.slot = slots++;
+                    for (p.split = 0; p.split < p.splits; ++p.split) {
+                        p.begin = (int32_t)((int64_t)steps * p.split / p.splits);
+                        p.steps = (int32_t)((int64_t)steps * (p.split + 1) / p.splits) - p.begin;
+                        parts.push_back(p);
+                    }
+                });
+                o->split_tiles = std::max(o->split_tiles, (int64_t)slots * cg * cg);
+                cl.gram_end = (int64_t)parts.size();
+                symmetric([&](const Matrix& t, Part p) {
+                    p.steps = steps_of(t.m);
+                    parts.push_back(p);
+                });
                 cl.symmetric_end = cl.next = (int64_t)parts.size();
                 std::sort(these.begin(), these.end(), [&](int32_t x, int32_t y) {
                     return o->mats[x].m != o->mats[y].m ? o->mats[x].m > o->mats[y].m : x < y;
                 });
                 for (int32_t q : these)
                     for (int32_t c = 0; c < (o->mats[q].nb / 2 + cg - 1) / cg; ++c)
-                        for (int32_t r = 0; r < (o->mats[q].mt + cg - 1) / cg; ++r) parts.push_back({q, (int16_t)r, (int16_t)c});
+                        for (int32_t r = 0; r < (o->mats[q].mt + cg - 1) / cg; ++r)
+                            parts.push_back(Part{q, r, c, 0, steps_of(o->mats[q].m), 0, 1, 0});
                 cl.next_end = (int64_t)parts.size();
             }
         }
@@ -922,7 +1325,8 @@ int allocate(choco_muon* o, const std::vector<Unit>& units, const std::vector<Pa
     const int64_t n = (int64_t)o->mats.size();
     const int64_t mats = carve<Matrix>(at, n), un = carve<Unit>(at, (int64_t)units.size()), pa = carve<Part>(at, (int64_t)parts.size()),
                   bl = carve<Block>(at, (int64_t)blocks.size()), pt = carve<double>(at, o->nunits), done = carve<uint32_t>(at, n),
-                  err = carve<uint32_t>(at, 1), sc = carve<Scale>(at, n);
+                  err = carve<uint32_t>(at, 1), arr = carve<uint32_t>(at, o->split_tiles), sc = carve<Scale>(at, n), sm = carve<int32_t>(at, (int64_t)o->small.size()),
+                  sp = carve<float>(at, o->split_tiles * kMostSplits * kSide * kSide);
     at = (at + 1023) / 1024 * 1024;
     const int64_t wk = at;
     at += work;
@@ -936,6 +1340,9 @@ int allocate(choco_muon* o, const std::vector<Unit>& units, const std::vector<Pa
     o->d_done = reinterpret_cast<uint32_t*>(base + done);
     o->d_errors = reinterpret_cast<uint32_t*>(base + err);
     o->d_scale = reinterpret_cast<Scale*>(base + sc);
+    o->d_small = reinterpret_cast<int32_t*>(base + sm);
+    o->d_arrived = reinterpret_cast<uint32_t*>(base + arr);
+    o->d_split = reinterpret_cast<float*>(base + sp);
     o->d_work = base + wk;
     cudaStream_t st;
     if (cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking) != cudaSuccess) return CHOCO_ERR_CUDA;
@@ -943,11 +1350,14 @@ int allocate(choco_muon* o, const std::vector<Unit>& units, const std::vector<Pa
         return from.empty() || cudaMemcpyAsync(to, from.data(), sizeof(from[0]) * from.size(), cudaMemcpyHostToDevice, st) == cudaSuccess;
     };
     bool ok = cudaMemsetAsync(o->d_done, 0, (size_t)(sc - done), st) == cudaSuccess; // counts and errors
-    ok = ok && send(o->d_mats, o->mats) && send(o->d_units, units) && send(o->d_parts, parts) && send(o->d_blocks, blocks);
+    ok = ok && send(o->d_mats, o->mats) && send(o->d_units, units) && send(o->d_small, o->small) && send(o->d_parts, parts) && send(o->d_blocks, blocks);
     ok = cudaStreamSynchronize(st) == cudaSuccess && ok;
     cudaStreamDestroy(st);
     if (!ok) return CHOCO_ERR_CUDA;
-    return allow_shared<1>() == cudaSuccess && allow_shared<2>() == cudaSuccess ? CHOCO_OK : CHOCO_ERR_CUDA;
+    return allow_shared<1>() == cudaSuccess && allow_shared<2>() == cudaSuccess &&
+                   cudaFuncSetAttribute((const void*)small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallShared) == cudaSuccess
+               ? CHOCO_OK
+               : CHOCO_ERR_CUDA;
 }
 
 cudaError_t launch_products(const choco_muon* o, const Wave& w, int kind, int step, cudaStream_t st)
@@ -957,10 +1367,11 @@ cudaError_t launch_products(const choco_muon* o, const Wave& w, int kind, int st
     for (int three = 0; three < 2; ++three)
         for (int pairs = 0; pairs < 2; ++pairs) {
             const Class& cl = w.classes[three][pairs];
-            const int64_t begin = kind == kNext ? cl.next : cl.symmetric, end = kind == kNext ? cl.next_end : cl.symmetric_end;
+            const int64_t begin = kind == kNext ? cl.next : kind == kSquare ? cl.gram_end : cl.symmetric;
+            const int64_t end = kind == kNext ? cl.next_end : kind == kSquare ? cl.symmetric_end : cl.gram_end;
             if (begin == end || e != cudaSuccess) continue;
             const ProductArgs a = {o->d_mats, o->d_parts + begin, o->d_work, o->d_errors, (int32_t)(end - begin), (float)p.a, (float)p.b, (float)p.c,
-                                   step & 1, three || step == 0 ? 2 : 1};
+                                   step & 1, o->d_split, o->d_arrived, three || step == 0 ? 2 : 1};
             const Launch l = pairs ? launch_of<2>(kind, three, step == 0) : launch_of<1>(kind, three, step == 0);
             const int64_t most = (int64_t)o->sms * l.blocks / (pairs + 1);
             e = launch_overlapped(l.kernel, dim3((unsigned)(std::min(end - begin, most) * (pairs + 1))), dim3(l.threads), l.shared, st, HotRange{}, a);
@@ -971,11 +1382,11 @@ cudaError_t launch_products(const choco_muon* o, const Wave& w, int kind, int st
 int run(choco_muon* o, float* m, double lr, const float* factor, bool update, cudaStream_t st)
 {
     const choco_muon_params& p = o->params;
-    if (o->nunits == 0) return CHOCO_OK;
     const MomentArgs ma = {o->d_mats, o->d_units, m, factor, o->d_partial, o->d_done, o->d_scale, (float)p.beta, (float)(1.0 - p.beta), p.nesterov};
-    cudaError_t e = launch_overlapped(moment_kernel, dim3((unsigned)o->nunits), dim3(kUnitThreads), 0, st, HotRange{}, ma);
+    TileArgs ta = {o->d_mats, nullptr, o->d_work, o->d_scale, m, factor, (float)p.beta, (float)(1.0 - p.beta), (float)lr, p.nesterov, 0, 0, update};
+    cudaError_t e = cudaSuccess;
+    if (o->nunits > 0) e = launch_overlapped(moment_kernel, dim3((unsigned)o->nunits), dim3(kUnitThreads), 0, st, HotRange{}, ma);
     for (const Wave& w : o->waves) {
-        TileArgs ta = {o->d_mats, nullptr, o->d_work, o->d_scale, m, factor, (float)p.beta, (float)(1.0 - p.beta), (float)lr, p.nesterov, 0, 0, update};
         auto tiles = [&](void (*kernel)(TileArgs)) {
             for (int three = 0; three < 2; ++three) {
                 if (w.blocks[three] == w.blocks_end[three] || e != cudaSuccess) continue;
@@ -990,6 +1401,10 @@ int run(choco_muon* o, float* m, double lr, const float* factor, bool update, cu
                 if (e == cudaSuccess) e = launch_products(o, w, kind, k, st);
         ta.which = p.steps & 1;
         tiles(apply_kernel);
+    }
+    if (!o->small.empty() && e == cudaSuccess) {
+        const SmallArgs sa = {ma, ta, o->d_small, o->d_errors, (float)p.a, (float)p.b, (float)p.c, p.steps};
+        e = launch_overlapped(small_kernel, dim3((unsigned)o->small.size()), dim3(kSmallThreads), (size_t)o->small_shared, st, HotRange{}, sa);
     }
     return status_of(e);
 }
@@ -1015,13 +1430,13 @@ int choco_muon_init(choco_muon** out, int32_t n_matrices, const choco_muon_matri
         std::vector<Part> parts;
         std::vector<Block> blocks;
         int64_t work = 0;
+        if (cudaGetDevice(&o->device) != cudaSuccess || cudaDeviceGetAttribute(&o->sms, cudaDevAttrMultiProcessorCount, o->device) != cudaSuccess)
+            o->sms = 0; // (arguments are refused before the missing device is)
         rc = plan(o, n_matrices, matrices, units, parts, blocks, &work);
         if (rc == CHOCO_OK && overlap(o)) rc = CHOCO_ERR_INVALID_ARG;
         for (const Matrix& t : o->mats)
             if (rc == CHOCO_OK && is_written(o, t, t.g)) rc = CHOCO_ERR_INVALID_ARG;
-        if (rc == CHOCO_OK && (cudaGetDevice(&o->device) != cudaSuccess ||
-                               cudaDeviceGetAttribute(&o->sms, cudaDevAttrMultiProcessorCount, o->device) != cudaSuccess))
-            rc = CHOCO_ERR_CUDA;
+        if (rc == CHOCO_OK && o->sms == 0) rc = CHOCO_ERR_CUDA;
         if (rc == CHOCO_OK) rc = allocate(o, units, parts, blocks, work);
     } catch (const std::exception&) {
         rc = CHOCO_ERR_ALLOC;

@@ -26,7 +26,14 @@ __device__ __forceinline__ void tmem_free(uint32_t base, uint32_t columns)
     else
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns) : "memory");
 }
-// 32 or 64 columns of this warp's 32 lanes; the warp's lanes are those of its rank modulo 4
+// 8, 32 or 64 columns of this warp's 32 lanes; the warp's lanes are those of its rank modulo 4
+__device__ __forceinline__ void tmem_load8(uint32_t addr, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(addr)
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32])
 {
     asm volatile(
@@ -59,6 +66,15 @@ __device__ __forceinline__ void tmem_load64(uint32_t addr, uint32_t (&r)[64])
 }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// One thread of a converged warp.  Copies and products take their operands from registers of the whole warp: issued from code
+// that lane 0 alone runs each one costs some hundred cycles more than from a warp that runs it together and elects the issuer.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
 
 // ------------------------------------------------------------------------------------ operands
 // Tiles are rows of 128 bytes (64 halves), 16-byte pieces of a row exchanged by the row's last three bits: piece c of row r
@@ -111,15 +127,6 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity)
     for (uint32_t i = 0; i < kSpinLimit; ++i)
         if (mbar_try_wait(bar, parity)) return true;
     return false;
-}
-__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) // without waiting
-{
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(ok)
-                 : "r"(smem_u32(bar)), "r"(parity)
-                 : "memory");
-    return ok != 0;
 }
 // Arrive at the barrier of CTA `rank` of the cluster that lies where `bar` lies in this one.  Says that copies have landed or tensor
 // memory has been read, neither of which needs the flush of a release to the cluster (which cost 0.8 us each time).
