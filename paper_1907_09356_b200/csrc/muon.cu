@@ -60,6 +60,7 @@ struct Matrix {
     int8_t x_dtype, g_dtype, copy_dtype;
     bool tall;              // rows > cols
     bool whole;             // rows of g behind one another, and its elements in aligned fours
+    bool aligned;           // rows of all its arrays start on 16-byte boundaries
 };
 struct Unit {
     int32_t matrix;
@@ -264,91 +265,122 @@ __device__ __forceinline__ void join8(uint4 hi, uint4 lo, float* v, bool has_lo)
     }
 }
 
-// Eight neighbouring elements, of which the first `valid` are there (others: 0): one or two accesses of 16 bytes where the address allows
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, int valid, float* v)
+// N neighbouring elements, of which the first `valid` are there (others: 0): accesses of up to 16 bytes where the address allows
+template <int N, typename T>
+__device__ __forceinline__ void load_some(const T* p, int valid, float* v)
 {
-    if (valid >= 8 && ((uintptr_t)p & 15) == 0) {
-        Raw<T, 8> r;
+    constexpr int kAlign = N * (int)sizeof(T) < 16 ? N * (int)sizeof(T) : 16;
+    if (valid >= N && ((uintptr_t)p & (kAlign - 1)) == 0) {
+        Raw<T, N> r;
         load_raw(r, p);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = raw_get(r, q);
+        for (int q = 0; q < N; ++q) v[q] = raw_get(r, q);
     } else {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = q < valid ? to_float(p[q]) : 0.f;
+        for (int q = 0; q < N; ++q) v[q] = q < valid ? to_float(p[q]) : 0.f;
     }
 }
-__device__ __forceinline__ void load8(const void* p, int64_t at, int32_t dtype, int valid, float* v)
+template <int N>
+__device__ __forceinline__ void load_some(const void* p, int64_t at, int32_t dtype, int valid, float* v)
 {
-    if (dtype == CHOCO_F32) load8(static_cast<const float*>(p) + at, valid, v);
-    else if (dtype == CHOCO_BF16) load8(static_cast<const __nv_bfloat16*>(p) + at, valid, v);
-    else load8(static_cast<const __half*>(p) + at, valid, v);
+    if (dtype == CHOCO_F32) load_some<N>(static_cast<const float*>(p) + at, valid, v);
+    else if (dtype == CHOCO_BF16) load_some<N>(static_cast<const __nv_bfloat16*>(p) + at, valid, v);
+    else load_some<N>(static_cast<const __half*>(p) + at, valid, v);
 }
-template <typename T>
-__device__ __forceinline__ void store8(T* p, int valid, const float* v)
+template <int N, typename T>
+__device__ __forceinline__ void store_some(T* p, int valid, const float* v)
 {
-    if (valid >= 8 && ((uintptr_t)p & 15) == 0) {
-        store_vec<T, 8>(p, v);
+    constexpr int kAlign = N * (int)sizeof(T) < 16 ? N * (int)sizeof(T) : 16;
+    if (valid >= N && ((uintptr_t)p & (kAlign - 1)) == 0) {
+        store_vec<T, N>(p, v);
     } else {
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
+        for (int q = 0; q < N; ++q)
             if (q < valid) p[q] = from_float<T>(v[q]);
     }
 }
-__device__ __forceinline__ void store8(void* p, int64_t at, int32_t dtype, int valid, const float* v)
+template <int N>
+__device__ __forceinline__ void store_some(void* p, int64_t at, int32_t dtype, int valid, const float* v)
 {
-    if (dtype == CHOCO_F32) store8(static_cast<float*>(p) + at, valid, v);
-    else if (dtype == CHOCO_BF16) store8(static_cast<__nv_bfloat16*>(p) + at, valid, v);
-    else store8(static_cast<__half*>(p) + at, valid, v);
+    if (dtype == CHOCO_F32) store_some<N>(static_cast<float*>(p) + at, valid, v);
+    else if (dtype == CHOCO_BF16) store_some<N>(static_cast<__nv_bfloat16*>(p) + at, valid, v);
+    else store_some<N>(static_cast<__half*>(p) + at, valid, v);
 }
 // U from (row, col) on
-__device__ __forceinline__ void update8(const TileArgs& a, const Matrix& t, int row, int col, int valid, float c, float* u)
+template <int N>
+__device__ __forceinline__ void update_some(const TileArgs& a, const Matrix& t, int row, int col, int valid, float c, float* u)
 {
-    load8(t.g, (int64_t)row * t.g_ld + col, t.g_dtype, valid, u);
+    load_some<N>(t.g, (int64_t)row * t.g_ld + col, t.g_dtype, valid, u);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) u[q] *= c;
+    for (int q = 0; q < N; ++q) u[q] *= c;
     if (!a.m) return;
-    float m[8];
-    load8(a.m + t.state + (int64_t)row * t.cols + col, valid, m);
+    float m[N];
+    load_some<N>(a.m + t.state + (int64_t)row * t.cols + col, valid, m);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) u[q] = a.nesterov ? averaged(m[q], u[q], a.beta, a.omb) : m[q];
+    for (int q = 0; q < N; ++q) u[q] = a.nesterov ? averaged(m[q], u[q], a.beta, a.omb) : m[q];
 }
 // x (and its copy) from (row, col) on
-__device__ __forceinline__ void apply8(const TileArgs& a, const Matrix& t, int row, int col, int valid, float* o)
+template <int N>
+__device__ __forceinline__ void apply_some(const TileArgs& a, const Matrix& t, int row, int col, int valid, float* o)
 {
     const int64_t at = (int64_t)row * t.x_ld + col;
     if (a.update) {
-        float x[8];
-        load8(t.x, at, t.x_dtype, valid, x);
+        float x[N];
+        load_some<N>(t.x, at, t.x_dtype, valid, x);
         const float lr = a.lr * t.lr_scale, decay = a.lr * t.weight_decay;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) o[q] = x[q] - (o[q] * lr + x[q] * decay);
-        if (t.copy) store8(t.copy, (int64_t)row * t.copy_ld + col, t.copy_dtype, valid, o);
+        for (int q = 0; q < N; ++q) o[q] = x[q] - (o[q] * lr + x[q] * decay);
+        if (t.copy) store_some<N>(t.copy, (int64_t)row * t.copy_ld + col, t.copy_dtype, valid, o);
     }
-    store8(t.x, at, t.x_dtype, valid, o);
+    store_some<N>(t.x, at, t.x_dtype, valid, o);
 }
 
-// A tile of X_0: 128 rows x 64 columns of U, turned where the matrix is tall.
+// A turned tile in shared memory, columns as rows: a gap after every eight elements keeps threads that take eight each on banks of their own
+constexpr int kTurnRow = kSide + kSide / 8 + 1;
+__device__ __forceinline__ int turned_at(int row) { return row + (row >> 3); }
+
+// Where a tile's matrix has its elements, N neighbours to a thread: along rows of the tile, or along its columns where the matrix is tall
+template <int N, typename Work>
+__device__ __forceinline__ void each_place(const Matrix& t, int row0, int col0, Work work) // work(row of the tile, column, how many are there)
+{
+    constexpr int kAlong = kSide / N, kAcross = kHalves / N, kUnroll = 16 / N;
+#pragma unroll kUnroll
+    for (int e = threadIdx.x; e < kSide * kHalves / N; e += kTileThreads2) {
+        const int r = t.tall ? e % kAlong * N : e / kAcross, q = t.tall ? e / kAlong : e % kAcross * N;
+        work(r, q, row0 + r < t.m && col0 + q < t.k ? (t.tall ? t.m - row0 - r : t.k - col0 - q) : 0);
+    }
+}
+template <int N>
+__device__ __forceinline__ void apply_turned(const TileArgs& a, const Matrix& t, int row0, int col0, float (*turn)[kTurnRow])
+{
+    each_place<N>(t, row0, col0, [&](int r, int q, int valid) {
+        if (valid <= 0) return;
+        float o[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) o[k] = turn[t.tall ? q : q + k][turned_at(t.tall ? r + k : r)];
+        apply_some<N>(a, t, t.tall ? col0 + q : row0 + r, t.tall ? row0 + r : col0 + q, valid, o);
+    });
+}
+
+// A tile of X_0: 128 rows x 64 columns of U; those of tall matrices go by way of shared memory.
 __global__ void __launch_bounds__(kTileThreads2) cut_kernel(TileArgs a)
 {
-    __shared__ float turn[kHalves][kSide + 1];
+    __shared__ float turn[kHalves][kTurnRow];
     const Block bl = a.blocks[blockIdx.x];
     const Matrix& t = a.mats[bl.matrix];
     const int row0 = bl.row * kSide, col0 = bl.col * kHalves;
     allow_next_kernel();
     wait_for_previous_kernel();
     const Scale sc = a.scale[bl.matrix];
-    const bool live = sc.second != 0.f;     // (true for NaN)
+    const bool live = sc.second != 0.f; // (true for NaN)
     const float c = a.factor ? a.factor[t.group] : 1.f;
-    if (t.tall && live) {
-#pragma unroll 2
-        for (int e = threadIdx.x; e < kHalves * kSide / 8; e += kTileThreads2) {
-            const int q = e / (kSide / 8), r = e % (kSide / 8) * 8;
+    if (live && t.tall) {
+        each_place<8>(t, row0, col0, [&](int r, int q, int valid) {
             float u[8] = {};
-            if (col0 + q < t.k && row0 + r < t.m) update8(a, t, col0 + q, row0 + r, t.m - row0 - r, c, u);
+            if (valid > 0) update_some<8>(a, t, col0 + q, row0 + r, valid, c, u);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) turn[q][r + k] = u[k];
-        }
+            for (int k = 0; k < 8; ++k) turn[q][turned_at(r + k)] = u[k];
+        });
         __syncthreads();
     }
     uint8_t* to = a.work + t.at[0] + ((int64_t)bl.row * t.nb + bl.col) * 2 * kTileBytes;
@@ -358,9 +390,9 @@ __global__ void __launch_bounds__(kTileThreads2) cut_kernel(TileArgs a)
         float v[8] = {};
         if (live && t.tall) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = turn[piece * 8 + q][r];
+            for (int q = 0; q < 8; ++q) v[q] = turn[piece * 8 + q][turned_at(r)];
         } else if (live && row0 + r < t.m && col < t.k) {
-            update8(a, t, row0 + r, col, t.k - col, c, v);
+            update_some<8>(a, t, row0 + r, col, t.k - col, c, v);
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = v[q] * sc.first * sc.second;
@@ -371,10 +403,11 @@ __global__ void __launch_bounds__(kTileThreads2) cut_kernel(TileArgs a)
     }
 }
 
-// The last X of a matrix, tile by tile, to where it goes.
+// The last X of a matrix, tile by tile, to where it goes: by way of shared memory where the matrix is tall, and in pairs of elements, so that a
+// warp's accesses lie side by side, where rows are off 16-byte boundaries (32 of 2600 x 650 bf16: 123 -> 100 us).
 __global__ void __launch_bounds__(kTileThreads2) apply_kernel(TileArgs a)
 {
-    __shared__ float turn[kHalves][kSide + 1];
+    __shared__ float turn[kHalves][kTurnRow];
     const Block bl = a.blocks[blockIdx.x];
     const Matrix& t = a.mats[bl.matrix];
     const int row0 = bl.row * kSide, col0 = bl.col * kHalves;
@@ -383,6 +416,7 @@ __global__ void __launch_bounds__(kTileThreads2) apply_kernel(TileArgs a)
     if (a.factor && !isfinite(a.factor[t.group])) return;
     const uint8_t* from = a.work + t.at[a.which] + ((int64_t)bl.row * t.nb + bl.col) * a.planes * kTileBytes;
     const float unscale = exp2f((float)-t.ex);
+    const bool straight = t.aligned && !t.tall;
     const int piece = threadIdx.x & 7, col = col0 + piece * 8;
 #pragma unroll 2
     for (int r = threadIdx.x >> 3; r < kSide; r += kTileThreads2 / 8) {
@@ -393,21 +427,14 @@ __global__ void __launch_bounds__(kTileThreads2) apply_kernel(TileArgs a)
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             v[q] *= unscale;
-            if (t.tall) turn[piece * 8 + q][r] = v[q];
+            if (!straight) turn[piece * 8 + q][turned_at(r)] = v[q];
         }
-        if (!t.tall && row0 + r < t.m && col < t.k) apply8(a, t, row0 + r, col, t.k - col, v);
+        if (straight && row0 + r < t.m && col < t.k) apply_some<8>(a, t, row0 + r, col, t.k - col, v);
     }
-    if (!t.tall) return;
+    if (straight) return;
     __syncthreads();
-#pragma unroll 2
-    for (int e = threadIdx.x; e < kHalves * kSide / 8; e += kTileThreads2) {
-        const int q = e / (kSide / 8), r = e % (kSide / 8) * 8;
-        if (col0 + q >= t.k || row0 + r >= t.m) continue;
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = turn[q][r + k];
-        apply8(a, t, col0 + q, row0 + r, t.m - row0 - r, v);
-    }
+    if (t.aligned) apply_turned<8>(a, t, row0, col0, turn);
+    else apply_turned<2>(a, t, row0, col0, turn);
 }
 
 // ---------------------------------------------------------------------------------------- products
@@ -857,7 +884,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
             for (int e = tid; e < l.rows * l.blocks * 8; e += kSmallThreads) {
                 const int row = e / (l.blocks * 8), piece = e % (l.blocks * 8);
                 float v[8] = {};
-                if (live && row < t.m && piece * 8 < t.k) update8(a.tile, t, row, piece * 8, t.k - piece * 8, c, v);
+                if (live && row < t.m && piece * 8 < t.k) update_some<8>(a.tile, t, row, piece * 8, t.k - piece * 8, c, v);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) v[q] = v[q] * sc.first * sc.second;
                 put(x_tile(piece >> 3, 0), row, piece & 7, v);
@@ -867,7 +894,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
             for (int e = tid; e < l.blocks * kHalves * (l.rows / 8); e += kSmallThreads) {
                 const int col = e % (l.blocks * kHalves), row = e / (l.blocks * kHalves) * 8;
                 float v[8] = {};
-                if (live && row < t.m && col < t.k) update8(a.tile, t, col, row, t.m - row, c, v);
+                if (live && row < t.m && col < t.k) update_some<8>(a.tile, t, col, row, t.m - row, c, v);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
                     const float u = v[q] * sc.first * sc.second;
@@ -999,7 +1026,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
                 join8(*reinterpret_cast<const uint4*>(at), *reinterpret_cast<const uint4*>(at + l.tile), v, true);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) v[q] *= unscale;
-                apply8(a.tile, t, r, piece * 8, t.k - piece * 8, v);
+                apply_some<8>(a.tile, t, r, piece * 8, t.k - piece * 8, v);
             }
         } else {
             for (int e = tid; e < l.blocks * kHalves * (l.rows / 8); e += kSmallThreads) {
@@ -1011,7 +1038,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
                     const uint8_t* at = x_tile(col >> 6, 0) + piece_at(r + q, (col & 63) >> 3) + (col & 7) * 2;
                     v[q] = (__half2float(*reinterpret_cast<const __half*>(at)) + __half2float(*reinterpret_cast<const __half*>(at + l.tile))) * unscale;
                 }
-                apply8(a.tile, t, col, r, t.m - r, v);
+                apply_some<8>(a.tile, t, col, r, t.m - r, v);
             }
         }
     }
@@ -1158,6 +1185,14 @@ int64_t carve(int64_t& at, int64_t count)
     return here;
 }
 
+// What depends on the gradient's address
+void look_at_gradient(Matrix& t)
+{
+    t.whole = (t.g_ld == t.cols || t.rows == 1) && aligned_to(t.g, 4 * dtype_size(t.g_dtype));
+    auto rows = [&](const void* p, int64_t ld, int32_t dtype) { return aligned_to(p, 16) && (t.rows == 1 || ld * dtype_size(dtype) % 16 == 0); };
+    t.aligned = rows(t.x, t.x_ld, t.x_dtype) && rows(t.g, t.g_ld, t.g_dtype) && rows(nullptr, t.cols, CHOCO_F32) && (!t.copy || rows(t.copy, t.copy_ld, t.copy_dtype));
+}
+
 // Fills the host tables.  Throws std::bad_alloc.
 int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit>& units, std::vector<Part>& parts, std::vector<Block>& blocks,
          int64_t* work)
@@ -1195,7 +1230,7 @@ int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit
         t.group = q.group;
         t.weight_decay = (float)q.weight_decay; t.lr_scale = (float)q.lr_scale;
         t.x_dtype = (int8_t)q.x_dtype; t.g_dtype = (int8_t)q.g_dtype; t.copy_dtype = (int8_t)q.copy_dtype;
-        t.whole = (t.g_ld == t.cols || t.rows == 1) && aligned_to(q.g, 4 * dtype_size(q.g_dtype));
+        look_at_gradient(t);
         t.unit0 = (int32_t)units.size();
         const int64_t count = (int64_t)t.rows * t.cols;
         const bool small = is_small(t.m, t.k);
@@ -1479,7 +1514,7 @@ int choco_muon_set_grads(choco_muon* opt, const void* const* g, void* stream)
         std::vector<Matrix> mats = opt->mats;
         for (size_t i = 0; i < mats.size(); ++i) {
             mats[i].g = g[i];
-            mats[i].whole = (mats[i].g_ld == mats[i].cols || mats[i].rows == 1) && aligned_to(g[i], 4 * dtype_size(mats[i].g_dtype));
+            look_at_gradient(mats[i]);
         }
         if (cudaStreamSynchronize(st) != cudaSuccess) return CHOCO_ERR_CUDA;
         opt->broken = true; // until the table on the device is whole
