@@ -159,7 +159,7 @@ __device__ __forceinline__ Scale scale_of(double sum, int ex)
         const double f = ldexp(1.0, ex) / sqrt(sum);     // from 1e-44 to 1e49: in two factors where float32 ends
         const double pre = f > 1e30 ? 0x1p100 : f < 1e-30 ? 0x1p-100 : 1.0;
         s.first = (float)pre;
-        s.second = (float)(f / pre);
+        s.second = isfinite(sum) ? (float)(f / pre) : __int_as_float(0x7fc00000); // (not 0, which stands for matrices left alone)
     }
     return s;
 }
