@@ -28,6 +28,7 @@ constexpr int kNormThreads = 128;
 constexpr int kNormWarps = kNormThreads / 32;
 constexpr int kNormBlocks = 4;          // to an SM, by registers
 constexpr int kAtOnce = 4;              // pixels whose loads a thread has under way where it keeps no more
+constexpr int kApart = 64;             // pixels that a thread adds up on their own: what is rounded grows with the length of a sum
 constexpr int kWaits = 2;               // groups in which a thread's copies to shared memory are waited for
 constexpr int64_t kMostSlice = 2048;    // channels of a slice, and of a group: their sums are in shared memory
 
@@ -463,12 +464,12 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) forward_kernel(Norm
                     if (VEC > 1) l.channel[c0 + 2 * p + 1].w = v.y;
                 }
             }
-            auto take = [&](const Raw<XT, VEC>& r) {
+            auto take = [&](const Raw<XT, VEC>& r, Pair* t1, Pair* t2) {
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
                     const Pair d = add2(raw_pair(r, p), pivot[p]);
-                    s1[p] = add2(s1[p], d);
-                    s2[p] = fma2(d, d, s2[p]);
+                    t1[p] = add2(t1[p], d);
+                    t2[p] = fma2(d, d, t2[p]);
                 }
             };
             uint32_t slot = slot_of<XT, VEC>(l.kept, round * sh.steps);
@@ -480,18 +481,28 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) forward_kernel(Norm
                 for (int i = group_begin(kept, g); i < end; ++i) {
                     Raw<XT, VEC> r;
                     kept_raw(r, slot);
-                    take(r);
+                    take(r, s1, s2);
                     slot += kSlot<XT, VEC>;
                 }
             }
-            for (int i0 = kept; i0 < sh.mine; i0 += kAtOnce) {
-                Raw<XT, VEC> r[kAtOnce];
+            for (int begin = kept; begin < sh.mine; begin += kApart) {
+                Pair t1[NP], t2[NP];
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j)
-                    if (i0 + j < sh.mine) load_raw(r[j], from + (i0 + j) * from_step);
+                for (int p = 0; p < NP; ++p) t1[p] = t2[p] = pair_of(0.f, 0.f);
+                for (int i0 = begin; i0 < min(begin + kApart, sh.mine); i0 += kAtOnce) {
+                    Raw<XT, VEC> r[kAtOnce];
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j)
-                    if (i0 + j < sh.mine) take(r[j]);
+                    for (int j = 0; j < kAtOnce; ++j)
+                        if (i0 + j < sh.mine) load_raw(r[j], from + (i0 + j) * from_step);
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j)
+                        if (i0 + j < sh.mine) take(r[j], t1, t2);
+                }
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    s1[p] = add2(s1[p], t1[p]);
+                    s2[p] = add2(s2[p], t2[p]);
+                }
             }
         }
         add_up(sh, a, round, s1, s2, l.red, l.parts, cluster_rank());
@@ -548,7 +559,6 @@ __device__ __forceinline__ float4 channel_of(const NormArgs& a, float2 st, int64
 template <typename XT, typename YT, int VEC, int ACT>
 struct Slopes {
     static constexpr int NP = (VEC + 1) / 2;
-    [[maybe_unused]] static constexpr bool kFast = sizeof(XT) == 2 && sizeof(YT) == 2;
     static constexpr bool kPacked = ACT == kRelu && sizeof(XT) == 2 && std::is_same_v<XT, YT> && VEC > 1;
     Pair mean[NP], scale[NP], shift[NP];
     uint32_t border[kPacked ? NP : 1], sign[kPacked ? NP : 2 * NP];
@@ -600,6 +610,7 @@ struct Slopes {
         } else if constexpr (ACT == kNone) {
             return raw_pair(ry, p);
         } else {
+            constexpr bool kFast = sizeof(XT) == 2 && sizeof(YT) == 2;
             const float2 z = floats_of(fma2(add2(x, mean[p]), scale[p], shift[p])), dy = floats_of(raw_pair(ry, p));
             return pair_of(dy.x * slope_of<ACT, kFast>(z.x), dy.y * slope_of<ACT, kFast>(z.y));
         }
@@ -651,7 +662,7 @@ __device__ __forceinline__ void backward_pass(const NormArgs& a, const Share<VEC
                     if constexpr (kFolds) s1[p] = fma2(sl.mean[p], s2[p], s1[p]);
                 }
             }
-            auto take = [&](const Raw<XT, VEC>& rx, const Raw<YT, VEC>& ry) {
+            auto take = [&](const Raw<XT, VEC>& rx, const Raw<YT, VEC>& ry, Pair* t1, Pair* t2) {
                 Pair f[NP];
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
@@ -659,8 +670,8 @@ __device__ __forceinline__ void backward_pass(const NormArgs& a, const Share<VEC
                     if (FINISH) {
                         f[p] = fma2(dz, sl.scale[p], fma2(kFolds ? xp : add2(xp, sl.mean[p]), s2[p], s1[p]));
                     } else {
-                        s1[p] = add2(s1[p], dz);
-                        s2[p] = fma2(dz, add2(xp, sl.mean[p]), s2[p]);
+                        t1[p] = add2(t1[p], dz);
+                        t2[p] = fma2(dz, add2(xp, sl.mean[p]), t2[p]);
                     }
                 }
                 if (FINISH) {
@@ -683,26 +694,38 @@ __device__ __forceinline__ void backward_pass(const NormArgs& a, const Share<VEC
                         sl.mask(rx, ry);
                         keep_raw(ry, slot_y);                    // for the second pass
                     }
-                    take(rx, ry);
+                    take(rx, ry, s1, s2);
                     slot_x += kSlot<XT, VEC>;
                     slot_y += kSlot<YT, VEC>;
                 }
             }
-            for (int i0 = kept; i0 < sh.mine; i0 += kAtOnce) {
-                Raw<XT, VEC> rx[kAtOnce];
-                Raw<YT, VEC> ry[kAtOnce];
+            for (int begin = kept; begin < sh.mine; begin += kApart) {
+                Pair t1[NP], t2[NP];
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j)
-                    if (i0 + j < sh.mine) {
-                        load_raw(rx[j], from_x + (i0 + j) * step_x);
-                        load_raw(ry[j], from_y + (i0 + j) * step_y);
-                    }
+                for (int p = 0; p < NP; ++p) t1[p] = t2[p] = pair_of(0.f, 0.f);
+                for (int i0 = begin; i0 < min(begin + kApart, sh.mine); i0 += kAtOnce) {
+                    Raw<XT, VEC> rx[kAtOnce];
+                    Raw<YT, VEC> ry[kAtOnce];
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j)
-                    if (i0 + j < sh.mine) {
-                        sl.mask(rx[j], ry[j]);
-                        take(rx[j], ry[j]);
+                    for (int j = 0; j < kAtOnce; ++j)
+                        if (i0 + j < sh.mine) {
+                            load_raw(rx[j], from_x + (i0 + j) * step_x);
+                            load_raw(ry[j], from_y + (i0 + j) * step_y);
+                        }
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j)
+                        if (i0 + j < sh.mine) {
+                            sl.mask(rx[j], ry[j]);
+                            take(rx[j], ry[j], t1, t2);
+                        }
+                }
+                if (!FINISH) {
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) {
+                        s1[p] = add2(s1[p], t1[p]);
+                        s2[p] = add2(s2[p], t2[p]);
                     }
+                }
             }
         }
         if (!FINISH) add_up(sh, a, round, s1, s2, l.red, l.parts, cluster_rank());
