@@ -1,7 +1,7 @@
 """A small language model trained by n workers that gossip: token lookup, tied output layer, gradient
-of the lookup, per-worker clipping, AdamW and the CHOCO-Gossip step, all on the rows of X and G.
+of the lookup, per-worker clipping, AdamW (the square matrix by Muon, if asked) and the CHOCO-Gossip step, all on the rows of X and G.
 
-    python examples/language_model.py [--workers 8] [--steps 200] [--bits 8] [--q topk]
+    python examples/language_model.py [--workers 8] [--steps 200] [--bits 8] [--q topk] [--optimizer muon]
 
 The model is a bigram model: logits = scale * E[token] W E^T with one table E for input and output and a
 square matrix W, trained on the sequences of a random Markov chain, every worker on a chain of its
@@ -21,7 +21,7 @@ import workloads  # noqa: E402
 
 
 def train(workers=8, steps=200, bits=32, q="topk", vocab=512, dim=64, batch=16, length=33, lr=3e-3, gamma=None, clip=1.0, seed=0,
-          log=None):
+          log=None, optimizer="adamw"):
     """Returns (mean loss per step, consensus distance per step)."""
     if gamma is None:       # consensus stepsizes in the stable range of each operator
         gamma = {"topk": 0.1, "randk": 0.03, "qsgd": 0.1, "sign": 0.4, "identity": 1.0}[q]
@@ -42,7 +42,10 @@ def train(workers=8, steps=200, bits=32, q="topk", vocab=512, dim=64, batch=16, 
     count = batch * (length - 1)
     scale = dim ** 0.5
     emb = choco.Embedding(workers, vocab, dim, count, table_ld=d, scale=scale)
-    opt = choco.AdamW(X, G, off, weight_decay=[0.01, 0.01, 0.0], state_bits=bits, rounding="random" if bits == 8 else "nearest", seed=seed)
+    norms = choco.AdamW(None, G, off)                           # clipping looks at all layers
+    opt = choco.AdamW(X, G, off, weight_decay=[0.01, 0.01, 0.0], state_bits=bits, rounding="random" if bits == 8 else "nearest", seed=seed,
+                      layers=[0, 2] if optimizer == "muon" else None)
+    muon = choco.Muon(X, G, off, [None, (dim, dim), None], weight_decay=0.01) if optimizer == "muon" else None
     kw = dict(k=max(1, d // 20)) if q in ("topk", "randk") else dict(s=16, bucket=512) if q == "qsgd" else {}
     gossip = choco.Choco(w, d, q, seed=seed, **kw)
     choco.choco_set_carry(gossip.ctx, False)                    # AdamW changes X between two gossip steps
@@ -72,14 +75,19 @@ def train(workers=8, steps=200, bits=32, q="topk", vocab=512, dim=64, batch=16, 
         G[:, off[1]:off[2]] = (rows.transpose(1, 2) @ dhidden).flatten(1)
         G[:, off[2]:] = dhidden.sum(1)
         emb.backward(tokens, dhidden @ W.transpose(1, 2), G, accumulate=True)   # and the lookup's, added to it
-        opt.grad_norm(clip, norm, factor)
+        norms.grad_norm(clip, norm, factor)
         opt.step(lr, factor)
+        if muon:
+            muon.step(lr, factor)
         gossip.gossip_step(X, Xhat, S, gamma)
         distances.append(choco.choco_consensus_error(gossip.ctx, X))
         if log and (t % 20 == 0 or t == steps - 1):
             log(f"step {t:4d}  loss {losses[-1]:.4f}  consensus distance {distances[-1]:.4f}  largest norm {float(norm.max()):.3f}")
     emb.close()
+    norms.close()
     opt.close()
+    if muon:
+        muon.close()
     gossip.close()
     return np.asarray(losses), np.asarray(distances)
 
@@ -90,5 +98,6 @@ if __name__ == "__main__":
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--bits", type=int, choices=(8, 32), default=32)
     ap.add_argument("--q", choices=sorted(choco.Q_KINDS), default="topk")
+    ap.add_argument("--optimizer", choices=("adamw", "muon"), default="adamw")
     a = ap.parse_args()
-    train(a.workers, a.steps, a.bits, a.q, log=print)
+    train(a.workers, a.steps, a.bits, a.q, log=print, optimizer=a.optimizer)

@@ -900,22 +900,24 @@ def choco_group_norm_backward(gn, x, dy, weight, bias, mean, rstd, dx, dweight, 
     if mean is None or rstd is None:
         raise ChocoError("libchoco: mean and rstd of the forward call are needed", -1)
     _check_stats(gn, images, mean, rstd)
-    _check(load().choco_group_norm_backward(gn, images, pixels, ax, ay, ad, _ptr(weight), _ptr(bias), ld, kind, _ptr(mean), _ptr(rstd), _ptr(dweight), _ptr(dbias), gld, gkind,
-                                            1 if accumulate else 0, _stream_of(stream, gn.device)))
+    _check(load().choco_group_norm_backward(gn, images, pixels, ax, ay, ad, _ptr(weight), _ptr(bias), ld, kind, _ptr(mean), _ptr(rstd),
+                                            _ptr(dweight), _ptr(dbias), gld, gkind, 1 if accumulate else 0, _stream_of(stream, gn.device)))
 
 
 # --------------------------------------------------------------------------- convenience
 
 
-def adamw_layer_tensors(X, G, layer_off, weight_decay=0.0, lr_scale=1.0, copy=None):
+def adamw_layer_tensors(X, G, layer_off, weight_decay=0.0, lr_scale=1.0, copy=None, layers=None):
     """The list of tensors (worker by worker, layer by layer, group = worker) for rows of X and G
     [n, >= layer_off[-1]] cut at layer_off; weight_decay and lr_scale are numbers or one per layer.
-    X may be None (a list for norms only)."""
+    X may be None (a list for norms only).  layers: which of them are in the list (others are another optimizer's), all without it."""
     import numpy as np
     off = np.asarray(layer_off, dtype=np.int64)
-    n, layers = G.shape[0], len(off) - 1
+    which, n, layers = layers, G.shape[0], len(off) - 1
     if layers < 1 or off[0] != 0 or np.any(np.diff(off) < 0):
         raise ChocoError("libchoco: layer_off must start at 0 and not decrease", -1)
+    if which is not None and (len(which) == 0 or len(set(which)) < len(which) or min(which) < 0 or max(which) >= layers):
+        raise ChocoError(f"libchoco: layers must be different ones of 0 .. {layers - 1}, one at least", -1)
     t = np.zeros((n, layers), dtype=ADAMW_TENSOR)
     rows = np.arange(n, dtype=np.int64)[:, None]
     for name, a in (("x", X), ("g", G), ("copy", copy)):
@@ -931,7 +933,7 @@ def adamw_layer_tensors(X, G, layer_off, weight_decay=0.0, lr_scale=1.0, copy=No
     t["group"] = rows
     t["weight_decay"] = np.broadcast_to(np.asarray(weight_decay, dtype=np.float64), (layers,))[None]
     t["lr_scale"] = np.broadcast_to(np.asarray(lr_scale, dtype=np.float64), (layers,))[None]
-    return t.reshape(-1)
+    return (t if which is None else t[:, list(which)]).reshape(-1)
 
 
 def muon_layer_matrices(X, G, layer_off, shapes, weight_decay=0.0, lr_scale=None, copy=None):
@@ -1056,15 +1058,16 @@ class AdamW:
     Owns the handle and (unless `states` hands them over) the moments: (m, v), or with 8-bit
     moments (m, v, m_scale, v_scale), flat arrays in the layout choco.h gives.  With X = None only
     grad_norm can be called.  rounding: of 8-bit moments, "nearest" or "random" (drawn from `seed`); long
-    runs want "random", see choco_adamw_set_rounding."""
+    runs want "random", see choco_adamw_set_rounding.  layers: those that it has, where another optimizer (Muon) has the rest;
+    grad_norm then is that of these layers."""
 
     def __init__(self, X, G, layer_off, weight_decay=0.0, lr_scale=1.0, copy=None, beta1: float = 0.9,
                  beta2: float = 0.999, eps: float = 1e-8, state_bits: int = 32, states=None, step: int = 0,
-                 rounding: str = "nearest", seed: int = 0):
+                 rounding: str = "nearest", seed: int = 0, layers=None):
         import torch
         if rounding not in ("nearest", "random"):
             raise ChocoError(f"libchoco: rounding is nearest or random, not {rounding}", -1)
-        tensors = adamw_layer_tensors(X, G, layer_off, weight_decay, lr_scale, copy)
+        tensors = adamw_layer_tensors(X, G, layer_off, weight_decay, lr_scale, copy, layers)
         if G.get_device() != torch.cuda.current_device():
             raise ChocoError(f"libchoco: a handle belongs to the current device ({torch.cuda.current_device()}), and G is on {G.device}", -1)
         self.groups = G.shape[0]
