@@ -40,7 +40,7 @@ constexpr int kBlock = 256;                        // matrices start on multiple
 constexpr int kUnit = 4096;                        // elements of one block of the momentum kernel
 constexpr int kUnitThreads = 256;
 constexpr int kMostSplits = 4;                     // of a part of X X^T along K
-constexpr int kTileThreads2 = 256;                 // of the kernels that cut matrices into tiles and put them together
+constexpr int kCutThreads = 256;                  // of the kernels that cut matrices into tiles and put them together
 
 struct Matrix {
     void* x;
@@ -345,7 +345,7 @@ __device__ __forceinline__ void each_place(const Matrix& t, int row0, int col0, 
 {
     constexpr int kAlong = kSide / N, kAcross = kHalves / N, kUnroll = 16 / N;
 #pragma unroll kUnroll
-    for (int e = threadIdx.x; e < kSide * kHalves / N; e += kTileThreads2) {
+    for (int e = threadIdx.x; e < kSide * kHalves / N; e += kCutThreads) {
         const int r = t.tall ? e % kAlong * N : e / kAcross, q = t.tall ? e / kAlong : e % kAcross * N;
         work(r, q, row0 + r < t.m && col0 + q < t.k ? (t.tall ? t.m - row0 - r : t.k - col0 - q) : 0);
     }
@@ -363,7 +363,7 @@ __device__ __forceinline__ void apply_turned(const TileArgs& a, const Matrix& t,
 }
 
 // A tile of X_0: 128 rows x 64 columns of U; those of tall matrices go by way of shared memory.
-__global__ void __launch_bounds__(kTileThreads2) cut_kernel(TileArgs a)
+__global__ void __launch_bounds__(kCutThreads) cut_kernel(TileArgs a)
 {
     __shared__ float turn[kHalves][kTurnRow];
     const Block bl = a.blocks[blockIdx.x];
@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(kTileThreads2) cut_kernel(TileArgs a)
     uint8_t* to = a.work + t.at[0] + ((int64_t)bl.row * t.nb + bl.col) * 2 * kTileBytes;
     const int piece = threadIdx.x & 7, col = col0 + piece * 8;
 #pragma unroll 2
-    for (int r = threadIdx.x >> 3; r < kSide; r += kTileThreads2 / 8) {
+    for (int r = threadIdx.x >> 3; r < kSide; r += kCutThreads / 8) {
         float v[8] = {};
         if (live && t.tall) {
 #pragma unroll
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(kTileThreads2) cut_kernel(TileArgs a)
 
 // The last X of a matrix, tile by tile, to where it goes: by way of shared memory where the matrix is tall, and in pairs of elements, so that a
 // warp's accesses lie side by side, where rows are off 16-byte boundaries (32 of 2600 x 650 bf16: 123 -> 100 us).
-__global__ void __launch_bounds__(kTileThreads2) apply_kernel(TileArgs a)
+__global__ void __launch_bounds__(kCutThreads) apply_kernel(TileArgs a)
 {
     __shared__ float turn[kHalves][kTurnRow];
     const Block bl = a.blocks[blockIdx.x];
@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(kTileThreads2) apply_kernel(TileArgs a)
     const bool straight = t.aligned && !t.tall;
     const int piece = threadIdx.x & 7, col = col0 + piece * 8;
 #pragma unroll 2
-    for (int r = threadIdx.x >> 3; r < kSide; r += kTileThreads2 / 8) {
+    for (int r = threadIdx.x >> 3; r < kSide; r += kCutThreads / 8) {
         const uint4 hi = *reinterpret_cast<const uint4*>(from + piece_at(r, piece));
         const uint4 lo = a.planes == 2 ? *reinterpret_cast<const uint4*>(from + kTileBytes + piece_at(r, piece)) : make_uint4(0, 0, 0, 0);
         float v[8];
@@ -590,6 +590,7 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
     if (CG == 2) cluster_sync();
     tmem_fence_after();
     const uint32_t acc = tmem_at;
+    const Job<KIND, CG, L::kLeave> first_job(a, begin, rank);    // (the tables do not change: read while the kernel before ends)
     allow_next_kernel();
     wait_for_previous_kernel();
 
@@ -613,7 +614,7 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
         };
         uint32_t ch = 0;                                         // sets of sums so far
         for (int index = begin; index < a.count && ok; index += step) {
-            const Job<KIND, CG, L::kLeave> job(a, index, rank);
+            const Job<KIND, CG, L::kLeave> job = index == begin ? first_job : Job<KIND, CG, L::kLeave>(a, index, rank);
             const Matrix& t = *job.t;
             float v[L::kLeave ? kSide : 1];
 #pragma unroll
@@ -716,7 +717,7 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
             uint32_t n = 0;                                      // steps of 64 of K so far
             bool ok = true;
             for (int index = begin; index < a.count && ok; index += step) {
-                const Job<KIND, CG, L::kLeave> job(a, index, rank);
+                const Job<KIND, CG, L::kLeave> job = index == begin ? first_job : Job<KIND, CG, L::kLeave>(a, index, rank);
                 const uint8_t* x = a.work + job.t->at[a.which];
                 const uint8_t* first = KIND == kGram ? x : a.work + (KIND == kSquare ? job.t->s_at : job.t->b_at);
                 const bool load_b = job.has_b && !job.same;
@@ -753,7 +754,7 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
             uint32_t n = 0, ch = 0;
             bool ok = true;
             for (int index = begin; index < a.count && ok; index += step) {
-                const Job<KIND, CG, L::kLeave> job(a, index, rank);
+                const Job<KIND, CG, L::kLeave> job = index == begin ? first_job : Job<KIND, CG, L::kLeave>(a, index, rank);
                 for (int kb = 0; kb < job.nk; ++kb, ++n) {
                     const uint32_t s = n % ST;
                     if (CG == 2 && rank == 1) {                  // the other CTA of a pair tells the first what has come
@@ -809,7 +810,7 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
 
 // ---------------------------------------------------------------------------------------- small matrices
 // A matrix that fits a block's shared memory takes one launch for the whole step: momentum, norm, all products and the new
-// parameters, with X, S, T and B where the tensor cores read them.  (64 x 576, 18 launches: 187 us; this: TIME_SMALL us.)  Rows of tiles are cut
+// parameters, with X, S, T and B where the tensor cores read them.  (64 x 576 by 17 launches: 187 us; this way: 65.)  Rows of tiles are cut
 // to the smaller side, a multiple of 16; the first factor of a product always has 128 rows and reads on into what lies behind, which
 // makes rows of sums that nobody looks at.
 constexpr int kSmallThreads = 512;
@@ -1088,7 +1089,9 @@ struct Wave {
     Class classes[2][2];                // [three products][pairs]
 };
 
-constexpr int64_t kWaveBytes = (int64_t)2 << 30; // workspace that matrices are taken together up to
+// Workspace that matrices are taken together up to.  (Waves that stay in L2 cost more by their launches and their ends than they save: 4 ResNet-50s
+// 3.9 ms, in waves of 512 MiB 4.6, of 256 MiB 5.7.)
+constexpr int64_t kWaveBytes = (int64_t)2 << 30;
 constexpr int64_t kMostElements = (int64_t)1 << 30;
 constexpr int32_t kMostSide = 1 << 14;           // of the smaller side: S is m x m
 
@@ -1427,7 +1430,7 @@ int run(choco_muon* o, float* m, double lr, const float* factor, bool update, cu
                 if (w.blocks[three] == w.blocks_end[three] || e != cudaSuccess) continue;
                 ta.blocks = o->d_blocks + w.blocks[three];
                 ta.planes = three || p.steps == 0 ? 2 : 1;
-                e = launch_overlapped(kernel, dim3((unsigned)(w.blocks_end[three] - w.blocks[three])), dim3(kTileThreads2), 0, st, HotRange{}, ta);
+                e = launch_overlapped(kernel, dim3((unsigned)(w.blocks_end[three] - w.blocks[three])), dim3(kCutThreads), 0, st, HotRange{}, ta);
             }
         };
         tiles(cut_kernel);
