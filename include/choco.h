@@ -596,7 +596,8 @@ typedef struct {
     int32_t nesterov;     /* 0 or 1                                                                */
     int32_t steps;        /* 0 .. 64                                                               */
     int32_t products;     /* 3: X, S and B carry 22 bits; 1: 11 bits, a third of the work; 0: 1 for  */
-                          /* matrices whose x is bfloat16, 3 for others                             */
+                          /* matrices whose x is bfloat16 and whose smaller side is above 128, 3 for */
+                          /* others.  Matrices that fit a block's shared memory always take 3.      */
     int32_t groups;       /* >= 1                                                                  */
 } choco_muon_params;
 
@@ -605,8 +606,9 @@ typedef struct {
  * list, every matrix starting on a multiple of 256 elements (the gaps are neither read nor written): choco_muon_state_size
  * elements in all, 16-byte aligned; zeros for a fresh run.  The list is copied; the arrays it points to have to stay where
  * they are.  The addresses from the first element of an x or copy to its last (padding between rows included) overlap no
- * other x, copy or g (CHOCO_ERR_INVALID_ARG); gradients may overlap each other.  init allocates the workspace: 4 to 8 bytes for each
- * element of a matrix and of its m x m square, sides rounded up to 128, for as many matrices at a time as 2 GiB holds (or the largest).
+ * other x, copy or g (CHOCO_ERR_INVALID_ARG); gradients may overlap each other.  init allocates the workspace: 6 to 8 bytes for each
+ * element of a matrix and 6 to 12 for each of its m x m square (m the smaller side), sides rounded up to 128, for as many matrices at a
+ * time as 2 GiB holds (or the largest).  Calls on one handle, replays of graphs that captured them included, follow one another.
  */
 int choco_muon_init(choco_muon** out, int32_t n_matrices, const choco_muon_matrix* matrices, const choco_muon_params* p);
 int choco_muon_destroy(choco_muon* opt);
@@ -617,15 +619,15 @@ int choco_muon_set_grads(choco_muon* opt, const void* const* g, void* stream);
 /*
  * choco_muon_step -- one step of all matrices, lr >= 0 and finite as a float32.  factor: DEVICE float [groups] (for
  * instance choco_adamw_grad_norm's), or NULL for 1.  A group whose factor is infinite or NaN is left as it is, parameters, momentum and copy.
- * Infinite or NaN gradients that no factor keeps out leave their matrix without meaning.  The result does not
- * depend on the other matrices of the list.  May be captured; a replay takes the captured lr.  X has then changed outside
+ * Infinite or NaN gradients that no factor keeps out leave their matrix without meaning.  Equal calls
+ * give equal bits; the other matrices of a list say how a long X X^T is cut into sums, and nothing else.  May be captured; a replay takes the captured lr.  X has then changed outside
  * the gossip step: call choco_invalidate (or run with choco_set_carry(ctx, 0)) before the next choco_gossip_step.
  */
 int choco_muon_step(choco_muon* opt, float* m, double lr, const float* factor, void* stream);
 /* x = the X above of u = g for every matrix of the list: no momentum, no decay, copy is not written. */
 int choco_muon_orthogonalize(choco_muon* opt, void* stream);
 /* Synchronises `stream`.  CHOCO_ERR_TIMEOUT if a bounded wait in a kernel of this handle ever ran out ("Device-side waits" above):
- * the part of a matrix that it was to write was not written. */
+ * the part of a matrix that it was to write was not written, nor may it be by later calls: destroy the handle. */
 int choco_muon_status(choco_muon* opt, void* stream);
 
 /*

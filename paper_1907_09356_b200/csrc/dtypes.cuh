@@ -1,4 +1,4 @@
-// Element types of the embedding and AdamW kernels: values are float32 inside the kernels and
+// Element types of the embedding, AdamW, Muon and group norm kernels: values are float32 inside the kernels and
 // rounded once, to nearest even, when they are stored.
 #pragma once
 

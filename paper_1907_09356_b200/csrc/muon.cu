@@ -8,16 +8,23 @@
 // Numbers.  The products run on the tensor cores, float16 factors and float32 sums.  X, S and B are scaled
 // by powers of two into the middle of float16's range (X by 2^ex with 2^ex ~ sqrt(m k), so that its elements start
 // near 1; S, T and B by 2^es ~ m, so that their diagonals do) and kept as a float16 value and, with three products, the
-// float16 value of what that leaves: hi hi + hi lo + lo hi carries 22 bits.  One product carries 11 and is what 16-bit
-// results take: over five steps its roundings come to 0.0012 .. 0.0017 of the result (2-norm), as much as rounding the
-// result to bfloat16 (0.0017); with three they come to 4e-7.
+// float16 value of what that leaves: hi hi + hi lo + lo hi carries 22 bits.  One product carries 11 and is what bfloat16
+// results take where the products set the time (smaller sides above 128; below, three cost little): over five steps its roundings
+// come to 0.0012 .. 0.0017 of the result (2-norm), as much as rounding the result to bfloat16 (0.0017): 0.0023 together.  With three
+// they come to 4e-7 and, the tensor cores' sums cutting bits off, 1e-6 .. 3e-6 together, as with products of plain float32.
 //
-// Layout.  X, S and B lie in the workspace as tiles of 128 rows x 64 halves, in the very bytes that the tensor
+// Layout.  X, S, T and B lie in the workspace as tiles of 128 rows x 64 halves, in the very bytes that the tensor
 // cores read from shared memory (tensor.cuh), high part and low part behind one another.  A tile is one contiguous
 // copy in either direction and needs no descriptor.  The side of a matrix with fewer elements is the row side (tall ones
-// are turned on the way in and out), padding is zero and stays zero.  S and B are symmetric: only tiles on or below the
+// are turned on the way in and out), padding is zero and stays zero.  S, T and B are symmetric: only tiles on or below the
 // diagonal are computed, stored and read; a product that needs one above it reads the stored one turned.
+//
+// What bounds it.  4096 x 4096 floats, 3.3 ms (2.9 ms in a burst of calls): the tensor cores, 76 .. 80 % of whose cycles three products
+// take at the clock that the card's power leaves; 2.5 ms is their floor.  Eight of 650 x 2600 bfloat16, 1.1 ms: parts have 11 or 41
+// steps of K, so their beginnings and ends count (29 .. 53 % of the tensor cores' cycles), and the reads behind them (11 TB/s from
+// L2).  The 176 small matrices of eight ResNet-20, 87 us: the fifteen products of the longest chain, one block's.
 #include <math.h>
+
 #include <cstring>
 
 #include <algorithm>
@@ -59,7 +66,7 @@ struct Matrix {
     int32_t unit0, units;   // blocks of the momentum kernel (small matrices: none)
     int8_t x_dtype, g_dtype, copy_dtype;
     bool tall;              // rows > cols
-    bool whole;             // rows of g behind one another, and its elements in aligned fours
+    bool whole;             // rows of g behind one another
     bool aligned;           // rows of all its arrays start on 16-byte boundaries
 };
 struct Unit {
@@ -83,6 +90,21 @@ struct Scale {              // of a matrix in this step: X_0 = (U first) second;
 
 __device__ __forceinline__ float averaged(float m, float g, float beta, float omb) { return m * beta + g * omb; }
 
+// N neighbouring elements, of which the first `valid` are there (others: 0): accesses of up to 16 bytes where the address allows
+template <int N, typename T>
+__device__ __forceinline__ void load_some(const T* p, int valid, float* v)
+{
+    constexpr int kAlign = N * (int)sizeof(T) < 16 ? N * (int)sizeof(T) : 16;
+    if (valid >= N && ((uintptr_t)p & (kAlign - 1)) == 0) {
+        Raw<T, N> r;
+        load_raw(r, p);
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] = raw_get(r, q);
+    } else {
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] = q < valid ? to_float(p[q]) : 0.f;
+    }
+}
 // ---------------------------------------------------------------------------------------- momentum and norms
 struct MomentArgs {
     const Matrix* mats;
@@ -108,38 +130,52 @@ __device__ double moment_unit(const MomentArgs& a, const Matrix& t, int64_t begi
         const int64_t quads = end / 4 * 4;
 #pragma unroll 4
         for (int64_t e = begin + 4 * (int64_t)threadIdx.x; e < quads; e += 4 * THREADS) {
-            Raw<GT, 4> raw;
-            load_raw(raw, g + e);
-            float u[4];
+            float ge[4], u[4];
+            load_some<4>(g + e, 4, ge);
             if (m) {
                 const float4 old = *reinterpret_cast<const float4*>(m + e);
                 float v[4] = {old.x, old.y, old.z, old.w};
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float gq = raw_get(raw, q) * c;
+                    const float gq = ge[q] * c;
                     v[q] = averaged(v[q], gq, a.beta, a.omb);
                     u[q] = a.nesterov ? averaged(v[q], gq, a.beta, a.omb) : v[q];
                 }
                 *reinterpret_cast<float4*>(m + e) = make_float4(v[0], v[1], v[2], v[3]);
             } else {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) u[q] = raw_get(raw, q) * c;
+                for (int q = 0; q < 4; ++q) u[q] = ge[q] * c;
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) sum = fma((double)u[q], (double)u[q], sum);
         }
         begin = quads > begin ? quads : begin;
     }
-    for (int64_t e = begin + threadIdx.x; e < end; e += THREADS) {
-        const int64_t row = (uint32_t)e / (uint32_t)t.cols, col = (uint32_t)e % (uint32_t)t.cols;
-        const float ge = to_float(g[row * t.g_ld + col]) * c;
-        float u = ge;
-        if (m) {
-            const float v = averaged(m[e], ge, a.beta, a.omb);
-            m[e] = v;
-            u = a.nesterov ? averaged(v, ge, a.beta, a.omb) : v;
+    // single elements, eight of a thread under way
+    for (int64_t e0 = begin + threadIdx.x; e0 < end; e0 += 8 * THREADS) {
+        float ge[8], me[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t e = e0 + j * THREADS;
+            ge[j] = me[j] = 0.f;
+            if (e < end) {
+                const int64_t row = (uint32_t)e / (uint32_t)t.cols, col = (uint32_t)e % (uint32_t)t.cols;
+                ge[j] = to_float(g[t.g_ld == t.cols ? e : row * t.g_ld + col]);
+                if (m) me[j] = m[e];
+            }
         }
-        sum = fma((double)u, (double)u, sum);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t e = e0 + j * THREADS;
+            if (e >= end) break;
+            float u = ge[j] * c;
+            if (m) {
+                const float v = averaged(me[j], u, a.beta, a.omb);
+                m[e] = v;
+                u = a.nesterov ? averaged(v, u, a.beta, a.omb) : v;
+            }
+            sum = fma((double)u, (double)u, sum);
+        }
     }
     return sum;
 }
@@ -265,21 +301,6 @@ __device__ __forceinline__ void join8(uint4 hi, uint4 lo, float* v, bool has_lo)
     }
 }
 
-// N neighbouring elements, of which the first `valid` are there (others: 0): accesses of up to 16 bytes where the address allows
-template <int N, typename T>
-__device__ __forceinline__ void load_some(const T* p, int valid, float* v)
-{
-    constexpr int kAlign = N * (int)sizeof(T) < 16 ? N * (int)sizeof(T) : 16;
-    if (valid >= N && ((uintptr_t)p & (kAlign - 1)) == 0) {
-        Raw<T, N> r;
-        load_raw(r, p);
-#pragma unroll
-        for (int q = 0; q < N; ++q) v[q] = raw_get(r, q);
-    } else {
-#pragma unroll
-        for (int q = 0; q < N; ++q) v[q] = q < valid ? to_float(p[q]) : 0.f;
-    }
-}
 template <int N>
 __device__ __forceinline__ void load_some(const void* p, int64_t at, int32_t dtype, int valid, float* v)
 {
@@ -881,7 +902,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
             *reinterpret_cast<uint4*>(tile + l.tile + piece_at(row, piece)) = lo;
         };
         if (!t.tall) {
-#pragma unroll 2
+#pragma unroll 3
             for (int e = tid; e < l.rows * l.blocks * 8; e += kSmallThreads) {
                 const int row = e / (l.blocks * 8), piece = e % (l.blocks * 8);
                 float v[8] = {};
@@ -891,7 +912,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
                 put(x_tile(piece >> 3, 0), row, piece & 7, v);
             }
         } else {
-#pragma unroll 2
+#pragma unroll 3
             for (int e = tid; e < l.blocks * kHalves * (l.rows / 8); e += kSmallThreads) {
                 const int col = e % (l.blocks * kHalves), row = e / (l.blocks * kHalves) * 8;
                 float v[8] = {};
@@ -1019,6 +1040,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
         if (!ok) {
             if (tid == 0) atomicAdd(a.errors, 1u);
         } else if (!t.tall) {
+#pragma unroll 3
             for (int e = tid; e < t.m * l.blocks * 8; e += kSmallThreads) {
                 const int r = e / (l.blocks * 8), piece = e % (l.blocks * 8);
                 if (piece * 8 >= t.k) continue;
@@ -1030,6 +1052,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
                 apply_some<8>(a.tile, t, r, piece * 8, t.k - piece * 8, v);
             }
         } else {
+#pragma unroll 3
             for (int e = tid; e < l.blocks * kHalves * (l.rows / 8); e += kSmallThreads) {
                 const int col = e % (l.blocks * kHalves), r = e / (l.blocks * kHalves) * 8;
                 if (col >= t.k || r >= t.m) continue;
@@ -1191,7 +1214,7 @@ int64_t carve(int64_t& at, int64_t count)
 // What depends on the gradient's address
 void look_at_gradient(Matrix& t)
 {
-    t.whole = (t.g_ld == t.cols || t.rows == 1) && aligned_to(t.g, 4 * dtype_size(t.g_dtype));
+    t.whole = t.g_ld == t.cols || t.rows == 1;
     auto rows = [&](const void* p, int64_t ld, int32_t dtype) { return aligned_to(p, 16) && (t.rows == 1 || ld * dtype_size(dtype) % 16 == 0); };
     t.aligned = rows(t.x, t.x_ld, t.x_dtype) && rows(t.g, t.g_ld, t.g_dtype) && rows(nullptr, t.cols, CHOCO_F32) && (!t.copy || rows(t.copy, t.copy_ld, t.copy_dtype));
 }
