@@ -861,6 +861,10 @@ constexpr int kMostShared = 227 * 1024;
 // 112 / 33.4; backward 2 x 64 of 56 x 56 x 256 bf16 / 4 x 32 of 7 x 7 x 2048 f16: 34 KiB 205 / 66, 50 KiB 190 / 60, 72 KiB 197 / 62.)  And at least
 // where few images ask for more blocks.
 constexpr int64_t kShareForward = 72 * 1024, kShareBackward = 50 * 1024, kLeast = 32 * 1024;
+// A share that is larger, in quarters of that, is kept by that much only and the rest read twice: more blocks to an SM are worth more than
+// the bytes.  (us, all that fits / this: forward 6 x 17 images of 91 x 91 x 96 f32, 1.8 times, 211 / 225; 2 x 64 of 112 x 112 x 64 bf16, just
+// above it, 122 / 154; backward 10 x 117 of 9717 x 8 f32, 1.5 times, 332 / 246; 4 x 64 of 6000 x 64 bf16, 1.9 times, 209 / 180; 3 x 24 of 6762 x 188, 1290 / 742.)
+constexpr int64_t kSlackForward = 8, kSlackBackward = 5;
 constexpr int64_t kMostSize = (int64_t)1 << 40; // elements that strides may span
 
 } // namespace
@@ -946,7 +950,8 @@ struct Cut {
     size_t shared;
 };
 // A slice is a whole number of groups and of accesses.
-Cut cut_of(const choco_group_norm_params& p, int64_t images, int64_t pixels, int vec, int64_t es /* bytes of an element of x */, int64_t bytes /* kept of one */, int64_t most)
+Cut cut_of(const choco_group_norm_params& p, int64_t images, int64_t pixels, int vec, int64_t es /* bytes of an element of x */, int64_t bytes /* kept of one */, int64_t most,
+           int64_t slack)
 {
     const int64_t per = p.channels / p.groups, unit = per / gcd(per, vec) * vec, rows = p.n * images;
     Cut best = {};
@@ -973,7 +978,9 @@ Cut cut_of(const choco_group_norm_params& p, int64_t images, int64_t pixels, int
     best.steps = (best.share + best.lanes - 1) / best.lanes;
     const int64_t steps = (int64_t)best.rounds * best.steps;
     const size_t fixed = fixed_bytes(vec, best.slice, cluster), each = (size_t)kNormThreads * vec * bytes;
-    best.kept = (int)std::min<int64_t>(steps, ((int64_t)kMostShared - (int64_t)fixed) / (int64_t)each);
+    const bool whole = (int64_t)best.share * best.slice * bytes * 4 <= most * slack;
+    const int64_t room = std::min<int64_t>((int64_t)kMostShared - (int64_t)fixed, whole ? kMostShared : most);
+    best.kept = (int)std::min<int64_t>(steps, std::max<int64_t>(room / (int64_t)each, 1));
     best.shared = fixed + each * best.kept;
     return best;
 }
@@ -1032,7 +1039,7 @@ int launch(choco_group_norm* gn, NormArgs& a, bool backward, const choco_pixels&
     const choco_group_norm_params& p = gn->params;
     const int vec = widest(p, a.images, a.pixels, x, y, dx);
     const Cut c = cut_of(p, a.images, a.pixels, vec, dtype_size(x.dtype), dtype_size(x.dtype) + (backward ? dtype_size(y.dtype) : 0),
-                         backward ? kShareBackward : kShareForward);
+                         backward ? kShareBackward : kShareForward, backward ? kSlackBackward : kSlackForward);
     a.slice = c.slice;
     a.slices = a.channels / c.slice;
     a.cluster = c.cluster;
