@@ -27,7 +27,6 @@ enum Activation { kNone, kRelu, kSilu, kGelu };
 constexpr int kNormThreads = 128;
 constexpr int kNormWarps = kNormThreads / 32;
 constexpr int kNormBlocks = 4;          // to an SM, by registers
-constexpr int kAtOnce = 4;              // pixels whose loads a thread has under way where it keeps no more
 constexpr int kApart = 64;             // pixels that a thread adds up on their own: what is rounded grows with the length of a sum
 constexpr int kWaits = 2;               // groups in which a thread's copies to shared memory are waited for
 constexpr int64_t kMostSlice = 2048;    // channels of a slice, and of a group: their sums are in shared memory
@@ -298,6 +297,10 @@ __device__ __forceinline__ float param(const void* p, int64_t at, int32_t dtype,
     return p ? bits_to_float(load_bits(p, at, dtype), dtype) : other;
 }
 
+// Pixels whose loads a thread has under way where it keeps no more: short accesses take few registers (us, backward,
+// 3 x 24 images of 6762 x 188 bf16 in accesses of 4 bytes: 745 with 4, 545 with 8, 478 with 16)
+template <typename T, int VEC>
+constexpr int kAtOnce = Raw<T, VEC>::kBytes > 8 ? 4 : Raw<T, VEC>::kBytes > 4 ? 8 : 16;
 // One access of a thread from memory to its slot (an address in shared memory): copied past the registers, so that a thread
 // has many under way (a copy has 4 bytes at least).  Copies are committed and waited for in groups.
 template <typename T, int VEC>
@@ -397,13 +400,13 @@ __device__ __forceinline__ void finish_forward(const NormArgs& a, const Share<VE
             to += to_step;
             slot += kSlot<XT, VEC>;
         }
-        for (int i0 = kept; i0 < sh.mine; i0 += kAtOnce) {
-            Raw<XT, VEC> r[kAtOnce];
+        for (int i0 = kept; i0 < sh.mine; i0 += kAtOnce<XT, VEC>) {
+            Raw<XT, VEC> r[kAtOnce<XT, VEC>];
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j)
+            for (int j = 0; j < kAtOnce<XT, VEC>; ++j)
                 if (i0 + j < sh.mine) load_raw(r[j], from + (i0 + j) * from_step);
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j)
+            for (int j = 0; j < kAtOnce<XT, VEC>; ++j)
                 if (i0 + j < sh.mine) {
                     take(r[j], to);
                     to += to_step;
@@ -489,13 +492,13 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) forward_kernel(Norm
                 Pair t1[NP], t2[NP];
 #pragma unroll
                 for (int p = 0; p < NP; ++p) t1[p] = t2[p] = pair_of(0.f, 0.f);
-                for (int i0 = begin; i0 < min(begin + kApart, sh.mine); i0 += kAtOnce) {
-                    Raw<XT, VEC> r[kAtOnce];
+                for (int i0 = begin; i0 < min(begin + kApart, sh.mine); i0 += kAtOnce<XT, VEC>) {
+                    Raw<XT, VEC> r[kAtOnce<XT, VEC>];
 #pragma unroll
-                    for (int j = 0; j < kAtOnce; ++j)
+                    for (int j = 0; j < kAtOnce<XT, VEC>; ++j)
                         if (i0 + j < sh.mine) load_raw(r[j], from + (i0 + j) * from_step);
 #pragma unroll
-                    for (int j = 0; j < kAtOnce; ++j)
+                    for (int j = 0; j < kAtOnce<XT, VEC>; ++j)
                         if (i0 + j < sh.mine) take(r[j], t1, t2);
                 }
 #pragma unroll
@@ -703,17 +706,17 @@ __device__ __forceinline__ void backward_pass(const NormArgs& a, const Share<VEC
                 Pair t1[NP], t2[NP];
 #pragma unroll
                 for (int p = 0; p < NP; ++p) t1[p] = t2[p] = pair_of(0.f, 0.f);
-                for (int i0 = begin; i0 < min(begin + kApart, sh.mine); i0 += kAtOnce) {
-                    Raw<XT, VEC> rx[kAtOnce];
-                    Raw<YT, VEC> ry[kAtOnce];
+                for (int i0 = begin; i0 < min(begin + kApart, sh.mine); i0 += kAtOnce<XT, VEC>) {
+                    Raw<XT, VEC> rx[kAtOnce<XT, VEC>];
+                    Raw<YT, VEC> ry[kAtOnce<XT, VEC>];
 #pragma unroll
-                    for (int j = 0; j < kAtOnce; ++j)
+                    for (int j = 0; j < kAtOnce<XT, VEC>; ++j)
                         if (i0 + j < sh.mine) {
                             load_raw(rx[j], from_x + (i0 + j) * step_x);
                             load_raw(ry[j], from_y + (i0 + j) * step_y);
                         }
 #pragma unroll
-                    for (int j = 0; j < kAtOnce; ++j)
+                    for (int j = 0; j < kAtOnce<XT, VEC>; ++j)
                         if (i0 + j < sh.mine) {
                             sl.mask(rx[j], ry[j]);
                             take(rx[j], ry[j], t1, t2);
@@ -864,7 +867,8 @@ constexpr int64_t kShareForward = 72 * 1024, kShareBackward = 50 * 1024, kLeast 
 // A share that is larger, in quarters of that, is kept by that much only and the rest read twice: more blocks to an SM are worth more than
 // the bytes.  (us, all that fits / this: forward 6 x 17 images of 91 x 91 x 96 f32, 1.8 times, 211 / 225; 2 x 64 of 112 x 112 x 64 bf16, just
 // above it, 122 / 154; backward 10 x 117 of 9717 x 8 f32, 1.5 times, 332 / 246; 4 x 64 of 6000 x 64 bf16, 1.9 times, 209 / 180; 3 x 24 of 6762 x 188, 1290 / 742.)
-constexpr int64_t kSlackForward = 8, kSlackBackward = 5;
+// Exponentials in full float32 need the warps as well.  (Forward 6 x 17 of 8281 x 96 f32, silu: 560 / 393.)
+constexpr int64_t kSlackForward = 8, kSlackSmooth = 4, kSlackBackward = 5;
 constexpr int64_t kMostSize = (int64_t)1 << 40; // elements that strides may span
 
 } // namespace
@@ -1039,7 +1043,7 @@ int launch(choco_group_norm* gn, NormArgs& a, bool backward, const choco_pixels&
     const choco_group_norm_params& p = gn->params;
     const int vec = widest(p, a.images, a.pixels, x, y, dx);
     const Cut c = cut_of(p, a.images, a.pixels, vec, dtype_size(x.dtype), dtype_size(x.dtype) + (backward ? dtype_size(y.dtype) : 0),
-                         backward ? kShareBackward : kShareForward, backward ? kSlackBackward : kSlackForward);
+                         backward ? kShareBackward : kShareForward, backward ? kSlackBackward : a.activation >= kSilu && y.dtype == CHOCO_F32 ? kSlackSmooth : kSlackForward);
     a.slice = c.slice;
     a.slices = a.channels / c.slice;
     a.cluster = c.cluster;
