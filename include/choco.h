@@ -595,9 +595,8 @@ typedef struct {
                           /* |a + b s^2 + c s^4|, |b + c s^2| below 15 (CHOCO_ERR_INVALID_ARG)       */
     int32_t nesterov;     /* 0 or 1                                                                */
     int32_t steps;        /* 0 .. 64                                                               */
-    int32_t products;     /* 3: X, S and B carry 22 bits; 1: 11 bits, a third of the work; 0: 1 for  */
-                          /* matrices whose x is bfloat16 and whose smaller side is above 128, 3 for */
-                          /* others.  Matrices that fit a block's shared memory always take 3.      */
+    int32_t products;     /* 3, or 0: X, S and B carry 22 bits; 1: 11 bits (results 0.002 off), a    */
+                          /* third of the work.  Matrices that fit a block's shared memory take 3.  */
     int32_t groups;       /* >= 1                                                                  */
 } choco_muon_params;
 

@@ -8,10 +8,9 @@
 // Numbers.  The products run on the tensor cores, float16 factors and float32 sums.  X, S and B are scaled
 // by powers of two into the middle of float16's range (X by 2^ex with 2^ex ~ sqrt(m k), so that its elements start
 // near 1; S, T and B by 2^es ~ m, so that their diagonals do) and kept as a float16 value and, with three products, the
-// float16 value of what that leaves: hi hi + hi lo + lo hi carries 22 bits.  One product carries 11 and is what bfloat16
-// results take where the products set the time (smaller sides above 128; below, three cost little): over five steps its roundings
-// come to 0.0012 .. 0.0017 of the result (2-norm), as much as rounding the result to bfloat16 (0.0017): 0.0023 together.  With three
-// they come to 4e-7 and, the tensor cores' sums cutting bits off, 1e-6 .. 3e-6 together, as with products of plain float32.
+// float16 value of what that leaves: hi hi + hi lo + lo hi carries 22 bits.  Over five steps its roundings come to 4e-7 of the result
+// (2-norm) and, the tensor cores' sums cutting bits off, 1e-6 .. 3e-6 together, as with products of plain float32.  One product carries 11
+// bits, 0.0012 .. 0.0017 over five steps, as much again as rounding a result to bfloat16 (0.0017): it is taken where the caller asks for it.
 //
 // Layout.  X, S, T and B lie in the workspace as tiles of 128 rows x 64 halves, in the very bytes that the tensor
 // cores read from shared memory (tensor.cuh), high part and low part behind one another.  A tile is one contiguous
@@ -1269,7 +1268,7 @@ int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit
         if (units.size() > 0x7fffffff) return CHOCO_ERR_TOO_LARGE;
         o->mats.push_back(t);
         o->offsets.push_back(at);
-        kinds.push_back(small || !some ? -1 : o->params.products == 3 || (o->params.products == 0 && (q.x_dtype != CHOCO_BF16 || t.m <= kSide)));
+        kinds.push_back(small || !some ? -1 : o->params.products != 1);
         at += (count + kBlock - 1) / kBlock * kBlock;
         if (at > (int64_t)1 << 38) return CHOCO_ERR_TOO_LARGE;
         if (some) {
