@@ -28,6 +28,7 @@ constexpr int kNormThreads = 128;
 constexpr int kNormWarps = kNormThreads / 32;
 constexpr int kNormBlocks = 4;          // to an SM, by registers
 constexpr int kApart = 64;             // pixels that a thread adds up on their own: what is rounded grows with the length of a sum
+constexpr double kMostLost = 16.0;      // squares about a pivot, over those about the mean: as many bits of float32 sums are lost (4)
 constexpr int kWaits = 2;               // groups in which a thread's copies to shared memory are waited for
 constexpr int64_t kMostSlice = 2048;    // channels of a slice, and of a group: their sums are in shared memory
 
@@ -274,6 +275,7 @@ __device__ __forceinline__ Layout layout_of(uint8_t* raw, const NormArgs& a)
 
 // For every channel of the slice what its group says: number(channel, group, first channel to add, step to the next, sum over those
 // who add together) and then use(channel, the two numbers).  Small groups are added up by each of their channels, others by a warp.
+// A barrier has to follow.
 template <typename Number, typename Use>
 __device__ __forceinline__ void each_channel(const NormArgs& a, const Layout& l, Number number, Use use)
 {
@@ -290,7 +292,6 @@ __device__ __forceinline__ void each_channel(const NormArgs& a, const Layout& l,
             for (int c = g * a.per_group + lane; c < (g + 1) * a.per_group; c += 32) use(c, v);
         }
     }
-    __syncthreads();
 }
 __device__ __forceinline__ float param(const void* p, int64_t at, int32_t dtype, float other)
 {
@@ -439,102 +440,164 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) forward_kernel(Norm
             keep_commit();
         }
     };
-    // Sums of x - p and (x - p)^2 with p the channel's value at the image's first pixel: float32 loses nothing where
-    // the mean is far from zero
-    for (int round = 0; round < sh.rounds; ++round) {
-        ask_round(round);
-        if (round == 0)
-            for (int c = threadIdx.x; c < a.slice; c += kNormThreads) {
-                const int64_t at = (int64_t)worker * a.param_ld + slice0 + c;
-                l.channel[c].y = param(a.weight, at, a.param_dtype, 1.f);
-                l.channel[c].z = param(a.bias, at, a.param_dtype, 0.f);
-            }
-        Pair s1[NP], s2[NP], pivot[NP];
-#pragma unroll
-        for (int p = 0; p < NP; ++p) s1[p] = s2[p] = pair_of(0.f, 0.f);
-        if (sh.active(round)) {
-            const int c0 = sh.channel(round), kept = sh.kept(a.kept, round);
-            const XT* from = x + sh.first * a.x.pixel + c0;
-            const int64_t from_step = sh.lanes * a.x.pixel;
-            Raw<XT, VEC> first;
-            load_raw(first, x + c0);
-#pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                const float2 v = floats_of(raw_pair(first, p));
-                pivot[p] = pair_of(-v.x, -v.y);
-                if (sh.lane == 0) {
-                    l.channel[c0 + 2 * p].w = v.x;
-                    if (VEC > 1) l.channel[c0 + 2 * p + 1].w = v.y;
-                }
-            }
-            auto take = [&](const Raw<XT, VEC>& r, Pair* t1, Pair* t2) {
-#pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    const Pair d = add2(raw_pair(r, p), pivot[p]);
-                    t1[p] = add2(t1[p], d);
-                    t2[p] = fma2(d, d, t2[p]);
-                }
-            };
-            uint32_t slot = slot_of<XT, VEC>(l.kept, round * sh.steps);
-#pragma unroll 1
-            for (int g = 0; g < kWaits; ++g) {
-                keep_wait(g);
-                const int end = group_begin(kept, g + 1);
-#pragma unroll 4
-                for (int i = group_begin(kept, g); i < end; ++i) {
-                    Raw<XT, VEC> r;
-                    kept_raw(r, slot);
-                    take(r, s1, s2);
-                    slot += kSlot<XT, VEC>;
-                }
-            }
-            for (int begin = kept; begin < sh.mine; begin += kApart) {
-                Pair t1[NP], t2[NP];
-#pragma unroll
-                for (int p = 0; p < NP; ++p) t1[p] = t2[p] = pair_of(0.f, 0.f);
-                for (int i0 = begin; i0 < min(begin + kApart, sh.mine); i0 += kAtOnce<XT, VEC>) {
-                    Raw<XT, VEC> r[kAtOnce<XT, VEC>];
-#pragma unroll
-                    for (int j = 0; j < kAtOnce<XT, VEC>; ++j)
-                        if (i0 + j < sh.mine) load_raw(r[j], from + (i0 + j) * from_step);
-#pragma unroll
-                    for (int j = 0; j < kAtOnce<XT, VEC>; ++j)
-                        if (i0 + j < sh.mine) take(r[j], t1, t2);
-                }
-#pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    s1[p] = add2(s1[p], t1[p]);
-                    s2[p] = add2(s2[p], t2[p]);
-                }
-            }
-        }
-        add_up(sh, a, round, s1, s2, l.red, l.parts, cluster_rank());
-    }
-    exchange(a, l.parts, l.total);
-    // the sums of x and x^2 of a group in float64, which bears the difference of the two
     const double count = (double)a.pixels;
-    each_channel(a, l, [&](int c, int g, int from, int step, auto sum) {
-        double t1 = 0.0, t2 = 0.0;
-        for (int k = g * a.per_group + from; k < (g + 1) * a.per_group; k += step) {
-            const float2 v = l.total[k];
-            const double p = (double)l.channel[k].w, s = (double)v.x, n = count * p;
-            t1 += n + s;
-            t2 = fma(p, n + 2.0 * s, t2) + (double)v.y;
+    // Sums of x - p and (x - p)^2 with p the channel's value at the image's first pixel, so that float32 loses nothing where the mean is far
+    // from zero.  Where that pixel turns out to lie far from the others (a border, padding, a spike) the sums are formed once
+    // more, with the channels' means as p.  All blocks of a cluster have the same sums, and decide alike.
+    for (int pass = 0;; ++pass) {
+        for (int round = 0; round < sh.rounds; ++round) {
+            if (pass == 0) ask_round(round);
+            if (round == 0)
+                for (int c = threadIdx.x; c < a.slice; c += kNormThreads) {
+                    const int64_t at = (int64_t)worker * a.param_ld + slice0 + c;
+                    l.channel[c].y = param(a.weight, at, a.param_dtype, 1.f);
+                    l.channel[c].z = param(a.bias, at, a.param_dtype, 0.f);
+                }
+            Pair s1[NP], s2[NP], pivot[NP];
+#pragma unroll
+            for (int p = 0; p < NP; ++p) s1[p] = s2[p] = pair_of(0.f, 0.f);
+            if (sh.active(round)) {
+                const int c0 = sh.channel(round), kept = sh.kept(a.kept, round);
+                const XT* from = x + sh.first * a.x.pixel + c0;
+                const int64_t from_step = sh.lanes * a.x.pixel;
+                if (pass == 0) {
+                    Raw<XT, VEC> first;
+                    load_raw(first, x + c0);
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) {
+                        const float2 v = floats_of(raw_pair(first, p));
+                        pivot[p] = pair_of(-v.x, -v.y);
+                        if (sh.lane == 0) {
+                            l.channel[c0 + 2 * p].w = v.x;
+                            if (VEC > 1) l.channel[c0 + 2 * p + 1].w = v.y;
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) pivot[p] = pair_of(-l.channel[c0 + 2 * p].w, VEC > 1 ? -l.channel[c0 + 2 * p + 1].w : 0.f);
+                }
+                Pair t1[NP], t2[NP];
+                auto take = [&](const Raw<XT, VEC>& r) {
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) {
+                        const Pair d = add2(raw_pair(r, p), pivot[p]);
+                        t1[p] = add2(t1[p], d);
+                        t2[p] = fma2(d, d, t2[p]);
+                    }
+                };
+                // Four by themselves first, and up to kApart, before they are added to all: values of 16 bits are few different ones, whose squares
+                // a large sum rounds in the same direction each time.
+                auto take_four = [&](const Raw<XT, VEC>* r) {
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) {
+                        Pair u = add2(raw_pair(r[0], p), pivot[p]), v = fma2(u, u, pair_of(0.f, 0.f));
+#pragma unroll
+                        for (int j = 1; j < 4; ++j) {
+                            const Pair d = add2(raw_pair(r[j], p), pivot[p]);
+                            u = add2(u, d);
+                            v = fma2(d, d, v);
+                        }
+                        t1[p] = add2(t1[p], u);
+                        t2[p] = add2(t2[p], v);
+                    }
+                };
+                auto begin_apart = [&]() {
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) t1[p] = t2[p] = pair_of(0.f, 0.f);
+                };
+                auto end_apart = [&]() {
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) {
+                        s1[p] = add2(s1[p], t1[p]);
+                        s2[p] = add2(s2[p], t2[p]);
+                    }
+                };
+                uint32_t slot = slot_of<XT, VEC>(l.kept, round * sh.steps);
+#pragma unroll 1
+                for (int g = 0; g < kWaits; ++g) {
+                    keep_wait(g);
+                    const int last = group_begin(kept, g + 1);
+#pragma unroll 1
+                    for (int i = group_begin(kept, g); i < last;) {
+                        const int end = min(i + kApart, last);
+                        begin_apart();
+#pragma unroll 1
+                        for (; i + 4 <= end; i += 4) {
+                            Raw<XT, VEC> r[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) kept_raw(r[j], slot + j * kSlot<XT, VEC>);
+                            take_four(r);
+                            slot += 4 * kSlot<XT, VEC>;
+                        }
+#pragma unroll 1
+                        for (; i < end; ++i) {
+                            Raw<XT, VEC> r;
+                            kept_raw(r, slot);
+                            take(r);
+                            slot += kSlot<XT, VEC>;
+                        }
+                        end_apart();
+                    }
+                }
+                for (int begin = kept; begin < sh.mine; begin += kApart) {
+                    const int end = min(begin + kApart, sh.mine);
+                    begin_apart();
+                    for (int i0 = begin; i0 < end; i0 += kAtOnce<XT, VEC>) {
+                        Raw<XT, VEC> r[kAtOnce<XT, VEC>];
+#pragma unroll
+                        for (int j = 0; j < kAtOnce<XT, VEC>; ++j)
+                            if (i0 + j < end) load_raw(r[j], from + (i0 + j) * from_step);
+#pragma unroll
+                        for (int j = 0; j < kAtOnce<XT, VEC>; j += 4) {
+                            if (i0 + j + 4 <= end) {
+                                take_four(r + j);
+                            } else {
+#pragma unroll
+                                for (int k = j; k < j + 4; ++k)
+                                    if (i0 + k < end) take(r[k]);
+                            }
+                        }
+                    }
+                    end_apart();
+                }
+            }
+            add_up(sh, a, round, s1, s2, l.red, l.parts, cluster_rank());
         }
-        t1 = sum(t1) * a.inverse;
-        t2 = sum(t2) * a.inverse;
-        const double var = fma(-t1, t1, t2);
-        const float2 st = make_float2((float)t1, 1.f / sqrtf((float)((var > 0.0 || var != var ? var : 0.0) + a.eps)));
-        if (rank == 0 && c == g * a.per_group) {
-            const int64_t at = (int64_t)row * a.groups + slice0 / a.per_group + g;
-            if (a.mean) a.mean[at] = st.x;
-            if (a.rstd) a.rstd[at] = st.y;
+        exchange(a, l.parts, l.total);
+        // the sums of x and x^2 of a group in float64, which bears the difference of the two
+        bool lost = false;
+        each_channel(a, l, [&](int c, int g, int from, int step, auto sum) {
+            double t1 = 0.0, t2 = 0.0, squares = 0.0;
+            for (int k = g * a.per_group + from; k < (g + 1) * a.per_group; k += step) {
+                const float2 v = l.total[k];
+                const double p = (double)l.channel[k].w, s = (double)v.x, n = count * p;
+                t1 += n + s;
+                t2 = fma(p, n + 2.0 * s, t2) + (double)v.y;
+                squares += (double)v.y;
+            }
+            t1 = sum(t1) * a.inverse;
+            t2 = sum(t2) * a.inverse;
+            const double var = fma(-t1, t1, t2), positive = var > 0.0 || var != var ? var : 0.0;
+            if (sum(squares) * a.inverse > kMostLost * (positive + a.eps)) lost = true;
+            const float2 st = make_float2((float)t1, 1.f / sqrtf((float)(positive + a.eps)));
+            if (rank == 0 && c == g * a.per_group) {
+                const int64_t at = (int64_t)row * a.groups + slice0 / a.per_group + g;
+                if (a.mean) a.mean[at] = st.x;
+                if (a.rstd) a.rstd[at] = st.y;
+            }
+            return st;
+        }, [&](int c, float2 st) {
+            l.channel[c].x = -st.x;
+            l.channel[c].y *= st.y;
+        });
+        if (!__syncthreads_or(lost) || pass > 0) break;
+        if (a.cluster > 1) {                                         // the others have read what will be written once more
+            cluster_arrive();
+            cluster_wait();
         }
-        return st;
-    }, [&](int c, float2 st) {
-        l.channel[c].x = -st.x;
-        l.channel[c].y *= st.y;
-    });
+        for (int c = threadIdx.x; c < a.slice; c += kNormThreads) l.channel[c].w = (float)((double)l.channel[c].w + (double)l.total[c].x / count);
+        __syncthreads();
+    }
     switch (a.activation) {
     case kRelu: finish_forward<XT, YT, VEC, kRelu>(a, sh, l, x, y); break;
     case kSilu: finish_forward<XT, YT, VEC, kSilu>(a, sh, l, x, y); break;
@@ -790,6 +853,7 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) backward_kernel(Nor
             const float r = l.channel[c].w;
             l.parts[c] = make_float2(k.x, k.y * r * r);  // (the blocks' sums are done with)
         });
+        __syncthreads();
         backward_pass_act<XT, YT, VEC, true>(a, sh, l, x, dy, dx);
     }
 }
