@@ -628,6 +628,9 @@ int choco_muon_orthogonalize(choco_muon* opt, void* stream);
 /* Synchronises `stream`.  CHOCO_ERR_TIMEOUT if a bounded wait in a kernel of this handle ever ran out ("Device-side waits" above):
  * the part of a matrix that it was to write was not written, nor may it be by later calls: destroy the handle. */
 int choco_muon_status(choco_muon* opt, void* stream);
+/* Test hook, as choco_debug_set_wait_polls: with 0 every wait of this handle's kernels counts as run out at once, and is then sat out.  Calls
+ * from now on; not for production use. */
+int choco_debug_muon_set_wait_polls(choco_muon* opt, uint32_t polls);
 
 /*
  * Group norm with an activation, channels last, for n workers with parameters of their own (a scale and a shift for

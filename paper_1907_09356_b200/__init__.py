@@ -33,7 +33,7 @@ EXPORTS = [
     "choco_adamw_init", "choco_adamw_destroy", "choco_adamw_state_size", "choco_adamw_set_grads", "choco_adamw_grad_norm",
     "choco_adamw_set_rounding", "choco_adamw_step", "choco_adamw_read_state", "choco_adamw_get_steps", "choco_adamw_set_steps",
     "choco_muon_init", "choco_muon_destroy", "choco_muon_state_size", "choco_muon_set_grads", "choco_muon_step", "choco_muon_orthogonalize",
-    "choco_muon_status",
+    "choco_muon_status", "choco_debug_muon_set_wait_polls",
     "choco_group_norm_init", "choco_group_norm_destroy", "choco_group_norm_forward", "choco_group_norm_backward",
 ]
 
@@ -180,6 +180,7 @@ def load() -> ctypes.CDLL:
         lib.choco_muon_step.argtypes = [vp, vp, f64, vp, vp]
         lib.choco_muon_orthogonalize.argtypes = [vp, vp]
         lib.choco_muon_status.argtypes = [vp, vp]
+        lib.choco_debug_muon_set_wait_polls.argtypes = [vp, ctypes.c_uint32]
         px = ctypes.POINTER(choco_pixels)
         lib.choco_group_norm_init.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(choco_group_norm_params)]
         lib.choco_group_norm_destroy.argtypes = [vp]
@@ -785,6 +786,11 @@ def choco_muon_orthogonalize(opt, stream=None) -> None:
 def choco_muon_status(opt, stream=None) -> None:
     """Waits for `stream`; raises if a bounded wait in a kernel ever ran out."""
     _check(load().choco_muon_status(opt, _stream_of(stream, opt.device)))
+
+
+def choco_debug_muon_set_wait_polls(opt, polls: int) -> None:
+    """Test hook: see choco.h."""
+    _check(load().choco_debug_muon_set_wait_polls(opt, polls))
 
 
 class GroupNormHandle(ctypes.c_void_p):

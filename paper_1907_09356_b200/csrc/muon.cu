@@ -468,6 +468,7 @@ struct ProductArgs {
     int32_t count;          // of the parts
     float a, b, c;
     int32_t which;          // of the two X: the one that is read
+    uint32_t polls;         // of a wait before it counts as run out
     float* partial;         // sums of split parts, 128 x 128 each
     uint32_t* arrived;      // how many splits are there, 0 between launches
     int32_t planes;         // parts of its tiles in the workspace (S, T and B and the next X have as many as take part in products)
@@ -516,6 +517,16 @@ template <int THREADS>
 __device__ __forceinline__ void warps_sync(int barrier) // of four warps of a block
 {
     asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(THREADS) : "memory");
+}
+template <int THREADS>
+__device__ __forceinline__ bool warps_agree(int barrier, bool yes)
+{
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all)
+                 : "r"((uint32_t)yes), "r"(barrier), "n"(THREADS)
+                 : "memory");
+    return all != 0;
 }
 template <int N>
 __device__ __forceinline__ void add_at(float (&w)[N], int column, float x)
@@ -586,9 +597,9 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
     using L = Plan<PA, PB, CG>;
     constexpr int PL = PA, ST = L::kStages;                      // PL: parts of the results
     extern __shared__ __align__(1024) uint8_t stage[];           // (all other shared memory lies behind it)
-    __shared__ uint64_t full[ST], empty[ST], sums[2], taken[2];
+    __shared__ uint64_t full[ST], empty[ST], sums[2], taken[2], drained;
     __shared__ uint32_t tmem_at;
-    __shared__ volatile uint32_t failed;
+    __shared__ volatile uint32_t failed;                         // a wait ran out
     __shared__ volatile bool last[2];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
@@ -602,14 +613,17 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
             mbar_init(&sums[s], 1);
             mbar_init(&taken[s], L::kWarps * CG);
         }
+        mbar_init(&drained, 1);
         failed = 0;
     }
+    __syncwarp();
     if (warp == 0) tmem_alloc<CG>(&tmem_at, 2 * L::kColumns);
     tmem_fence_before();
     __syncthreads();
     if (CG == 2) cluster_sync();
     tmem_fence_after();
     const uint32_t acc = tmem_at;
+    const Patience patience = {a.polls, &failed};
     const Job<KIND, CG, L::kLeave> first_job(a, begin, rank);    // (the tables do not change: read while the kernel before ends)
     allow_next_kernel();
     wait_for_previous_kernel();
@@ -623,7 +637,7 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
         const uint32_t rows = (warp & 3) * L::kSend;             // of a tile, in bytes
         bool ok = true;
         auto wait_sums = [&](uint32_t ch) {
-            ok = mbar_wait(&sums[ch & 1], (ch >> 1) & 1);
+            ok = ok && mbar_wait_warp(&sums[ch & 1], (ch >> 1) & 1, patience);
             tmem_fence_after();
             return ok;
         };
@@ -633,7 +647,8 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
             if (lane == 0) mbar_arrive_at(&taken[ch & 1], 0);
         };
         uint32_t ch = 0;                                         // sets of sums so far
-        for (int index = begin; index < a.count && ok; index += step) {
+        // (a warp whose wait gave up goes through all parts nevertheless, without waiting: it is wanted at the votes of split ones)
+        for (int index = begin; index < a.count; index += step) {
             const Job<KIND, CG, L::kLeave> job = index == begin ? first_job : Job<KIND, CG, L::kLeave>(a, index, rank);
             const Matrix& t = *job.t;
             float v[L::kLeave ? kSide : 1];
@@ -654,11 +669,11 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
             } else {
                 wait_sums(ch);
             }
-            if (!ok) break;
             const int tile = job.part.j * CG + h;                // of 128 columns
             const bool there = job.has_a && tile < job.columns;
             const int own = job.it == tile ? r : -1;             // this thread's column on the diagonal
             const int splits = KIND == kGram ? job.part.splits : 1;
+            if (!ok && splits == 1) continue;
             float* partial = nullptr;                            // of this CTA's tile: split after split, column after column
             if (KIND == kGram && splits > 1) {
                 const int64_t place = ((int64_t)job.part.slot * CG + rank) * CG + h;
@@ -666,16 +681,18 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
                 float* here = partial + job.part.split * (kSide * kSide);
 #pragma unroll
                 for (int q32 = 0; q32 < kSide / 32; ++q32) {
+                    if (!ok) break;
                     uint32_t bits[32];
                     if constexpr (!L::kLeave) tmem_load32(from + (ch & 1) * L::kColumns + q32 * 32, bits);
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
                         __stcg(here + (q32 * 32 + e) * kSide, L::kLeave ? v[L::kLeave ? q32 * 32 + e : 0] : __uint_as_float(bits[e]));
                 }
-                if (!L::kLeave) leave_sums(ch);
+                if (!L::kLeave && ok) leave_sums(ch);
                 // the last split to arrive adds them all up in their order
                 __threadfence();
-                warps_sync<128>(1 + h);
+                ok = warps_agree<128>(1 + h, ok);
+                if (!ok) continue;
                 if (r == 0) last[h] = atomicAdd(a.arrived + place, 1u) == (uint32_t)splits - 1;
                 warps_sync<128>(1 + h);
                 const bool mine_to_do = last[h];
@@ -744,7 +761,7 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
                 const uint32_t bytes = (job.has_a ? L::kFirst : 0) + (load_b ? L::kSecond : 0);
                 for (int kb = 0; kb < job.nk; ++kb, ++n) {
                     const uint32_t s = n % ST;
-                    if (n >= ST) ok = mbar_wait(&empty[s], (n / ST - 1) & 1);
+                    if (n >= ST) ok = mbar_wait_warp(&empty[s], (n / ST - 1) & 1, patience);
                     if (!ok) break;
                     uint8_t* to_a = stage + s * L::kStage;
                     uint8_t* to_b = to_a + L::kFirst;
@@ -768,7 +785,7 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
             }
             if (!ok) {                                           // copies under way are sat out
                 failed = 1;
-                for (uint32_t q = n > ST ? n - ST : 0; q < n; ++q) mbar_wait(&full[q % ST], (q / ST) & 1);
+                for (uint32_t q = n > ST ? n - ST : 0; q < n; ++q) mbar_wait_warp(&full[q % ST], (q / ST) & 1, patience);
             }
         } else if (warp == L::kWarps + 1) {                      // the products
             uint32_t n = 0, ch = 0;
@@ -778,15 +795,15 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
                 for (int kb = 0; kb < job.nk; ++kb, ++n) {
                     const uint32_t s = n % ST;
                     if (CG == 2 && rank == 1) {                  // the other CTA of a pair tells the first what has come
-                        ok = mbar_wait(&full[s], (n / ST) & 1);
+                        ok = mbar_wait_warp(&full[s], (n / ST) & 1, patience);
                         if (!ok) break;
                         if (elect_one()) mbar_arrive_at(&full[s], 0);
                         __syncwarp();
                         continue;
                     }
                     const bool begins = kb % job.leave == 0, ends = kb + 1 == job.nk || (kb + 1) % job.leave == 0;
-                    if (begins && ch >= 2) ok = mbar_wait(&taken[ch & 1], (ch / 2 - 1) & 1);
-                    ok = ok && mbar_wait(&full[s], (n / ST) & 1);
+                    if (begins && ch >= 2) ok = mbar_wait_warp(&taken[ch & 1], (ch / 2 - 1) & 1, patience);
+                    ok = ok && mbar_wait_warp(&full[s], (n / ST) & 1, patience);
                     if (!ok) break;
                     tmem_fence_after();
                     const bool turn_a = job.turns_a(kb), turn_b = job.turns_b(kb);
@@ -818,12 +835,17 @@ __global__ void __launch_bounds__(Plan<PA, PB, CG>::kThreads, Plan<PA, PB, CG>::
                 }
             }
             if (!ok) failed = 1;
+            // products that nobody waits for any more are sat out too
+            if (rank == 0 && elect_one()) products_done<CG>(&drained);
+            __syncwarp();
+            mbar_wait_warp(&drained, 0, patience);
         }
     }
     __syncwarp();
     tmem_fence_before();
     __syncthreads();
     if (tid == 0 && failed) atomicAdd(a.errors, 1u);
+    __syncwarp();
     if (CG == 2) cluster_sync();
     if (warp == 0) tmem_free<CG>(acc, 2 * L::kColumns);
 }
@@ -864,6 +886,7 @@ struct SmallArgs {
     uint32_t* errors;
     float a, b, c;
     int32_t steps;
+    uint32_t polls;
 };
 
 __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
@@ -872,11 +895,16 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
     __shared__ double ws[kSmallThreads / 32];
     __shared__ uint64_t done;
     __shared__ uint32_t tmem_at;
+    __shared__ volatile uint32_t failed;                         // a wait ran out
     __shared__ Scale scale;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Matrix& t = a.moment.mats[a.list[blockIdx.x]];
     const SmallLayout l(t.m, t.k);
-    if (tid == 0) mbar_init(&done, 1);
+    if (tid == 0) {
+        mbar_init(&done, 1);
+        failed = 0;
+    }
+    __syncwarp();
     if (warp == 0) tmem_alloc<1>(&tmem_at, kTmemColumns);
     tmem_fence_before();
     __syncthreads();
@@ -934,7 +962,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
             tmem_fence_after();
         };
         auto wait_products = [&]() {
-            ok = __syncthreads_and(mbar_wait(&done, phase));
+            ok = __syncthreads_and(mbar_wait(&done, phase, {a.polls, &failed}));
             phase ^= 1;
             tmem_fence_after();
             return ok;
@@ -1036,8 +1064,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
         }
         __syncthreads();
         const float unscale = exp2f((float)-t.ex);
+        if (tid == 0 && failed) atomicAdd(a.errors, 1u);
         if (!ok) {
-            if (tid == 0) atomicAdd(a.errors, 1u);
         } else if (!t.tall) {
 #pragma unroll 3
             for (int e = tid; e < t.m * l.blocks * 8; e += kSmallThreads) {
@@ -1130,6 +1158,7 @@ struct choco_muon {
     choco_muon_params params;
     int device, sms;
     bool broken;                   // the table on the device may be half written
+    uint32_t polls;                // of a wait in a kernel before it counts as run out
     std::vector<Matrix> mats;      // as on the device
     std::vector<Range> written;
     std::vector<int64_t> offsets;
@@ -1431,7 +1460,7 @@ cudaError_t launch_products(const choco_muon* o, const Wave& w, int kind, int st
             const int64_t end = kind == kNext ? cl.next_end : kind == kSquare ? cl.symmetric_end : cl.gram_end;
             if (begin == end || e != cudaSuccess) continue;
             const ProductArgs a = {o->d_mats, o->d_parts + begin, o->d_work, o->d_errors, (int32_t)(end - begin), (float)p.a, (float)p.b, (float)p.c,
-                                   step & 1, o->d_split, o->d_arrived, three || step == 0 ? 2 : 1};
+                                   step & 1, o->polls, o->d_split, o->d_arrived, three || step == 0 ? 2 : 1};
             const Launch l = pairs ? launch_of<2>(kind, three, step == 0) : launch_of<1>(kind, three, step == 0);
             const int64_t most = (int64_t)o->sms * l.blocks / (pairs + 1);
             e = launch_overlapped(l.kernel, dim3((unsigned)(std::min(end - begin, most) * (pairs + 1))), dim3(l.threads), l.shared, st, HotRange{}, a);
@@ -1463,7 +1492,7 @@ int run(choco_muon* o, float* m, double lr, const float* factor, bool update, cu
         tiles(apply_kernel);
     }
     if (!o->small.empty() && e == cudaSuccess) {
-        const SmallArgs sa = {ma, ta, o->d_small, o->d_errors, (float)p.a, (float)p.b, (float)p.c, p.steps};
+        const SmallArgs sa = {ma, ta, o->d_small, o->d_errors, (float)p.a, (float)p.b, (float)p.c, p.steps, o->polls};
         e = launch_overlapped(small_kernel, dim3((unsigned)o->small.size()), dim3(kSmallThreads), (size_t)o->small_shared, st, HotRange{}, sa);
     }
     return status_of(e);
@@ -1484,6 +1513,7 @@ int choco_muon_init(choco_muon** out, int32_t n_matrices, const choco_muon_matri
     choco_muon* o = new (std::nothrow) choco_muon();
     if (!o) return CHOCO_ERR_ALLOC;
     o->params = *p;
+    o->polls = kSpinLimit;
     int rc = CHOCO_OK;
     try {
         std::vector<Unit> units;
@@ -1578,6 +1608,13 @@ int choco_muon_status(choco_muon* opt, void* stream)
     if (cudaMemcpyAsync(&errors, opt->d_errors, sizeof(errors), cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
         return CHOCO_ERR_CUDA;
     return errors ? CHOCO_ERR_TIMEOUT : CHOCO_OK;
+}
+
+int choco_debug_muon_set_wait_polls(choco_muon* opt, uint32_t polls)
+{
+    if (!opt) return CHOCO_ERR_INVALID_ARG;
+    opt->polls = polls > kSpinLimit ? kSpinLimit : polls;
+    return CHOCO_OK;
 }
 
 } // extern "C"

@@ -122,12 +122,23 @@ __device__ __forceinline__ void products_done(uint64_t* bar)
 }
 
 // ------------------------------------------------------------------------------------ barriers and copies
-__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity)
+// A wait that `polls` polls do not end is noted in `late` (shared memory) and goes on for up to kSpinLimit more, so that what is merely late
+// is sat out.  False after that: nothing more can be waited for.
+struct Patience {
+    uint32_t polls;
+    volatile uint32_t* late;
+};
+__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, const Patience& p)
 {
+    for (uint32_t i = 0; i < p.polls; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    *p.late = 1;
     for (uint32_t i = 0; i < kSpinLimit; ++i)
         if (mbar_try_wait(bar, parity)) return true;
     return false;
 }
+// By a whole warp, with one verdict: what comes next (tensor memory's loads, votes, barriers) wants all lanes or none
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, const Patience& p) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, p)); }
 // Arrive at the barrier of CTA `rank` of the cluster that lies where `bar` lies in this one.  Says that copies have landed or tensor
 // memory has been read, neither of which needs the flush of a release to the cluster (which cost 0.8 us each time).
 __device__ __forceinline__ void mbar_arrive_at(uint64_t* bar, uint32_t rank)
