@@ -625,8 +625,13 @@ int choco_muon_set_grads(choco_muon* opt, const void* const* g, void* stream);
 int choco_muon_step(choco_muon* opt, float* m, double lr, const float* factor, void* stream);
 /* x = the X above of u = g for every matrix of the list: no momentum, no decay, copy is not written. */
 int choco_muon_orthogonalize(choco_muon* opt, void* stream);
-/* Synchronises `stream`.  CHOCO_ERR_TIMEOUT if a bounded wait in a kernel of this handle ever ran out ("Device-side waits" above):
- * the part of a matrix that it was to write was not written, nor may it be by later calls: destroy the handle. */
+/*
+ * Synchronises `stream`.  CHOCO_ERR_TIMEOUT if a bounded wait in a kernel of this handle ever ran out ("Device-side waits" above).  No x, copy or
+ * result is built from what was not there: the matrix whose wait it was, and those written after it, keep their parameters, in this
+ * call and in later ones, replays of graphs included; the momentum of that call may be the new one.  Once this call has seen
+ * it, choco_muon_step, _orthogonalize and _set_grads return CHOCO_ERR_TIMEOUT without enqueuing anything.  Restore parameters and
+ * momentum from a checkpoint into a fresh handle.
+ */
 int choco_muon_status(choco_muon* opt, void* stream);
 /* Test hook, as choco_debug_set_wait_polls: with 0 every wait of this handle's kernels counts as run out at once, and is then sat out.  Calls
  * from now on; not for production use. */

@@ -113,6 +113,7 @@ struct MomentArgs {
     double* partial;        // per unit
     uint32_t* done;         // per matrix, 0 between calls
     Scale* scale;           // per matrix
+    const uint32_t* errors; // waits of this handle that ran out: nothing is written any more
     float beta, omb;
     int32_t nesterov;
 };
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(kUnitThreads) moment_kernel(MomentArgs a)
     allow_next_kernel();
     wait_for_previous_kernel();
     const float c = a.factor ? a.factor[t.group] : 1.f;
-    const bool skip = !isfinite(c);
+    const bool skip = !isfinite(c) || __ldcg(a.errors) != 0;
     double sum = 0.0;
     if (!skip) {
         const int64_t begin = (int64_t)un.part * kUnit, all = (int64_t)t.rows * t.cols;
@@ -253,6 +254,7 @@ struct TileArgs {
     const Block* blocks;
     uint8_t* work;
     const Scale* scale;
+    const uint32_t* errors;
     float* m;
     const float* factor;
     float beta, omb, lr;
@@ -433,7 +435,7 @@ __global__ void __launch_bounds__(kCutThreads) apply_kernel(TileArgs a)
     const int row0 = bl.row * kSide, col0 = bl.col * kHalves;
     allow_next_kernel();
     wait_for_previous_kernel();
-    if (a.factor && !isfinite(a.factor[t.group])) return;
+    if ((a.factor && !isfinite(a.factor[t.group])) || __ldcg(a.errors) != 0) return;
     const uint8_t* from = a.work + t.at[a.which] + ((int64_t)bl.row * t.nb + bl.col) * a.planes * kTileBytes;
     const float unscale = exp2f((float)-t.ex);
     const bool straight = t.aligned && !t.tall;
@@ -913,7 +915,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
     allow_next_kernel();
     wait_for_previous_kernel();
     const float c = a.moment.factor ? a.moment.factor[t.group] : 1.f;
-    const bool skip = !isfinite(c);
+    const bool skip = __syncthreads_or(!isfinite(c) || __ldcg(a.moment.errors) != 0); // (other blocks may add to the errors)
     bool ok = true;
     if (!skip) {
         const double sum = block_sum<kSmallThreads>(moment_unit<kSmallThreads>(a.moment, t, 0, (int64_t)t.rows * t.cols, c), ws);
@@ -1064,8 +1066,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
         }
         __syncthreads();
         const float unscale = exp2f((float)-t.ex);
-        if (tid == 0 && failed) atomicAdd(a.errors, 1u);
-        if (!ok) {
+        if (failed) {
+            if (tid == 0) atomicAdd(a.errors, 1u);
         } else if (!t.tall) {
 #pragma unroll 3
             for (int e = tid; e < t.m * l.blocks * 8; e += kSmallThreads) {
@@ -1159,6 +1161,7 @@ struct choco_muon {
     int device, sms;
     bool broken;                   // the table on the device may be half written
     uint32_t polls;                // of a wait in a kernel before it counts as run out
+    bool timed_out;                // one was seen to have run out
     std::vector<Matrix> mats;      // as on the device
     std::vector<Range> written;
     std::vector<int64_t> offsets;
@@ -1471,8 +1474,8 @@ cudaError_t launch_products(const choco_muon* o, const Wave& w, int kind, int st
 int run(choco_muon* o, float* m, double lr, const float* factor, bool update, cudaStream_t st)
 {
     const choco_muon_params& p = o->params;
-    const MomentArgs ma = {o->d_mats, o->d_units, m, factor, o->d_partial, o->d_done, o->d_scale, (float)p.beta, (float)(1.0 - p.beta), p.nesterov};
-    TileArgs ta = {o->d_mats, nullptr, o->d_work, o->d_scale, m, factor, (float)p.beta, (float)(1.0 - p.beta), (float)lr, p.nesterov, 0, 0, update};
+    const MomentArgs ma = {o->d_mats, o->d_units, m, factor, o->d_partial, o->d_done, o->d_scale, o->d_errors, (float)p.beta, (float)(1.0 - p.beta), p.nesterov};
+    TileArgs ta = {o->d_mats, nullptr, o->d_work, o->d_scale, o->d_errors, m, factor, (float)p.beta, (float)(1.0 - p.beta), (float)lr, p.nesterov, 0, 0, update};
     cudaError_t e = cudaSuccess;
     if (o->nunits > 0) e = launch_overlapped(moment_kernel, dim3((unsigned)o->nunits), dim3(kUnitThreads), 0, st, HotRange{}, ma);
     for (const Wave& w : o->waves) {
@@ -1558,6 +1561,7 @@ int choco_muon_state_size(const choco_muon* opt, int64_t* elements, int64_t* off
 int choco_muon_set_grads(choco_muon* opt, const void* const* g, void* stream)
 {
     if (!opt || !g || !on_device(opt)) return CHOCO_ERR_INVALID_ARG;
+    if (opt->timed_out) return CHOCO_ERR_TIMEOUT;
     for (size_t i = 0; i < opt->mats.size(); ++i) {
         const Matrix& t = opt->mats[i];
         if (t.rows > 0 && !g[i]) return CHOCO_ERR_INVALID_ARG;
@@ -1589,6 +1593,7 @@ int choco_muon_step(choco_muon* opt, float* m, double lr, const float* factor, v
     if (!opt || !(lr >= 0.0) || !std::isfinite((float)lr) || !on_device(opt)) return CHOCO_ERR_INVALID_ARG;
     if (opt->elements > 0 && !m) return CHOCO_ERR_INVALID_ARG;
     if (!aligned_to(m, 16) || !aligned_to(factor, 4)) return CHOCO_ERR_MISALIGNED;
+    if (opt->timed_out) return CHOCO_ERR_TIMEOUT;
     if (opt->broken) return CHOCO_ERR_CUDA;
     return run(opt, m, lr, factor, true, (cudaStream_t)stream);
 }
@@ -1596,6 +1601,7 @@ int choco_muon_step(choco_muon* opt, float* m, double lr, const float* factor, v
 int choco_muon_orthogonalize(choco_muon* opt, void* stream)
 {
     if (!opt || !on_device(opt)) return CHOCO_ERR_INVALID_ARG;
+    if (opt->timed_out) return CHOCO_ERR_TIMEOUT;
     if (opt->broken) return CHOCO_ERR_CUDA;
     return run(opt, nullptr, 0.0, nullptr, false, (cudaStream_t)stream);
 }
@@ -1607,7 +1613,8 @@ int choco_muon_status(choco_muon* opt, void* stream)
     cudaStream_t st = (cudaStream_t)stream;
     if (cudaMemcpyAsync(&errors, opt->d_errors, sizeof(errors), cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
         return CHOCO_ERR_CUDA;
-    return errors ? CHOCO_ERR_TIMEOUT : CHOCO_OK;
+    if (errors) opt->timed_out = true;
+    return opt->timed_out ? CHOCO_ERR_TIMEOUT : CHOCO_OK;
 }
 
 int choco_debug_muon_set_wait_polls(choco_muon* opt, uint32_t polls)
