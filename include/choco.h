@@ -603,7 +603,7 @@ typedef struct {
 /*
  * The momentum m is a caller-owned DEVICE float32 array over all matrices, row after row without gaps, in the order of the
  * list, every matrix starting on a multiple of 256 elements (the gaps are neither read nor written): choco_muon_state_size
- * elements in all, 16-byte aligned; zeros for a fresh run.  The list is copied; the arrays it points to have to stay where
+ * elements in all, 16-byte aligned, apart from all x, copies and g (CHOCO_ERR_INVALID_ARG); zeros for a fresh run.  The list is copied; the arrays it points to have to stay where
  * they are.  The addresses from the first element of an x or copy to its last (padding between rows included) overlap no
  * other x, copy or g (CHOCO_ERR_INVALID_ARG); gradients may overlap each other.  init allocates the workspace: 6 to 8 bytes for each
  * element of a matrix and 6 to 12 for each of its m x m square (m the smaller side), sides rounded up to 128, for as many matrices at a

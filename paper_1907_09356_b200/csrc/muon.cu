@@ -1163,7 +1163,8 @@ struct choco_muon {
     uint32_t polls;                // of a wait in a kernel before it counts as run out
     bool timed_out;                // one was seen to have run out
     std::vector<Matrix> mats;      // as on the device
-    std::vector<Range> written;
+    std::vector<Range> written;    // in order, disjoint
+    std::vector<Range> read;       // gradients likewise, those that meet joined
     std::vector<int64_t> offsets;
     std::vector<Wave> waves;
     std::vector<int32_t> small;    // matrices that one block of threads takes through the whole step
@@ -1403,12 +1404,26 @@ bool overlap(choco_muon* o)
         if (w[i].begin < w[i - 1].end) return true;
     return false;
 }
+bool meets(const std::vector<Range>& ranges, const Range& r)
+{
+    auto next = std::lower_bound(ranges.begin(), ranges.end(), r.end, [](const Range& a, uintptr_t e) { return a.begin < e; });
+    return next != ranges.begin() && (next - 1)->end > r.begin;
+}
 bool is_written(const choco_muon* o, const Matrix& t, const void* g)
 {
-    if (t.rows == 0) return false;
-    const Range r = range_of(g, t.rows, t.cols, t.g_ld, t.g_dtype);
-    auto next = std::lower_bound(o->written.begin(), o->written.end(), r.end, [](const Range& a, uintptr_t e) { return a.begin < e; });
-    return next != o->written.begin() && (next - 1)->end > r.begin;
+    return t.rows > 0 && meets(o->written, range_of(g, t.rows, t.cols, t.g_ld, t.g_dtype));
+}
+std::vector<Range> gradient_ranges(const std::vector<Matrix>& mats) // throws std::bad_alloc
+{
+    std::vector<Range> all, joined;
+    for (const Matrix& t : mats)
+        if (t.rows > 0) all.push_back(range_of(t.g, t.rows, t.cols, t.g_ld, t.g_dtype));
+    std::sort(all.begin(), all.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+    for (const Range& r : all) {
+        if (!joined.empty() && r.begin <= joined.back().end) joined.back().end = std::max(joined.back().end, r.end);
+        else joined.push_back(r);
+    }
+    return joined;
 }
 
 int allocate(choco_muon* o, const std::vector<Unit>& units, const std::vector<Part>& parts, const std::vector<Block>& blocks, int64_t work)
@@ -1529,6 +1544,7 @@ int choco_muon_init(choco_muon** out, int32_t n_matrices, const choco_muon_matri
         if (rc == CHOCO_OK && overlap(o)) rc = CHOCO_ERR_INVALID_ARG;
         for (const Matrix& t : o->mats)
             if (rc == CHOCO_OK && is_written(o, t, t.g)) rc = CHOCO_ERR_INVALID_ARG;
+        if (rc == CHOCO_OK) o->read = gradient_ranges(o->mats);
         if (rc == CHOCO_OK && o->sms == 0) rc = CHOCO_ERR_CUDA;
         if (rc == CHOCO_OK) rc = allocate(o, units, parts, blocks, work);
     } catch (const std::exception&) {
@@ -1575,12 +1591,14 @@ int choco_muon_set_grads(choco_muon* opt, const void* const* g, void* stream)
             mats[i].g = g[i];
             look_at_gradient(mats[i]);
         }
+        std::vector<Range> read = gradient_ranges(mats);
         if (cudaStreamSynchronize(st) != cudaSuccess) return CHOCO_ERR_CUDA;
         opt->broken = true; // until the table on the device is whole
         if (cudaMemcpyAsync(opt->d_mats, mats.data(), sizeof(Matrix) * mats.size(), cudaMemcpyHostToDevice, st) != cudaSuccess ||
             cudaStreamSynchronize(st) != cudaSuccess)
             return CHOCO_ERR_CUDA;
         opt->mats.swap(mats);
+        opt->read.swap(read);
         opt->broken = false;
     } catch (const std::exception&) {
         return CHOCO_ERR_ALLOC;
@@ -1593,6 +1611,10 @@ int choco_muon_step(choco_muon* opt, float* m, double lr, const float* factor, v
     if (!opt || !(lr >= 0.0) || !std::isfinite((float)lr) || !on_device(opt)) return CHOCO_ERR_INVALID_ARG;
     if (opt->elements > 0 && !m) return CHOCO_ERR_INVALID_ARG;
     if (!aligned_to(m, 16) || !aligned_to(factor, 4)) return CHOCO_ERR_MISALIGNED;
+    if (opt->elements > 0) {
+        const Range r = range_of(m, 1, opt->elements, 0, CHOCO_F32);
+        if (meets(opt->written, r) || meets(opt->read, r)) return CHOCO_ERR_INVALID_ARG;
+    }
     if (opt->timed_out) return CHOCO_ERR_TIMEOUT;
     if (opt->broken) return CHOCO_ERR_CUDA;
     return run(opt, m, lr, factor, true, (cudaStream_t)stream);
