@@ -583,7 +583,7 @@ typedef struct {
     const void* g;        /* gradients, read-only                                                  */
     void* copy;           /* second copy of the new parameters in another type, or NULL            */
     int64_t rows, cols;   /* >= 0; min(rows, cols) <= 2^14, rows cols <= 2^30                       */
-    int64_t x_ld, g_ld, copy_ld; /* elements between rows, >= cols; 0 = cols                       */
+    int64_t x_ld, g_ld, copy_ld; /* elements between rows, >= cols; 0 = cols; rows ld <= 2^40      */
     int32_t x_dtype, g_dtype, copy_dtype;
     int32_t group;        /* in [0, groups)                                                        */
     double weight_decay;  /* >= 0, finite as a float32                                             */

@@ -1270,7 +1270,7 @@ int plan(choco_muon* o, int32_t n, const choco_muon_matrix* ms, std::vector<Unit
         if (!aligned_to(q.x, dtype_size(q.x_dtype)) || !aligned_to(q.g, dtype_size(q.g_dtype)) || !aligned_to(q.copy, dtype_size(q.copy_dtype)))
             return CHOCO_ERR_MISALIGNED;
         if (some && (std::min(q.rows, q.cols) > kMostSide || std::max(q.rows, q.cols) > kMostElements / std::min(q.rows, q.cols) ||
-                     std::max({q.x_ld, q.g_ld, q.copy_ld}) > (int64_t)1 << 38))
+                     std::max({q.x_ld, q.g_ld, q.copy_ld}) > std::min((int64_t)1 << 38, ((int64_t)1 << 40) / q.rows)))
             return CHOCO_ERR_TOO_LARGE;
         Matrix t = {};
         t.x = q.x; t.g = q.g; t.copy = q.copy;
