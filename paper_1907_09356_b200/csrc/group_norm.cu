@@ -979,27 +979,35 @@ int check(const choco_group_norm_params& p, int64_t images, int64_t pixels, cons
     }
     return CHOCO_OK;
 }
-bool same_place(const choco_pixels& a, const choco_pixels& b)
+// (strides of axes with one element say nothing)
+bool same_place(const choco_group_norm_params& p, int64_t images, int64_t pixels, const choco_pixels& a, const choco_pixels& b)
 {
-    return a.data == b.data && a.dtype == b.dtype && a.worker == b.worker && a.image == b.image && a.pixel == b.pixel;
+    return a.data == b.data && a.dtype == b.dtype && (p.n == 1 || a.worker == b.worker) && (images == 1 || a.image == b.image) &&
+           (pixels == 1 || a.pixel == b.pixel);
 }
+int64_t gcd(int64_t a, int64_t b) { return b ? gcd(b, a % b) : a; }
+
 // Whether an array that is written may share elements with one that is read: their addresses meet, they are not the same array,
 // and they are not two sets of channels of one wider array.
 bool mixes(const choco_group_norm_params& p, int64_t images, int64_t pixels, const choco_pixels& w, const choco_pixels& r)
 {
-    if (same_place(w, r)) return false;
+    if (same_place(p, images, pixels, w, r)) return false;
     auto end = [&](const choco_pixels& a) {
         return (uintptr_t)a.data + (uintptr_t)(((pixels - 1) * a.pixel + (images - 1) * a.image + (p.n - 1) * a.worker + p.channels) * dtype_size(a.dtype));
     };
     if (end(w) <= (uintptr_t)r.data || end(r) <= (uintptr_t)w.data) return false;
-    if (w.dtype == r.dtype && w.worker == r.worker && w.image == r.image && w.pixel == r.pixel && pixels > 1) {
-        const int64_t apart = ((int64_t)(uintptr_t)w.data - (int64_t)(uintptr_t)r.data) / dtype_size(w.dtype);
-        const int64_t to = apart < 0 ? -apart : apart;
-        bool grid = to >= p.channels && to + p.channels <= w.pixel;
-        grid = grid && (images == 1 || w.image % w.pixel == 0) && (p.n == 1 || w.worker % w.pixel == 0);
-        if (grid) return false;
+    if (w.dtype != r.dtype) return true;
+    // channels of the wider array: what all strides are multiples of (of axes with one element they say nothing)
+    int64_t wide = 0;
+    const struct { int64_t count, w, r; } dims[3] = {{pixels, w.pixel, r.pixel}, {images, w.image, r.image}, {p.n, w.worker, r.worker}};
+    for (const auto& d : dims) {
+        if (d.count == 1) continue;
+        if (d.w != d.r) return true;
+        wide = gcd(d.w, wide);
     }
-    return true;
+    const int64_t apart = ((int64_t)(uintptr_t)w.data - (int64_t)(uintptr_t)r.data) / dtype_size(w.dtype);
+    const int64_t to = apart < 0 ? -apart : apart;
+    return to < p.channels || (wide > 0 && to + p.channels > wide);
 }
 
 // Elements that one access may take: all arrays allow it at every pixel
@@ -1009,8 +1017,6 @@ bool allows(const choco_group_norm_params& p, int64_t images, int64_t pixels, co
     return aligned_to(a.data, bytes) && (pixels == 1 || a.pixel * es % bytes == 0) && (images == 1 || a.image * es % bytes == 0) &&
            (p.n == 1 || a.worker * es % bytes == 0);
 }
-
-int64_t gcd(int64_t a, int64_t b) { return b ? gcd(b, a % b) : a; }
 
 // How a call is cut: channels of a slice, blocks of a cluster, pixels that a thread keeps.
 struct Cut {
