@@ -686,7 +686,8 @@ int choco_group_norm_forward(choco_group_norm* gn, int64_t images, int64_t pixel
  *     dweight = sum over images and pixels of dz xhat ;   dbias = sum of dz       (added to what is there with accumulate = 1)
  * mean and rstd are those of the forward call (and stand for themselves: relu's slope is 1 exactly where z of these numbers is above
  * 0).  Sums in a fixed order.  dx: NULL or of x's type, with the rules for y, against x and dy.  dweight, dbias: worker i's at i grad_ld,
- * [channels], of type grad_dtype, either may be NULL; images <= max_images where there is one.  They share no memory with the other arrays.
+ * [channels], of type grad_dtype, either may be NULL; images <= max_images where there is one.  They share no memory with each other
+ * (CHOCO_ERR_INVALID_ARG) or with the other arrays.
  */
 int choco_group_norm_backward(choco_group_norm* gn, int64_t images, int64_t pixels, const choco_pixels* x, const choco_pixels* dy, const choco_pixels* dx,
                               const void* weight, const void* bias, int64_t param_ld, int32_t param_dtype, const float* mean, const float* rstd,

@@ -1010,6 +1010,17 @@ bool mixes(const choco_group_norm_params& p, int64_t images, int64_t pixels, con
     return to < p.channels || (wide > 0 && to + p.channels > wide);
 }
 
+// Whether rows of two arrays [n, channels] of one pitch share elements
+bool rows_meet(const choco_group_norm_params& p, const void* a, const void* b, int64_t ld, int64_t size)
+{
+    const uintptr_t u = (uintptr_t)a, v = (uintptr_t)b;
+    const uintptr_t apart = (u < v ? v - u : u - v) / (uintptr_t)size;
+    if (apart < (uintptr_t)p.channels) return true;
+    if (p.n == 1) return false;
+    const uintptr_t rows = apart / (uintptr_t)ld, rest = apart % (uintptr_t)ld; // from a row of one to that before the other's, and on
+    return (rows < (uintptr_t)p.n && rest < (uintptr_t)p.channels) || (rows + 1 < (uintptr_t)p.n && ld - (int64_t)rest < p.channels);
+}
+
 // Elements that one access may take: all arrays allow it at every pixel
 bool allows(const choco_group_norm_params& p, int64_t images, int64_t pixels, const choco_pixels& a, int vec)
 {
@@ -1196,6 +1207,7 @@ int choco_group_norm_backward(choco_group_norm* gn, int64_t images, int64_t pixe
     const bool grads = dweight || dbias;
     if (grads && (!dtype_ok(grad_dtype) || (p.n > 1 && grad_ld < p.channels) || grad_ld > kMostSize / p.n)) return CHOCO_ERR_INVALID_ARG;
     if (grads && (!aligned_to(dweight, dtype_size(grad_dtype)) || !aligned_to(dbias, dtype_size(grad_dtype)))) return CHOCO_ERR_MISALIGNED;
+    if (dweight && dbias && rows_meet(p, dweight, dbias, grad_ld, dtype_size(grad_dtype))) return CHOCO_ERR_INVALID_ARG;
     if (pixels > 0x7fffffff || images > 0x7fffffff / p.n || (grads && (images > p.max_images || (p.channels + 31) / 32 > 0x7fffffff / p.n)))
         return CHOCO_ERR_TOO_LARGE;
     const bool some = images > 0 && pixels > 0;
