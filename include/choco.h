@@ -672,7 +672,8 @@ int choco_group_norm_init(choco_group_norm** out, const choco_group_norm_params*
 int choco_group_norm_destroy(choco_group_norm* gn);
 /*
  * choco_group_norm_forward -- y from x, in float32 (the statistics' last step in float64), rounded once to y's type.
- *   images, pixels   of a worker, of an image; 0: nothing is done.
+ *   images, pixels   of a worker, of an image; 0: nothing is done.  images n and pixels are below 2^31 (CHOCO_ERR_TOO_LARGE, as for pixels of the
+ *                    widest groups that a cluster of blocks cannot count through: 2^27 of them are taken in any case).
  *   y                no element belongs to two places; y is x itself (address, strides and type alike), or another set of channels
  *                    of the same wider array, or shares no addresses with it (CHOCO_ERR_INVALID_ARG).
  *   weight, bias     worker i's at i param_ld, [channels], of type param_dtype; NULL: 1 and 0.  param_ld = 0: the same for all workers.

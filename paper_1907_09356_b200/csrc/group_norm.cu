@@ -1125,6 +1125,7 @@ int launch(choco_group_norm* gn, NormArgs& a, bool backward, const choco_pixels&
     const int vec = widest(p, a.images, a.pixels, x, y, dx);
     const Cut c = cut_of(p, a.images, a.pixels, vec, dtype_size(x.dtype), dtype_size(x.dtype) + (backward ? dtype_size(y.dtype) : 0),
                          backward ? kShareBackward : kShareForward, backward ? kSlackBackward : a.activation >= kSilu && y.dtype == CHOCO_F32 ? kSlackSmooth : kSlackForward);
+    if ((int64_t)c.rounds * c.steps > 0x7fffffff) return CHOCO_ERR_TOO_LARGE; // (of arrays that repeat one pixel; steps of all rounds are counted through)
     a.slice = c.slice;
     a.slices = a.channels / c.slice;
     a.cluster = c.cluster;
