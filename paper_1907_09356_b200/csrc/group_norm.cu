@@ -28,7 +28,10 @@ constexpr int kNormThreads = 128;
 constexpr int kNormWarps = kNormThreads / 32;
 constexpr int kNormBlocks = 4;          // to an SM, by registers
 constexpr int kApart = 64;             // pixels that a thread adds up on their own: what is rounded grows with the length of a sum
-constexpr double kMostLost = 16.0;      // squares about a pivot, over those about the mean: as many bits of float32 sums are lost (4)
+// Squares about a pivot, over those about the mean, of sums that are good enough: of R, rstd is off by up to 1.5 R roundings (R of the squares'
+// sum, twice R of the square of the sum, half of which reaches the root): 4e-7.
+constexpr double kMostLost = 4.0;
+constexpr int kLookedAt = 4;            // pixels whose mean is the first pivot
 constexpr int kWaits = 2;               // groups in which a thread's copies to shared memory are waited for
 constexpr int64_t kMostSlice = 2048;    // channels of a slice, and of a group: their sums are in shared memory
 
@@ -46,6 +49,7 @@ struct NormArgs {
     float* rstd;
     float2* sums;                       // backward: of the channels of every image
     int64_t pixels;
+    int64_t looked_at[kLookedAt];       // of x, in elements from an image's first
     int32_t images, channels, per_group, groups;
     int32_t slice, slices;              // channels of a slice, slices of an image
     int32_t cluster;
@@ -72,6 +76,8 @@ __device__ __forceinline__ int cluster_at() // of the clusters along the grid's 
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float or_zero(float v) { return isfinite(v) ? v : 0.f; } // where it is no number to take sums about
 
 // Two neighbouring channels at a time, in the register pairs that sm_100's float32 instructions for two take (as structs of two
 // floats the moves between them cost what the instructions save).
@@ -441,8 +447,8 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) forward_kernel(Norm
         }
     };
     const double count = (double)a.pixels;
-    // Sums of x - p and (x - p)^2 with p the channel's value at the image's first pixel, so that float32 loses nothing where the mean is far
-    // from zero.  Where that pixel turns out to lie far from the others (a border, padding, a spike) the sums are formed once
+    // Sums of x - p and (x - p)^2 with p the mean of the channel's values at a few pixels, so that float32 loses nothing where the mean is far
+    // from zero.  Where these pixels turn out to lie far from the others (a border, padding, a spike) the sums are formed once
     // more, with the channels' means as p.  All blocks of a cluster have the same sums, and decide alike.
     for (int pass = 0;; ++pass) {
         for (int round = 0; round < sh.rounds; ++round) {
@@ -461,15 +467,18 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) forward_kernel(Norm
                 const XT* from = x + sh.first * a.x.pixel + c0;
                 const int64_t from_step = sh.lanes * a.x.pixel;
                 if (pass == 0) {
-                    Raw<XT, VEC> first;
-                    load_raw(first, x + c0);
+                    Raw<XT, VEC> seen[kLookedAt];
+#pragma unroll
+                    for (int k = 0; k < kLookedAt; ++k) load_raw(seen[k], x + c0 + a.looked_at[k]);
 #pragma unroll
                     for (int p = 0; p < NP; ++p) {
-                        const float2 v = floats_of(raw_pair(first, p));
-                        pivot[p] = pair_of(-v.x, -v.y);
+                        const Pair mean = add2(add2(raw_pair(seen[0], p), raw_pair(seen[1], p)), add2(raw_pair(seen[2], p), raw_pair(seen[3], p)));
+                        const float2 v = floats_of(mean);
+                        const float u = or_zero(v.x / kLookedAt), w = or_zero(v.y / kLookedAt);
+                        pivot[p] = pair_of(-u, -w);
                         if (sh.lane == 0) {
-                            l.channel[c0 + 2 * p].w = v.x;
-                            if (VEC > 1) l.channel[c0 + 2 * p + 1].w = v.y;
+                            l.channel[c0 + 2 * p].w = u;
+                            if (VEC > 1) l.channel[c0 + 2 * p + 1].w = w;
                         }
                     }
                 } else {
@@ -1116,6 +1125,9 @@ int fill(const choco_group_norm* gn, int64_t images, int64_t pixels, const void*
     a.activation = p.activation;
     a.eps = p.eps;
     a.inverse = 1.0 / ((double)pixels * a.per_group);
+    // (seventeenths: pixels of different columns in images of the usual widths)
+    const int at[kLookedAt] = {1, 6, 10, 15};
+    for (int k = 0; k < kLookedAt; ++k) a.looked_at[k] = pixels * at[k] / 17;
     return CHOCO_OK;
 }
 
@@ -1195,6 +1207,7 @@ int choco_group_norm_forward(choco_group_norm* gn, int64_t images, int64_t pixel
     if (rc == CHOCO_OK) rc = fill(gn, images, pixels, weight, bias, param_ld, param_dtype, a);
     if (rc != CHOCO_OK) return rc;
     a.x = device_of(*x); a.y = device_of(*y);
+    for (int64_t& at : a.looked_at) at *= a.x.pixel;
     a.mean = mean; a.rstd = rstd;
     return launch(gn, a, false, *x, *y, nullptr, (cudaStream_t)stream);
 }
