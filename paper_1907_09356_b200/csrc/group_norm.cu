@@ -1056,8 +1056,8 @@ Cut cut_of(const choco_group_norm_params& p, int64_t images, int64_t pixels, int
         for (--u; u > 1 && count % u;) --u;
         return u;
     };
-    int64_t units = count;
-    while (units > 1 && (units * unit > kMostSlice || (units * unit * bytes * pixels > most && part_below(units) * unit * es >= 64))) units = part_below(units);
+    int64_t units = part_below(std::min(count, kMostSlice / unit) + 1); // (looked for below kMostSlice, however many channels there are)
+    while (units > 1 && units * unit * bytes * pixels > most && part_below(units) * unit * es >= 64) units = part_below(units);
     best.slice = (int)(units * unit);
     const int64_t slices = p.channels / best.slice, total = best.slice * bytes * pixels;
     // blocks: enough for `most` each, and for all SMs where there are few rows (but no share below kLeast)
