@@ -74,8 +74,9 @@ __device__ __forceinline__ int cluster_at() // of the clusters along the grid's 
     asm volatile("mov.u32 %0, %%clusterid.x;" : "=r"(c));
     return c;
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+// (threads of a warp may reach them one by one)
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 __device__ __forceinline__ float or_zero(float v) { return isfinite(v) ? v : 0.f; } // where it is no number to take sums about
 

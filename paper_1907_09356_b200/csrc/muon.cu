@@ -1095,6 +1095,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(SmallArgs a)
             }
         }
     }
+    __syncwarp();
     tmem_fence_before();
     __syncthreads();
     if (warp == 0) tmem_free<1>(acc, kTmemColumns);
