@@ -667,7 +667,10 @@ typedef struct {
     int32_t unused;
 } choco_pixels;
 
-/* Allocates 8 n max_images channels bytes for sums of channels (max_images = 0: forward, and dx, only). */
+/*
+ * Allocates 8 n max_images channels bytes for sums of channels (max_images = 0: forward, and dx, only).  These are the handle's: calls for
+ * gradients of parameters on one handle, replays of graphs that captured them included, follow one another.  One host thread at a time.
+ */
 int choco_group_norm_init(choco_group_norm** out, const choco_group_norm_params* p);
 int choco_group_norm_destroy(choco_group_norm* gn);
 /*

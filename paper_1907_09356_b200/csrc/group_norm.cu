@@ -7,7 +7,8 @@
 // dx; the sums that every element waits for lie between.  So a cluster of blocks takes a slice of an image (all pixels, as
 // many whole groups of channels as make long enough rows), each block a share of the pixels.  A block reads its share once,
 // keeps the raw values in shared memory while it adds up, exchanges sums of channels with the other blocks of the
-// cluster through their shared memory, and finishes from there.  What a block cannot keep it reads again.
+// cluster through their shared memory, and finishes from there.  What a block cannot keep it reads again.  (2 x 64 images of 112 x 112 x 64
+// bf16: forward 117 .. 121 us of 64; of 56 x 56 x 256: backward 187 us of 96; 8 x 128 of 32 x 32 x 16 f32: forward 30 us of 21.)
 //
 // A thread has the same few channels throughout (one access of up to 16 bytes to a pixel), so sums and parameters of
 // channels live in registers, and a value it kept is its own: no barrier between writing and reading it.

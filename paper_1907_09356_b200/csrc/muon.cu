@@ -19,9 +19,10 @@
 // diagonal are computed, stored and read; a product that needs one above it reads the stored one turned.
 //
 // What bounds it.  4096 x 4096 floats, 3.3 ms (2.9 ms in a burst of calls): the tensor cores, 76 .. 80 % of whose cycles three products
-// take at the clock that the card's power leaves; 2.5 ms is their floor.  32 of 2600 x 650 bfloat16, 1.1 .. 1.27 ms: parts have 11 or 41
-// steps of K, so their beginnings and ends count (29 .. 53 % of the tensor cores' cycles), and the reads behind them (11 TB/s from
-// L2).  The 176 small matrices of eight ResNet-20, 87 us: the fifteen products of the longest chain, one block's.
+// take at the clock that the card's power leaves; 2.5 ms is their floor.  32 of 2600 x 650 bfloat16, 2.4 .. 2.8 ms (1.25 with one
+// product): parts have 11 or 41 steps of K, so their beginnings and ends count (with one product 29 .. 53 % of the tensor cores' cycles are
+// used, and the reads behind them come to 11 TB/s from L2), and 650 rows are three parts of 256, 1.6 times the useful operations.  The 176
+// small matrices of eight ResNet-20, 87 us: the fifteen products of the longest chain, one block's.
 #include <math.h>
 
 #include <cstring>
