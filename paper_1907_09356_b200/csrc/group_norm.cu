@@ -474,9 +474,11 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) forward_kernel(Norm
                     for (int k = 0; k < kLookedAt; ++k) load_raw(seen[k], x + c0 + a.looked_at[k]);
 #pragma unroll
                     for (int p = 0; p < NP; ++p) {
-                        const Pair mean = add2(add2(raw_pair(seen[0], p), raw_pair(seen[1], p)), add2(raw_pair(seen[2], p), raw_pair(seen[3], p)));
+                        const Pair part = pair_of(1.f / kLookedAt, 1.f / kLookedAt), none = pair_of(0.f, 0.f); // (of each: the sum of all may leave float32)
+                        const Pair mean = add2(fma2(raw_pair(seen[0], p), part, fma2(raw_pair(seen[1], p), part, none)),
+                                               fma2(raw_pair(seen[2], p), part, fma2(raw_pair(seen[3], p), part, none)));
                         const float2 v = floats_of(mean);
-                        const float u = or_zero(v.x / kLookedAt), w = or_zero(v.y / kLookedAt);
+                        const float u = or_zero(v.x), w = or_zero(v.y);
                         pivot[p] = pair_of(-u, -w);
                         if (sh.lane == 0) {
                             l.channel[c0 + 2 * p].w = u;
